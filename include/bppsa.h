@@ -495,6 +495,134 @@ bppsa_status bppsa_spscan(int n, const bppsa_csr* Jt, const float* seed, float* 
                           int up_levels, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * A selective state space layer and the optimiser over many tensors.
+ * ---------------------------------------------------------------------- */
+
+/* Element types of activations.  Parameters, states and their gradients are fp32 throughout. */
+typedef enum { BPPSA_F32 = 0, BPPSA_BF16 = 1, BPPSA_F16 = 2 } bppsa_type;
+
+/* An array [T,B,C] of activations: element (t,b,c) lies at data + t stride_t + b stride_b + c elements.  The strides may
+ * be those of a transposed array or of a column slice of a wider one. */
+typedef struct bppsa_rows {
+  void* data;
+  int64_t stride_t, stride_b;
+} bppsa_rows;
+
+/*
+ * The selective scan.  With s = softplus(dt[t,b,d] + dt_bias[d]) and g = d / (D / G), for every sample b, channel d and
+ * state n
+ *     h[t] = exp(s A[d,n]) h[t-1] + s u[t,b,d] Bm[t,b,g,n]
+ *     y[t,b,d] = ( sum_n Cm[t,b,g,n] h[t] + skip[d] u[t,b,d] ) * ( z ? silu(z[t,b,d]) : 1 )
+ * u, dt, z are [T,B,D]; Bm, Cm are [T,B,G,N] (row strides as above, (g,n) in g N + n order); A [D,N], skip [D], dt_bias
+ * [D], h0 [B,D,N] fp32.  z.data, skip, dt_bias, h0 and lengths may be NULL (no gate, 0, 0, zeros, all of T).
+ * lengths [B]: sample b has lengths[b] tokens (clamped to 0..T).  What lies behind them is never read; outputs and
+ * gradients there are zero, and the last state is the one after the sample's own last token.
+ * D has to be a multiple of G, N at most BPPSA_SSM_MAX_N (BPPSA_EUNSUPPORTED beyond).
+ * The struct is host memory, its pointers device memory.
+ */
+#define BPPSA_SSM_MAX_N 64
+typedef struct bppsa_ssm {
+  int32_t T, B, D, N, G, type;
+  bppsa_rows u, dt, z, Bm, Cm;
+  const float *A, *skip, *dt_bias, *h0;
+  const int32_t* lengths;
+} bppsa_ssm;
+
+/*
+ * Forward over whole sequences.  Writes y [T,B,D]; h_last [B,D,N], the state after each sample's last token, if not
+ * NULL; `states`, bppsa_ssm_scan_states_bytes bytes of device memory in a layout of the library's own, if not NULL: what
+ * the backward pass reads.  The results are the same bits on every call with the same sizes.
+ */
+size_t bppsa_ssm_scan_states_bytes(int T, int B, int D, int N);
+size_t bppsa_ssm_scan_workspace_bytes(int T, int B, int D, int N, int G);
+bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows* y, float* h_last, void* states,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of sum(y dy).  layer and states are those of the forward call.  du, ddt, dz are [T,B,D] and dBm, dCm
+ * [T,B,G,N] of the activations' type, written in full; dz.data is NULL where there is no gate.  dA [D,N], dskip [D],
+ * ddt_bias [D] are overwritten; dskip and ddt_bias may be NULL, and dh0 [B,D,N] too.  The gradient of h_last is taken
+ * as zero.  Sums over samples and time run in a fixed order: the same bits on every call.
+ */
+typedef struct bppsa_ssm_grads {
+  bppsa_rows du, ddt, dz;
+  void *dBm, *dCm;
+  float *dA, *dskip, *ddt_bias, *dh0;
+} bppsa_ssm_grads;
+size_t bppsa_ssm_scan_backward_workspace_bytes(int T, int B, int D, int N, int G);
+bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bppsa_rows* dy, const void* states,
+                                     const bppsa_ssm_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One token of each of B streams (layer->T = 1; h0 and lengths NULL).  state [slots_in_state,D,N] is advanced in place:
+ * row i of the batch uses slot slots[i] (slot i where slots is NULL).  A row whose slot lies outside [0, slots_in_state)
+ * belongs to no stream: its y is zero and no state changes.  No two rows may share a slot.
+ */
+bppsa_status bppsa_ssm_scan_step(const bppsa_ssm* layer, const bppsa_rows* y, float* state, int slots_in_state,
+                                 const int32_t* slots, void* stream);
+
+/*
+ * The short causal convolution in front of the scan, channel by channel, of width W = 2 .. BPPSA_SSM_MAX_W:
+ *     p[t] = bias[d] + sum_k weight[d,k] x[t - (W-1) + k],   y[t] = silu ? p sigmoid(p) : p
+ * with x[-(W-1)..-1] = state0 [B,W-1,D] of the activations' type (oldest first; NULL: zeros).  x and y are [T,B,D], weight
+ * [D,W] and bias [D] (NULL: 0) fp32.  state_last [B,W-1,D] (may be NULL) receives the last W-1 inputs of each sample.
+ */
+#define BPPSA_SSM_MAX_W 4
+typedef struct bppsa_conv {
+  int32_t T, B, D, W, type, silu;
+  bppsa_rows x;
+  const float *weight, *bias;
+  const void* state0;
+  const int32_t* lengths;
+} bppsa_conv;
+bppsa_status bppsa_ssm_conv(const bppsa_conv* conv, const bppsa_rows* y, void* state_last, void* stream);
+
+/* Gradients of sum(y dy): dx [T,B,D], dweight [D,W] and dbias [D] (may be NULL) overwritten, dstate0 [B,W-1,D] or NULL. */
+size_t bppsa_ssm_conv_backward_workspace_bytes(int T, int B, int D, int W);
+bppsa_status bppsa_ssm_conv_backward(const bppsa_conv* conv, const bppsa_rows* dy, const bppsa_rows* dx, float* dweight,
+                                     float* dbias, void* dstate0, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token of each of B streams (conv->T = 1; state0 and lengths NULL): state [slots_in_state,W-1,D] of the activations'
+ * type is moved on in place; slots as in bppsa_ssm_scan_step. */
+bppsa_status bppsa_ssm_conv_step(const bppsa_conv* conv, const bppsa_rows* y, void* state, int slots_in_state,
+                                 const int32_t* slots, void* stream);
+
+/*
+ * One AdamW update (decoupled weight decay) of many tensors by one launch:
+ *     m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
+ *     theta <- theta (1 - lr decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps).
+ * theta is fp32, grad of grad_type, copy (NULL: none) a bfloat16 copy of the new theta.
+ * state_bits 32: m and v are fp32.  state_bits 8: m holds m, and v holds the ROOT of v, in e4m3 (OCP), with one fp32 scale
+ * for each BPPSA_ADAMW_BLOCK values of a tensor, the last block being what is left: value = e4m3 * scale, scale = the
+ * block's largest magnitude (2^-100 at least) / 448.  m is rounded to the nearest; the root goes up or down by chance, so
+ * that steps smaller than its spacing add up, and does not become zero.  The chance of value `place` of tensor number
+ * `tensor` comes from hashing them with `seed` (bppsa_adamw_chance in the source; the same bits for the same seed).
+ * A gradient that is not finite makes its values, in 8 bits its whole block of moments, not finite.
+ *
+ * `tensors` [n_tensors] and `pieces` [n_pieces] are DEVICE copies of what the caller fills in on the host once:
+ * bppsa_adamw_pieces writes the list of pieces of lengths n[0..n_tensors) (host memory) and returns how many there are
+ * (pieces NULL: only counts; 0: invalid), each a tensor's number and the first of its at most BPPSA_ADAMW_PIECE values.
+ */
+#define BPPSA_ADAMW_BLOCK 256
+#define BPPSA_ADAMW_PIECE 4096
+typedef struct bppsa_adamw_tensor {
+  float* theta;
+  const void* grad;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  void* copy;
+  int64_t n;
+  double decay;
+} bppsa_adamw_tensor;
+typedef struct bppsa_adamw_piece {
+  int32_t tensor, piece;
+} bppsa_adamw_piece;
+int64_t bppsa_adamw_pieces(int n_tensors, const int64_t* n, bppsa_adamw_piece* pieces);
+bppsa_status bppsa_adamw_step(int n_tensors, const bppsa_adamw_tensor* tensors, int64_t n_pieces,
+                              const bppsa_adamw_piece* pieces, int grad_type, int state_bits, int step, double lr,
+                              double beta1, double beta2, double eps, uint32_t seed, void* stream);
+
+/* ------------------------------------------------------------------------
  * Measurement aid (not part of the method).
  * ---------------------------------------------------------------------- */
 

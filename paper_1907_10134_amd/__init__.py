@@ -13,3 +13,8 @@ from .binding import (  # noqa: F401
     calibration_copy, rnn_scan_fused, scan_static, scan_h20_diag, scan_h128_diag, scan_h128_relay_diag, scan_h128_schedule, scan_h128_units,
     check_scan, gru_scan_fused, gru_scan_fused_workspace_bytes, gru_scan_fused_relay_diag, head_backward, adam_step, rnn_param_count, RnnTrainer, RNN_PARAM_ORDER,
 )
+from .ssm import (  # noqa: F401
+    SsmGrads, SsmConvGrads, ssm_scan, ssm_scan_states, ssm_scan_workspace_bytes, ssm_scan_backward,
+    ssm_scan_backward_workspace_bytes, ssm_scan_step, ssm_conv, ssm_conv_backward, ssm_conv_step,
+)
+from .optim import AdamW  # noqa: F401

@@ -1,0 +1,194 @@
+// One AdamW update of many tensors by one launch, moments in 32 or in 8 bits.
+#include <cmath>
+
+#include "ssm_common.h"
+
+namespace {
+
+using ssm::bf16_t;
+
+constexpr int kThreads = 256;
+constexpr int kBlock = BPPSA_ADAMW_BLOCK;
+constexpr int kPiece = BPPSA_ADAMW_PIECE;
+static_assert(kBlock == BPPSA_WAVE * 4, "a wave holds a block, four values a lane");
+
+struct Step {
+  float beta1, one_minus_beta1, beta2, one_minus_beta2, correct1, root_correct2, eps, lr;
+  double lr_exact;
+  uint32_t seed;
+};
+
+// Whether the root of v goes up: [0, 1) for a place of a tensor, two rounds of multiply and fold.
+__device__ __forceinline__ float chance(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0xBB67AE85u;
+  x = (x ^ (x >> 16)) * 0x3C6EF373u;
+  x ^= x >> 15;
+  return (float)(x >> 8) * 0x1p-24f;
+}
+
+// q >= 0 in units of its block's scale, on the grid of e4m3 below or above it by chance; above zero stays above zero.
+__device__ __forceinline__ float up_or_down(float q, float up) {
+  // 2^(floor(log2 q) - 3), the spacing of e4m3 at q (2^-9 below 2^-6), from the exponent bits
+  const uint32_t e = __float_as_uint(fmaxf(q, 0x1p-6f)) & 0x7F800000u;
+  const float unit = __uint_as_float(e - (3u << 23)), per = __uint_as_float(0x7F000000u - (e - (3u << 23)));
+  const float low = floorf(q * per) * unit;
+  const float chosen = (q - low) * per + up >= 1.0f ? low + unit : low;
+  return q > 0.0f ? fminf(fmaxf(chosen, 0x1p-9f), 448.0f) : q;
+}
+
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Pack {
+  T v[N];
+};
+
+// Four values in a row; `full`: all four exist and the address is aligned for one access.
+template <typename T>
+__device__ __forceinline__ void get4(const T* p, int n, bool full, T (&v)[4]) {
+  if (full) {
+    const Pack<T, 4> x = *reinterpret_cast<const Pack<T, 4>*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = x.v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = i < n ? p[i] : T(0);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void put4(T* p, int n, bool full, const T (&v)[4]) {
+  if (full) {
+    Pack<T, 4> x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.v[i] = v[i];
+    *reinterpret_cast<Pack<T, 4>*>(p) = x;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) p[i] = v[i];
+  }
+}
+
+// Largest magnitude of a wave's values by their bits, so that a NaN among them wins.
+__device__ __forceinline__ float wave_largest(const float (&x)[4]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int k = 32; k; k >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, k));
+  return __uint_as_float(m);
+}
+
+__device__ __forceinline__ float scale_of(float largest) {
+  return (largest < 0x1p-100f ? 0x1p-100f : largest) * (1.0f / 448.0f);
+}
+
+__device__ __forceinline__ void unpack(uint32_t w, float (&x)[4]) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  x[0] = lo[0], x[1] = lo[1], x[2] = hi[0], x[3] = hi[1];
+}
+__device__ __forceinline__ float within(float q) { return q > 448.0f ? 448.0f : (q < -448.0f ? -448.0f : q); }   // keeps NaN
+__device__ __forceinline__ uint32_t pack(const float (&q)[4]) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(within(q[0]), within(q[1]), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(within(q[2]), within(q[3]), w, true);
+}
+
+// A workgroup takes a piece; a wave every fourth block of it, four values a lane.  Bound by memory.
+template <typename G, bool EIGHT>
+__global__ void __launch_bounds__(kThreads)
+adamw_kernel(const bppsa_adamw_tensor* __restrict__ tensors, const bppsa_adamw_piece* __restrict__ pieces, const Step c) {
+  const bppsa_adamw_piece piece = pieces[blockIdx.x];
+  const bppsa_adamw_tensor t = tensors[piece.tensor];
+  const int64_t first = (int64_t)piece.piece * kPiece;
+  const int count = (int)(t.n - first < kPiece ? t.n - first : kPiece);
+  const int lane = threadIdx.x & 63;
+  const float keep = (float)(1.0 - c.lr_exact * t.decay);
+  const bool aligned = (((uintptr_t)t.theta | ((uintptr_t)t.grad * (16 / (sizeof(G) * 4))) |
+                         (EIGHT ? ((uintptr_t)t.m | (uintptr_t)t.v) * 4 : (uintptr_t)t.m | (uintptr_t)t.v) |
+                         (uintptr_t)t.copy * 2) & 15) == 0;
+  for (int at = (threadIdx.x >> 6) * kBlock; at < count; at += kThreads / BPPSA_WAVE * kBlock) {
+    const int64_t i = first + at + lane * 4;
+    const int n = count - at - lane * 4;       // values that are left for this lane
+    const bool full = aligned && n >= 4;
+    G g[4];
+    float theta[4], m[4], v[4];
+    get4(static_cast<const G*>(t.grad) + i, n, full, g);
+    get4(t.theta + i, n, full, theta);
+    if constexpr (EIGHT) {
+      uint8_t wm[4], wv[4];
+      get4(static_cast<const uint8_t*>(t.m) + i, n, full, wm);
+      get4(static_cast<const uint8_t*>(t.v) + i, n, full, wv);
+      const float sm = t.m_scale[(first + at) / kBlock], sv = t.v_scale[(first + at) / kBlock];
+      unpack(__builtin_bit_cast(uint32_t, wm), m);
+      unpack(__builtin_bit_cast(uint32_t, wv), v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m[k] *= sm, v[k] *= sv, v[k] *= v[k];
+    } else {
+      get4(static_cast<const float*>(t.m) + i, n, full, m);
+      get4(static_cast<const float*>(t.v) + i, n, full, v);
+    }
+    float root[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float gk = static_cast<float>(g[k]);
+      m[k] = fmaf(c.one_minus_beta1, gk, c.beta1 * m[k]);
+      v[k] = fmaf(c.one_minus_beta2, gk * gk, c.beta2 * v[k]);
+      root[k] = sqrtf(v[k]);
+      theta[k] = fmaf(theta[k], keep, -c.lr * ((m[k] / c.correct1) / (root[k] / c.root_correct2 + c.eps)));
+    }
+    put4(t.theta + i, n, full, theta);
+    if (t.copy) {
+      bf16_t small[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) small[k] = static_cast<bf16_t>(theta[k]);
+      put4(static_cast<bf16_t*>(t.copy) + i, n, full, small);
+    }
+    if constexpr (EIGHT) {
+      const float sm = scale_of(wave_largest(m)), sv = scale_of(wave_largest(root));
+      const float im = 1.0f / sm, iv = 1.0f / sv;
+      const uint32_t place = c.seed * 0x9E3779B1u + (uint32_t)piece.tensor * 0x6A09E667u + (uint32_t)i;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        m[k] *= im;
+        root[k] = up_or_down(root[k] * iv, chance(place + k));
+      }
+      put4(static_cast<uint8_t*>(t.m) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(m)).v);
+      put4(static_cast<uint8_t*>(t.v) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(root)).v);
+      if (lane == 0) t.m_scale[(first + at) / kBlock] = sm, t.v_scale[(first + at) / kBlock] = sv;
+    } else {
+      put4(static_cast<float*>(t.m) + i, n, full, m);
+      put4(static_cast<float*>(t.v) + i, n, full, v);
+    }
+  }
+}
+
+}  // namespace
+
+extern "C" int64_t bppsa_adamw_pieces(int n_tensors, const int64_t* n, bppsa_adamw_piece* pieces) {
+  if (n_tensors < 1 || !n) return 0;
+  int64_t count = 0;
+  for (int k = 0; k < n_tensors; ++k) {
+    if (n[k] < 0 || n[k] > (int64_t)1 << 40) return 0;
+    for (int64_t p = 0; p * kPiece < n[k]; ++p, ++count)
+      if (pieces) pieces[count] = bppsa_adamw_piece{k, (int32_t)p};
+  }
+  return count;
+}
+
+extern "C" bppsa_status bppsa_adamw_step(int n_tensors, const bppsa_adamw_tensor* tensors, int64_t n_pieces,
+                                         const bppsa_adamw_piece* pieces, int grad_type, int state_bits, int step, double lr,
+                                         double beta1, double beta2, double eps, uint32_t seed, void* stream) {
+  if (n_tensors < 1 || !tensors || n_pieces < 1 || !pieces || step < 1) return BPPSA_EINVAL;
+  if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps > 0) || !std::isfinite(lr)) return BPPSA_EINVAL;
+  if (state_bits != 32 && state_bits != 8) return BPPSA_EUNSUPPORTED;
+  if (n_pieces > 0x7FFFFFFF) return BPPSA_EOVERFLOW;
+  const Step c{(float)beta1, (float)(1 - beta1), (float)beta2, (float)(1 - beta2), (float)(1 - std::pow(beta1, step)),
+               (float)std::sqrt(1 - std::pow(beta2, step)), (float)eps, (float)lr, lr, seed};
+  return ssm::by_type(grad_type, [&](auto g) -> bppsa_status {
+    using G = decltype(g);
+    if (state_bits == 8)
+      adamw_kernel<G, true><<<(unsigned)n_pieces, kThreads, 0, (hipStream_t)stream>>>(tensors, pieces, c);
+    else
+      adamw_kernel<G, false><<<(unsigned)n_pieces, kThreads, 0, (hipStream_t)stream>>>(tensors, pieces, c);
+    BPPSA_CHECK_LAUNCH();
+    return BPPSA_OK;
+  });
+}

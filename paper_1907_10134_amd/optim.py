@@ -1,0 +1,89 @@
+"""ctypes binding of the optimiser over many tensors (bppsa_adamw_step in include/bppsa.h)."""
+from __future__ import annotations
+
+import ctypes
+import struct
+
+import torch
+
+from .binding import _check, _lib, _ptr, _stream
+
+BLOCK = 256                        # BPPSA_ADAMW_BLOCK
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+_c_int, _c_void_p, _c_double, _c_int64 = ctypes.c_int, ctypes.c_void_p, ctypes.c_double, ctypes.c_int64
+_lib.bppsa_adamw_pieces.restype = _c_int64
+_lib.bppsa_adamw_pieces.argtypes = [_c_int, _c_void_p, _c_void_p]
+_lib.bppsa_adamw_step.restype = _c_int
+_lib.bppsa_adamw_step.argtypes = [_c_int, _c_void_p, _c_int64, _c_void_p, _c_int, _c_int, _c_int] + [_c_double] * 4 + \
+    [ctypes.c_uint32, _c_void_p]
+
+
+class AdamW:
+    """AdamW over many tensors by one launch a step, with the moments in 32 bits or in 8.
+
+    params: contiguous float32 tensors, updated in place; grads: their gradients, contiguous, all of one type (float32,
+    bfloat16 or float16), read where they are at every step; copies: bfloat16 tensors that receive the new parameters, or
+    None.  weight_decay: one number or one for each tensor.  `state` (made here unless given) is a dict of lists, a tensor for
+    each parameter: "m" and "v", float32; with state_bits=8 float8_e4m3fn, with "m_scale" and "v_scale", float32 of one value
+    for each 256, and "v" then stands for the root of the second moment.  The tensors' addresses are taken once, here: replace
+    their values, not the tensors.  `t` counts the steps; lr, beta1, beta2 and eps are read at every step."""
+
+    def __init__(self, params, grads, state_bits=32, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, copies=None,
+                 state=None):
+        params, grads = list(params), list(grads)
+        if not params or len(params) != len(grads):
+            raise ValueError("AdamW needs as many gradients as parameters, and one at least")
+        if state_bits not in (32, 8):
+            raise ValueError("state_bits must be 32 or 8, got %r" % (state_bits,))
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(params)
+        if len(decay) != len(params) or (copies is not None and len(copies) != len(params)):
+            raise ValueError("weight_decay and copies need one entry for each parameter")
+        if not isinstance(grads[0], torch.Tensor) or grads[0].dtype not in _TYPES:
+            raise ValueError("gradients must be float32, bfloat16 or float16 tensors")
+        self.params, self.grads, self.copies = params, grads, None if copies is None else list(copies)
+        self.state_bits, self.lr, self.beta1, self.beta2, self.eps, self.t = state_bits, lr, beta1, beta2, eps, 0
+        kind = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+        names = {"m": kind, "v": kind}
+        if state_bits == 8:
+            names.update(m_scale=torch.float32, v_scale=torch.float32)
+        size = lambda p, name: -(-p.numel() // BLOCK) if name.endswith("scale") else p.numel()
+        if state is None:
+            make = lambda p, name, t: torch.zeros(size(p, name), dtype=torch.uint8 if t is torch.float8_e4m3fn else t,
+                                                  device=p.device).view(t)
+            state = {name: [make(p, name, t) for p in params] for name, t in names.items()}
+        if set(state) != set(names) or any(len(x) != len(params) for x in state.values()):
+            raise ValueError("state must hold %s for each parameter" % ", ".join(names))
+        self.state = {name: list(x) for name, x in state.items()}
+        device, self._grad_type, rows, lengths = params[0].device, _TYPES[grads[0].dtype], [], []
+        for k, p in enumerate(params):
+            n = p.numel() if isinstance(p, torch.Tensor) else 0
+            known = [("params[%d]" % k, p, torch.float32, n), ("grads[%d]" % k, grads[k], grads[0].dtype, n)]
+            known += [("state[%r][%d]" % (name, k), self.state[name][k], t, size(p, name) if n else 0) for name, t in names.items()]
+            if copies is not None:
+                known.append(("copies[%d]" % k, copies[k], torch.bfloat16, n))
+            at = {}
+            for name, x, t, count in known:
+                at[name.split("[")[0] if "state" not in name else name.split("'")[1]] = _ptr(x, t, name)
+                if x is None or x.numel() != count or x.device != device:
+                    raise ValueError("%s must have %d values on %s" % (name, count, device))
+            rows.append(struct.pack("@7Pqd", at["params"], at["grads"], at["m"], at["v"], at.get("m_scale", 0),
+                                    at.get("v_scale", 0), at.get("copies", 0), n, float(decay[k])))
+            lengths.append(n)
+        n = (ctypes.c_int64 * len(params))(*lengths)
+        self._n_pieces = int(_lib.bppsa_adamw_pieces(len(params), n, None))
+        if self._n_pieces < 1:
+            raise ValueError("AdamW: nothing to update")
+        pieces = torch.empty((self._n_pieces, 2), dtype=torch.int32)
+        _lib.bppsa_adamw_pieces(len(params), n, pieces.data_ptr())
+        self._pieces = pieces.to(device)
+        self._tensors = torch.frombuffer(bytearray(b"".join(rows)), dtype=torch.uint8).to(device)
+
+    def step(self, seed=None, stream=None):
+        """One update.  With 8-bit moments `seed` (the number of the step unless given) decides which roots go up."""
+        t = self.t + 1
+        seed = t if seed is None else int(seed)
+        _check(_lib.bppsa_adamw_step(len(self.params), self._tensors.data_ptr(), self._n_pieces, self._pieces.data_ptr(),
+                                     self._grad_type, self.state_bits, t, self.lr, self.beta1, self.beta2, self.eps,
+                                     seed & 0xFFFFFFFF, _stream(stream)), "bppsa_adamw_step")
+        self.t = t

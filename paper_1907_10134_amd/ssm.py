@@ -1,0 +1,250 @@
+"""ctypes binding of the selective state space layer: the scan, the short convolution in front of it, their gradients and
+their steps for single tokens, with the names of the C ABI in include/bppsa.h.
+
+Activations are float32, bfloat16 or float16, all of one call the same, [T, B, channels] with the channels contiguous and any
+strides of time and sample; parameters, states and their gradients are contiguous float32.
+"""
+from __future__ import annotations
+
+import ctypes
+import struct
+from collections import namedtuple
+
+import torch
+
+from .binding import _check, _lib, _ptr, _stream, _workspace
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_i32 = torch.int32
+
+_c_int, _c_void_p, _c_size_t = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
+for _name, _res, _args in (
+        ("bppsa_ssm_scan_states_bytes", _c_size_t, [_c_int] * 4),
+        ("bppsa_ssm_scan_workspace_bytes", _c_size_t, [_c_int] * 5),
+        ("bppsa_ssm_scan", _c_int, [_c_void_p] * 5 + [_c_size_t, _c_void_p]),
+        ("bppsa_ssm_scan_backward_workspace_bytes", _c_size_t, [_c_int] * 5),
+        ("bppsa_ssm_scan_backward", _c_int, [_c_void_p] * 5 + [_c_size_t, _c_void_p]),
+        ("bppsa_ssm_scan_step", _c_int, [_c_void_p] * 3 + [_c_int] + [_c_void_p] * 2),
+        ("bppsa_ssm_conv", _c_int, [_c_void_p] * 4),
+        ("bppsa_ssm_conv_backward_workspace_bytes", _c_size_t, [_c_int] * 4),
+        ("bppsa_ssm_conv_backward", _c_int, [_c_void_p] * 7 + [_c_size_t, _c_void_p]),
+        ("bppsa_ssm_conv_step", _c_int, [_c_void_p] * 3 + [_c_int] + [_c_void_p] * 2)):
+    getattr(_lib, _name).restype = _res
+    getattr(_lib, _name).argtypes = _args
+
+# The C structs as bytes: a struct module's pack takes 1 us where a ctypes Structure of as many fields takes 6.
+_pack_rows = struct.Struct("@Pqq").pack
+_pack_layer = struct.Struct("@6i" + "Pqq" * 5 + "P" * 5).pack
+_pack_grads = struct.Struct("@" + "Pqq" * 3 + "P" * 6).pack
+_pack_conv = struct.Struct("@6iPqq" + "P" * 4).pack
+
+
+def _rows(t, shape, dtype, name, groups=False):
+    """(pointer, time stride, sample stride) of an activation [T, B, channels] or [T, B, G, N]."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must live on the GPU" % name)
+    if t.dtype is not dtype:
+        raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    s = t.stride()
+    if groups:
+        if (s[-1] != 1 and shape[-1] > 1) or (s[-2] != shape[-1] and shape[-2] > 1):
+            raise ValueError("%s must be contiguous in its last two dimensions" % name)
+    elif s[-1] != 1 and shape[-1] > 1:
+        raise ValueError("%s must be contiguous in its channels" % name)
+    return t.data_ptr(), s[0], s[1]
+
+
+def _param(t, shape, name, dtype=torch.float32):
+    if t is None:
+        return 0
+    p = _ptr(t, dtype, name)
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return p
+
+
+_NONE = (0, 0, 0)
+
+
+def _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths):
+    """The bytes of bppsa_ssm and (T, B, D, N, G)."""
+    if not (isinstance(u, torch.Tensor) and isinstance(Bm, torch.Tensor)):
+        raise TypeError("u and Bm must be torch.Tensors")
+    if u.dim() != 3 or Bm.dim() != 4:
+        raise ValueError("u must be [T, B, D] and Bm [T, B, G, N]")
+    T, B, D = u.shape
+    G, N = Bm.shape[2], Bm.shape[3]
+    t, wide, narrow = u.dtype, u.shape, (T, B, G, N)
+    if t not in _TYPES:
+        raise ValueError("activations must be float32, bfloat16 or float16, got %s" % t)
+    if A is None:
+        raise TypeError("A must be a torch.Tensor")
+    return _pack_layer(T, B, D, N, G, _TYPES[t], *_rows(u, wide, t, "u"), *_rows(dt, wide, t, "dt"),
+                       *(_NONE if z is None else _rows(z, wide, t, "z")), *_rows(Bm, narrow, t, "Bm", True),
+                       *_rows(Cm, narrow, t, "Cm", True), _param(A, (D, N), "A"), _param(skip, (D,), "skip"),
+                       _param(dt_bias, (D,), "dt_bias"), _param(h0, (B, D, N), "h0"),
+                       _param(lengths, (B,), "lengths", _i32)), (T, B, D, N, G)
+
+
+def _opaque(workspace, nbytes, device, stream):
+    """(tensor that has to live through the call, pointer, bytes) of a scratch array."""
+    if workspace is None:
+        if not nbytes:
+            return None, None, 0
+        workspace = _workspace(nbytes, device, stream)
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def ssm_scan_workspace_bytes(T, B, D, N, G):
+    return int(_lib.bppsa_ssm_scan_workspace_bytes(T, B, D, N, G))
+
+
+def ssm_scan_states(T, B, D, N, device="cuda"):
+    """The array that ssm_scan(states=) fills for ssm_scan_backward: bppsa_ssm_scan_states_bytes(T, B, D, N) bytes."""
+    n = int(_lib.bppsa_ssm_scan_states_bytes(T, B, D, N))
+    if not n:
+        raise ValueError("ssm_scan_states: no such sizes (%d, %d, %d, %d)" % (T, B, D, N))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _states(states, dims):
+    if states is None:
+        return None
+    if states.numel() * states.element_size() < _lib.bppsa_ssm_scan_states_bytes(*dims[:4]):
+        raise ValueError("states is too small for these sizes")
+    return _ptr(states, torch.uint8, "states")
+
+
+def ssm_scan(u, dt, A, Bm, Cm, skip=None, z=None, dt_bias=None, h0=None, lengths=None, y=None, h_last=None, states=None,
+             workspace=None, stream=None):
+    """bppsa_ssm_scan: y [T, B, D] of the selective scan of u under steps softplus(dt + dt_bias).
+
+    u, dt, z [T, B, D]; Bm, Cm [T, B, G, N]; A [D, N]; skip, dt_bias [D]; h0 [B, D, N]; lengths [B] int32.  h_last [B, D, N]
+    receives the last states, states (see ssm_scan_states) what ssm_scan_backward needs."""
+    layer, dims = _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
+    T, B, D, N, G = dims
+    if y is None:
+        y = torch.empty_like(u)
+    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_workspace_bytes(T, B, D, N, G), u.device, stream)
+    _check(_lib.bppsa_ssm_scan(layer, _pack_rows(*_rows(y, u.shape, u.dtype, "y")), _param(h_last, (B, D, N), "h_last"),
+                               _states(states, dims), ws, nbytes, _stream(stream)), "bppsa_ssm_scan")
+    return y
+
+
+SsmGrads = namedtuple("SsmGrads", "du ddt dA dBm dCm dskip dz ddt_bias dh0")
+
+
+def ssm_scan_backward_workspace_bytes(T, B, D, N, G):
+    return int(_lib.bppsa_ssm_scan_backward_workspace_bytes(T, B, D, N, G))
+
+
+def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=None, h0=None, lengths=None, dh0=None,
+                      workspace=None, stream=None):
+    """bppsa_ssm_scan_backward: the gradients of sum(y dy), as SsmGrads; the other arguments are those of the ssm_scan call
+    that filled `states`.  dskip, dz and ddt_bias are None where there is no such input; dh0 [B, D, N] is filled if given."""
+    layer, dims = _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
+    T, B, D, N, G = dims
+    if states is None:
+        raise TypeError("states must be the array that ssm_scan filled")
+    t, dev = u.dtype, u.device
+    f32 = dict(dtype=torch.float32, device=dev)
+    du, ddt = torch.empty_like(u), torch.empty_like(dt)
+    dz = None if z is None else torch.empty_like(u)
+    dBm, dCm = torch.empty((T, B, G, N), dtype=t, device=dev), torch.empty((T, B, G, N), dtype=t, device=dev)
+    dA = torch.empty((D, N), **f32)
+    dskip = None if skip is None else torch.empty((D,), **f32)
+    dbias = None if dt_bias is None else torch.empty((D,), **f32)
+    out = _pack_grads(*_rows(du, u.shape, t, "du"), *_rows(ddt, u.shape, t, "ddt"),
+                      *(_NONE if dz is None else _rows(dz, u.shape, t, "dz")), dBm.data_ptr(), dCm.data_ptr(), dA.data_ptr(),
+                      0 if dskip is None else dskip.data_ptr(), 0 if dbias is None else dbias.data_ptr(),
+                      _param(dh0, (B, D, N), "dh0"))
+    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_backward_workspace_bytes(T, B, D, N, G), dev, stream)
+    _check(_lib.bppsa_ssm_scan_backward(layer, _pack_rows(*_rows(dy, u.shape, t, "dy")), _states(states, dims), out, ws, nbytes,
+                                        _stream(stream)), "bppsa_ssm_scan_backward")
+    return SsmGrads(du, ddt, dA, dBm, dCm, dskip, dz, dbias, dh0)
+
+
+def _slots(slots, B, state, name="slots"):
+    if slots is None:
+        if state.shape[0] < B:
+            raise ValueError("state has fewer slots than the batch has rows")
+        return None
+    return _param(slots, (B,), name, _i32)
+
+
+def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slots=None, y=None, stream=None):
+    """bppsa_ssm_scan_step: y [B, D] of one token of each stream; state [slots, D, N] float32 is advanced in place.
+
+    u, dt, z [B, D]; Bm, Cm [B, G, N]; slots [B] int32, a row with one outside the state (-1, say) belongs to no stream."""
+    if y is None:
+        y = torch.empty_like(u)
+    up = lambda x: None if x is None else x.unsqueeze(0)
+    layer, (_, B, D, N, _) = _layer(up(u), up(dt), A, up(Bm), up(Cm), skip, up(z), dt_bias, None, None)
+    if state.dim() != 3 or state.shape[1:] != (D, N):
+        raise ValueError("state must be [slots, %d, %d], got %s" % (D, N, tuple(state.shape)))
+    _check(_lib.bppsa_ssm_scan_step(layer, _pack_rows(*_rows(up(y), (1, B, D), u.dtype, "y")),
+                                    _ptr(state, torch.float32, "state"), state.shape[0], _slots(slots, B, state),
+                                    _stream(stream)), "bppsa_ssm_scan_step")
+    return y
+
+
+def _conv(x, weight, bias, silu, state0, lengths):
+    if not (isinstance(x, torch.Tensor) and isinstance(weight, torch.Tensor)):
+        raise TypeError("x and weight must be torch.Tensors")
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x must be [T, B, D] and weight [D, W]")
+    T, B, D = x.shape
+    W = weight.shape[1]
+    if x.dtype not in _TYPES:
+        raise ValueError("activations must be float32, bfloat16 or float16, got %s" % x.dtype)
+    return _pack_conv(T, B, D, W, _TYPES[x.dtype], bool(silu), *_rows(x, x.shape, x.dtype, "x"), _param(weight, (D, W), "weight"),
+                      _param(bias, (D,), "bias"), _param(state0, (B, W - 1, D), "state0", x.dtype),
+                      _param(lengths, (B,), "lengths", _i32)), (T, B, D, W)
+
+
+def ssm_conv(x, weight, bias=None, silu=True, state0=None, lengths=None, y=None, state_last=None, stream=None):
+    """bppsa_ssm_conv: the causal convolution of x [T, B, D] with weight [D, W], channel by channel, and silu.
+
+    state0 [B, W-1, D] holds the inputs in front of the first; state_last, of the same shape, receives the last ones."""
+    conv, (_, B, D, W) = _conv(x, weight, bias, silu, state0, lengths)
+    if y is None:
+        y = torch.empty_like(x)
+    _check(_lib.bppsa_ssm_conv(conv, _pack_rows(*_rows(y, x.shape, x.dtype, "y")),
+                               _param(state_last, (B, W - 1, D), "state_last", x.dtype), _stream(stream)), "bppsa_ssm_conv")
+    return y
+
+
+SsmConvGrads = namedtuple("SsmConvGrads", "dx dweight dbias dstate0")
+
+
+def ssm_conv_backward(dy, x, weight, bias=None, silu=True, state0=None, lengths=None, dstate0=None, workspace=None,
+                      stream=None):
+    """bppsa_ssm_conv_backward: the gradients of sum(y dy), as SsmConvGrads; dstate0 [B, W-1, D] is filled if given."""
+    conv, (T, B, D, W) = _conv(x, weight, bias, silu, state0, lengths)
+    dx = torch.empty_like(x)
+    dweight = torch.empty((D, W), dtype=torch.float32, device=x.device)
+    dbias = None if bias is None else torch.empty((D,), dtype=torch.float32, device=x.device)
+    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_conv_backward_workspace_bytes(T, B, D, W), x.device, stream)
+    _check(_lib.bppsa_ssm_conv_backward(conv, _pack_rows(*_rows(dy, x.shape, x.dtype, "dy")),
+                                        _pack_rows(*_rows(dx, x.shape, x.dtype, "dx")), dweight.data_ptr(),
+                                        None if dbias is None else dbias.data_ptr(),
+                                        _param(dstate0, (B, W - 1, D), "dstate0", x.dtype), ws, nbytes, _stream(stream)),
+           "bppsa_ssm_conv_backward")
+    return SsmConvGrads(dx, dweight, dbias, dstate0)
+
+
+def ssm_conv_step(x, weight, bias, state, silu=True, slots=None, y=None, stream=None):
+    """bppsa_ssm_conv_step: y [B, D] of one token of each stream; state [slots, W-1, D] is moved on in place."""
+    if y is None:
+        y = torch.empty_like(x)
+    conv, (_, B, D, W) = _conv(x.unsqueeze(0), weight, bias, silu, None, None)
+    if state.dim() != 3 or state.shape[1:] != (W - 1, D):
+        raise ValueError("state must be [slots, %d, %d], got %s" % (W - 1, D, tuple(state.shape)))
+    _check(_lib.bppsa_ssm_conv_step(conv, _pack_rows(*_rows(y.unsqueeze(0), (1, B, D), x.dtype, "y")),
+                                    _ptr(state, x.dtype, "state"), state.shape[0], _slots(slots, B, state), _stream(stream)),
+           "bppsa_ssm_conv_step")
+    return y
