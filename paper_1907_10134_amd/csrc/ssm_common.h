@@ -1,6 +1,8 @@
 // Shared by the state space kernels: the types of activations, strided rows, the step's softplus and the gate.
 #pragma once
 
+#include <type_traits>
+
 #include "bppsa_internal.h"
 
 namespace ssm {
@@ -26,37 +28,51 @@ __device__ __forceinline__ float load(const E* p) { return static_cast<float>(*p
 template <typename E>
 __device__ __forceinline__ void store(E* p, float v) { *p = static_cast<E>(v); }
 
+// Element i of a row whose address is the same for the whole wave: the row in scalar registers, 32 bits of offset a lane.
+template <typename E>
+__device__ __forceinline__ E& element(E* row, uint32_t byte) {
+  return *reinterpret_cast<E*>(reinterpret_cast<std::conditional_t<std::is_const_v<E>, const char, char>*>(row) + byte);
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp, 2^x
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// exp(-|x|).  The product with log2(e) loses |x| 2^-24 of the result; its rounding and the constant's own come back as a
-// first-order term, which leaves v_exp_f32's error.
-__device__ __forceinline__ float exp_of_minus(float x) {
-  const float a = -fabsf(x), p = a * kLog2e;
-  float lost = fmaf(a, kLog2e, -p);
-  lost = fmaf(a, 1.92596299112661746887e-8f, lost);
+// exp(a) for a of at most 87.  EXACT: the product with log2(e) loses |x| 2^-24 of the
+// result; its rounding and the constant's own come back as a first-order term, which leaves v_exp_f32's error.  Without, for
+// activations of 16 bits, whose own rounding is 2^8 times as much.
+template <bool EXACT>
+__device__ __forceinline__ float exp_of(float a) {
+  const float p = a * kLog2e;
   const float e = exp2_fast(p);
-  return p < -150.0f ? 0.0f : fmaf(e, lost * 0.69314718055994530942f, e);      // an infinite x: infinity minus itself above
+  if (!EXACT) return e;
+  const float lost = fmaf(a, 1.92596299112661746887e-8f, fmaf(a, kLog2e, -p));
+  return a < -87.0f ? e : fmaf(e, lost * 0.69314718055994530942f, e);          // a = -infinity: p - p is none
 }
 
-// 1 / y, v_rcp_f32 and a correction: to half a step.
+// 1 / y, v_rcp_f32 (1 ulp) and a correction: to half a step.
+template <bool EXACT>
 __device__ __forceinline__ float reciprocal(float y) {
   const float r = __builtin_amdgcn_rcpf(y);
-  return fmaf(fmaf(-y, r, 1.0f), r, r);
+  return EXACT ? fmaf(fmaf(-y, r, 1.0f), r, r) : r;
 }
 
-// 1 / (1 + exp(-x)): exp of the negative magnitude only, so nothing overflows.
+template <typename E>
+constexpr bool kExact = sizeof(E) == 4;
+
+// 1 / (1 + exp(-x)), exp(-x) of 87 at most, which is finite.  A NaN counts as -87 here: it is a factor elsewhere wherever
+// this is one.
+template <typename E>
 __device__ __forceinline__ float sigmoid(float x) {
-  const float e = exp_of_minus(x), r = reciprocal(1.0f + e);
-  return x >= 0.0f ? r : e * r;
+  return reciprocal<kExact<E>>(1.0f + exp_of<kExact<E>>(fminf(-x, 87.0f)));
 }
 
 // max(x, 0) + log1p(exp(-|x|)).  log1p(e) = 2 atanh(s), s = e / (2 + e) <= 1/3, as an odd polynomial in s: log(1 + e)
 // by the logarithm instruction would lose the small steps (e = 1e-3 keeps 2^-14 of its value in 1 + e).
 // Series terms to s^15; the next is 2^-29 of the first at s = 1/3.
+template <typename E>
 __device__ __forceinline__ float softplus(float x) {
-  const float e = exp_of_minus(x);
-  const float s = e * reciprocal(2.0f + e);
+  const float e = exp_of<kExact<E>>(-fabsf(x));
+  const float s = e * reciprocal<kExact<E>>(2.0f + e);
   const float w = s * s;
   float p = 1.0f / 15;
   p = fmaf(p, w, 1.0f / 13);

@@ -50,7 +50,7 @@ conv_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state_last) {
     float p = bias;
 #pragma unroll
     for (int k = 0; k < W; ++k) p = fmaf(w[k], seen[k], p);
-    store(y.at(t, b) + d, t < len ? (c.silu ? p * sigmoid(p) : p) : 0.0f);
+    store(y.at(t, b) + d, t < len ? (c.silu ? p * sigmoid<E>(p) : p) : 0.0f);
   }
   if (state_last && blockIdx.z == 0)
 #pragma unroll
@@ -71,7 +71,7 @@ __device__ __forceinline__ float outer(const Conv<E>& c, const Rows<const E>& dy
   float p = bias;
 #pragma unroll
   for (int k = 0; k < W; ++k) p = fmaf(w[k], seen[k], p);
-  const float sg = sigmoid(p);
+  const float sg = sigmoid<E>(p);
   return g * sg * fmaf(p, 1.0f - sg, 1.0f);
 }
 
@@ -151,7 +151,7 @@ conv_step_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state, int slots_in
   }
 #pragma unroll
   for (int k = 0; k + 1 < W; ++k) s[(int64_t)k * c.D] = seen[k + 1];
-  store(y.at(0, b) + d, c.silu ? p * sigmoid(p) : p);
+  store(y.at(0, b) + d, c.silu ? p * sigmoid<E>(p) : p);
 }
 
 template <typename F>
