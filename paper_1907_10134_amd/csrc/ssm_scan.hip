@@ -1,19 +1,9 @@
-// The selective scan: forward over sequences, its gradients, and the step of single tokens.
+// The selective scan, forward: over sequences, and the step of single tokens.
 #include "ssm_scan_parts.h"
 
 namespace {
 
 using namespace ssm;
-
-// A long sequence with few channels is cut into spans.  A first launch scans each span from a state of zero and keeps
-// only where that ends and the sum of its steps; a channel's decay over a span is exp(A sum), so that the second launch
-// can join the spans in front of its own in a few multiply-adds and scan it from its true start.
-struct Summary {
-  float *ends, *sums;              // [span][b][wave][d][4], [span][b][d]
-};
-
-// Steps of a pass: a multiple of kKept that divides kPad.
-constexpr int pass_of(int waves) { return waves > 2 && waves <= 8 ? 16 : 8; }
 
 // One workgroup: 64 channels, one sample, one span, in passes of PASS steps.  In each pass a wave turns ROWS of the steps
 // into (s, s u) in LDS for all waves, all waves walk the PASS steps of their states and leave their share of the sum over
@@ -24,7 +14,7 @@ template <typename E, int WAVES, bool SUMMARY, bool GATE>
 __global__ void __launch_bounds__(WAVES * 64)
 scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, const float* __restrict__ coef,
             const Summary sum, const Spans spans) {
-  constexpr int PASS = pass_of(WAVES), ROWS = (PASS + WAVES - 1) / WAVES;   // a wave prepares and finishes ROWS steps
+  constexpr int PASS = kKept, ROWS = (PASS + WAVES - 1) / WAVES;   // a wave prepares and finishes ROWS steps
   __shared__ float2 step_in[2][PASS][kTile];
   __shared__ float share[SUMMARY ? 1 : 2][SUMMARY ? 1 : WAVES][SUMMARY ? 1 : PASS][kTile];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -165,157 +155,18 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   }
 }
 
-// Spans: as many as give every SIMD some four waves, none shorter than 64 steps (a multiple of 32), 64 at most.
-Spans spans_of(int T, int B, int D, int N, int G) {
-  const int64_t waves = (int64_t)G * bppsa_ceil_div(D / G, kTile) * B * waves_of(N);
-  int64_t count = (int64_t)bppsa_compute_units() * 4 * 3 / waves;
-  if (count > T / 64) count = T / 64;
-  if (count > 64) count = 64;
-  if (count < 2) return Spans{1, T};
-  const int steps = bppsa_ceil_div(bppsa_ceil_div(T, (int)count), kPad) * kPad;
-  return Spans{bppsa_ceil_div(T, steps), steps};
-}
-
 // The workspace of a forward call: Bm and Cm as floats, and the spans' summaries.
 struct Scratch {
   size_t coef, ends, sums, bytes;
   Spans spans;
-  Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G)) {
-    size_t at = 0;
-    auto take = [&](int64_t n) { const size_t o = at; at += bppsa_align_up((size_t)n * sizeof(float), 256); return o; };
+  Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G, 6)) {
+    Arena take;
     coef = take(coef_floats(T, B, N, G));
     const int64_t parts = spans.count > 1 ? (int64_t)spans.count * B * D : 0;
     ends = take(parts * waves_of(N) * kHeld), sums = take(parts);
-    bytes = at;
+    bytes = take.at;
   }
 };
-
-template <typename E>
-struct Grads {
-  Rows<E> du, ddt, dz;
-  float *bc, *dA, *dskip, *ddt_bias, *dh0;     // bc, dA, dskip and ddt_bias are partial sums, see Partials
-};
-
-// Sums that more than one workgroup has a part of: of dB and dC [tiles][T][B][G][2N], one part a tile of channels; of dA
-// [B][D][N], dskip and ddt_bias [B][D], one a sample.
-struct Partials {
-  size_t bc, dA, dskip, ddt_bias, bytes;
-  Partials(int64_t T, int64_t B, int64_t D, int64_t N, int64_t G) {
-    const int64_t tiles = (D / G + kTile - 1) / kTile;
-    size_t at = 0;
-    auto take = [&](int64_t n) { const size_t o = at; at += bppsa_align_up((size_t)n * sizeof(float), 256); return o; };
-    bc = take(tiles * T * B * G * 2 * N), dA = take(B * D * N), dskip = take(B * D), ddt_bias = take(B * D);
-    bytes = at;
-  }
-};
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k);
-  return v;
-}
-
-template <typename E, int NP>
-__global__ void __launch_bounds__(kTile)
-scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ states, int waves, const Grads<E> o) {
-  const int g = blockIdx.x / l.tiles, tile = blockIdx.x % l.tiles, in = tile * kTile + threadIdx.x, b = blockIdx.y;
-  const bool on = in < l.wide;                 // lanes beyond the group's last channel take part in the sums with zeros
-  const int d = on ? g * l.wide + in : g * l.wide, len = clamp_length(l.lengths, b, l.T);
-  const int64_t bd = (int64_t)b * l.D + d;
-  float A2[NP], A[NP], carry[NP], dA[NP];
-#pragma unroll
-  for (int n = 0; n < NP; ++n) {
-    A[n] = n < l.N ? l.A[(int64_t)d * l.N + n] : 0.0f;
-    A2[n] = A[n] * kLog2e;
-    carry[n] = dA[n] = 0.0f;
-  }
-  const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f, skip = l.skip ? l.skip[d] : 0.0f;
-  float dskip = 0.0f, dbias = 0.0f;
-  float* bc = o.bc + (int64_t)tile * l.T * l.B * l.G * 2 * l.N;
-  for (int t = len; t < l.T; ++t) {
-    if (on) {
-      store(o.du.at(t, b) + d, 0.0f), store(o.ddt.at(t, b) + d, 0.0f);
-      if (o.dz.data) store(o.dz.at(t, b) + d, 0.0f);
-    }
-    for (int n = threadIdx.x; n < 2 * l.N; n += kTile) bc[(((int64_t)t * l.B + b) * l.G + g) * 2 * l.N + n] = 0.0f;
-  }
-  for (int k = (len + kKept - 1) / kKept - 1; k >= 0; --k) {
-    float h[kKept + 1][NP];
-#pragma unroll
-    for (int n = 0; n < NP; ++n) h[0][n] = n < l.N ? states[state_at(k, l.B, b, waves, n / kHeld, l.D, d) + n % kHeld] : 0.0f;
-    const int steps = len - k * kKept < kKept ? len - k * kKept : kKept;
-    for (int i = 0; i < steps; ++i) {
-      const int t = k * kKept + i;
-      const float s = softplus<E>(load(l.dt.at(t, b) + d) + bias), su = s * load(l.u.at(t, b) + d);
-      const E* Bt = l.Bm.at(t, b) + g * l.N;
-#pragma unroll
-      for (int n = 0; n < NP; ++n)
-        h[i + 1][n] = n < l.N ? fmaf(exp2_fast(s * A2[n]), h[i][n], su * load(Bt + n)) : 0.0f;
-    }
-    for (int i = steps - 1; i >= 0; --i) {
-      const int t = k * kKept + i;
-      const float u = load(l.u.at(t, b) + d), raw = load(l.dt.at(t, b) + d) + bias, s = softplus<E>(raw), su = s * u;
-      const E *Bt = l.Bm.at(t, b) + g * l.N, *Ct = l.Cm.at(t, b) + g * l.N;
-      const float go = load(dy.at(t, b) + d), z = l.z.data ? load(l.z.at(t, b) + d) : 0.0f;
-      const float sg = sigmoid<E>(z), q = l.z.data ? go * z * sg : go;
-      float s1 = 0.0f, s2 = 0.0f, plain = skip * u;
-#pragma unroll
-      for (int n = 0; n < NP; ++n)
-        if (n < l.N) {
-          const float Bn = load(Bt + n), Cn = load(Ct + n);
-          const float gh = fmaf(q, Cn, carry[n]);
-          carry[n] = exp2_fast(s * A2[n]) * gh;
-          const float ga = carry[n] * h[i][n];
-          plain = fmaf(Cn, h[i + 1][n], plain);
-          s1 = fmaf(gh, Bn, s1);
-          s2 = fmaf(ga, A[n], s2);
-          dA[n] = fmaf(ga, s, dA[n]);
-          const float sumB = wave_sum(on ? gh * su : 0.0f), sumC = wave_sum(on ? h[i + 1][n] * q : 0.0f);
-          if (threadIdx.x == 0) {
-            float* at = bc + (((int64_t)t * l.B + b) * l.G + g) * 2 * l.N;
-            at[n] = sumB, at[l.N + n] = sumC;
-          }
-        }
-      const float ddt = fmaf(u, s1, s2) * sigmoid<E>(raw);
-      dbias += ddt;
-      dskip = fmaf(q, u, dskip);
-      if (on) {
-        store(o.du.at(t, b) + d, fmaf(s, s1, skip * q)), store(o.ddt.at(t, b) + d, ddt);
-        if (o.dz.data) store(o.dz.at(t, b) + d, go * plain * sg * fmaf(z, 1.0f - sg, 1.0f));
-      }
-    }
-  }
-  if (!on) return;
-#pragma unroll
-  for (int n = 0; n < NP; ++n)
-    if (n < l.N) {
-      o.dA[bd * l.N + n] = dA[n];
-      if (o.dh0) o.dh0[bd * l.N + n] = carry[n];
-    }
-  o.dskip[bd] = dskip, o.ddt_bias[bd] = dbias;
-}
-
-// dB and dC from the tiles' parts, in the tiles' order.
-template <typename E>
-__global__ void __launch_bounds__(256)
-join_bc_kernel(const float* __restrict__ bc, int tiles, int64_t rows, int N, E* __restrict__ dBm, E* __restrict__ dCm) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = rows * 2 * N;
-  if (i >= all) return;
-  float sum = 0.0f;
-  for (int k = 0; k < tiles; ++k) sum += bc[k * all + i];
-  const int64_t row = i / (2 * N);
-  const int n = (int)(i - row * 2 * N);
-  store((n < N ? dBm : dCm) + row * N + (n < N ? n : n - N), sum);
-}
-
-__global__ void __launch_bounds__(256)
-join_kernel(const float* __restrict__ parts, int count, int64_t n, float* __restrict__ out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float sum = 0.0f;
-  for (int k = 0; k < count; ++k) sum += parts[k * n + i];
-  out[i] = sum;
-}
 
 template <typename E>
 __global__ void __launch_bounds__(kTile)
@@ -342,34 +193,6 @@ scan_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int slo
     sum *= z * sigmoid<E>(z);
   }
   store(y.at(0, b) + d, sum);
-}
-
-template <typename F>
-bppsa_status by_states(int N, F&& f) {
-  if (N <= 4) return f(std::integral_constant<int, 4>{});
-  if (N <= 8) return f(std::integral_constant<int, 8>{});
-  if (N <= 16) return f(std::integral_constant<int, 16>{});
-  if (N <= 32) return f(std::integral_constant<int, 32>{});
-  return f(std::integral_constant<int, 64>{});
-}
-
-bool sizes_ok(int T, int B, int D, int N, int G) {
-  return T > 0 && B > 0 && D > 0 && N > 0 && G > 0 && N <= BPPSA_SSM_MAX_N && D % G == 0;
-}
-
-bppsa_status check_layer(const bppsa_ssm* l) {
-  if (!l || l->T < 1 || l->B < 1 || l->D < 1 || l->N < 1 || l->G < 1) return BPPSA_EINVAL;
-  if (!l->u.data || !l->dt.data || !l->Bm.data || !l->Cm.data || !l->A) return BPPSA_EINVAL;
-  if (l->D % l->G) return BPPSA_ESHAPE;
-  if (l->N > BPPSA_SSM_MAX_N || l->type < BPPSA_F32 || l->type > BPPSA_F16) return BPPSA_EUNSUPPORTED;
-  if (bppsa_mul_overflows(l->T, l->B, l->D, 2) || bppsa_mul_overflows(l->B, l->D, l->N, 1) || l->B > 65535)
-    return BPPSA_EOVERFLOW;
-  return BPPSA_OK;
-}
-
-bppsa_status check_workspace(const void* workspace, size_t have, size_t need) {
-  if (need && (!workspace || have < need)) return BPPSA_EWORKSPACE;
-  return need && ((uintptr_t)workspace & 255) ? BPPSA_EINVAL : BPPSA_OK;
 }
 
 }  // namespace
@@ -407,44 +230,6 @@ extern "C" bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows*
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     });
-  });
-}
-
-extern "C" size_t bppsa_ssm_scan_backward_workspace_bytes(int T, int B, int D, int N, int G) {
-  return sizes_ok(T, B, D, N, G) ? Partials(T, B, D, N, G).bytes : 0;
-}
-
-extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bppsa_rows* dy, const void* states,
-                                                const bppsa_ssm_grads* grads, void* workspace, size_t workspace_bytes,
-                                                void* stream) {
-  BPPSA_TRY(check_layer(layer));
-  if (!dy || !dy->data || !states || !grads || !grads->dBm || !grads->dCm || !grads->dA) return BPPSA_EINVAL;
-  if (!writable(grads->du, layer->T, layer->B) || !writable(grads->ddt, layer->T, layer->B)) return BPPSA_EINVAL;
-  if (!layer->z.data != !grads->dz.data || (layer->z.data && !writable(grads->dz, layer->T, layer->B))) return BPPSA_EINVAL;
-  const Partials at(layer->T, layer->B, layer->D, layer->N, layer->G);
-  BPPSA_TRY(check_workspace(workspace, workspace_bytes, at.bytes));
-  const hipStream_t s = (hipStream_t)stream;
-  return by_type(layer->type, [&](auto e) -> bppsa_status {
-    using E = decltype(e);
-    const Layer<E> l = layer_of<E>(*layer);
-    auto part = [&](size_t o) { return reinterpret_cast<float*>(static_cast<char*>(workspace) + o); };
-    const Grads<E> o{rows_of<E>(grads->du), rows_of<E>(grads->ddt), rows_of<E>(grads->dz), part(at.bc), part(at.dA),
-                     part(at.dskip), part(at.ddt_bias), grads->dh0};
-    BPPSA_TRY(by_states(l.N, [&](auto np) {
-      scan_backward_kernel<E, np.value><<<dim3(l.G * l.tiles, l.B), kTile, 0, s>>>(
-          l, rows_of<const E>(*dy), static_cast<const float*>(states), waves_of(l.N), o);
-      BPPSA_CHECK_LAUNCH();
-      return BPPSA_OK;
-    }));
-    const int64_t rows = (int64_t)l.T * l.B * l.G;
-    join_bc_kernel<E><<<(unsigned)((rows * 2 * l.N + 255) / 256), 256, 0, s>>>(
-        o.bc, l.tiles, rows, l.N, static_cast<E*>(grads->dBm), static_cast<E*>(grads->dCm));
-    auto join = [&](const float* parts, int64_t n, float* out) {
-      if (out) join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(parts, l.B, n, out);
-    };
-    join(o.dA, (int64_t)l.D * l.N, grads->dA), join(o.dskip, l.D, grads->dskip), join(o.ddt_bias, l.D, grads->ddt_bias);
-    BPPSA_CHECK_LAUNCH();
-    return BPPSA_OK;
   });
 }
 

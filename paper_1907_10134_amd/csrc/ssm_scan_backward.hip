@@ -1,0 +1,471 @@
+// The selective scan's gradients.
+//
+// With q = dy silu(z) and g[t] = dL/dh[t] = q C[t] + a[t+1] g[t+1], the walk from the end carries w[t] = a[t] g[t], and per
+// state
+//     dB[t] += g s u, dC[t] += h q (sums over the channels), dA += w h[t-1] s (over time and samples),
+//     du = s sum_n g B + skip q,  ddt = (u sum_n g B + sum_n w h[t-1] A) sigmoid(raw),
+//     dz = dy (sum_n C h + skip u) silu'(z).
+// The forward call kept the states every kKept steps, so h and a of a pass of so many steps are found again in registers.
+#include "ssm_scan_parts.h"
+
+namespace {
+
+using namespace ssm;
+
+template <typename E>
+struct Grads {
+  Rows<E> du, ddt, dz;
+  float *bc, *dA, *dskip, *ddt_bias, *dh0;     // all but dh0 parts of sums, see Scratch
+};
+
+constexpr int PASS = kKept;
+
+// Sums over the wave's 64 lanes of the 8 products of each of 8 steps; lane l is left with product `bits reversed(l)` of the
+// 64, counted 8 step + 2 state + (0: dB, 1: dC).  A level halves the registers and doubles the lanes that are summed: two
+// registers exchange halves and are added, one slot a register and level, 126 in all, where 64 full sums would take 384.
+// Levels one to three run as soon as a step's products are there.
+__device__ __forceinline__ float swap32_add(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float swap16_add(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// Lanes 0-7 of a row of 16: a summed with lanes 8-15; lanes 8-15: b.  (A DPP read of a register needs two wait states behind
+// the write of it, which the compiler does not count inside asm.)
+__device__ __forceinline__ float half_row_add(float a, float b) {
+  float t;
+  asm("s_nop 1\n\t"
+      "v_add_f32_dpp %0, %1, %1 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+      "v_add_f32_dpp %0, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xc"
+      : "=&v"(t) : "v"(a), "v"(b));
+  return t;
+}
+// Even fours of lanes: a summed with the next four; odd ones: b with the four before.
+__device__ __forceinline__ float four_add(float a, float b) {
+  float t;
+  asm("s_nop 1\n\t"
+      "v_add_f32_dpp %0, %1, %1 row_shl:4 row_mask:0xf bank_mask:0x5\n\t"
+      "v_add_f32_dpp %0, %2, %2 row_shr:4 row_mask:0xf bank_mask:0xa"
+      : "=&v"(t) : "v"(a), "v"(b));
+  return t;
+}
+template <int QUAD_PERM>
+__device__ __forceinline__ float in_four_add(float a, float b, bool second) {
+  const float keep = second ? b : a, give = second ? a : b;
+  return keep + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(give), QUAD_PERM, 0xf, 0xf, true));
+}
+__host__ __device__ __forceinline__ int product_of_lane(int lane) {
+  return (lane & 1) << 5 | (lane & 2) << 3 | (lane & 4) << 1 | (lane & 8) >> 1 | (lane & 16) >> 3 | (lane & 32) >> 5;
+}
+
+// Where a span's walk from its end with nothing carried in arrives, and the sum of its steps; the cut and the passes are
+// those of the main kernel below.
+template <typename E, int WAVES, bool GATE>
+__global__ void __launch_bounds__(WAVES * 64)
+scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ coef, const Summary sum,
+                             const Spans spans) {
+  constexpr int ROWS = (PASS + WAVES - 1) / WAVES;
+  __shared__ float2 step_in[2][PASS][kTile];             // (s, q)
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int span = blockIdx.x % (spans.count - 1) + 1, tile = blockIdx.x / (spans.count - 1), g = tile / l.tiles, b = blockIdx.y;
+  const int in = tile % l.tiles * kTile + lane;
+  const bool on = in < l.wide;
+  const int d = g * l.wide + (on ? in : 0);
+  const int len = clamp_length(l.lengths, b, l.T), t0 = span * spans.steps;
+  const int t1 = t0 + spans.steps < l.T ? t0 + spans.steps : l.T, stop = t1 < len ? t1 : len;
+  float A2[kHeld], carry[kHeld], total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int n = w * kHeld + i;
+    A2[i] = n < l.N ? l.A[(int64_t)d * l.N + n] * kLog2e : 0.0f;
+    carry[i] = 0.0f;
+  }
+  const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f;
+  const uint32_t byte = (uint32_t)d * sizeof(E);
+  E dt[ROWS], go[ROWS], z[ROWS];
+  auto fetch = [&](int first) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int t = first + w * ROWS + r, at = t < stop ? t : stop - 1;
+      dt[r] = element(l.dt.at(at, b), byte), go[r] = element(dy.at(at, b), byte);
+      if (GATE) z[r] = element(l.z.at(at, b), byte);
+    }
+  };
+  auto prepare = [&](int first, int buffer) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (w * ROWS + r >= PASS) break;
+      const bool real = first + w * ROWS + r < stop;
+      const float s = real ? softplus<E>((float)dt[r] + bias) : 0.0f;
+      float q = (float)go[r];
+      if (GATE) q *= (float)z[r] * sigmoid<E>((float)z[r]);
+      total += s;
+      step_in[buffer][w * ROWS + r][lane] = make_float2(s, real ? q : 0.0f);
+    }
+  };
+  const int padded = (l.T + kPad - 1) / kPad * kPad;
+  const int passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0;
+  const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + t0 + (int64_t)(passes - 1) * PASS) * 2 * kHeld;
+  Coef now, next;
+  if (passes) {
+    fetch(t0 + (passes - 1) * PASS);
+    prepare(t0 + (passes - 1) * PASS, (passes - 1) & 1);
+    now.ask(from + kBatch * 2 * kHeld);
+  }
+  __syncthreads();
+  for (int p = passes - 1; p >= 0; --p) {
+    const int first = t0 + p * PASS, buffer = p & 1;
+    float2 in_now[kBatch], in_next[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) in_now[i] = step_in[buffer][PASS - kBatch + i][lane];
+    if (p) fetch(first - PASS);
+#pragma unroll
+    for (int j = PASS - kBatch; j >= 0; j -= kBatch) {
+      wait_for_scalars();
+      next.ask(from + (j ? j - kBatch : p ? -kBatch : 0) * 2 * kHeld);
+      if (j)
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) in_next[i] = step_in[buffer][j - kBatch + i][lane];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = kBatch - 1; i >= 0; --i)
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) carry[k] = exp2_fast(in_now[i].x * A2[k]) * fmaf(in_now[i].y, now.C(i, k), carry[k]);
+      __builtin_amdgcn_sched_barrier(0);
+      now = next;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) in_now[i] = in_next[i];
+    }
+    from -= PASS * 2 * kHeld;
+    if (p) prepare(first - PASS, buffer ^ 1);
+    __syncthreads();
+  }
+  static_assert(sizeof(step_in) >= WAVES * kTile * sizeof(float));
+  float* totals = &step_in[0][0][0].x;
+  totals[w * kTile + lane] = total;
+  __syncthreads();
+  if (!on) return;
+  *reinterpret_cast<float4*>(sum.ends + state_at(span, l.B, b, WAVES, w, l.D, d)) = make_float4(carry[0], carry[1], carry[2], carry[3]);
+  if (w == 0) {
+    for (int k = 1; k < WAVES; ++k) total += totals[k * kTile + lane];
+    sum.sums[((int64_t)span * l.B + b) * l.D + d] = total;
+  }
+}
+
+// The cut of the work is the forward kernel's; the passes run from the span's end.  In a pass every wave first finds a and h
+// of its states, then walks back; the sums over the states go through LDS (s1 = sum g B, s2 = sum w h A, and with a gate
+// sum C h), those over the channels through registers.
+template <typename E, int WAVES, bool GATE>
+__global__ void __launch_bounds__(WAVES * 64)
+scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ states, const float* __restrict__ coef,
+                     const Summary sum, const Spans spans, const Grads<E> o) {
+  constexpr int ROWS = (PASS + WAVES - 1) / WAVES, SUMS = GATE ? 3 : 2;
+  // with many waves one set of shares has to do (160 KB of LDS), and a second barrier a pass keeps it
+  constexpr int SETS = WAVES <= 4 ? 2 : 1;
+  __shared__ float2 step_in[2][PASS][kTile];             // (s, s u)
+  __shared__ float step_q[2][PASS][kTile];
+  __shared__ float share[SETS][SUMS][WAVES][PASS][kTile];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int span = blockIdx.x % spans.count, tile = blockIdx.x / spans.count, g = tile / l.tiles, b = blockIdx.y;
+  const int in = tile % l.tiles * kTile + lane;
+  const bool on = in < l.wide;                           // lanes without a channel count in the sums with s u = q = 0
+  const int d = g * l.wide + (on ? in : 0);
+  const int len = clamp_length(l.lengths, b, l.T), t0 = span * spans.steps;
+  const int t1 = t0 + spans.steps < l.T ? t0 + spans.steps : l.T, stop = t1 < len ? t1 : len;
+
+  float A[kHeld], A2[kHeld], carry[kHeld], dA[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int n = w * kHeld + i;
+    A[i] = n < l.N ? l.A[(int64_t)d * l.N + n] : 0.0f;
+    A2[i] = A[i] * kLog2e;
+    carry[i] = dA[i] = 0.0f;
+  }
+  for (int k = spans.count - 1; k > span; --k) {
+    const float4 end = *reinterpret_cast<const float4*>(sum.ends + state_at(k, l.B, b, WAVES, w, l.D, d));
+    const float s = sum.sums[((int64_t)k * l.B + b) * l.D + d];
+    carry[0] = fmaf(exp2_fast(A2[0] * s), carry[0], end.x), carry[1] = fmaf(exp2_fast(A2[1] * s), carry[1], end.y);
+    carry[2] = fmaf(exp2_fast(A2[2] * s), carry[2], end.z), carry[3] = fmaf(exp2_fast(A2[3] * s), carry[3], end.w);
+  }
+
+  const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f, skip = l.skip ? l.skip[d] : 0.0f;
+  const uint32_t byte = (uint32_t)d * sizeof(E);
+  float dskip = 0.0f, dbias = 0.0f;
+  E u[ROWS], dt[ROWS], go[ROWS], z[ROWS];
+  struct Row {                                           // of a step: what its outputs are made of
+    float s, u, q, slope, gate;                          // slope: sigmoid(raw), gate: dy silu'(z)
+  } row[ROWS], was[ROWS];
+  float4 kept;
+  auto fetch = [&](int first) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int t = first + w * ROWS + r, at = t < stop ? t : stop - 1;
+      u[r] = element(l.u.at(at, b), byte), dt[r] = element(l.dt.at(at, b), byte), go[r] = element(dy.at(at, b), byte);
+      if (GATE) z[r] = element(l.z.at(at, b), byte);
+    }
+    kept = *reinterpret_cast<const float4*>(states + state_at(first / kKept, l.B, b, WAVES, w, l.D, d));
+  };
+  auto prepare = [&](int first, int buffer) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (w * ROWS + r >= PASS) break;
+      const bool real = on && first + w * ROWS + r < stop;
+      const float raw = (float)dt[r] + bias;
+      Row v{softplus<E>(raw), (float)u[r], (float)go[r], sigmoid<E>(raw), 0.0f};
+      if (GATE) {
+        const float x = (float)z[r], sg = sigmoid<E>(x);
+        v.gate = v.q * sg * fmaf(x, 1.0f - sg, 1.0f);
+        v.q *= x * sg;                                   // silu(z) first, as the forward pass has it
+      }
+      if (!real) v = Row{0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      row[r] = v;
+      step_in[buffer][w * ROWS + r][lane] = make_float2(v.s, v.s * v.u);
+      step_q[buffer][w * ROWS + r][lane] = v.q;
+    }
+  };
+  auto finish = [&](int first, int set) {
+    float du[ROWS], ddt[ROWS], dz[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int i = w * ROWS + r < PASS ? w * ROWS + r : 0;
+      const Row v = was[r];
+      float s1 = 0.0f, s2 = 0.0f, plain = skip * v.u;
+#pragma unroll
+      for (int k = 0; k < WAVES; ++k) {
+        s1 += share[set][0][k][i][lane], s2 += share[set][1][k][i][lane];
+        if (GATE) plain += share[set][SUMS - 1][k][i][lane];
+      }
+      du[r] = fmaf(v.s, s1, skip * v.q);
+      ddt[r] = fmaf(v.u, s1, s2) * v.slope;
+      dz[r] = v.gate * plain;
+      if (w * ROWS + r < PASS) dbias += ddt[r], dskip = fmaf(v.q, v.u, dskip);
+    }
+    if (!on) return;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int t = first + w * ROWS + r;
+      if (w * ROWS + r < PASS && t < stop) {
+        element(o.du.at(t, b), byte) = static_cast<E>(du[r]), element(o.ddt.at(t, b), byte) = static_cast<E>(ddt[r]);
+        if (GATE) element(o.dz.at(t, b), byte) = static_cast<E>(dz[r]);
+      }
+    }
+  };
+
+  const int padded = (l.T + kPad - 1) / kPad * kPad;
+  const int passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0;
+  const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + t0 + (int64_t)(passes - 1) * PASS) * 2 * kHeld;
+  Coef early, late;                                      // of the pass's first and last four steps
+  static_assert(PASS == 2 * kBatch);
+  if (passes) {
+    fetch(t0 + (passes - 1) * PASS);
+    prepare(t0 + (passes - 1) * PASS, (passes - 1) & 1);
+    early.ask(from);
+  }
+  __syncthreads();
+  for (int p = passes - 1; p >= 0; --p) {
+    const int first = t0 + p * PASS, buffer = p & 1, set = p % SETS;
+    float2 in_[PASS];
+    float q[PASS];
+#pragma unroll
+    for (int i = 0; i < PASS; ++i) in_[i] = step_in[buffer][i][lane], q[i] = step_q[buffer][i][lane];
+    float a[PASS][kHeld], h[PASS + 1][kHeld];
+    h[0][0] = kept.x, h[0][1] = kept.y, h[0][2] = kept.z, h[0][3] = kept.w;
+    if (p + 1 < passes) finish(first + PASS, (p + 1) % SETS);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) was[r] = row[r];
+    if (p) fetch(first - PASS);
+    auto forward = [&](const Coef& c, int j) {
+#pragma unroll
+      for (int i = j; i < j + kBatch; ++i)
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+          a[i][k] = exp2_fast(in_[i].x * A2[k]);
+          h[i + 1][k] = fmaf(a[i][k], h[i][k], in_[i].y * c.B(i - j, k));
+        }
+    };
+    float step_sum[PASS];
+    auto backward = [&](const Coef& c, int j) {
+#pragma unroll
+      for (int i = j + kBatch - 1; i >= j; --i) {
+        float s1 = 0.0f, s2 = 0.0f, plain = 0.0f, pair[kHeld];
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+          const float gh = fmaf(q[i], c.C(i - j, k), carry[k]);
+          carry[k] = a[i][k] * gh;
+          const float through = carry[k] * h[i][k];
+          s1 = k ? fmaf(gh, c.B(i - j, k), s1) : gh * c.B(i - j, k);
+          s2 = k ? fmaf(through, A[k], s2) : through * A[k];
+          dA[k] = fmaf(through, in_[i].x, dA[k]);
+          if (GATE) plain = k ? fmaf(c.C(i - j, k), h[i + 1][k], plain) : c.C(i - j, k) * h[i + 1][k];
+          pair[k] = swap32_add(gh * in_[i].y, h[i + 1][k] * q[i]);
+        }
+        step_sum[i] = half_row_add(swap16_add(pair[0], pair[1]), swap16_add(pair[2], pair[3]));
+        share[set][0][w][i][lane] = s1, share[set][1][w][i][lane] = s2;
+        if (GATE) share[set][SUMS - 1][w][i][lane] = plain;
+      }
+    };
+    wait_for_scalars();
+    late.ask(from + kBatch * 2 * kHeld);
+    __builtin_amdgcn_sched_barrier(0);
+    forward(early, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    if (SETS == 1) __syncthreads();                      // the last pass's shares have been read
+    wait_for_scalars();
+    early.ask(from);
+    __builtin_amdgcn_sched_barrier(0);
+    forward(late, kBatch);
+    backward(late, kBatch);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_for_scalars();
+    late.ask(from - (p ? PASS * 2 * kHeld : 0));
+    __builtin_amdgcn_sched_barrier(0);
+    backward(early, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    early = late;
+    const bool odd = lane & 1, high = lane & 2;
+    const float low = in_four_add<0x4E>(four_add(step_sum[0], step_sum[1]), four_add(step_sum[2], step_sum[3]), high);
+    const float top = in_four_add<0x4E>(four_add(step_sum[4], step_sum[5]), four_add(step_sum[6], step_sum[7]), high);
+    const float part = in_four_add<0xB1>(low, top, odd);
+    o.bc[(((((int64_t)(tile % l.tiles) * l.B + b) * l.G + g) * (padded / PASS) + first / PASS) * WAVES + w) * 64 + lane] = part;
+    from -= PASS * 2 * kHeld;
+    if (p) prepare(first - PASS, buffer ^ 1);
+    __syncthreads();
+  }
+  if (passes) finish(t0, 0);
+
+  // dskip and ddt_bias: every wave has the steps of its rows
+  __syncthreads();
+  float* totals = &share[0][0][0][0][0];
+  static_assert(sizeof(share) >= 2 * WAVES * kTile * sizeof(float));
+  totals[w * kTile + lane] = dskip, totals[(WAVES + w) * kTile + lane] = dbias;
+  __syncthreads();
+  if (!on) return;
+  const int64_t part = (int64_t)span * l.B + b;
+  if (w == 0) {
+    for (int k = 1; k < WAVES; ++k) dskip += totals[k * kTile + lane], dbias += totals[(WAVES + k) * kTile + lane];
+    o.dskip[part * l.D + d] = dskip, o.ddt_bias[part * l.D + d] = dbias;
+  }
+  *reinterpret_cast<float4*>(o.dA + state_at(span, l.B, b, WAVES, w, l.D, d)) = make_float4(dA[0], dA[1], dA[2], dA[3]);
+  if (o.dh0 && span == 0)
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (w * kHeld + i < l.N) o.dh0[((int64_t)b * l.D + d) * l.N + w * kHeld + i] = carry[i];
+  for (int t = (t0 > len ? t0 : len) + w; t < t1; t += WAVES) {
+    element(o.du.at(t, b), byte) = static_cast<E>(0.0f), element(o.ddt.at(t, b), byte) = static_cast<E>(0.0f);
+    if (GATE) element(o.dz.at(t, b), byte) = static_cast<E>(0.0f);
+  }
+}
+
+// dB and dC: the tiles' parts in the tiles' order.  A thread has the place of a lane of the main kernel.
+template <typename E>
+__global__ void __launch_bounds__(256)
+join_bc_kernel(const Layer<E> l, const float* __restrict__ bc, int waves, int64_t all, E* __restrict__ dBm, E* __restrict__ dCm) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= all) return;
+  const int padded = (l.T + kPad - 1) / kPad * kPad, product = product_of_lane((int)(i & 63));
+  const int w = (int)(i / 64 % waves), t = (int)(i / 64 / waves % (padded / PASS)) * PASS + product / 8;
+  const int64_t bg = i / 64 / waves / (padded / PASS);
+  const int g = (int)(bg % l.G), b = (int)(bg / l.G), n = w * kHeld + product / 2 % kHeld;
+  if (t >= l.T || n >= l.N) return;
+  float sum = 0.0f;
+  if (t < clamp_length(l.lengths, b, l.T)) {
+#pragma unroll 8
+    for (int k = 0; k < l.tiles; ++k) sum += bc[k * all + i];
+  }
+  store((product & 1 ? dCm : dBm) + (((int64_t)t * l.B + b) * l.G + g) * l.N + n, sum);
+}
+
+// dA, dskip and ddt_bias: the parts of the samples and spans, in order: four waves a quarter each, then the quarters.
+__global__ void __launch_bounds__(256)
+join_params_kernel(int parts, int waves, int D, int N, const float* __restrict__ dA, const float* __restrict__ dskip,
+                   const float* __restrict__ ddt_bias, float* __restrict__ out_dA, float* __restrict__ out_dskip,
+                   float* __restrict__ out_ddt_bias) {
+  __shared__ float quarter[4][64];
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, of_dA = waves * kHeld * D;
+  const int i = blockIdx.x * 64 + lane, all = of_dA + 2 * D;
+  const float* from = i < of_dA ? dA + i : i < of_dA + D ? dskip + (i - of_dA) : ddt_bias + (i - of_dA - D);
+  const int64_t step = i < of_dA ? of_dA : D;
+  const int each = (parts + 3) / 4, last = (q + 1) * each < parts ? (q + 1) * each : parts;
+  float sum = 0.0f;
+  if (i < all)
+#pragma unroll 8
+    for (int k = q * each; k < last; ++k) sum += from[k * step];
+  quarter[q][lane] = sum;
+  __syncthreads();
+  if (q || i >= all) return;
+  sum = (quarter[0][lane] + quarter[1][lane]) + (quarter[2][lane] + quarter[3][lane]);
+  if (i < of_dA) {
+    const int w = i / (kHeld * D), d = i / kHeld % D, n = w * kHeld + i % kHeld;
+    if (n < N) out_dA[(int64_t)d * N + n] = sum;
+  } else if (i < of_dA + D) {
+    if (out_dskip) out_dskip[i - of_dA] = sum;
+  } else if (out_ddt_bias) {
+    out_ddt_bias[i - of_dA - D] = sum;
+  }
+}
+
+// bc: parts of dB and dC [tile of the group][b][g][pass][w][64 lanes]; dA, dskip, ddt_bias: one part a span and sample.
+struct Scratch {
+  Spans spans;
+  size_t coef, ends, sums, bc, dA, dskip, ddt_bias, bytes;
+  int64_t bc_floats;                           // of one tile
+  Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G, 2)) {
+    const int64_t waves = waves_of(N), tiles = bppsa_ceil_div(D / G, kTile), parts = (int64_t)spans.count * B * D;
+    bc_floats = (int64_t)B * G * ((T + kPad - 1) / kPad * kPad / PASS) * waves * 64;
+    Arena take;
+    coef = take(coef_floats(T, B, N, G));
+    ends = take(spans.count > 1 ? parts * waves * kHeld : 0), sums = take(spans.count > 1 ? parts : 0);
+    bc = take(tiles * bc_floats);
+    dA = take(parts * waves * kHeld), dskip = take(parts), ddt_bias = take(parts);
+    bytes = take.at;
+  }
+};
+
+}  // namespace
+
+extern "C" size_t bppsa_ssm_scan_backward_workspace_bytes(int T, int B, int D, int N, int G) {
+  return sizes_ok(T, B, D, N, G) ? Scratch(T, B, D, N, G).bytes : 0;
+}
+
+extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bppsa_rows* dy, const void* states,
+                                                const bppsa_ssm_grads* grads, void* workspace, size_t workspace_bytes,
+                                                void* stream) {
+  BPPSA_TRY(check_layer(layer));
+  if (!dy || !dy->data || !states || !grads || !grads->dBm || !grads->dCm || !grads->dA) return BPPSA_EINVAL;
+  if (!writable(grads->du, layer->T, layer->B) || !writable(grads->ddt, layer->T, layer->B)) return BPPSA_EINVAL;
+  if (!layer->z.data != !grads->dz.data || (layer->z.data && !writable(grads->dz, layer->T, layer->B))) return BPPSA_EINVAL;
+  const Scratch at(layer->T, layer->B, layer->D, layer->N, layer->G);
+  BPPSA_TRY(check_workspace(workspace, workspace_bytes, at.bytes));
+  const hipStream_t s = (hipStream_t)stream;
+  return by_type(layer->type, [&](auto e) {
+    using E = decltype(e);
+    const Layer<E> l = layer_of<E>(*layer);
+    const int waves = waves_of(l.N);
+    auto part = [&](size_t o) { return reinterpret_cast<float*>(static_cast<char*>(workspace) + o); };
+    const Grads<E> o{rows_of<E>(grads->du), rows_of<E>(grads->ddt), rows_of<E>(grads->dz), part(at.bc), part(at.dA),
+                     part(at.dskip), part(at.ddt_bias), grads->dh0};
+    const Summary sum{part(at.ends), part(at.sums)};
+    const Rows<const E> out = rows_of<const E>(*dy);
+    launch_coef(l, part(at.coef), s);
+    auto walk = [&](auto waves_, auto gate) {
+      constexpr int W = waves_.value;
+      constexpr bool GATE = gate.value;
+      if (at.spans.count > 1)
+        scan_backward_summary_kernel<E, W, GATE><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
+            l, out, part(at.coef), sum, at.spans);
+      scan_backward_kernel<E, W, GATE><<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(
+          l, out, static_cast<const float*>(states), part(at.coef), sum, at.spans, o);
+      BPPSA_CHECK_LAUNCH();
+      return BPPSA_OK;
+    };
+    BPPSA_TRY(by_waves(waves, [&](auto w) { return l.z.data ? walk(w, std::true_type{}) : walk(w, std::false_type{}); }));
+    join_bc_kernel<E><<<(unsigned)((at.bc_floats + 255) / 256), 256, 0, s>>>(l, o.bc, waves, at.bc_floats,
+                                                                           static_cast<E*>(grads->dBm), static_cast<E*>(grads->dCm));
+    join_params_kernel<<<(unsigned)((((int64_t)waves * kHeld + 2) * l.D + 63) / 64), 256, 0, s>>>(
+        at.spans.count * l.B, waves, l.D, l.N, o.dA, o.dskip, o.ddt_bias, grads->dA, grads->dskip, grads->ddt_bias);
+    BPPSA_CHECK_LAUNCH();
+    return BPPSA_OK;
+  });
+}

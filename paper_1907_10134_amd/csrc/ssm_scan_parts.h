@@ -64,7 +64,7 @@ static inline int64_t coef_floats(int64_t T, int64_t B, int64_t N, int64_t G) {
 }
 
 template <typename E>
-__global__ void __launch_bounds__(256)
+static __global__ void __launch_bounds__(256)
 coef_kernel(const Layer<E> l, int waves, int64_t all, float* __restrict__ coef) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= all) return;
@@ -100,14 +100,62 @@ __device__ __forceinline__ void wait_for_scalars() {
 }
 
 template <typename E>
-void launch_coef(const Layer<E>& l, float* coef, hipStream_t s) {
+static void launch_coef(const Layer<E>& l, float* coef, hipStream_t s) {
   const int64_t all = coef_floats(l.T, l.B, l.N, l.G);
   coef_kernel<E><<<(unsigned)((all + 255) / 256), 256, 0, s>>>(l, waves_of(l.N), all, coef);
 }
 
-// How many spans the time is cut into, each scanned by workgroups of its own, and the steps of one.
+// A long sequence with few channels is cut into spans, each scanned by workgroups of its own.  A first launch scans each
+// span from a state of zero and keeps only where that ends and the sum of its steps; a channel's decay over a span is
+// exp(A sum), so that the second launch can join the spans between its own and the start in a multiply-add each, and scan
+// its own from its true start.
 struct Spans {
   int count, steps;
 };
+struct Summary {
+  float *ends, *sums;              // [span][b][wave][d][4], [span][b][d]
+};
+
+// As many spans as give every SIMD `waves` waves, none shorter than 64 steps (a multiple of kPad), 64 at most.
+static inline Spans spans_of(int T, int B, int D, int N, int G, int waves) {
+  const int64_t have = (int64_t)G * bppsa_ceil_div(D / G, kTile) * B * waves_of(N);
+  int64_t count = (int64_t)bppsa_compute_units() * 4 * waves / have;
+  if (count > T / 64) count = T / 64;
+  if (count > 64) count = 64;
+  if (count < 2) return Spans{1, T};
+  const int steps = bppsa_ceil_div(bppsa_ceil_div(T, (int)count), kPad) * kPad;
+  return Spans{bppsa_ceil_div(T, steps), steps};
+}
+
+// Offsets of a workspace's arrays.
+struct Arena {
+  size_t at = 0;
+  size_t operator()(int64_t floats) {
+    const size_t o = at;
+    at += bppsa_align_up((size_t)floats * sizeof(float), 256);
+    return o;
+  }
+};
+
+static inline bool sizes_ok(int T, int B, int D, int N, int G) {
+  return T > 0 && B > 0 && D > 0 && N > 0 && G > 0 && N <= BPPSA_SSM_MAX_N && D % G == 0;
+}
+
+static inline bppsa_status check_layer(const bppsa_ssm* l) {
+  if (!l || l->T < 1 || l->B < 1 || l->D < 1 || l->N < 1 || l->G < 1) return BPPSA_EINVAL;
+  if (!l->u.data || !l->dt.data || !l->Bm.data || !l->Cm.data || !l->A) return BPPSA_EINVAL;
+  if (l->D % l->G) return BPPSA_ESHAPE;
+  if (l->N > BPPSA_SSM_MAX_N || l->type < BPPSA_F32 || l->type > BPPSA_F16) return BPPSA_EUNSUPPORTED;
+  // one grid axis counts the samples; rows are addressed by 32 bits of bytes
+  if (bppsa_mul_overflows(l->T, l->B, l->D, 2) || bppsa_mul_overflows(l->B, l->D, l->N, 1) || l->B > 65535 || l->D > 1 << 28 ||
+      l->T > 0x7FFFFFFF - 64)
+    return BPPSA_EOVERFLOW;
+  return BPPSA_OK;
+}
+
+static inline bppsa_status check_workspace(const void* workspace, size_t have, size_t need) {
+  if (need && (!workspace || have < need)) return BPPSA_EWORKSPACE;
+  return need && ((uintptr_t)workspace & 255) ? BPPSA_EINVAL : BPPSA_OK;
+}
 
 }  // namespace ssm
