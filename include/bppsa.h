@@ -518,7 +518,9 @@ typedef struct bppsa_rows {
  * lengths [B]: sample b has lengths[b] tokens (clamped to 0..T).  What lies behind them is never read; outputs and
  * gradients there are zero, and the last state is the one after the sample's own last token.
  * D has to be a multiple of G, N at most BPPSA_SSM_MAX_N (BPPSA_EUNSUPPORTED beyond).
- * The struct is host memory, its pointers device memory.
+ * The struct is host memory, its pointers device memory.  Here and in all calls of this section an output may not overlap
+ * an input or another output (h_last = h0 and state_last = state0 are refused: BPPSA_EINVAL), except what is said to be
+ * changed in place.
  */
 #define BPPSA_SSM_MAX_N 64
 typedef struct bppsa_ssm {

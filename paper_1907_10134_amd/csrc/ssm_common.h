@@ -28,10 +28,36 @@ __device__ __forceinline__ float load(const E* p) { return static_cast<float>(*p
 template <typename E>
 __device__ __forceinline__ void store(E* p, float v) { *p = static_cast<E>(v); }
 
-// Element i of a row whose address is the same for the whole wave: the row in scalar registers, 32 bits of offset a lane.
+// The rows of an array that a wave walks through: the row's address in scalar registers, a lane's 32 bits of bytes added by
+// the access itself.  (The asm keeps the compiler from adding the lane's offset to the array's start once and the row's
+// to that with a vector instruction for every access.)
 template <typename E>
-__device__ __forceinline__ E& element(E* row, uint32_t byte) {
-  return *reinterpret_cast<E*>(reinterpret_cast<std::conditional_t<std::is_const_v<E>, const char, char>*>(row) + byte);
+struct Walk {
+  uint64_t row;
+  int64_t step;
+  __device__ __forceinline__ Walk(const Rows<E>& r, int t, int b) : row((uint64_t)r.at(t, b)), step(r.st * (int64_t)sizeof(E)) {}
+  __device__ __forceinline__ __attribute__((address_space(1))) E& at(int rows_on, uint32_t byte) const {
+    uint64_t p = row + rows_on * step;
+    asm("" : "+s"(p));
+    return *(__attribute__((address_space(1))) E*)((const __attribute__((address_space(1))) char*)p + byte);
+  }
+  __device__ __forceinline__ void move(int rows) { row += rows * step; }
+};
+
+// V neighbouring elements by one access of any alignment: the memory path takes 16 bytes from an odd element as well, and a
+// line that is crossed costs less than eight accesses do.
+template <typename E, int V>
+struct __attribute__((packed, aligned(sizeof(E)))) Some {
+  E v[V];
+};
+template <typename E, int V>
+__device__ __forceinline__ Some<E, V> load_some(const E* p) { return *reinterpret_cast<const Some<E, V>*>(p); }
+template <typename E, int V>
+__device__ __forceinline__ void store_some(E* p, const float (&x)[V]) {
+  Some<E, V> s;
+#pragma unroll
+  for (int i = 0; i < V; ++i) s.v[i] = static_cast<E>(x[i]);
+  *reinterpret_cast<Some<E, V>*>(p) = s;
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp, 2^x

@@ -1,11 +1,17 @@
 // The short causal convolution in front of the selective scan.
+#include <algorithm>
+
 #include "ssm_common.h"
 
 namespace {
 
 using namespace ssm;
 
-constexpr int kSpan = 64;        // steps of a workgroup
+// All kernels here are bound by memory.  A thread takes V neighbouring channels (16 bytes forward, 8 backward, where a
+// window of inputs and one of gradients and the sums of the weights' gradients have to stay in registers too) and a span
+// of steps, the window of the last W inputs in registers.  The last thread of a row starts early enough to have V channels
+// too and repeats some of its neighbour's, with the same results; fewer than V channels go one to a thread.
+constexpr int kAhead = 4;        // rows that are asked for together
 
 template <typename E>
 struct Conv {
@@ -13,146 +19,217 @@ struct Conv {
   const float *weight, *bias;
   const E* state0;
   const int32_t* lengths;
-  int T, B, D, silu;
+  int T, B, D, silu, span;
 };
 
 template <typename E>
-Conv<E> conv_of(const bppsa_conv& c) {
-  return Conv<E>{rows_of<const E>(c.x), c.weight, c.bias, static_cast<const E*>(c.state0), c.lengths, c.T, c.B, c.D, c.silu};
+Conv<E> conv_of(const bppsa_conv& c, int span) {
+  return Conv<E>{rows_of<const E>(c.x), c.weight, c.bias, static_cast<const E*>(c.state0), c.lengths, c.T, c.B, c.D, c.silu, span};
 }
+
+template <int V, int W>
+struct Taps {
+  float w[V][W], bias[V];
+  template <typename E>
+  __device__ __forceinline__ Taps(const Conv<E>& c, int d) {
+    const Some<float, V * W> all = load_some<float, V * W>(c.weight + (int64_t)d * W);
+    Some<float, V> b = {};
+    if (c.bias) b = load_some<float, V>(c.bias + d);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      bias[i] = b.v[i];
+#pragma unroll
+      for (int k = 0; k < W; ++k) w[i][k] = all.v[i * W + k];
+    }
+  }
+  __device__ __forceinline__ float sum(const float (&seen)[W][V], int i) const {
+    float p = bias[i];
+#pragma unroll
+    for (int k = 0; k < W; ++k) p = fmaf(w[i][k], seen[k][i], p);
+    return p;
+  }
+};
 
 // Input t of a sample, t from -(W-1): the carried state in front of the first, nothing behind its end.
-template <typename E, int W>
-__device__ __forceinline__ float input(const Conv<E>& c, int t, int b, int d, int len) {
-  if (t >= len) return 0.0f;
-  if (t >= 0) return load(c.x.at(t, b) + d);
-  return c.state0 ? load(c.state0 + ((int64_t)b * (W - 1) + t + W - 1) * c.D + d) : 0.0f;
+template <typename E, int W, int V>
+__device__ __forceinline__ void input(const Conv<E>& c, int t, int b, int d, int len, float (&x)[V]) {
+  Some<E, V> s = {};
+  if (t >= 0 && t < len) s = load_some<E, V>(c.x.at(t, b) + d);
+  else if (t < 0 && c.state0) s = load_some<E, V>(c.state0 + ((int64_t)b * (W - 1) + t + W - 1) * c.D + d);
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = (float)s.v[i];
 }
 
-// One thread a channel and span of steps, the window in registers.
-template <typename E, int W>
+template <typename E, int W, int V>
 __global__ void __launch_bounds__(64)
 conv_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state_last) {
-  const int d = blockIdx.x * 64 + threadIdx.x, b = blockIdx.y, t0 = blockIdx.z * kSpan;
-  if (d >= c.D) return;
-  const int len = clamp_length(c.lengths, b, c.T), t1 = t0 + kSpan < c.T ? t0 + kSpan : c.T;
-  float w[W], seen[W];
-#pragma unroll
-  for (int k = 0; k < W; ++k) {
-    w[k] = c.weight[(int64_t)d * W + k];
-    seen[k] = k ? input<E, W>(c, t0 - W + k, b, d, len) : 0.0f;
-  }
-  const float bias = c.bias ? c.bias[d] : 0.0f;
-  for (int t = t0; t < t1; ++t) {
-#pragma unroll
-    for (int k = 0; k + 1 < W; ++k) seen[k] = seen[k + 1];
-    seen[W - 1] = input<E, W>(c, t, b, d, len);
-    float p = bias;
-#pragma unroll
-    for (int k = 0; k < W; ++k) p = fmaf(w[k], seen[k], p);
-    store(y.at(t, b) + d, t < len ? (c.silu ? p * sigmoid<E>(p) : p) : 0.0f);
-  }
+  const int first = (blockIdx.x * 64 + threadIdx.x) * V, d = first + V <= c.D ? first : c.D - V;
+  const int b = blockIdx.y, t0 = blockIdx.z * c.span;
+  if (first >= c.D) return;
+  const int len = clamp_length(c.lengths, b, c.T), t1 = t0 + c.span < c.T ? t0 + c.span : c.T, stop = t1 < len ? t1 : len;
   if (state_last && blockIdx.z == 0)
 #pragma unroll
-    for (int k = 0; k + 1 < W; ++k)
-      store(state_last + ((int64_t)b * (W - 1) + k) * c.D + d, input<E, W>(c, len - (W - 1) + k, b, d, len));
+    for (int k = 0; k + 1 < W; ++k) {
+      float x[V];
+      input<E, W, V>(c, len - (W - 1) + k, b, d, len, x);
+      store_some<E, V>(state_last + ((int64_t)b * (W - 1) + k) * c.D + d, x);
+    }
+  float seen[W][V];
+  if (t0 < stop) {
+    const Taps<V, W> taps(c, d);
+#pragma unroll
+    for (int k = 1; k < W; ++k) input<E, W, V>(c, t0 - W + k, b, d, len, seen[k]);
+    for (int t = t0; t < stop; t += kAhead) {
+      Some<E, V> x[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) x[j] = load_some<E, V>(c.x.at(t + j < stop ? t + j : stop - 1, b) + d);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (t + j >= stop) break;
+        float out[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+#pragma unroll
+          for (int k = 0; k + 1 < W; ++k) seen[k][i] = seen[k + 1][i];
+          seen[W - 1][i] = (float)x[j].v[i];
+          const float p = taps.sum(seen, i);
+          out[i] = c.silu ? p * sigmoid<E>(p) : p;
+        }
+        store_some<E, V>(y.at(t + j, b) + d, out);
+      }
+    }
+  }
+  const float zero[V] = {};
+  for (int t = t0 > len ? t0 : len; t < t1; ++t) store_some<E, V>(y.at(t, b) + d, zero);
 }
 
-// dL/dp[t], p recomputed from its window.
-template <typename E, int W>
-__device__ __forceinline__ float outer(const Conv<E>& c, const Rows<const E>& dy, int t, int b, int d, int len, const float (&w)[W],
-                                       float bias, float (&seen)[W]) {
-#pragma unroll
-  for (int k = 0; k + 1 < W; ++k) seen[k] = seen[k + 1];
-  seen[W - 1] = input<E, W>(c, t, b, d, len);
-  if (t >= len) return 0.0f;
-  const float g = load(dy.at(t, b) + d);
-  if (!c.silu) return g;
-  float p = bias;
-#pragma unroll
-  for (int k = 0; k < W; ++k) p = fmaf(w[k], seen[k], p);
-  const float sg = sigmoid<E>(p);
-  return g * sg * fmaf(p, 1.0f - sg, 1.0f);
-}
-
-// dx[t] = sum_k w[k] dp[t + W-1 - k].  A span forms the dp of its steps, and of W-1 behind it for its last dx; its sums of
-// dweight and dbias go to parts [span][b][W+1][D].  The first span also has the gradient of the carried state: dx at
-// t = -(W-1)..-1.
-template <typename E, int W>
+// dx[t] = sum_k w[k] dp[t + W-1 - k], dp = dL/dp with p recomputed from its window.  A span forms the dp of its steps, and of
+// W-1 behind it for its last dx; its sums of dweight and dbias go to parts [span][b][W+1][D].  The first span also has the
+// gradient of the carried state: dx at t = -(W-1)..-1.
+template <typename E, int W, int V>
 __global__ void __launch_bounds__(64)
 conv_backward_kernel(const Conv<E> c, Rows<const E> dy, Rows<E> dx, E* __restrict__ dstate0, float* __restrict__ parts) {
-  const int d = blockIdx.x * 64 + threadIdx.x, b = blockIdx.y, t0 = blockIdx.z * kSpan;
-  if (d >= c.D) return;
-  const int len = clamp_length(c.lengths, b, c.T), t1 = t0 + kSpan < c.T ? t0 + kSpan : c.T;
-  float w[W], seen[W], dp[W], dw[W], db = 0.0f;
+  const int first = (blockIdx.x * 64 + threadIdx.x) * V, d = first + V <= c.D ? first : c.D - V;
+  const int b = blockIdx.y, t0 = blockIdx.z * c.span;
+  if (first >= c.D) return;
+  const int len = clamp_length(c.lengths, b, c.T), t1 = t0 + c.span < c.T ? t0 + c.span : c.T;
+  float seen[W][V], dp[W][V] = {}, dw[W + 1][V] = {};
+  const Taps<V, W> taps(c, d);
 #pragma unroll
-  for (int k = 0; k < W; ++k) {
-    w[k] = c.weight[(int64_t)d * W + k];
-    seen[k] = k ? input<E, W>(c, t0 - W + k, b, d, len) : 0.0f;
-    dp[k] = dw[k] = 0.0f;
-  }
-  const float bias = c.bias ? c.bias[d] : 0.0f;
+  for (int k = 1; k < W; ++k) input<E, W, V>(c, t0 - W + k, b, d, len, seen[k]);
   // at step t dp[j] holds dL/dp[t - (W-1) + j]; it completes dx[t - (W-1)]
-  for (int t = t0; t < t1 + W - 1; ++t) {
+  for (int t = t0; t < t1 + W - 1; t += kAhead) {
+    Some<E, V> x[kAhead] = {}, go[kAhead] = {};
+    if (len)
 #pragma unroll
-    for (int k = 0; k + 1 < W; ++k) dp[k] = dp[k + 1];
-    dp[W - 1] = outer<E, W>(c, dy, t, b, d, len, w, bias, seen);
-    if (t < t1) {
-      db += dp[W - 1];
+      for (int j = 0; j < kAhead; ++j) {
+        const int at = t + j < len ? t + j : len - 1;
+        x[j] = load_some<E, V>(c.x.at(at, b) + d), go[j] = load_some<E, V>(dy.at(at, b) + d);
+      }
 #pragma unroll
-      for (int k = 0; k < W; ++k) dw[k] = fmaf(dp[W - 1], seen[k], dw[k]);
-    }
-    const int at = t - (W - 1);
-    float sum = 0.0f;
+    for (int j = 0; j < kAhead; ++j) {
+      const int now = t + j, done = now - (W - 1);
+      if (now >= t1 + W - 1) break;
+      float out[V];
 #pragma unroll
-    for (int k = 0; k < W; ++k) sum = fmaf(w[k], dp[W - 1 - k], sum);
-    if (at >= t0) {
-      store(dx.at(at, b) + d, at < len ? sum : 0.0f);
-    } else if (t0 == 0 && dstate0) {
-      store(dstate0 + ((int64_t)b * (W - 1) + t) * c.D + d, sum);
+      for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int k = 0; k + 1 < W; ++k) seen[k][i] = seen[k + 1][i], dp[k][i] = dp[k + 1][i];
+        seen[W - 1][i] = now < len ? (float)x[j].v[i] : 0.0f;
+        float g = now < len ? (float)go[j].v[i] : 0.0f;
+        if (c.silu) {
+          const float p = taps.sum(seen, i), sg = sigmoid<E>(p);
+          g *= sg * fmaf(p, 1.0f - sg, 1.0f);
+        }
+        dp[W - 1][i] = g;
+        const float mine = now < t1 ? g : 0.0f;
+        dw[W][i] += mine;
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          dw[k][i] = fmaf(mine, seen[k][i], dw[k][i]);
+          sum = fmaf(taps.w[i][k], dp[W - 1 - k][i], sum);
+        }
+        out[i] = done < len ? sum : 0.0f;
+      }
+      if (done >= t0) {
+        store_some<E, V>(dx.at(done, b) + d, out);
+      } else if (t0 == 0 && dstate0) {
+        store_some<E, V>(dstate0 + ((int64_t)b * (W - 1) + now) * c.D + d, out);
+      }
     }
   }
-  float* out = parts + ((int64_t)blockIdx.z * c.B + b) * (W + 1) * c.D + d;
+  float* to = parts + ((int64_t)blockIdx.z * c.B + b) * (W + 1) * c.D + d;
 #pragma unroll
-  for (int k = 0; k < W; ++k) out[(int64_t)k * c.D] = dw[k];
-  out[(int64_t)W * c.D] = db;
+  for (int k = 0; k <= W; ++k) store_some<float, V>(to + (int64_t)k * c.D, dw[k]);
 }
 
+// The parts in order: sixteen waves a share each, then the shares.
 template <int W>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 join_weights_kernel(const float* __restrict__ parts, int count, int D, float* __restrict__ dweight, float* __restrict__ dbias) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)(W + 1) * D;
-  if (i >= all) return;
+  __shared__ float share[16][64];
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
+  const int64_t i = (int64_t)blockIdx.x * 64 + lane, all = (int64_t)(W + 1) * D;
+  const int each = (count + 15) / 16, last = (q + 1) * each < count ? (q + 1) * each : count;
   float sum = 0.0f;
-  for (int k = 0; k < count; ++k) sum += parts[k * all + i];
+  if (i < all)
+#pragma unroll 8
+    for (int k = q * each; k < last; ++k) sum += parts[k * all + i];
+  share[q][lane] = sum;
+  __syncthreads();
+  if (q || i >= all) return;
+#pragma unroll
+  for (int k = 1; k < 16; ++k) sum += share[k][lane];
   const int tap = (int)(i / D), d = (int)(i - (int64_t)tap * D);
   if (tap < W) dweight[(int64_t)d * W + tap] = sum;
   else if (dbias) dbias[d] = sum;
 }
 
-template <typename E, int W>
+template <typename E, int W, int V>
 __global__ void __launch_bounds__(64)
 conv_step_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state, int slots_in_state, const int32_t* __restrict__ slots) {
-  const int d = blockIdx.x * 64 + threadIdx.x, b = blockIdx.y;
+  const int d = (blockIdx.x * 64 + threadIdx.x) * V, b = blockIdx.y;     // V divides D: a window that two threads move is moved twice
   if (d >= c.D) return;
   const int slot = slots ? slots[b] : b;
-  if (slot < 0 || slot >= slots_in_state) {
-    store(y.at(0, b) + d, 0.0f);
-    return;
-  }
-  E* s = state + (int64_t)slot * (W - 1) * c.D + d;
-  const E* x = c.x.at(0, b) + d;
-  float p = c.bias ? c.bias[d] : 0.0f;
-  E seen[W];
+  float out[V] = {};
+  if (slot >= 0 && slot < slots_in_state) {
+    E* s = state + (int64_t)slot * (W - 1) * c.D + d;
+    Some<E, V> held[W];
 #pragma unroll
-  for (int k = 0; k < W; ++k) {
-    seen[k] = k < W - 1 ? s[(int64_t)k * c.D] : *x;
-    p = fmaf(c.weight[(int64_t)d * W + k], load(&seen[k]), p);
-  }
+    for (int k = 0; k < W; ++k) held[k] = load_some<E, V>(k < W - 1 ? s + (int64_t)k * c.D : c.x.at(0, b) + d);
+    const Taps<V, W> taps(c, d);
+    float seen[W][V];
 #pragma unroll
-  for (int k = 0; k + 1 < W; ++k) s[(int64_t)k * c.D] = seen[k + 1];
-  store(y.at(0, b) + d, c.silu ? p * sigmoid<E>(p) : p);
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+      for (int k = 0; k < W; ++k) seen[k][i] = (float)held[k].v[i];
+      const float p = taps.sum(seen, i);
+      out[i] = c.silu ? p * sigmoid<E>(p) : p;
+    }
+#pragma unroll
+    for (int k = 0; k + 1 < W; ++k) *reinterpret_cast<Some<E, V>*>(s + (int64_t)k * c.D) = held[k + 1];
+  }
+  store_some<E, V>(y.at(0, b) + d, out);
 }
+
+// Steps of a span: 64, or fewer, to 8, while the device would have less than four waves a SIMD; every span reads W-1 rows twice.
+int span_of(int T, int64_t waves_a_step) {
+  int span = 64;
+  while (span > 8 && waves_a_step * bppsa_ceil_div(T, span) < (int64_t)bppsa_compute_units() * 16) span /= 2;
+  return span;
+}
+// Channels of a thread.
+template <typename E>
+constexpr int kWide = 16 / sizeof(E);
+template <typename E>
+constexpr int kNarrow = 8 / sizeof(E);
+int waves_for(int D, int V) { return bppsa_ceil_div(bppsa_ceil_div(D, V), 64); }
+int backward_width(int D, int type) {
+  const int V = type == BPPSA_F32 ? kNarrow<float> : kNarrow<bf16_t>;
+  return D >= V ? V : 1;
+}
+int backward_span(int T, int B, int D, int type) { return span_of(T, (int64_t)B * waves_for(D, backward_width(D, type))); }
 
 template <typename F>
 bppsa_status by_width(int W, F&& f) {
@@ -166,7 +243,7 @@ bppsa_status by_width(int W, F&& f) {
 bppsa_status check_conv(const bppsa_conv* c) {
   if (!c || c->T < 1 || c->B < 1 || c->D < 1 || c->W < 1 || !c->x.data || !c->weight) return BPPSA_EINVAL;
   if (c->W < 2 || c->W > BPPSA_SSM_MAX_W || c->type < BPPSA_F32 || c->type > BPPSA_F16) return BPPSA_EUNSUPPORTED;
-  if (bppsa_mul_overflows(c->T, c->B, c->D, 2) || c->B > 65535 || c->T > 65535 * kSpan) return BPPSA_EOVERFLOW;
+  if (bppsa_mul_overflows(c->T, c->B, c->D, 2) || c->B > 65535 || c->T > 65535 * 8) return BPPSA_EOVERFLOW;
   return BPPSA_OK;
 }
 
@@ -174,21 +251,28 @@ bppsa_status check_conv(const bppsa_conv* c) {
 
 extern "C" bppsa_status bppsa_ssm_conv(const bppsa_conv* conv, const bppsa_rows* y, void* state_last, void* stream) {
   BPPSA_TRY(check_conv(conv));
-  if (!y || !writable(*y, conv->T, conv->B)) return BPPSA_EINVAL;
+  if (!y || !writable(*y, conv->T, conv->B) || (state_last && state_last == conv->state0)) return BPPSA_EINVAL;
   return by_type(conv->type, [&](auto e) {
     using E = decltype(e);
     return by_width(conv->W, [&](auto w) {
-      conv_kernel<E, w.value><<<dim3(bppsa_ceil_div(conv->D, 64), conv->B, bppsa_ceil_div(conv->T, kSpan)), 64, 0,
-                                (hipStream_t)stream>>>(conv_of<E>(*conv), rows_of<E>(*y), static_cast<E*>(state_last));
-      BPPSA_CHECK_LAUNCH();
-      return BPPSA_OK;
+      auto run = [&](auto v) {
+        constexpr int V = v.value;
+        const int wide = waves_for(conv->D, V), span = span_of(conv->T, (int64_t)conv->B * wide);
+        conv_kernel<E, w.value, V><<<dim3(wide, conv->B, bppsa_ceil_div(conv->T, span)), 64, 0, (hipStream_t)stream>>>(
+            conv_of<E>(*conv, span), rows_of<E>(*y), static_cast<E*>(state_last));
+        BPPSA_CHECK_LAUNCH();
+        return BPPSA_OK;
+      };
+      return conv->D >= kWide<E> ? run(std::integral_constant<int, kWide<E>>{}) : run(std::integral_constant<int, 1>{});
     });
   });
 }
 
 extern "C" size_t bppsa_ssm_conv_backward_workspace_bytes(int T, int B, int D, int W) {
   if (T < 1 || B < 1 || D < 1 || W < 2 || W > BPPSA_SSM_MAX_W) return 0;
-  return (size_t)bppsa_ceil_div(T, kSpan) * B * (W + 1) * D * sizeof(float);
+  // the type is not asked for: the shorter spans of the two
+  const int span = std::min(backward_span(T, B, D, BPPSA_F32), backward_span(T, B, D, BPPSA_BF16));
+  return (size_t)bppsa_ceil_div(T, span) * B * (W + 1) * D * sizeof(float);
 }
 
 extern "C" bppsa_status bppsa_ssm_conv_backward(const bppsa_conv* conv, const bppsa_rows* dy, const bppsa_rows* dx,
@@ -205,11 +289,16 @@ extern "C" bppsa_status bppsa_ssm_conv_backward(const bppsa_conv* conv, const bp
     using E = decltype(e);
     return by_width(conv->W, [&](auto w) {
       constexpr int W = w.value;
-      const int spans = bppsa_ceil_div(conv->T, kSpan);
-      conv_backward_kernel<E, W><<<dim3(bppsa_ceil_div(conv->D, 64), conv->B, spans), 64, 0, s>>>(
-          conv_of<E>(*conv), rows_of<const E>(*dy), rows_of<E>(*dx), static_cast<E*>(dstate0), parts);
-      join_weights_kernel<W><<<(unsigned)(((int64_t)(W + 1) * conv->D + 255) / 256), 256, 0, s>>>(
-          parts, spans * conv->B, conv->D, dweight, dbias);
+      const int span = backward_span(conv->T, conv->B, conv->D, conv->type), spans = bppsa_ceil_div(conv->T, span);
+      auto run = [&](auto v) {
+        constexpr int V = v.value;
+        conv_backward_kernel<E, W, V><<<dim3(waves_for(conv->D, V), conv->B, spans), 64, 0, s>>>(
+            conv_of<E>(*conv, span), rows_of<const E>(*dy), rows_of<E>(*dx), static_cast<E*>(dstate0), parts);
+      };
+      if (backward_width(conv->D, conv->type) == 1) run(std::integral_constant<int, 1>{});
+      else run(std::integral_constant<int, kNarrow<E>>{});
+      join_weights_kernel<W><<<(unsigned)(((int64_t)(W + 1) * conv->D + 63) / 64), 1024, 0, s>>>(parts, spans * conv->B, conv->D,
+                                                                                               dweight, dbias);
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     });
@@ -224,10 +313,14 @@ extern "C" bppsa_status bppsa_ssm_conv_step(const bppsa_conv* conv, const bppsa_
   return by_type(conv->type, [&](auto e) {
     using E = decltype(e);
     return by_width(conv->W, [&](auto w) {
-      conv_step_kernel<E, w.value><<<dim3(bppsa_ceil_div(conv->D, 64), conv->B), 64, 0, (hipStream_t)stream>>>(
-          conv_of<E>(*conv), rows_of<E>(*y), static_cast<E*>(state), slots_in_state, slots);
-      BPPSA_CHECK_LAUNCH();
-      return BPPSA_OK;
+      auto run = [&](auto v) {
+        constexpr int V = v.value;
+        conv_step_kernel<E, w.value, V><<<dim3(waves_for(conv->D, V), conv->B), 64, 0, (hipStream_t)stream>>>(
+            conv_of<E>(*conv, 1), rows_of<E>(*y), static_cast<E*>(state), slots_in_state, slots);
+        BPPSA_CHECK_LAUNCH();
+        return BPPSA_OK;
+      };
+      return conv->D % 4 == 0 ? run(std::integral_constant<int, 4>{}) : run(std::integral_constant<int, 1>{});
     });
   });
 }

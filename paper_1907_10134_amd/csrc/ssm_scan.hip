@@ -15,6 +15,7 @@ __global__ void __launch_bounds__(WAVES * 64)
 scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, const float* __restrict__ coef,
             const Summary sum, const Spans spans) {
   constexpr int PASS = kKept, ROWS = (PASS + WAVES - 1) / WAVES;   // a wave prepares and finishes ROWS steps
+  constexpr int BATCH = SUMMARY ? 4 : 2;
   __shared__ float2 step_in[2][PASS][kTile];
   __shared__ float share[SUMMARY ? 1 : 2][SUMMARY ? 1 : WAVES][SUMMARY ? 1 : PASS][kTile];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -25,6 +26,9 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   const int d = g * l.wide + (on ? in : 0);              // lanes without a channel compute the group's first, and store nothing
   const int len = clamp_length(l.lengths, b, l.T), t0 = span * spans.steps;
   const int t1 = t0 + spans.steps < l.T ? t0 + spans.steps : l.T, stop = t1 < len ? t1 : len;
+
+  if (!SUMMARY && on)
+    for (int t = (t0 > len ? t0 : len) + w; t < t1; t += WAVES) store(y.at(t, b) + d, 0.0f);
 
   float A2[kHeld], h[kHeld];
 #pragma unroll
@@ -43,50 +47,54 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
 
   const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f, skip = l.skip ? l.skip[d] : 0.0f;
   const uint32_t byte = (uint32_t)d * sizeof(E);
+  const int mine = w * ROWS;                             // this wave's first step of a pass
+  Walk<const E> at_u(l.u, t0 + mine, b), at_dt(l.dt, t0 + mine, b), at_z(l.z, t0 + mine, b);
+  Walk<E> at_y(y, t0 + mine, b);
   E u[ROWS], dt[ROWS], z[ROWS], u_was[ROWS], z_was[ROWS];
   float total = 0.0f;
-  // Steps behind the last one read the last one's row and count as steps of size zero.  The values stay as they are loaded
-  // until they are needed: a conversion here would wait for each load by itself.
+  // The values stay as they are loaded until they are needed: a conversion here would wait for each load by itself.
   auto fetch = [&](int first) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int t = first + w * ROWS + r, at = t < stop ? t : stop - 1;
-      u[r] = element(l.u.at(at, b), byte), dt[r] = element(l.dt.at(at, b), byte);
-      if (GATE) z[r] = element(l.z.at(at, b), byte);
+      u[r] = dt[r] = z[r] = E(0.0f);
+      if (mine + r < PASS && first + mine + r < stop) {
+        u[r] = at_u.at(r, byte), dt[r] = at_dt.at(r, byte);
+        if (GATE) z[r] = at_z.at(r, byte);
+      }
     }
+    at_u.move(PASS), at_dt.move(PASS);
+    if (GATE) at_z.move(PASS);
   };
   auto prepare = [&](int first, int buffer) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (w * ROWS + r >= PASS) break;
-      const bool real = first + w * ROWS + r < stop;
-      const float s = real ? softplus<E>((float)dt[r] + bias) : 0.0f;
+      if (mine + r >= PASS) break;
+      float s = softplus<E>((float)dt[r] + bias);
+      s = first + mine + r < stop ? s : 0.0f;            // u is zero there
       if (SUMMARY) total += s;
-      step_in[buffer][w * ROWS + r][lane] = make_float2(s, real ? s * (float)u[r] : 0.0f);
+      step_in[buffer][mine + r][lane] = make_float2(s, s * (float)u[r]);
     }
   };
   auto finish = [&](int first, int buffer) {
     float v[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int row = w * ROWS + r < PASS ? w * ROWS + r : 0;
+      const int row = mine + r < PASS ? mine + r : 0;
       v[r] = skip * (float)u_was[r];
 #pragma unroll
       for (int k = 0; k < WAVES; ++k) v[r] += share[buffer][k][row][lane];
       if (GATE) v[r] *= (float)z_was[r] * sigmoid<E>((float)z_was[r]);
     }
-    if (!on) return;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      const int t = first + w * ROWS + r;
-      if (w * ROWS + r < PASS && t < stop) element(y.at(t, b), byte) = static_cast<E>(v[r]);
-    }
+    for (int r = 0; r < ROWS; ++r)
+      if (mine + r < PASS && first + mine + r < stop && on) at_y.at(r, byte) = static_cast<E>(v[r]);
+    at_y.move(PASS);
   };
 
   const int padded = (l.T + kPad - 1) / kPad * kPad;
   const int passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0;
   const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + t0) * 2 * kHeld;
-  Coef now, next;
+  Coef<BATCH> now, next;
   if (passes) {
     fetch(t0);
     prepare(t0, 0);
@@ -95,37 +103,32 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   __syncthreads();
   for (int p = 0; p < passes; ++p) {
     const int first = t0 + p * PASS, buffer = p & 1;
-    float2 in_now[kBatch], in_next[kBatch];
+    float2 in_[PASS];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) in_now[i] = step_in[buffer][i][lane];
+    for (int i = 0; i < PASS; ++i) in_[i] = step_in[buffer][i][lane];
     if (!SUMMARY && p) finish(first - PASS, buffer ^ 1);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) u_was[r] = u[r], z_was[r] = z[r];
     if (p + 1 < passes) fetch(first + PASS);
+    if (!SUMMARY && states && on)
+      *reinterpret_cast<float4*>(states + state_at(first / kKept, l.B, b, WAVES, w, l.D, d)) = make_float4(h[0], h[1], h[2], h[3]);
 #pragma unroll
-    for (int j = 0; j < PASS; j += kBatch) {
+    for (int j = 0; j < PASS; j += BATCH) {
       wait_for_scalars();
-      next.ask(from + (j + kBatch < PASS || p + 1 < passes ? j + kBatch : 0) * 2 * kHeld);
-      if (j + kBatch < PASS)
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) in_next[i] = step_in[buffer][j + kBatch + i][lane];
+      next.ask(from + (j + BATCH < PASS || p + 1 < passes ? j + BATCH : 0) * 2 * kHeld);
       __builtin_amdgcn_sched_barrier(0);
-      if (!SUMMARY && states && j % kKept == 0 && on && first + j < stop)
-        *reinterpret_cast<float4*>(states + state_at((first + j) / kKept, l.B, b, WAVES, w, l.D, d)) = make_float4(h[0], h[1], h[2], h[3]);
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
+      for (int i = 0; i < BATCH; ++i) {
         float v = 0.0f;
 #pragma unroll
         for (int k = 0; k < kHeld; ++k) {
-          h[k] = fmaf(exp2_fast(in_now[i].x * A2[k]), h[k], in_now[i].y * now.B(i, k));
+          h[k] = fmaf(exp2_fast(in_[j + i].x * A2[k]), h[k], in_[j + i].y * now.B(i, k));
           if (!SUMMARY) v = k ? fmaf(now.C(i, k), h[k], v) : now.C(i, k) * h[k];
         }
         if (!SUMMARY) share[buffer][w][j + i][lane] = v;
       }
       __builtin_amdgcn_sched_barrier(0);
       now = next;
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) in_now[i] = in_next[i];
     }
     from += PASS * 2 * kHeld;
     if (p + 1 < passes) prepare(first + PASS, buffer ^ 1);
@@ -147,7 +150,6 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
     }
   } else {
     if (!on) return;
-    for (int t = (t0 > len ? t0 : len) + w; t < t1; t += WAVES) store(y.at(t, b) + d, 0.0f);
     if (h_last && (len ? t0 < len && len <= t1 : span == 0))
 #pragma unroll
       for (int i = 0; i < kHeld; ++i)
@@ -168,31 +170,74 @@ struct Scratch {
   }
 };
 
-template <typename E>
-__global__ void __launch_bounds__(kTile)
+// One token.  A thread holds four states of a channel, 2^LANES neighbouring lanes a channel, for kStreams rows of the batch
+// one after the other, so that A is read once for all of them and their states are on their way together.  Bound by the
+// states' memory: 16 bytes a lane, read and written in place.  VECTOR: N is a multiple of 4 and state and A lie on 16 bytes.
+constexpr int kStreams = 4;
+template <typename E, int LANES, bool VECTOR>
+__global__ void __launch_bounds__(256)
 scan_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int slots_in_state, const int32_t* __restrict__ slots) {
-  const int d = blockIdx.x * kTile + threadIdx.x, b = blockIdx.y;
-  if (d >= l.D) return;
-  const int slot = slots ? slots[b] : b;
-  if (slot < 0 || slot >= slots_in_state) {
-    store(y.at(0, b) + d, 0.0f);
-    return;
+  const int d = blockIdx.x * (256 >> LANES) + (threadIdx.x >> LANES), n = (threadIdx.x & ((1 << LANES) - 1)) * kHeld;
+  if (d >= l.D) return;                        // all lanes of a channel alike
+  const bool any = n < l.N;
+  auto get = [&](const float* p) {
+    if (VECTOR) return any ? *reinterpret_cast<const float4*>(p) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    return make_float4(any ? p[0] : 0.0f, n + 1 < l.N ? p[1] : 0.0f, n + 2 < l.N ? p[2] : 0.0f, n + 3 < l.N ? p[3] : 0.0f);
+  };
+  const float4 A = get(l.A + (int64_t)d * l.N + n);
+  const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f, skip = l.skip ? l.skip[d] : 0.0f;
+  const int g = d / l.wide, b0 = blockIdx.y * kStreams;
+  int slot[kStreams];
+  float4 h[kStreams];
+  E u[kStreams], dt[kStreams], z[kStreams], Bm[kStreams][kHeld], Cm[kStreams][kHeld];
+#pragma unroll
+  for (int r = 0; r < kStreams; ++r) {
+    const int b = b0 + r < l.B ? b0 + r : l.B - 1;
+    slot[r] = slots ? slots[b] : b;
+    if (slot[r] < 0 || slot[r] >= slots_in_state) slot[r] = -1;
   }
-  const int g = d / l.wide;
-  const float u = load(l.u.at(0, b) + d), s = softplus<E>(load(l.dt.at(0, b) + d) + (l.dt_bias ? l.dt_bias[d] : 0.0f));
-  const E *Bt = l.Bm.at(0, b) + g * l.N, *Ct = l.Cm.at(0, b) + g * l.N;
-  float* h = state + ((int64_t)slot * l.D + d) * l.N;
-  float sum = l.skip ? l.skip[d] * u : 0.0f;
-  for (int n = 0; n < l.N; ++n) {
-    const float v = fmaf(exp2_fast(s * l.A[(int64_t)d * l.N + n] * kLog2e), h[n], s * u * load(Bt + n));
-    h[n] = v;
-    sum = fmaf(load(Ct + n), v, sum);
+#pragma unroll
+  for (int r = 0; r < kStreams; ++r) {
+    const int b = b0 + r < l.B ? b0 + r : l.B - 1;
+    h[r] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (slot[r] >= 0) h[r] = get(state + ((int64_t)slot[r] * l.D + d) * l.N + n);
+    u[r] = *(l.u.at(0, b) + d), dt[r] = *(l.dt.at(0, b) + d), z[r] = l.z.data ? *(l.z.at(0, b) + d) : E(0.0f);
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+      const int at = g * l.N + (n + k < l.N ? n + k : 0);
+      Bm[r][k] = *(l.Bm.at(0, b) + at), Cm[r][k] = *(l.Cm.at(0, b) + at);
+    }
   }
-  if (l.z.data) {
-    const float z = load(l.z.at(0, b) + d);
-    sum *= z * sigmoid<E>(z);
+#pragma unroll
+  for (int r = 0; r < kStreams; ++r) {
+    if (b0 + r >= l.B) break;
+    const float x = (float)u[r], s = softplus<E>((float)dt[r] + bias), su = s * x, s2 = s * kLog2e;
+    float4 v;
+    v.x = fmaf(exp2_fast(s2 * A.x), h[r].x, su * (float)Bm[r][0]), v.y = fmaf(exp2_fast(s2 * A.y), h[r].y, su * (float)Bm[r][1]);
+    v.z = fmaf(exp2_fast(s2 * A.z), h[r].z, su * (float)Bm[r][2]), v.w = fmaf(exp2_fast(s2 * A.w), h[r].w, su * (float)Bm[r][3]);
+    float sum = any ? (float)Cm[r][0] * v.x : 0.0f;
+    sum = n + 1 < l.N ? fmaf((float)Cm[r][1], v.y, sum) : sum;
+    sum = n + 2 < l.N ? fmaf((float)Cm[r][2], v.z, sum) : sum;
+    sum = n + 3 < l.N ? fmaf((float)Cm[r][3], v.w, sum) : sum;
+#pragma unroll
+    for (int k = 1; k < 1 << LANES; k <<= 1) sum += __shfl_xor(sum, k);
+    if (slot[r] >= 0) {
+      float* to = state + ((int64_t)slot[r] * l.D + d) * l.N + n;
+      if (VECTOR) {
+        if (any) *reinterpret_cast<float4*>(to) = v;
+      } else {
+        if (any) to[0] = v.x;
+        if (n + 1 < l.N) to[1] = v.y;
+        if (n + 2 < l.N) to[2] = v.z;
+        if (n + 3 < l.N) to[3] = v.w;
+      }
+    }
+    if (n == 0) {
+      sum = fmaf(skip, x, sum);
+      if (l.z.data) sum *= (float)z[r] * sigmoid<E>((float)z[r]);
+      store(y.at(0, b0 + r) + d, slot[r] >= 0 ? sum : 0.0f);
+    }
   }
-  store(y.at(0, b) + d, sum);
 }
 
 }  // namespace
@@ -209,7 +254,7 @@ extern "C" size_t bppsa_ssm_scan_workspace_bytes(int T, int B, int D, int N, int
 extern "C" bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows* y, float* h_last, void* states,
                                        void* workspace, size_t workspace_bytes, void* stream) {
   BPPSA_TRY(check_layer(layer));
-  if (!y || !writable(*y, layer->T, layer->B)) return BPPSA_EINVAL;
+  if (!y || !writable(*y, layer->T, layer->B) || (h_last && h_last == layer->h0)) return BPPSA_EINVAL;
   const Scratch at(layer->T, layer->B, layer->D, layer->N, layer->G);
   BPPSA_TRY(check_workspace(workspace, workspace_bytes, at.bytes));
   const hipStream_t s = (hipStream_t)stream;
@@ -241,8 +286,21 @@ extern "C" bppsa_status bppsa_ssm_scan_step(const bppsa_ssm* layer, const bppsa_
   return by_type(layer->type, [&](auto e) {
     using E = decltype(e);
     const Layer<E> l = layer_of<E>(*layer);
-    scan_step_kernel<E><<<dim3(bppsa_ceil_div(l.D, kTile), l.B), kTile, 0, (hipStream_t)stream>>>(l, rows_of<E>(*y), state,
-                                                                                                slots_in_state, slots);
+    const bool vector = l.N % kHeld == 0 && (((uintptr_t)state | (uintptr_t)l.A) & 15) == 0;
+    auto run = [&](auto lanes, auto v) {
+      constexpr int L = lanes.value;
+      scan_step_kernel<E, L, v.value><<<dim3(bppsa_ceil_div(l.D, 256 >> L), bppsa_ceil_div(l.B, kStreams)), 256, 0,
+                                        (hipStream_t)stream>>>(l, rows_of<E>(*y), state, slots_in_state, slots);
+    };
+    auto by_lanes = [&](auto v) {
+      if (l.N <= 4) run(std::integral_constant<int, 0>{}, v);
+      else if (l.N <= 8) run(std::integral_constant<int, 1>{}, v);
+      else if (l.N <= 16) run(std::integral_constant<int, 2>{}, v);
+      else if (l.N <= 32) run(std::integral_constant<int, 3>{}, v);
+      else run(std::integral_constant<int, 4>{}, v);
+    };
+    if (vector) by_lanes(std::true_type{});
+    else by_lanes(std::false_type{});
     BPPSA_CHECK_LAUNCH();
     return BPPSA_OK;
   });

@@ -66,7 +66,7 @@ template <typename E, int WAVES, bool GATE>
 __global__ void __launch_bounds__(WAVES * 64)
 scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ coef, const Summary sum,
                              const Spans spans) {
-  constexpr int ROWS = (PASS + WAVES - 1) / WAVES;
+  constexpr int ROWS = (PASS + WAVES - 1) / WAVES, BATCH = 4;
   __shared__ float2 step_in[2][PASS][kTile];             // (s, q)
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int span = blockIdx.x % (spans.count - 1) + 1, tile = blockIdx.x / (spans.count - 1), g = tile / l.tiles, b = blockIdx.y;
@@ -84,59 +84,58 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const float* __
   }
   const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f;
   const uint32_t byte = (uint32_t)d * sizeof(E);
+  const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
+  Walk<const E> at_dt(l.dt, last + mine, b), at_dy(dy, last + mine, b), at_z(l.z, last + mine, b);
   E dt[ROWS], go[ROWS], z[ROWS];
   auto fetch = [&](int first) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int t = first + w * ROWS + r, at = t < stop ? t : stop - 1;
-      dt[r] = element(l.dt.at(at, b), byte), go[r] = element(dy.at(at, b), byte);
-      if (GATE) z[r] = element(l.z.at(at, b), byte);
+      dt[r] = go[r] = z[r] = E(0.0f);
+      if (mine + r < PASS && first + mine + r < stop) {
+        dt[r] = at_dt.at(r, byte), go[r] = at_dy.at(r, byte);
+        if (GATE) z[r] = at_z.at(r, byte);
+      }
     }
+    at_dt.move(-PASS), at_dy.move(-PASS);
+    if (GATE) at_z.move(-PASS);
   };
   auto prepare = [&](int first, int buffer) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (w * ROWS + r >= PASS) break;
-      const bool real = first + w * ROWS + r < stop;
-      const float s = real ? softplus<E>((float)dt[r] + bias) : 0.0f;
-      float q = (float)go[r];
+      if (mine + r >= PASS) break;
+      float s = softplus<E>((float)dt[r] + bias), q = (float)go[r];
+      s = first + mine + r < stop ? s : 0.0f;            // q is zero there
       if (GATE) q *= (float)z[r] * sigmoid<E>((float)z[r]);
       total += s;
-      step_in[buffer][w * ROWS + r][lane] = make_float2(s, real ? q : 0.0f);
+      step_in[buffer][mine + r][lane] = make_float2(s, q);
     }
   };
   const int padded = (l.T + kPad - 1) / kPad * kPad;
-  const int passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0;
-  const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + t0 + (int64_t)(passes - 1) * PASS) * 2 * kHeld;
-  Coef now, next;
+  const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + last) * 2 * kHeld;
+  Coef<BATCH> now, next;
   if (passes) {
-    fetch(t0 + (passes - 1) * PASS);
-    prepare(t0 + (passes - 1) * PASS, (passes - 1) & 1);
-    now.ask(from + kBatch * 2 * kHeld);
+    fetch(last);
+    prepare(last, (passes - 1) & 1);
+    now.ask(from + (PASS - BATCH) * 2 * kHeld);
   }
   __syncthreads();
   for (int p = passes - 1; p >= 0; --p) {
     const int first = t0 + p * PASS, buffer = p & 1;
-    float2 in_now[kBatch], in_next[kBatch];
+    float2 in_[PASS];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) in_now[i] = step_in[buffer][PASS - kBatch + i][lane];
+    for (int i = PASS - 1; i >= 0; --i) in_[i] = step_in[buffer][i][lane];
     if (p) fetch(first - PASS);
 #pragma unroll
-    for (int j = PASS - kBatch; j >= 0; j -= kBatch) {
+    for (int j = PASS - BATCH; j >= 0; j -= BATCH) {
       wait_for_scalars();
-      next.ask(from + (j ? j - kBatch : p ? -kBatch : 0) * 2 * kHeld);
-      if (j)
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) in_next[i] = step_in[buffer][j - kBatch + i][lane];
+      next.ask(from + (j || p ? j - BATCH : 0) * 2 * kHeld);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = kBatch - 1; i >= 0; --i)
+      for (int i = BATCH - 1; i >= 0; --i)
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) carry[k] = exp2_fast(in_now[i].x * A2[k]) * fmaf(in_now[i].y, now.C(i, k), carry[k]);
+        for (int k = 0; k < kHeld; ++k) carry[k] = exp2_fast(in_[j + i].x * A2[k]) * fmaf(in_[j + i].y, now.C(i, k), carry[k]);
       __builtin_amdgcn_sched_barrier(0);
       now = next;
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) in_now[i] = in_next[i];
     }
     from -= PASS * 2 * kHeld;
     if (p) prepare(first - PASS, buffer ^ 1);
@@ -161,7 +160,7 @@ template <typename E, int WAVES, bool GATE>
 __global__ void __launch_bounds__(WAVES * 64)
 scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ states, const float* __restrict__ coef,
                      const Summary sum, const Spans spans, const Grads<E> o) {
-  constexpr int ROWS = (PASS + WAVES - 1) / WAVES, SUMS = GATE ? 3 : 2;
+  constexpr int ROWS = (PASS + WAVES - 1) / WAVES, BATCH = 2, SUMS = GATE ? 3 : 2;
   // with many waves one set of shares has to do (160 KB of LDS), and a second barrier a pass keeps it
   constexpr int SETS = WAVES <= 4 ? 2 : 1;
   __shared__ float2 step_in[2][PASS][kTile];             // (s, s u)
@@ -174,6 +173,12 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   const int d = g * l.wide + (on ? in : 0);
   const int len = clamp_length(l.lengths, b, l.T), t0 = span * spans.steps;
   const int t1 = t0 + spans.steps < l.T ? t0 + spans.steps : l.T, stop = t1 < len ? t1 : len;
+
+  if (on)
+    for (int t = (t0 > len ? t0 : len) + w; t < t1; t += WAVES) {
+      store(o.du.at(t, b) + d, 0.0f), store(o.ddt.at(t, b) + d, 0.0f);
+      if (GATE) store(o.dz.at(t, b) + d, 0.0f);
+    }
 
   float A[kHeld], A2[kHeld], carry[kHeld], dA[kHeld];
 #pragma unroll
@@ -193,6 +198,10 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f, skip = l.skip ? l.skip[d] : 0.0f;
   const uint32_t byte = (uint32_t)d * sizeof(E);
   float dskip = 0.0f, dbias = 0.0f;
+  const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
+  Walk<const E> at_u(l.u, last + mine, b), at_dt(l.dt, last + mine, b), at_dy(dy, last + mine, b), at_z(l.z, last + mine, b);
+  Walk<E> at_du(o.du, last + mine, b), at_ddt(o.ddt, last + mine, b), at_dz(o.dz, last + mine, b);
+  const float* at_states = states + state_at(last / kKept, l.B, b, WAVES, w, l.D, 0);
   E u[ROWS], dt[ROWS], go[ROWS], z[ROWS];
   struct Row {                                           // of a step: what its outputs are made of
     float s, u, q, slope, gate;                          // slope: sigmoid(raw), gate: dy silu'(z)
@@ -201,17 +210,22 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   auto fetch = [&](int first) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int t = first + w * ROWS + r, at = t < stop ? t : stop - 1;
-      u[r] = element(l.u.at(at, b), byte), dt[r] = element(l.dt.at(at, b), byte), go[r] = element(dy.at(at, b), byte);
-      if (GATE) z[r] = element(l.z.at(at, b), byte);
+      u[r] = dt[r] = go[r] = z[r] = E(0.0f);
+      if (mine + r < PASS && first + mine + r < stop) {
+        u[r] = at_u.at(r, byte), dt[r] = at_dt.at(r, byte), go[r] = at_dy.at(r, byte);
+        if (GATE) z[r] = at_z.at(r, byte);
+      }
     }
-    kept = *reinterpret_cast<const float4*>(states + state_at(first / kKept, l.B, b, WAVES, w, l.D, d));
+    kept = reinterpret_cast<const float4*>(at_states)[d];
+    at_u.move(-PASS), at_dt.move(-PASS), at_dy.move(-PASS);
+    if (GATE) at_z.move(-PASS);
+    at_states -= (int64_t)l.B * WAVES * l.D * kHeld;
   };
   auto prepare = [&](int first, int buffer) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (w * ROWS + r >= PASS) break;
-      const bool real = on && first + w * ROWS + r < stop;
+      if (mine + r >= PASS) break;
+      const bool real = on && first + mine + r < stop;
       const float raw = (float)dt[r] + bias;
       Row v{softplus<E>(raw), (float)u[r], (float)go[r], sigmoid<E>(raw), 0.0f};
       if (GATE) {
@@ -219,17 +233,17 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
         v.gate = v.q * sg * fmaf(x, 1.0f - sg, 1.0f);
         v.q *= x * sg;                                   // silu(z) first, as the forward pass has it
       }
-      if (!real) v = Row{0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      if (!real) v.s = v.u = v.q = 0.0f;
       row[r] = v;
-      step_in[buffer][w * ROWS + r][lane] = make_float2(v.s, v.s * v.u);
-      step_q[buffer][w * ROWS + r][lane] = v.q;
+      step_in[buffer][mine + r][lane] = make_float2(v.s, v.s * v.u);
+      step_q[buffer][mine + r][lane] = v.q;
     }
   };
   auto finish = [&](int first, int set) {
     float du[ROWS], ddt[ROWS], dz[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int i = w * ROWS + r < PASS ? w * ROWS + r : 0;
+      const int i = mine + r < PASS ? mine + r : 0;
       const Row v = was[r];
       float s1 = 0.0f, s2 = 0.0f, plain = skip * v.u;
 #pragma unroll
@@ -240,28 +254,26 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       du[r] = fmaf(v.s, s1, skip * v.q);
       ddt[r] = fmaf(v.u, s1, s2) * v.slope;
       dz[r] = v.gate * plain;
-      if (w * ROWS + r < PASS) dbias += ddt[r], dskip = fmaf(v.q, v.u, dskip);
+      if (mine + r < PASS && first + mine + r < stop) dbias += ddt[r], dskip = fmaf(v.q, v.u, dskip);
     }
-    if (!on) return;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      const int t = first + w * ROWS + r;
-      if (w * ROWS + r < PASS && t < stop) {
-        element(o.du.at(t, b), byte) = static_cast<E>(du[r]), element(o.ddt.at(t, b), byte) = static_cast<E>(ddt[r]);
-        if (GATE) element(o.dz.at(t, b), byte) = static_cast<E>(dz[r]);
+    for (int r = 0; r < ROWS; ++r)
+      if (mine + r < PASS && first + mine + r < stop && on) {
+        at_du.at(r, byte) = static_cast<E>(du[r]), at_ddt.at(r, byte) = static_cast<E>(ddt[r]);
+        if (GATE) at_dz.at(r, byte) = static_cast<E>(dz[r]);
       }
-    }
+    at_du.move(-PASS), at_ddt.move(-PASS);
+    if (GATE) at_dz.move(-PASS);
   };
 
   const int padded = (l.T + kPad - 1) / kPad * kPad;
-  const int passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0;
-  const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + t0 + (int64_t)(passes - 1) * PASS) * 2 * kHeld;
-  Coef early, late;                                      // of the pass's first and last four steps
-  static_assert(PASS == 2 * kBatch);
+  const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + last) * 2 * kHeld;
+  float* at_bc = o.bc + (((((int64_t)(tile % l.tiles) * l.B + b) * l.G + g) * (padded / PASS) + last / PASS) * WAVES + w) * 64;
+  Coef<BATCH> now, next;
   if (passes) {
-    fetch(t0 + (passes - 1) * PASS);
-    prepare(t0 + (passes - 1) * PASS, (passes - 1) & 1);
-    early.ask(from);
+    fetch(last);
+    prepare(last, (passes - 1) & 1);
+    now.ask(from);
   }
   __syncthreads();
   for (int p = passes - 1; p >= 0; --p) {
@@ -276,29 +288,29 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) was[r] = row[r];
     if (p) fetch(first - PASS);
-    auto forward = [&](const Coef& c, int j) {
+    auto forward = [&](int j) {
 #pragma unroll
-      for (int i = j; i < j + kBatch; ++i)
+      for (int i = j; i < j + BATCH; ++i)
 #pragma unroll
         for (int k = 0; k < kHeld; ++k) {
           a[i][k] = exp2_fast(in_[i].x * A2[k]);
-          h[i + 1][k] = fmaf(a[i][k], h[i][k], in_[i].y * c.B(i - j, k));
+          h[i + 1][k] = fmaf(a[i][k], h[i][k], in_[i].y * now.B(i - j, k));
         }
     };
     float step_sum[PASS];
-    auto backward = [&](const Coef& c, int j) {
+    auto backward = [&](int j) {
 #pragma unroll
-      for (int i = j + kBatch - 1; i >= j; --i) {
+      for (int i = j + BATCH - 1; i >= j; --i) {
         float s1 = 0.0f, s2 = 0.0f, plain = 0.0f, pair[kHeld];
 #pragma unroll
         for (int k = 0; k < kHeld; ++k) {
-          const float gh = fmaf(q[i], c.C(i - j, k), carry[k]);
+          const float gh = fmaf(q[i], now.C(i - j, k), carry[k]);
           carry[k] = a[i][k] * gh;
           const float through = carry[k] * h[i][k];
-          s1 = k ? fmaf(gh, c.B(i - j, k), s1) : gh * c.B(i - j, k);
+          s1 = k ? fmaf(gh, now.B(i - j, k), s1) : gh * now.B(i - j, k);
           s2 = k ? fmaf(through, A[k], s2) : through * A[k];
           dA[k] = fmaf(through, in_[i].x, dA[k]);
-          if (GATE) plain = k ? fmaf(c.C(i - j, k), h[i + 1][k], plain) : c.C(i - j, k) * h[i + 1][k];
+          if (GATE) plain = k ? fmaf(now.C(i - j, k), h[i + 1][k], plain) : now.C(i - j, k) * h[i + 1][k];
           pair[k] = swap32_add(gh * in_[i].y, h[i + 1][k] * q[i]);
         }
         step_sum[i] = half_row_add(swap16_add(pair[0], pair[1]), swap16_add(pair[2], pair[3]));
@@ -306,29 +318,34 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
         if (GATE) share[set][SUMS - 1][w][i][lane] = plain;
       }
     };
-    wait_for_scalars();
-    late.ask(from + kBatch * 2 * kHeld);
-    __builtin_amdgcn_sched_barrier(0);
-    forward(early, 0);
-    __builtin_amdgcn_sched_barrier(0);
+    // Bm and Cm are asked for in the order 0 2 4 6 4 2 0 of steps: the last two are there when the walk turns
+#pragma unroll
+    for (int j = 0; j < PASS; j += BATCH) {
+      wait_for_scalars();
+      next.ask(from + (j + BATCH < PASS ? j + BATCH : j - BATCH) * 2 * kHeld);
+      __builtin_amdgcn_sched_barrier(0);
+      forward(j);
+      __builtin_amdgcn_sched_barrier(0);
+      if (j + BATCH < PASS) now = next;
+    }
     if (SETS == 1) __syncthreads();                      // the last pass's shares have been read
-    wait_for_scalars();
-    early.ask(from);
-    __builtin_amdgcn_sched_barrier(0);
-    forward(late, kBatch);
-    backward(late, kBatch);
-    __builtin_amdgcn_sched_barrier(0);
-    wait_for_scalars();
-    late.ask(from - (p ? PASS * 2 * kHeld : 0));
-    __builtin_amdgcn_sched_barrier(0);
-    backward(early, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    early = late;
+#pragma unroll
+    for (int j = PASS - BATCH; j >= 0; j -= BATCH) {
+      if (j < PASS - BATCH) {
+        wait_for_scalars();
+        next.ask(from + (j ? j - BATCH : p ? -PASS : 0) * 2 * kHeld);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      backward(j);
+      __builtin_amdgcn_sched_barrier(0);
+      now = next;
+    }
     const bool odd = lane & 1, high = lane & 2;
     const float low = in_four_add<0x4E>(four_add(step_sum[0], step_sum[1]), four_add(step_sum[2], step_sum[3]), high);
     const float top = in_four_add<0x4E>(four_add(step_sum[4], step_sum[5]), four_add(step_sum[6], step_sum[7]), high);
     const float part = in_four_add<0xB1>(low, top, odd);
-    o.bc[(((((int64_t)(tile % l.tiles) * l.B + b) * l.G + g) * (padded / PASS) + first / PASS) * WAVES + w) * 64 + lane] = part;
+    at_bc[lane] = part;
+    at_bc -= WAVES * 64;
     from -= PASS * 2 * kHeld;
     if (p) prepare(first - PASS, buffer ^ 1);
     __syncthreads();
@@ -352,10 +369,6 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
       if (w * kHeld + i < l.N) o.dh0[((int64_t)b * l.D + d) * l.N + w * kHeld + i] = carry[i];
-  for (int t = (t0 > len ? t0 : len) + w; t < t1; t += WAVES) {
-    element(o.du.at(t, b), byte) = static_cast<E>(0.0f), element(o.ddt.at(t, b), byte) = static_cast<E>(0.0f);
-    if (GATE) element(o.dz.at(t, b), byte) = static_cast<E>(0.0f);
-  }
 }
 
 // dB and dC: the tiles' parts in the tiles' order.  A thread has the place of a lane of the main kernel.

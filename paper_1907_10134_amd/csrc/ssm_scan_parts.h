@@ -77,18 +77,20 @@ coef_kernel(const Layer<E> l, int waves, int64_t all, float* __restrict__ coef) 
   coef[i] = in ? load((of < kHeld ? l.Bm : l.Cm).at(t, b) + g * l.N + n) : 0.0f;
 }
 
-// Bm and Cm of kBatch steps in scalar registers.  Scalar loads come back in any order, so the only wait for one is the wait
+// Bm and Cm of STEPS steps in scalar registers.  Scalar loads come back in any order, so the only wait for one is the wait
 // for all that are out, LDS reads among them: a batch's loads go out together, right behind the wait for the batch
 // before, and have the time of that one's steps.  (Left to the compiler, which asks for one step's at a time, a wave
-// waited 16 times a pass: 492 us instead of 283 at T = 30000, D = 2048.)
-constexpr int kBatch = 4;
+// waited for every one: 492 us instead of 344 at T = 30000, D = 2048.)  Batches of four steps, 64 registers for two of them,
+// suit the summaries; in the main kernels they left so few that a quarter of the backward pass's vector instructions moved
+// scalars to and from vector lanes: batches of two there.
 typedef float TwoSteps __attribute__((ext_vector_type(4 * kHeld)));
 typedef const __attribute__((address_space(4))) TwoSteps* ScalarCoef;       // read through the scalar cache
+template <int STEPS>
 struct Coef {
-  TwoSteps at[kBatch / 2];
+  TwoSteps at[STEPS / 2];
   __device__ __forceinline__ void ask(const float* from) {
 #pragma unroll
-    for (int k = 0; k < kBatch / 2; ++k) at[k] = ((ScalarCoef)from)[k];
+    for (int k = 0; k < STEPS / 2; ++k) at[k] = ((ScalarCoef)from)[k];
   }
   __device__ __forceinline__ float B(int i, int k) const { return at[i / 2][i % 2 * 2 * kHeld + k]; }
   __device__ __forceinline__ float C(int i, int k) const { return at[i / 2][i % 2 * 2 * kHeld + kHeld + k]; }

@@ -15,7 +15,7 @@ import torch
 from .binding import _check, _lib, _ptr, _stream, _workspace
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-_i32 = torch.int32
+_i32, _f32 = torch.int32, torch.float32
 
 _c_int, _c_void_p, _c_size_t = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
 for _name, _res, _args in (
@@ -56,6 +56,21 @@ def _rows(t, shape, dtype, name, groups=False):
     elif s[-1] != 1 and shape[-1] > 1:
         raise ValueError("%s must be contiguous in its channels" % name)
     return t.data_ptr(), s[0], s[1]
+
+
+def _token(t, shape, dtype, name, groups=False):
+    """The same of one token of each stream, [B, channels] or [B, G, N]: (pointer, 0, sample stride)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype is dtype and t.is_cuda and t.shape == shape:
+        s = t.stride()
+        if groups:
+            if (s[2] == 1 or shape[2] == 1) and (s[1] == shape[2] or shape[1] == 1):
+                return t.data_ptr(), 0, s[0]
+        elif s[1] == 1 or shape[1] == 1:
+            return t.data_ptr(), 0, s[0]
+    p, _, b = _rows(t.unsqueeze(0), (1,) + tuple(shape), dtype, name, groups)      # names what is wrong
+    return p, 0, b
 
 
 def _param(t, shape, name, dtype=torch.float32):
@@ -168,27 +183,43 @@ def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=N
     return SsmGrads(du, ddt, dA, dBm, dCm, dskip, dz, dbias, dh0)
 
 
-def _slots(slots, B, state, name="slots"):
+def _slots(slots, B, slots_in_state):
     if slots is None:
-        if state.shape[0] < B:
+        if slots_in_state < B:
             raise ValueError("state has fewer slots than the batch has rows")
         return None
-    return _param(slots, (B,), name, _i32)
+    return _param(slots, (B,), "slots", _i32)
 
 
 def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slots=None, y=None, stream=None):
     """bppsa_ssm_scan_step: y [B, D] of one token of each stream; state [slots, D, N] float32 is advanced in place.
 
     u, dt, z [B, D]; Bm, Cm [B, G, N]; slots [B] int32, a row with one outside the state (-1, say) belongs to no stream."""
-    if y is None:
-        y = torch.empty_like(u)
-    up = lambda x: None if x is None else x.unsqueeze(0)
-    layer, (_, B, D, N, _) = _layer(up(u), up(dt), A, up(Bm), up(Cm), skip, up(z), dt_bias, None, None)
-    if state.dim() != 3 or state.shape[1:] != (D, N):
+    if not (isinstance(u, torch.Tensor) and isinstance(Bm, torch.Tensor)):
+        raise TypeError("u and Bm must be torch.Tensors")
+    if u.dim() != 2 or Bm.dim() != 3:
+        raise ValueError("u must be [B, D] and Bm [B, G, N]")
+    wide, narrow, t = u.shape, Bm.shape, u.dtype
+    B, D = wide
+    if t not in _TYPES:
+        raise ValueError("activations must be float32, bfloat16 or float16, got %s" % t)
+    if narrow[0] != B:
+        raise ValueError("Bm must have %d rows, got %d" % (B, narrow[0]))
+    if A is None:
+        raise TypeError("A must be a torch.Tensor")
+    _, G, N = narrow
+    layer = _pack_layer(1, B, D, N, G, _TYPES[t], *_token(u, wide, t, "u"), *_token(dt, wide, t, "dt"),
+                        *(_NONE if z is None else _token(z, wide, t, "z")), *_token(Bm, narrow, t, "Bm", True),
+                        *_token(Cm, narrow, t, "Cm", True), _param(A, (D, N), "A"), _param(skip, (D,), "skip"),
+                        _param(dt_bias, (D,), "dt_bias"), 0, 0)
+    at = _ptr(state, _f32, "state")
+    slots_in_state = state.shape[0]
+    if state.shape != (slots_in_state, D, N):
         raise ValueError("state must be [slots, %d, %d], got %s" % (D, N, tuple(state.shape)))
-    _check(_lib.bppsa_ssm_scan_step(layer, _pack_rows(*_rows(up(y), (1, B, D), u.dtype, "y")),
-                                    _ptr(state, torch.float32, "state"), state.shape[0], _slots(slots, B, state),
-                                    _stream(stream)), "bppsa_ssm_scan_step")
+    if y is None:
+        y = torch.empty(wide, dtype=t, device=u.device)
+    _check(_lib.bppsa_ssm_scan_step(layer, _pack_rows(*_token(y, wide, t, "y")), at, slots_in_state,
+                                    _slots(slots, B, slots_in_state), _stream(stream)), "bppsa_ssm_scan_step")
     return y
 
 
@@ -239,12 +270,23 @@ def ssm_conv_backward(dy, x, weight, bias=None, silu=True, state0=None, lengths=
 
 def ssm_conv_step(x, weight, bias, state, silu=True, slots=None, y=None, stream=None):
     """bppsa_ssm_conv_step: y [B, D] of one token of each stream; state [slots, W-1, D] is moved on in place."""
-    if y is None:
-        y = torch.empty_like(x)
-    conv, (_, B, D, W) = _conv(x.unsqueeze(0), weight, bias, silu, None, None)
-    if state.dim() != 3 or state.shape[1:] != (W - 1, D):
+    if not (isinstance(x, torch.Tensor) and isinstance(weight, torch.Tensor)):
+        raise TypeError("x and weight must be torch.Tensors")
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x must be [B, D] and weight [D, W]")
+    shape, t = x.shape, x.dtype
+    B, D = shape
+    W = weight.shape[1]
+    if t not in _TYPES:
+        raise ValueError("activations must be float32, bfloat16 or float16, got %s" % t)
+    conv = _pack_conv(1, B, D, W, _TYPES[t], bool(silu), *_token(x, shape, t, "x"), _param(weight, (D, W), "weight"),
+                      _param(bias, (D,), "bias"), 0, 0)
+    at = _ptr(state, t, "state")
+    slots_in_state = state.shape[0]
+    if state.shape != (slots_in_state, W - 1, D):
         raise ValueError("state must be [slots, %d, %d], got %s" % (W - 1, D, tuple(state.shape)))
-    _check(_lib.bppsa_ssm_conv_step(conv, _pack_rows(*_rows(y.unsqueeze(0), (1, B, D), x.dtype, "y")),
-                                    _ptr(state, x.dtype, "state"), state.shape[0], _slots(slots, B, state), _stream(stream)),
-           "bppsa_ssm_conv_step")
+    if y is None:
+        y = torch.empty(shape, dtype=t, device=x.device)
+    _check(_lib.bppsa_ssm_conv_step(conv, _pack_rows(*_token(y, shape, t, "y")), at, slots_in_state,
+                                    _slots(slots, B, slots_in_state), _stream(stream)), "bppsa_ssm_conv_step")
     return y

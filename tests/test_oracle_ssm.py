@@ -140,6 +140,9 @@ def test_scan_refusals(lib):
     assert _call_scan(lib, _ssm(T=1 << 30, B=1 << 15, D=1 << 20)) == EOVERFLOW
     # outputs of which two elements share a place
     assert _call_scan(lib, _ssm(), y=Rows(ONE, 0, 64)) == EINVAL and _call_scan(lib, _ssm(), y=Rows(ONE, 64, 0)) == EINVAL
+    # the last states in the place of the first ones
+    assert lib.bppsa_ssm_scan(ctypes.byref(_ssm(h0=ONE)), ctypes.byref(_rows()), ctypes.c_void_p(ONE), None, ctypes.c_void_p(512),
+                              ctypes.c_size_t(1 << 40), None) == EINVAL
     need = lib.bppsa_ssm_scan_workspace_bytes(4000, 1, 32, 16, 1)
     if need:
         assert _call_scan(lib, _ssm(T=4000, B=1)) == EWORKSPACE
