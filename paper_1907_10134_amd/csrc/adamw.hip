@@ -13,7 +13,7 @@ constexpr int kPiece = BPPSA_ADAMW_PIECE;
 static_assert(kBlock == BPPSA_WAVE * 4, "a wave holds a block, four values a lane");
 
 struct Step {
-  float beta1, one_minus_beta1, beta2, one_minus_beta2, correct1, root_correct2, eps, lr;
+  float beta1, one_minus_beta1, beta2, one_minus_beta2, per_correct1, per_root_correct2, eps, lr;
   double lr_exact;
   uint32_t seed;
 };
@@ -91,7 +91,74 @@ __device__ __forceinline__ uint32_t pack(const float (&q)[4]) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(within(q[2]), within(q[3]), w, true);
 }
 
-// A workgroup takes a piece; a wave every fourth block of it, four values a lane.  Bound by memory.
+// What a lane has of a block: four values of everything.
+template <typename G, bool EIGHT>
+struct Held {
+  G g[4];
+  float theta[4];
+  std::conditional_t<EIGHT, uint8_t, float> m[4], v[4];
+  float m_scale, v_scale;
+  __device__ __forceinline__ void get(const bppsa_adamw_tensor& t, int64_t i, int n, bool full) {
+    typedef std::conditional_t<EIGHT, uint8_t, float> M;
+    get4(static_cast<const G*>(t.grad) + i, n, full, g);
+    get4(t.theta + i, n, full, theta);
+    get4(static_cast<const M*>(t.m) + i, n, full, m);
+    get4(static_cast<const M*>(t.v) + i, n, full, v);
+    if (EIGHT) m_scale = t.m_scale[i / kBlock], v_scale = t.v_scale[i / kBlock];
+  }
+};
+
+// One block by one wave.
+template <typename G, bool EIGHT>
+__device__ __forceinline__ void update(const bppsa_adamw_tensor& t, const Held<G, EIGHT>& x, int64_t i, int n, bool full, int lane,
+                                       float keep, uint32_t tensor, const Step& c) {
+  float theta[4], m[4], v[4], root[4];
+  if constexpr (EIGHT) {
+    unpack(__builtin_bit_cast(uint32_t, x.m), m);
+    unpack(__builtin_bit_cast(uint32_t, x.v), v);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m[k] *= x.m_scale, v[k] *= x.v_scale, v[k] *= v[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m[k] = x.m[k], v[k] = x.v[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float g = static_cast<float>(x.g[k]);
+    m[k] = fmaf(c.one_minus_beta1, g, c.beta1 * m[k]);
+    v[k] = fmaf(c.one_minus_beta2, g * g, c.beta2 * v[k]);
+    root[k] = sqrtf(v[k]);
+    // v_rcp_f32 is good to one step: 2^-23 of an update that is itself added to theta
+    const float update = (m[k] * c.per_correct1) * __builtin_amdgcn_rcpf(fmaf(root[k], c.per_root_correct2, c.eps));
+    theta[k] = fmaf(x.theta[k], keep, -c.lr * update);
+  }
+  put4(t.theta + i, n, full, theta);
+  if (t.copy) {
+    bf16_t small[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) small[k] = static_cast<bf16_t>(theta[k]);
+    put4(static_cast<bf16_t*>(t.copy) + i, n, full, small);
+  }
+  if constexpr (EIGHT) {
+    const float sm = scale_of(wave_largest(m)), sv = scale_of(wave_largest(root));
+    const float im = 1.0f / sm, iv = 1.0f / sv;
+    const uint32_t place = c.seed * 0x9E3779B1u + tensor * 0x6A09E667u + (uint32_t)i;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      m[k] *= im;
+      root[k] = up_or_down(root[k] * iv, chance(place + k));
+    }
+    put4(static_cast<uint8_t*>(t.m) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(m)).v);
+    put4(static_cast<uint8_t*>(t.v) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(root)).v);
+    if (lane == 0) t.m_scale[i / kBlock] = sm, t.v_scale[i / kBlock] = sv;
+  } else {
+    put4(static_cast<float*>(t.m) + i, n, full, m);
+    put4(static_cast<float*>(t.v) + i, n, full, v);
+  }
+}
+
+// A workgroup takes a piece; a wave four blocks of it in a row, four values a lane, and asks for all of a full piece's
+// before it works on the first.  Bound by memory.
 template <typename G, bool EIGHT>
 __global__ void __launch_bounds__(kThreads)
 adamw_kernel(const bppsa_adamw_tensor* __restrict__ tensors, const bppsa_adamw_piece* __restrict__ pieces, const Step c) {
@@ -99,64 +166,27 @@ adamw_kernel(const bppsa_adamw_tensor* __restrict__ tensors, const bppsa_adamw_p
   const bppsa_adamw_tensor t = tensors[piece.tensor];
   const int64_t first = (int64_t)piece.piece * kPiece;
   const int count = (int)(t.n - first < kPiece ? t.n - first : kPiece);
-  const int lane = threadIdx.x & 63;
+  constexpr int BLOCKS = kPiece / kBlock / (kThreads / BPPSA_WAVE);
+  const int lane = threadIdx.x & 63, start = (threadIdx.x >> 6) * BLOCKS * kBlock;
   const float keep = (float)(1.0 - c.lr_exact * t.decay);
   const bool aligned = (((uintptr_t)t.theta | ((uintptr_t)t.grad * (16 / (sizeof(G) * 4))) |
                          (EIGHT ? ((uintptr_t)t.m | (uintptr_t)t.v) * 4 : (uintptr_t)t.m | (uintptr_t)t.v) |
                          (uintptr_t)t.copy * 2) & 15) == 0;
-  for (int at = (threadIdx.x >> 6) * kBlock; at < count; at += kThreads / BPPSA_WAVE * kBlock) {
+  if (aligned && count == kPiece) {
+    Held<G, EIGHT> x[BLOCKS];
+#pragma unroll
+    for (int j = 0; j < BLOCKS; ++j) x[j].get(t, first + start + j * kBlock + lane * 4, 4, true);
+#pragma unroll
+    for (int j = 0; j < BLOCKS; ++j)
+      update(t, x[j], first + start + j * kBlock + lane * 4, 4, true, lane, keep, (uint32_t)piece.tensor, c);
+    return;
+  }
+  for (int at = start; at < count && at < start + BLOCKS * kBlock; at += kBlock) {
     const int64_t i = first + at + lane * 4;
     const int n = count - at - lane * 4;       // values that are left for this lane
-    const bool full = aligned && n >= 4;
-    G g[4];
-    float theta[4], m[4], v[4];
-    get4(static_cast<const G*>(t.grad) + i, n, full, g);
-    get4(t.theta + i, n, full, theta);
-    if constexpr (EIGHT) {
-      uint8_t wm[4], wv[4];
-      get4(static_cast<const uint8_t*>(t.m) + i, n, full, wm);
-      get4(static_cast<const uint8_t*>(t.v) + i, n, full, wv);
-      const float sm = t.m_scale[(first + at) / kBlock], sv = t.v_scale[(first + at) / kBlock];
-      unpack(__builtin_bit_cast(uint32_t, wm), m);
-      unpack(__builtin_bit_cast(uint32_t, wv), v);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) m[k] *= sm, v[k] *= sv, v[k] *= v[k];
-    } else {
-      get4(static_cast<const float*>(t.m) + i, n, full, m);
-      get4(static_cast<const float*>(t.v) + i, n, full, v);
-    }
-    float root[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float gk = static_cast<float>(g[k]);
-      m[k] = fmaf(c.one_minus_beta1, gk, c.beta1 * m[k]);
-      v[k] = fmaf(c.one_minus_beta2, gk * gk, c.beta2 * v[k]);
-      root[k] = sqrtf(v[k]);
-      theta[k] = fmaf(theta[k], keep, -c.lr * ((m[k] / c.correct1) / (root[k] / c.root_correct2 + c.eps)));
-    }
-    put4(t.theta + i, n, full, theta);
-    if (t.copy) {
-      bf16_t small[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) small[k] = static_cast<bf16_t>(theta[k]);
-      put4(static_cast<bf16_t*>(t.copy) + i, n, full, small);
-    }
-    if constexpr (EIGHT) {
-      const float sm = scale_of(wave_largest(m)), sv = scale_of(wave_largest(root));
-      const float im = 1.0f / sm, iv = 1.0f / sv;
-      const uint32_t place = c.seed * 0x9E3779B1u + (uint32_t)piece.tensor * 0x6A09E667u + (uint32_t)i;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        m[k] *= im;
-        root[k] = up_or_down(root[k] * iv, chance(place + k));
-      }
-      put4(static_cast<uint8_t*>(t.m) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(m)).v);
-      put4(static_cast<uint8_t*>(t.v) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(root)).v);
-      if (lane == 0) t.m_scale[(first + at) / kBlock] = sm, t.v_scale[(first + at) / kBlock] = sv;
-    } else {
-      put4(static_cast<float*>(t.m) + i, n, full, m);
-      put4(static_cast<float*>(t.v) + i, n, full, v);
-    }
+    Held<G, EIGHT> x;
+    x.get(t, i, n, aligned && n >= 4);
+    update(t, x, i, n, aligned && n >= 4, lane, keep, (uint32_t)piece.tensor, c);
   }
 }
 
@@ -180,8 +210,8 @@ extern "C" bppsa_status bppsa_adamw_step(int n_tensors, const bppsa_adamw_tensor
   if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps > 0) || !std::isfinite(lr)) return BPPSA_EINVAL;
   if (state_bits != 32 && state_bits != 8) return BPPSA_EUNSUPPORTED;
   if (n_pieces > 0x7FFFFFFF) return BPPSA_EOVERFLOW;
-  const Step c{(float)beta1, (float)(1 - beta1), (float)beta2, (float)(1 - beta2), (float)(1 - std::pow(beta1, step)),
-               (float)std::sqrt(1 - std::pow(beta2, step)), (float)eps, (float)lr, lr, seed};
+  const Step c{(float)beta1, (float)(1 - beta1), (float)beta2, (float)(1 - beta2), (float)(1 / (1 - std::pow(beta1, step))),
+               (float)(1 / std::sqrt(1 - std::pow(beta2, step))), (float)eps, (float)lr, lr, seed};
   return ssm::by_type(grad_type, [&](auto g) -> bppsa_status {
     using G = decltype(g);
     if (state_bits == 8)

@@ -28,20 +28,18 @@ __device__ __forceinline__ float load(const E* p) { return static_cast<float>(*p
 template <typename E>
 __device__ __forceinline__ void store(E* p, float v) { *p = static_cast<E>(v); }
 
-// The rows of an array that a wave walks through: the row's address in scalar registers, a lane's 32 bits of bytes added by
-// the access itself.  (The asm keeps the compiler from adding the lane's offset to the array's start once and the row's
-// to that with a vector instruction for every access.)
+// The rows of an array that a wave walks through: a lane's address in vector registers, moved on by a stride in scalar ones.
+// (Both in scalar registers, with the lane's offset added by the access, left too few of them for Bm and Cm.)
 template <typename E>
 struct Walk {
-  uint64_t row;
+  uint64_t lane;
   int64_t step;
-  __device__ __forceinline__ Walk(const Rows<E>& r, int t, int b) : row((uint64_t)r.at(t, b)), step(r.st * (int64_t)sizeof(E)) {}
-  __device__ __forceinline__ __attribute__((address_space(1))) E& at(int rows_on, uint32_t byte) const {
-    uint64_t p = row + rows_on * step;
-    asm("" : "+s"(p));
-    return *(__attribute__((address_space(1))) E*)((const __attribute__((address_space(1))) char*)p + byte);
+  __device__ __forceinline__ Walk(const Rows<E>& r, int t, int b, uint32_t byte)
+      : lane((uint64_t)r.at(t, b) + byte), step(r.st * (int64_t)sizeof(E)) {}
+  __device__ __forceinline__ __attribute__((address_space(1))) E& at(int rows_on) const {
+    return *(__attribute__((address_space(1))) E*)(lane + rows_on * step);
   }
-  __device__ __forceinline__ void move(int rows) { row += rows * step; }
+  __device__ __forceinline__ void move(int rows) { lane += rows * step; }
 };
 
 // V neighbouring elements by one access of any alignment: the memory path takes 16 bytes from an odd element as well, and a

@@ -12,6 +12,7 @@ using namespace ssm;
 // of steps, the window of the last W inputs in registers.  The last thread of a row starts early enough to have V channels
 // too and repeats some of its neighbour's, with the same results; fewer than V channels go one to a thread.
 constexpr int kAhead = 4;        // rows that are asked for together
+constexpr int kTogether = 4;     // spans of a workgroup of the backward pass
 
 template <typename E>
 struct Conv {
@@ -104,21 +105,24 @@ conv_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state_last) {
 }
 
 // dx[t] = sum_k w[k] dp[t + W-1 - k], dp = dL/dp with p recomputed from its window.  A span forms the dp of its steps, and of
-// W-1 behind it for its last dx; its sums of dweight and dbias go to parts [span][b][W+1][D].  The first span also has the
-// gradient of the carried state: dx at t = -(W-1)..-1.
+// W-1 behind it for its last dx.  The four waves of a workgroup take a span each and add their sums of dweight and dbias,
+// which go to parts [four spans][b][W+1][D].  The first span also has the gradient of the carried state: dx at
+// t = -(W-1)..-1.
 template <typename E, int W, int V>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(64 * kTogether)
 conv_backward_kernel(const Conv<E> c, Rows<const E> dy, Rows<E> dx, E* __restrict__ dstate0, float* __restrict__ parts) {
-  const int first = (blockIdx.x * 64 + threadIdx.x) * V, d = first + V <= c.D ? first : c.D - V;
-  const int b = blockIdx.y, t0 = blockIdx.z * c.span;
-  if (first >= c.D) return;
+  __shared__ float share[kTogether - 1][(W + 1) * V][64];
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
+  // threads behind the last channel repeat the last ones', with the same results
+  const int first = (blockIdx.x * 64 + lane) * V, d = first + V <= c.D ? first : c.D - V;
+  const int b = blockIdx.y, t0 = (blockIdx.z * kTogether + q) * c.span;
   const int len = clamp_length(c.lengths, b, c.T), t1 = t0 + c.span < c.T ? t0 + c.span : c.T;
   float seen[W][V], dp[W][V] = {}, dw[W + 1][V] = {};
   const Taps<V, W> taps(c, d);
 #pragma unroll
   for (int k = 1; k < W; ++k) input<E, W, V>(c, t0 - W + k, b, d, len, seen[k]);
   // at step t dp[j] holds dL/dp[t - (W-1) + j]; it completes dx[t - (W-1)]
-  for (int t = t0; t < t1 + W - 1; t += kAhead) {
+  for (int t = t0; t0 < t1 && t < t1 + W - 1; t += kAhead) {
     Some<E, V> x[kAhead] = {}, go[kAhead] = {};
     if (len)
 #pragma unroll
@@ -159,6 +163,19 @@ conv_backward_kernel(const Conv<E> c, Rows<const E> dy, Rows<E> dx, E* __restric
       }
     }
   }
+  if (q)
+#pragma unroll
+    for (int k = 0; k <= W; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) share[q - 1][k * V + i][lane] = dw[k][i];
+  __syncthreads();
+  if (q) return;
+#pragma unroll
+  for (int k = 0; k <= W; ++k)
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int j = 0; j + 1 < kTogether; ++j) dw[k][i] += share[j][k * V + i][lane];
   float* to = parts + ((int64_t)blockIdx.z * c.B + b) * (W + 1) * c.D + d;
 #pragma unroll
   for (int k = 0; k <= W; ++k) store_some<float, V>(to + (int64_t)k * c.D, dw[k]);
@@ -213,10 +230,11 @@ conv_step_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state, int slots_in
   store_some<E, V>(y.at(0, b) + d, out);
 }
 
-// Steps of a span: 64, or fewer, to 8, while the device would have less than four waves a SIMD; every span reads W-1 rows twice.
-int span_of(int T, int64_t waves_a_step) {
+// Steps of a span: 64, or fewer, to 8, while the device would have less than `waves` a SIMD; every span reads W-1 rows twice.
+// Forward at T = 4096, B = 4, D = 4096: 60.8 us in spans of 32 (four waves), 69.5 in spans of 64.
+int span_of(int T, int64_t waves_a_step, int waves) {
   int span = 64;
-  while (span > 8 && waves_a_step * bppsa_ceil_div(T, span) < (int64_t)bppsa_compute_units() * 16) span /= 2;
+  while (span > 8 && waves_a_step * bppsa_ceil_div(T, span) < (int64_t)bppsa_compute_units() * 4 * waves) span /= 2;
   return span;
 }
 // Channels of a thread.
@@ -229,7 +247,7 @@ int backward_width(int D, int type) {
   const int V = type == BPPSA_F32 ? kNarrow<float> : kNarrow<bf16_t>;
   return D >= V ? V : 1;
 }
-int backward_span(int T, int B, int D, int type) { return span_of(T, (int64_t)B * waves_for(D, backward_width(D, type))); }
+int backward_span(int T, int B, int D, int type) { return span_of(T, (int64_t)B * waves_for(D, backward_width(D, type)), 2); }
 
 template <typename F>
 bppsa_status by_width(int W, F&& f) {
@@ -257,7 +275,7 @@ extern "C" bppsa_status bppsa_ssm_conv(const bppsa_conv* conv, const bppsa_rows*
     return by_width(conv->W, [&](auto w) {
       auto run = [&](auto v) {
         constexpr int V = v.value;
-        const int wide = waves_for(conv->D, V), span = span_of(conv->T, (int64_t)conv->B * wide);
+        const int wide = waves_for(conv->D, V), span = span_of(conv->T, (int64_t)conv->B * wide, 4);
         conv_kernel<E, w.value, V><<<dim3(wide, conv->B, bppsa_ceil_div(conv->T, span)), 64, 0, (hipStream_t)stream>>>(
             conv_of<E>(*conv, span), rows_of<E>(*y), static_cast<E*>(state_last));
         BPPSA_CHECK_LAUNCH();
@@ -272,7 +290,7 @@ extern "C" size_t bppsa_ssm_conv_backward_workspace_bytes(int T, int B, int D, i
   if (T < 1 || B < 1 || D < 1 || W < 2 || W > BPPSA_SSM_MAX_W) return 0;
   // the type is not asked for: the shorter spans of the two
   const int span = std::min(backward_span(T, B, D, BPPSA_F32), backward_span(T, B, D, BPPSA_BF16));
-  return (size_t)bppsa_ceil_div(T, span) * B * (W + 1) * D * sizeof(float);
+  return (size_t)bppsa_ceil_div(T, span * kTogether) * B * (W + 1) * D * sizeof(float);
 }
 
 extern "C" bppsa_status bppsa_ssm_conv_backward(const bppsa_conv* conv, const bppsa_rows* dy, const bppsa_rows* dx,
@@ -289,10 +307,10 @@ extern "C" bppsa_status bppsa_ssm_conv_backward(const bppsa_conv* conv, const bp
     using E = decltype(e);
     return by_width(conv->W, [&](auto w) {
       constexpr int W = w.value;
-      const int span = backward_span(conv->T, conv->B, conv->D, conv->type), spans = bppsa_ceil_div(conv->T, span);
+      const int span = backward_span(conv->T, conv->B, conv->D, conv->type), spans = bppsa_ceil_div(conv->T, span * kTogether);
       auto run = [&](auto v) {
         constexpr int V = v.value;
-        conv_backward_kernel<E, W, V><<<dim3(waves_for(conv->D, V), conv->B, spans), 64, 0, s>>>(
+        conv_backward_kernel<E, W, V><<<dim3(waves_for(conv->D, V), conv->B, spans), 64 * kTogether, 0, s>>>(
             conv_of<E>(*conv, span), rows_of<const E>(*dy), rows_of<E>(*dx), static_cast<E*>(dstate0), parts);
       };
       if (backward_width(conv->D, conv->type) == 1) run(std::integral_constant<int, 1>{});

@@ -19,8 +19,8 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   __shared__ float2 step_in[2][PASS][kTile];
   __shared__ float share[SUMMARY ? 1 : 2][SUMMARY ? 1 : WAVES][SUMMARY ? 1 : PASS][kTile];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int count = SUMMARY ? spans.count - 1 : spans.count;       // nothing asks for the last span's summary
-  const int span = blockIdx.x % count, tile = blockIdx.x / count, g = tile / l.tiles, b = blockIdx.y;
+  // neighbours in the grid, which go to different dies, are tiles of a span: spans may lie behind a sample's end
+  const int tile = blockIdx.x % (l.G * l.tiles), span = blockIdx.x / (l.G * l.tiles), g = tile / l.tiles, b = blockIdx.y;
   const int in = tile % l.tiles * kTile + lane;
   const bool on = in < l.wide;
   const int d = g * l.wide + (on ? in : 0);              // lanes without a channel compute the group's first, and store nothing
@@ -38,28 +38,25 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
     h[i] = !SUMMARY && n < l.N && l.h0 ? l.h0[((int64_t)b * l.D + d) * l.N + n] : 0.0f;
   }
   if (!SUMMARY && stop > t0)
-    for (int k = 0; k < span; ++k) {
-      const float4 end = *reinterpret_cast<const float4*>(sum.ends + state_at(k, l.B, b, WAVES, w, l.D, d));
-      const float s = sum.sums[((int64_t)k * l.B + b) * l.D + d];
-      h[0] = fmaf(exp2_fast(A2[0] * s), h[0], end.x), h[1] = fmaf(exp2_fast(A2[1] * s), h[1], end.y);
-      h[2] = fmaf(exp2_fast(A2[2] * s), h[2], end.z), h[3] = fmaf(exp2_fast(A2[3] * s), h[3], end.w);
-    }
+    join_spans(sum, 0, 1, span, l.B, b, WAVES, w, l.D, d, A2, h);
 
   const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f, skip = l.skip ? l.skip[d] : 0.0f;
   const uint32_t byte = (uint32_t)d * sizeof(E);
   const int mine = w * ROWS;                             // this wave's first step of a pass
-  Walk<const E> at_u(l.u, t0 + mine, b), at_dt(l.dt, t0 + mine, b), at_z(l.z, t0 + mine, b);
-  Walk<E> at_y(y, t0 + mine, b);
+  Walk<const E> at_u(l.u, t0 + mine, b, byte), at_dt(l.dt, t0 + mine, b, byte), at_z(l.z, t0 + mine, b, byte);
+  Walk<E> at_y(y, t0 + mine, b, byte);
+  float* at_states = SUMMARY || !states ? nullptr : states + state_at(t0 / kKept, l.B, b, WAVES, w, l.D, d);
   E u[ROWS], dt[ROWS], z[ROWS], u_was[ROWS], z_was[ROWS];
   float total = 0.0f;
   // The values stay as they are loaded until they are needed: a conversion here would wait for each load by itself.
   auto fetch = [&](int first) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      u[r] = dt[r] = z[r] = E(0.0f);
       if (mine + r < PASS && first + mine + r < stop) {
-        u[r] = at_u.at(r, byte), dt[r] = at_dt.at(r, byte);
-        if (GATE) z[r] = at_z.at(r, byte);
+        u[r] = at_u.at(r), dt[r] = at_dt.at(r);
+        if (GATE) z[r] = at_z.at(r);
+      } else {
+        u[r] = dt[r] = z[r] = E(0.0f);
       }
     }
     at_u.move(PASS), at_dt.move(PASS);
@@ -87,7 +84,7 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
-      if (mine + r < PASS && first + mine + r < stop && on) at_y.at(r, byte) = static_cast<E>(v[r]);
+      if (mine + r < PASS && first + mine + r < stop && on) at_y.at(r) = static_cast<E>(v[r]);
     at_y.move(PASS);
   };
 
@@ -110,8 +107,10 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) u_was[r] = u[r], z_was[r] = z[r];
     if (p + 1 < passes) fetch(first + PASS);
-    if (!SUMMARY && states && on)
-      *reinterpret_cast<float4*>(states + state_at(first / kKept, l.B, b, WAVES, w, l.D, d)) = make_float4(h[0], h[1], h[2], h[3]);
+    if (!SUMMARY && states) {
+      if (on) *reinterpret_cast<float4*>(at_states) = make_float4(h[0], h[1], h[2], h[3]);
+      at_states += (int64_t)l.B * WAVES * l.D * kHeld;
+    }
 #pragma unroll
     for (int j = 0; j < PASS; j += BATCH) {
       wait_for_scalars();
@@ -266,7 +265,7 @@ extern "C" bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows*
     const Summary sum{part(at.ends), part(at.sums)};
     return by_waves(waves_of(l.N), [&](auto waves) {
       constexpr int W = waves.value;
-      if (at.spans.count > 1)
+      if (at.spans.count > 1)                  // nothing asks for the last span's summary
         scan_kernel<E, W, true, false><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
             l, Rows<E>{}, nullptr, nullptr, part(at.coef), sum, at.spans);
       const auto kernel = l.z.data ? scan_kernel<E, W, false, true> : scan_kernel<E, W, false, false>;

@@ -69,7 +69,7 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const float* __
   constexpr int ROWS = (PASS + WAVES - 1) / WAVES, BATCH = 4;
   __shared__ float2 step_in[2][PASS][kTile];             // (s, q)
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int span = blockIdx.x % (spans.count - 1) + 1, tile = blockIdx.x / (spans.count - 1), g = tile / l.tiles, b = blockIdx.y;
+  const int tile = blockIdx.x % (l.G * l.tiles), span = blockIdx.x / (l.G * l.tiles) + 1, g = tile / l.tiles, b = blockIdx.y;
   const int in = tile % l.tiles * kTile + lane;
   const bool on = in < l.wide;
   const int d = g * l.wide + (on ? in : 0);
@@ -85,15 +85,16 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const float* __
   const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f;
   const uint32_t byte = (uint32_t)d * sizeof(E);
   const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
-  Walk<const E> at_dt(l.dt, last + mine, b), at_dy(dy, last + mine, b), at_z(l.z, last + mine, b);
+  Walk<const E> at_dt(l.dt, last + mine, b, byte), at_dy(dy, last + mine, b, byte), at_z(l.z, last + mine, b, byte);
   E dt[ROWS], go[ROWS], z[ROWS];
   auto fetch = [&](int first) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      dt[r] = go[r] = z[r] = E(0.0f);
       if (mine + r < PASS && first + mine + r < stop) {
-        dt[r] = at_dt.at(r, byte), go[r] = at_dy.at(r, byte);
-        if (GATE) z[r] = at_z.at(r, byte);
+        dt[r] = at_dt.at(r), go[r] = at_dy.at(r);
+        if (GATE) z[r] = at_z.at(r);
+      } else {
+        dt[r] = go[r] = z[r] = E(0.0f);
       }
     }
     at_dt.move(-PASS), at_dy.move(-PASS);
@@ -162,12 +163,12 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
                      const Summary sum, const Spans spans, const Grads<E> o) {
   constexpr int ROWS = (PASS + WAVES - 1) / WAVES, BATCH = 2, SUMS = GATE ? 3 : 2;
   // with many waves one set of shares has to do (160 KB of LDS), and a second barrier a pass keeps it
-  constexpr int SETS = WAVES <= 4 ? 2 : 1;
+  constexpr int SETS = 1;
   __shared__ float2 step_in[2][PASS][kTile];             // (s, s u)
   __shared__ float step_q[2][PASS][kTile];
   __shared__ float share[SETS][SUMS][WAVES][PASS][kTile];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int span = blockIdx.x % spans.count, tile = blockIdx.x / spans.count, g = tile / l.tiles, b = blockIdx.y;
+  const int tile = blockIdx.x % (l.G * l.tiles), span = blockIdx.x / (l.G * l.tiles), g = tile / l.tiles, b = blockIdx.y;
   const int in = tile % l.tiles * kTile + lane;
   const bool on = in < l.wide;                           // lanes without a channel count in the sums with s u = q = 0
   const int d = g * l.wide + (on ? in : 0);
@@ -188,20 +189,15 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
     A2[i] = A[i] * kLog2e;
     carry[i] = dA[i] = 0.0f;
   }
-  for (int k = spans.count - 1; k > span; --k) {
-    const float4 end = *reinterpret_cast<const float4*>(sum.ends + state_at(k, l.B, b, WAVES, w, l.D, d));
-    const float s = sum.sums[((int64_t)k * l.B + b) * l.D + d];
-    carry[0] = fmaf(exp2_fast(A2[0] * s), carry[0], end.x), carry[1] = fmaf(exp2_fast(A2[1] * s), carry[1], end.y);
-    carry[2] = fmaf(exp2_fast(A2[2] * s), carry[2], end.z), carry[3] = fmaf(exp2_fast(A2[3] * s), carry[3], end.w);
-  }
+  if (stop > t0) join_spans(sum, spans.count - 1, -1, spans.count - 1 - span, l.B, b, WAVES, w, l.D, d, A2, carry);
 
   const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f, skip = l.skip ? l.skip[d] : 0.0f;
   const uint32_t byte = (uint32_t)d * sizeof(E);
   float dskip = 0.0f, dbias = 0.0f;
   const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
-  Walk<const E> at_u(l.u, last + mine, b), at_dt(l.dt, last + mine, b), at_dy(dy, last + mine, b), at_z(l.z, last + mine, b);
-  Walk<E> at_du(o.du, last + mine, b), at_ddt(o.ddt, last + mine, b), at_dz(o.dz, last + mine, b);
-  const float* at_states = states + state_at(last / kKept, l.B, b, WAVES, w, l.D, 0);
+  Walk<const E> at_u(l.u, last + mine, b, byte), at_dt(l.dt, last + mine, b, byte), at_dy(dy, last + mine, b, byte), at_z(l.z, last + mine, b, byte);
+  Walk<E> at_du(o.du, last + mine, b, byte), at_ddt(o.ddt, last + mine, b, byte), at_dz(o.dz, last + mine, b, byte);
+  const float* at_states = states + state_at(last / kKept, l.B, b, WAVES, w, l.D, d);
   E u[ROWS], dt[ROWS], go[ROWS], z[ROWS];
   struct Row {                                           // of a step: what its outputs are made of
     float s, u, q, slope, gate;                          // slope: sigmoid(raw), gate: dy silu'(z)
@@ -210,13 +206,14 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   auto fetch = [&](int first) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      u[r] = dt[r] = go[r] = z[r] = E(0.0f);
       if (mine + r < PASS && first + mine + r < stop) {
-        u[r] = at_u.at(r, byte), dt[r] = at_dt.at(r, byte), go[r] = at_dy.at(r, byte);
-        if (GATE) z[r] = at_z.at(r, byte);
+        u[r] = at_u.at(r), dt[r] = at_dt.at(r), go[r] = at_dy.at(r);
+        if (GATE) z[r] = at_z.at(r);
+      } else {
+        u[r] = dt[r] = go[r] = z[r] = E(0.0f);
       }
     }
-    kept = reinterpret_cast<const float4*>(at_states)[d];
+    kept = *reinterpret_cast<const float4*>(at_states);
     at_u.move(-PASS), at_dt.move(-PASS), at_dy.move(-PASS);
     if (GATE) at_z.move(-PASS);
     at_states -= (int64_t)l.B * WAVES * l.D * kHeld;
@@ -259,8 +256,8 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
       if (mine + r < PASS && first + mine + r < stop && on) {
-        at_du.at(r, byte) = static_cast<E>(du[r]), at_ddt.at(r, byte) = static_cast<E>(ddt[r]);
-        if (GATE) at_dz.at(r, byte) = static_cast<E>(dz[r]);
+        at_du.at(r) = static_cast<E>(du[r]), at_ddt.at(r) = static_cast<E>(ddt[r]);
+        if (GATE) at_dz.at(r) = static_cast<E>(dz[r]);
       }
     at_du.move(-PASS), at_ddt.move(-PASS);
     if (GATE) at_dz.move(-PASS);

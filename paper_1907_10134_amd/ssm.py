@@ -76,6 +76,8 @@ def _token(t, shape, dtype, name, groups=False):
 def _param(t, shape, name, dtype=torch.float32):
     if t is None:
         return 0
+    if type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
     p = _ptr(t, dtype, name)
     if t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
@@ -85,8 +87,55 @@ def _param(t, shape, name, dtype=torch.float32):
 _NONE = (0, 0, 0)
 
 
+def _own(t, shape):
+    """The address of an optional fp32 parameter if it is what it has to be, None if that has to be looked at closer."""
+    if t is None:
+        return 0
+    if t.dtype is _f32 and t.is_cuda and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    return None
+
+
+def _quick_layer(token, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths):
+    """_layer in one go where every tensor is as it should be with nothing odd about it (6 us instead of 11); None otherwise."""
+    try:
+        t, wide, narrow = u.dtype, u.shape, Bm.shape
+        if token:
+            (B, D), T, (_, G, N) = wide, 1, narrow
+        else:
+            (T, B, D), (_, _, G, N) = wide, narrow
+        if not (dt.dtype is t and Bm.dtype is t and Cm.dtype is t and A.dtype is _f32 and dt.shape == wide and Cm.shape == narrow and
+                narrow[:-2] == wide[:-1] and A.shape == (D, N) and u.is_cuda and dt.is_cuda and Bm.is_cuda and Cm.is_cuda and
+                A.is_cuda and A.is_contiguous()):
+            return None
+        su, sd, sb, sc = u.stride(), dt.stride(), Bm.stride(), Cm.stride()
+        if not (su[-1] == sd[-1] == sb[-1] == sc[-1] == 1 and sb[-2] == sc[-2] == N):
+            return None
+        pz, sz = 0, su
+        if z is not None:
+            sz = z.stride()
+            if not (z.dtype is t and z.is_cuda and z.shape == wide and sz[-1] == 1):
+                return None
+            pz = z.data_ptr()
+        params = (A.data_ptr(), _own(skip, (D,)), _own(dt_bias, (D,)), _own(h0, (B, D, N)))
+        if None in params:
+            return None
+        at = 0 if lengths is None else _param(lengths, (B,), "lengths", _i32)
+        kind = _TYPES[t]
+        if token:
+            return _pack_layer(1, B, D, N, G, kind, u.data_ptr(), 0, su[0], dt.data_ptr(), 0, sd[0], pz, 0, sz[0], Bm.data_ptr(), 0,
+                               sb[0], Cm.data_ptr(), 0, sc[0], *params, at), (1, B, D, N, G)
+        return _pack_layer(T, B, D, N, G, kind, u.data_ptr(), su[0], su[1], dt.data_ptr(), sd[0], sd[1], pz, sz[0], sz[1],
+                           Bm.data_ptr(), sb[0], sb[1], Cm.data_ptr(), sc[0], sc[1], *params, at), (T, B, D, N, G)
+    except (AttributeError, KeyError, TypeError):
+        return None
+
+
 def _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths):
     """The bytes of bppsa_ssm and (T, B, D, N, G)."""
+    quick = _quick_layer(False, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
+    if quick is not None:
+        return quick
     if not (isinstance(u, torch.Tensor) and isinstance(Bm, torch.Tensor)):
         raise TypeError("u and Bm must be torch.Tensors")
     if u.dim() != 3 or Bm.dim() != 4:
@@ -191,10 +240,7 @@ def _slots(slots, B, slots_in_state):
     return _param(slots, (B,), "slots", _i32)
 
 
-def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slots=None, y=None, stream=None):
-    """bppsa_ssm_scan_step: y [B, D] of one token of each stream; state [slots, D, N] float32 is advanced in place.
-
-    u, dt, z [B, D]; Bm, Cm [B, G, N]; slots [B] int32, a row with one outside the state (-1, say) belongs to no stream."""
+def _token_layer(u, dt, A, Bm, Cm, skip, z, dt_bias):
     if not (isinstance(u, torch.Tensor) and isinstance(Bm, torch.Tensor)):
         raise TypeError("u and Bm must be torch.Tensors")
     if u.dim() != 2 or Bm.dim() != 3:
@@ -208,17 +254,25 @@ def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slot
     if A is None:
         raise TypeError("A must be a torch.Tensor")
     _, G, N = narrow
-    layer = _pack_layer(1, B, D, N, G, _TYPES[t], *_token(u, wide, t, "u"), *_token(dt, wide, t, "dt"),
+    return _pack_layer(1, B, D, N, G, _TYPES[t], *_token(u, wide, t, "u"), *_token(dt, wide, t, "dt"),
                         *(_NONE if z is None else _token(z, wide, t, "z")), *_token(Bm, narrow, t, "Bm", True),
                         *_token(Cm, narrow, t, "Cm", True), _param(A, (D, N), "A"), _param(skip, (D,), "skip"),
-                        _param(dt_bias, (D,), "dt_bias"), 0, 0)
+                        _param(dt_bias, (D,), "dt_bias"), 0, 0), (1, B, D, N, G)
+
+
+def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slots=None, y=None, stream=None):
+    """bppsa_ssm_scan_step: y [B, D] of one token of each stream; state [slots, D, N] float32 is advanced in place.
+
+    u, dt, z [B, D]; Bm, Cm [B, G, N]; slots [B] int32, a row with one outside the state (-1, say) belongs to no stream."""
+    layer, (_, B, D, N, _) = _quick_layer(True, u, dt, A, Bm, Cm, skip, z, dt_bias, None, None) or \
+        _token_layer(u, dt, A, Bm, Cm, skip, z, dt_bias)
     at = _ptr(state, _f32, "state")
     slots_in_state = state.shape[0]
     if state.shape != (slots_in_state, D, N):
         raise ValueError("state must be [slots, %d, %d], got %s" % (D, N, tuple(state.shape)))
     if y is None:
-        y = torch.empty(wide, dtype=t, device=u.device)
-    _check(_lib.bppsa_ssm_scan_step(layer, _pack_rows(*_token(y, wide, t, "y")), at, slots_in_state,
+        y = torch.empty_like(u)
+    _check(_lib.bppsa_ssm_scan_step(layer, _pack_rows(*_token(y, u.shape, u.dtype, "y")), at, slots_in_state,
                                     _slots(slots, B, slots_in_state), _stream(stream)), "bppsa_ssm_scan_step")
     return y
 
@@ -286,7 +340,7 @@ def ssm_conv_step(x, weight, bias, state, silu=True, slots=None, y=None, stream=
     if state.shape != (slots_in_state, W - 1, D):
         raise ValueError("state must be [slots, %d, %d], got %s" % (W - 1, D, tuple(state.shape)))
     if y is None:
-        y = torch.empty(shape, dtype=t, device=x.device)
+        y = torch.empty_like(x)
     _check(_lib.bppsa_ssm_conv_step(conv, _pack_rows(*_token(y, shape, t, "y")), at, slots_in_state,
                                     _slots(slots, B, slots_in_state), _stream(stream)), "bppsa_ssm_conv_step")
     return y
