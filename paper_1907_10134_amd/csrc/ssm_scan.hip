@@ -243,7 +243,7 @@ scan_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int slo
 
 extern "C" size_t bppsa_ssm_scan_states_bytes(int T, int B, int D, int N) {
   if (!sizes_ok(T, B, D, N, 1)) return 0;
-  return (size_t)bppsa_ceil_div(T, kKept) * B * D * waves_of(N) * kHeld * sizeof(float);
+  return (kept_coef_floats(T, B, N) + (size_t)bppsa_ceil_div(T, kKept) * B * D * waves_of(N) * kHeld) * sizeof(float);
 }
 
 extern "C" size_t bppsa_ssm_scan_workspace_bytes(int T, int B, int D, int N, int G) {
@@ -261,16 +261,19 @@ extern "C" bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows*
     using E = decltype(e);
     const Layer<E> l = layer_of<E>(*layer);
     auto part = [&](size_t o) { return reinterpret_cast<float*>(static_cast<char*>(workspace) + o); };
-    launch_coef(l, part(at.coef), s);
+    float* kept = static_cast<float*>(states);
+    float* coef = kept && l.G <= kGroupsKept ? kept : part(at.coef);
+    if (kept) kept += kept_coef_floats(l.T, l.B, l.N);
+    launch_coef(l, coef, s);
     const Summary sum{part(at.ends), part(at.sums)};
     return by_waves(waves_of(l.N), [&](auto waves) {
       constexpr int W = waves.value;
       if (at.spans.count > 1)                  // nothing asks for the last span's summary
         scan_kernel<E, W, true, false><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
-            l, Rows<E>{}, nullptr, nullptr, part(at.coef), sum, at.spans);
+            l, Rows<E>{}, nullptr, nullptr, coef, sum, at.spans);
       const auto kernel = l.z.data ? scan_kernel<E, W, false, true> : scan_kernel<E, W, false, false>;
-      kernel<<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(l, rows_of<E>(*y), h_last, static_cast<float*>(states),
-                                                                        part(at.coef), sum, at.spans);
+      kernel<<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(l, rows_of<E>(*y), h_last, kept, coef, sum,
+                                                                        at.spans);
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     });

@@ -162,11 +162,9 @@ __global__ void __launch_bounds__(WAVES * 64)
 scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ states, const float* __restrict__ coef,
                      const Summary sum, const Spans spans, const Grads<E> o) {
   constexpr int ROWS = (PASS + WAVES - 1) / WAVES, BATCH = 2, SUMS = GATE ? 3 : 2;
-  // with many waves one set of shares has to do (160 KB of LDS), and a second barrier a pass keeps it
-  constexpr int SETS = 1;
   __shared__ float2 step_in[2][PASS][kTile];             // (s, s u)
   __shared__ float step_q[2][PASS][kTile];
-  __shared__ float share[SETS][SUMS][WAVES][PASS][kTile];
+  __shared__ float share[SUMS][WAVES][PASS][kTile];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = blockIdx.x % (l.G * l.tiles), span = blockIdx.x / (l.G * l.tiles), g = tile / l.tiles, b = blockIdx.y;
   const int in = tile % l.tiles * kTile + lane;
@@ -236,7 +234,7 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       step_q[buffer][mine + r][lane] = v.q;
     }
   };
-  auto finish = [&](int first, int set) {
+  auto finish = [&](int first) {
     float du[ROWS], ddt[ROWS], dz[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
@@ -245,8 +243,8 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       float s1 = 0.0f, s2 = 0.0f, plain = skip * v.u;
 #pragma unroll
       for (int k = 0; k < WAVES; ++k) {
-        s1 += share[set][0][k][i][lane], s2 += share[set][1][k][i][lane];
-        if (GATE) plain += share[set][SUMS - 1][k][i][lane];
+        s1 += share[0][k][i][lane], s2 += share[1][k][i][lane];
+        if (GATE) plain += share[SUMS - 1][k][i][lane];
       }
       du[r] = fmaf(v.s, s1, skip * v.q);
       ddt[r] = fmaf(v.u, s1, s2) * v.slope;
@@ -274,14 +272,14 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   }
   __syncthreads();
   for (int p = passes - 1; p >= 0; --p) {
-    const int first = t0 + p * PASS, buffer = p & 1, set = p % SETS;
+    const int first = t0 + p * PASS, buffer = p & 1;
     float2 in_[PASS];
     float q[PASS];
 #pragma unroll
     for (int i = 0; i < PASS; ++i) in_[i] = step_in[buffer][i][lane], q[i] = step_q[buffer][i][lane];
     float a[PASS][kHeld], h[PASS + 1][kHeld];
     h[0][0] = kept.x, h[0][1] = kept.y, h[0][2] = kept.z, h[0][3] = kept.w;
-    if (p + 1 < passes) finish(first + PASS, (p + 1) % SETS);
+    if (p + 1 < passes) finish(first + PASS);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) was[r] = row[r];
     if (p) fetch(first - PASS);
@@ -311,8 +309,8 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
           pair[k] = swap32_add(gh * in_[i].y, h[i + 1][k] * q[i]);
         }
         step_sum[i] = half_row_add(swap16_add(pair[0], pair[1]), swap16_add(pair[2], pair[3]));
-        share[set][0][w][i][lane] = s1, share[set][1][w][i][lane] = s2;
-        if (GATE) share[set][SUMS - 1][w][i][lane] = plain;
+        share[0][w][i][lane] = s1, share[1][w][i][lane] = s2;
+        if (GATE) share[SUMS - 1][w][i][lane] = plain;
       }
     };
     // Bm and Cm are asked for in the order 0 2 4 6 4 2 0 of steps: the last two are there when the walk turns
@@ -325,7 +323,9 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       __builtin_amdgcn_sched_barrier(0);
       if (j + BATCH < PASS) now = next;
     }
-    if (SETS == 1) __syncthreads();                      // the last pass's shares have been read
+    // the last pass's shares have been read: a second barrier a pass instead of a second set of them, whose LDS would let
+    // eight waves on a compute unit instead of twelve (1105 us against 925 at T = 4096, B = 4, D = 4096)
+    __syncthreads();
 #pragma unroll
     for (int j = PASS - BATCH; j >= 0; j -= BATCH) {
       if (j < PASS - BATCH) {
@@ -347,11 +347,11 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
     if (p) prepare(first - PASS, buffer ^ 1);
     __syncthreads();
   }
-  if (passes) finish(t0, 0);
+  if (passes) finish(t0);
 
   // dskip and ddt_bias: every wave has the steps of its rows
   __syncthreads();
-  float* totals = &share[0][0][0][0][0];
+  float* totals = &share[0][0][0][0];
   static_assert(sizeof(share) >= 2 * WAVES * kTile * sizeof(float));
   totals[w * kTile + lane] = dskip, totals[(WAVES + w) * kTile + lane] = dbias;
   __syncthreads();
@@ -368,36 +368,40 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       if (w * kHeld + i < l.N) o.dh0[((int64_t)b * l.D + d) * l.N + w * kHeld + i] = carry[i];
 }
 
-// dB and dC: the tiles' parts in the tiles' order.  A thread has the place of a lane of the main kernel.
+// The sums over parts.  The first workgroups have dB and dC, the tiles' parts in the tiles' order, a thread the place of a lane
+// of the main kernel; the others dA, dskip and ddt_bias, the parts of the samples and spans, in order: four waves a
+// quarter each, then the quarters.
+struct Joined {
+  void *dBm, *dCm;
+  float *dA, *dskip, *ddt_bias;
+  int64_t places;                              // of dB and dC: the parts of one tile
+  int first_groups, waves, parts;              // workgroups for dB and dC; waves of the main kernel; samples times spans
+};
 template <typename E>
 __global__ void __launch_bounds__(256)
-join_bc_kernel(const Layer<E> l, const float* __restrict__ bc, int waves, int64_t all, E* __restrict__ dBm, E* __restrict__ dCm) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= all) return;
-  const int padded = (l.T + kPad - 1) / kPad * kPad, product = product_of_lane((int)(i & 63));
-  const int w = (int)(i / 64 % waves), t = (int)(i / 64 / waves % (padded / PASS)) * PASS + product / 8;
-  const int64_t bg = i / 64 / waves / (padded / PASS);
-  const int g = (int)(bg % l.G), b = (int)(bg / l.G), n = w * kHeld + product / 2 % kHeld;
-  if (t >= l.T || n >= l.N) return;
-  float sum = 0.0f;
-  if (t < clamp_length(l.lengths, b, l.T)) {
+join_kernel(const Layer<E> l, const Grads<E> o, const Joined to) {
+  if ((int)blockIdx.x < to.first_groups) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= to.places) return;
+    const int passes = (l.T + PASS - 1) / PASS, product = product_of_lane((int)(i & 63));
+    const int w = (int)(i / 64 % to.waves), t = (int)(i / 64 / to.waves % passes) * PASS + product / 8;
+    const int64_t bg = i / 64 / to.waves / passes;
+    const int g = (int)(bg % l.G), b = (int)(bg / l.G), n = w * kHeld + product / 2 % kHeld;
+    if (t >= l.T || n >= l.N) return;
+    float sum = 0.0f;
+    if (t < clamp_length(l.lengths, b, l.T)) {
 #pragma unroll 8
-    for (int k = 0; k < l.tiles; ++k) sum += bc[k * all + i];
+      for (int k = 0; k < l.tiles; ++k) sum += o.bc[k * to.places + i];
+    }
+    store(static_cast<E*>(product & 1 ? to.dCm : to.dBm) + (((int64_t)t * l.B + b) * l.G + g) * l.N + n, sum);
+    return;
   }
-  store((product & 1 ? dCm : dBm) + (((int64_t)t * l.B + b) * l.G + g) * l.N + n, sum);
-}
-
-// dA, dskip and ddt_bias: the parts of the samples and spans, in order: four waves a quarter each, then the quarters.
-__global__ void __launch_bounds__(256)
-join_params_kernel(int parts, int waves, int D, int N, const float* __restrict__ dA, const float* __restrict__ dskip,
-                   const float* __restrict__ ddt_bias, float* __restrict__ out_dA, float* __restrict__ out_dskip,
-                   float* __restrict__ out_ddt_bias) {
   __shared__ float quarter[4][64];
-  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, of_dA = waves * kHeld * D;
-  const int i = blockIdx.x * 64 + lane, all = of_dA + 2 * D;
-  const float* from = i < of_dA ? dA + i : i < of_dA + D ? dskip + (i - of_dA) : ddt_bias + (i - of_dA - D);
-  const int64_t step = i < of_dA ? of_dA : D;
-  const int each = (parts + 3) / 4, last = (q + 1) * each < parts ? (q + 1) * each : parts;
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, of_dA = to.waves * kHeld * l.D;
+  const int i = ((int)blockIdx.x - to.first_groups) * 64 + lane, all = of_dA + 2 * l.D;
+  const float* from = i < of_dA ? o.dA + i : i < of_dA + l.D ? o.dskip + (i - of_dA) : o.ddt_bias + (i - of_dA - l.D);
+  const int64_t step = i < of_dA ? of_dA : l.D;
+  const int each = (to.parts + 3) / 4, last = (q + 1) * each < to.parts ? (q + 1) * each : to.parts;
   float sum = 0.0f;
   if (i < all)
 #pragma unroll 8
@@ -407,12 +411,12 @@ join_params_kernel(int parts, int waves, int D, int N, const float* __restrict__
   if (q || i >= all) return;
   sum = (quarter[0][lane] + quarter[1][lane]) + (quarter[2][lane] + quarter[3][lane]);
   if (i < of_dA) {
-    const int w = i / (kHeld * D), d = i / kHeld % D, n = w * kHeld + i % kHeld;
-    if (n < N) out_dA[(int64_t)d * N + n] = sum;
-  } else if (i < of_dA + D) {
-    if (out_dskip) out_dskip[i - of_dA] = sum;
-  } else if (out_ddt_bias) {
-    out_ddt_bias[i - of_dA - D] = sum;
+    const int w = i / (kHeld * l.D), d = i / kHeld % l.D, n = w * kHeld + i % kHeld;
+    if (n < l.N) to.dA[(int64_t)d * l.N + n] = sum;
+  } else if (i < of_dA + l.D) {
+    if (to.dskip) to.dskip[i - of_dA] = sum;
+  } else if (to.ddt_bias) {
+    to.ddt_bias[i - of_dA - l.D] = sum;
   }
 }
 
@@ -421,11 +425,11 @@ struct Scratch {
   Spans spans;
   size_t coef, ends, sums, bc, dA, dskip, ddt_bias, bytes;
   int64_t bc_floats;                           // of one tile
-  Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G, 2)) {
+  Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G, 8)) {
     const int64_t waves = waves_of(N), tiles = bppsa_ceil_div(D / G, kTile), parts = (int64_t)spans.count * B * D;
     bc_floats = (int64_t)B * G * ((T + kPad - 1) / kPad * kPad / PASS) * waves * 64;
     Arena take;
-    coef = take(coef_floats(T, B, N, G));
+    coef = take(G > kGroupsKept ? coef_floats(T, B, N, G) : 0);
     ends = take(spans.count > 1 ? parts * waves * kHeld : 0), sums = take(spans.count > 1 ? parts : 0);
     bc = take(tiles * bc_floats);
     dA = take(parts * waves * kHeld), dskip = take(parts), ddt_bias = take(parts);
@@ -458,23 +462,26 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
                      part(at.dskip), part(at.ddt_bias), grads->dh0};
     const Summary sum{part(at.ends), part(at.sums)};
     const Rows<const E> out = rows_of<const E>(*dy);
-    launch_coef(l, part(at.coef), s);
+    const float* kept = static_cast<const float*>(states);
+    const float* coef = kept;
+    kept += kept_coef_floats(l.T, l.B, l.N);
+    if (l.G > kGroupsKept) launch_coef(l, part(at.coef), s), coef = part(at.coef);
     auto walk = [&](auto waves_, auto gate) {
       constexpr int W = waves_.value;
       constexpr bool GATE = gate.value;
       if (at.spans.count > 1)
         scan_backward_summary_kernel<E, W, GATE><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
-            l, out, part(at.coef), sum, at.spans);
+            l, out, coef, sum, at.spans);
       scan_backward_kernel<E, W, GATE><<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(
-          l, out, static_cast<const float*>(states), part(at.coef), sum, at.spans, o);
+          l, out, kept, coef, sum, at.spans, o);
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     };
     BPPSA_TRY(by_waves(waves, [&](auto w) { return l.z.data ? walk(w, std::true_type{}) : walk(w, std::false_type{}); }));
-    join_bc_kernel<E><<<(unsigned)((at.bc_floats + 255) / 256), 256, 0, s>>>(l, o.bc, waves, at.bc_floats,
-                                                                           static_cast<E*>(grads->dBm), static_cast<E*>(grads->dCm));
-    join_params_kernel<<<(unsigned)((((int64_t)waves * kHeld + 2) * l.D + 63) / 64), 256, 0, s>>>(
-        at.spans.count * l.B, waves, l.D, l.N, o.dA, o.dskip, o.ddt_bias, grads->dA, grads->dskip, grads->ddt_bias);
+    const int64_t first = (at.bc_floats + 255) / 256;
+    const Joined to{grads->dBm, grads->dCm, grads->dA, grads->dskip, grads->ddt_bias, at.bc_floats, (int)first, waves,
+                    at.spans.count * l.B};
+    join_kernel<E><<<(unsigned)(first + ((waves * kHeld + 2) * (int64_t)l.D + 63) / 64), 256, 0, s>>>(l, o, to);
     BPPSA_CHECK_LAUNCH();
     return BPPSA_OK;
   });

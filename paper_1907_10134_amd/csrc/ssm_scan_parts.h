@@ -15,7 +15,7 @@ namespace ssm {
 constexpr int kTile = 64;        // channels of a workgroup, one a lane
 constexpr int kHeld = 4;         // states of a channel that a wave holds
 constexpr int kKept = 8;         // steps between two states kept for the backward pass
-constexpr int kPad = 32;         // `coef` reaches to the next multiple of so many steps: a span's last steps are not tested for
+constexpr int kPad = kKept;      // `coef` reaches to the next multiple of so many steps: a span's last steps are not tested for
 
 template <typename E>
 struct Layer {
@@ -61,6 +61,13 @@ __host__ __device__ __forceinline__ int64_t state_at(int64_t first, int B, int b
 // coef [b][g][w][t][8]: four Bm, then four Cm, zero beyond the states there are and behind a sample's end.
 static inline int64_t coef_floats(int64_t T, int64_t B, int64_t N, int64_t G) {
   return B * G * ((T + kPad - 1) / kPad * kPad) * waves_of((int)N) * 2 * kHeld;
+}
+
+// A forward call that keeps states for the backward pass keeps coef in front of them, up to this many groups (the size of
+// the states is asked for without G): one launch less there.
+constexpr int kGroupsKept = 4;
+static inline size_t kept_coef_floats(int64_t T, int64_t B, int64_t N) {
+  return bppsa_align_up((size_t)coef_floats(T, B, N, kGroupsKept), 64);
 }
 
 template <typename E>
@@ -141,11 +148,11 @@ __device__ __forceinline__ void join_spans(const Summary& sum, int first, int st
   }
 }
 
-// As many spans as give every SIMD `waves` waves, none shorter than 64 steps (a multiple of kPad), 64 at most.
+// As many spans as give every SIMD `waves` waves, none shorter than 32 steps (a multiple of kPad), 64 at most.
 static inline Spans spans_of(int T, int B, int D, int N, int G, int waves) {
   const int64_t have = (int64_t)G * bppsa_ceil_div(D / G, kTile) * B * waves_of(N);
   int64_t count = (int64_t)bppsa_compute_units() * 4 * waves / have;
-  if (count > T / 64) count = T / 64;
+  if (count > T / 32) count = T / 32;
   if (count > 64) count = 64;
   if (count < 2) return Spans{1, T};
   const int steps = bppsa_ceil_div(bppsa_ceil_div(T, (int)count), kPad) * kPad;

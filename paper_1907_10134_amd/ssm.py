@@ -15,7 +15,7 @@ import torch
 from .binding import _check, _lib, _ptr, _stream, _workspace
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-_i32, _f32 = torch.int32, torch.float32
+_i32, _f32, _plain = torch.int32, torch.float32, torch.contiguous_format
 
 _c_int, _c_void_p, _c_size_t = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
 for _name, _res, _args in (
@@ -127,7 +127,7 @@ def _quick_layer(token, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths):
                                sb[0], Cm.data_ptr(), 0, sc[0], *params, at), (1, B, D, N, G)
         return _pack_layer(T, B, D, N, G, kind, u.data_ptr(), su[0], su[1], dt.data_ptr(), sd[0], sd[1], pz, sz[0], sz[1],
                            Bm.data_ptr(), sb[0], sb[1], Cm.data_ptr(), sc[0], sc[1], *params, at), (T, B, D, N, G)
-    except (AttributeError, KeyError, TypeError):
+    except (AttributeError, KeyError, TypeError, ValueError):
         return None
 
 
@@ -214,18 +214,15 @@ def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=N
     T, B, D, N, G = dims
     if states is None:
         raise TypeError("states must be the array that ssm_scan filled")
-    t, dev = u.dtype, u.device
-    f32 = dict(dtype=torch.float32, device=dev)
-    du, ddt = torch.empty_like(u), torch.empty_like(dt)
-    dz = None if z is None else torch.empty_like(u)
-    dBm, dCm = torch.empty((T, B, G, N), dtype=t, device=dev), torch.empty((T, B, G, N), dtype=t, device=dev)
-    dA = torch.empty((D, N), **f32)
-    dskip = None if skip is None else torch.empty((D,), **f32)
-    dbias = None if dt_bias is None else torch.empty((D,), **f32)
-    out = _pack_grads(*_rows(du, u.shape, t, "du"), *_rows(ddt, u.shape, t, "ddt"),
-                      *(_NONE if dz is None else _rows(dz, u.shape, t, "dz")), dBm.data_ptr(), dCm.data_ptr(), dA.data_ptr(),
-                      0 if dskip is None else dskip.data_ptr(), 0 if dbias is None else dbias.data_ptr(),
-                      _param(dh0, (B, D, N), "dh0"))
+    t, dev, like = u.dtype, u.device, torch.empty_like
+    du, ddt = like(u), like(dt)
+    dz = None if z is None else like(u)
+    dBm, dCm = like(Bm, memory_format=_plain), like(Cm, memory_format=_plain)
+    dA, dskip, dbias = like(A), None if skip is None else like(skip), None if dt_bias is None else like(dt_bias)
+    su, sd = du.stride(), ddt.stride()
+    out = _pack_grads(du.data_ptr(), su[0], su[1], ddt.data_ptr(), sd[0], sd[1], 0 if dz is None else dz.data_ptr(), su[0], su[1],
+                      dBm.data_ptr(), dCm.data_ptr(), dA.data_ptr(), 0 if dskip is None else dskip.data_ptr(),
+                      0 if dbias is None else dbias.data_ptr(), _param(dh0, (B, D, N), "dh0"))
     _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_backward_workspace_bytes(T, B, D, N, G), dev, stream)
     _check(_lib.bppsa_ssm_scan_backward(layer, _pack_rows(*_rows(dy, u.shape, t, "dy")), _states(states, dims), out, ws, nbytes,
                                         _stream(stream)), "bppsa_ssm_scan_backward")
