@@ -28,6 +28,18 @@ __device__ __forceinline__ float load(const E* p) { return static_cast<float>(*p
 template <typename E>
 __device__ __forceinline__ void store(E* p, float v) { *p = static_cast<E>(v); }
 
+// An element as it was loaded, in a register of its own, and its value.
+template <typename E>
+__device__ __forceinline__ uint32_t bits_at(uint64_t address) {
+  typedef std::conditional_t<sizeof(E) == 4, uint32_t, uint16_t> U;
+  return *(const __attribute__((address_space(1))) U*)address;
+}
+template <typename E>
+__device__ __forceinline__ float value(uint32_t bits) {
+  if constexpr (sizeof(E) == 4) return __uint_as_float(bits);
+  else return static_cast<float>(__builtin_bit_cast(E, (uint16_t)bits));
+}
+
 // The rows of an array that a wave walks through: a lane's address in vector registers, moved on by a stride in scalar ones.
 // (Both in scalar registers, with the lane's offset added by the access, left too few of them for Bm and Cm.)
 template <typename E>
@@ -36,8 +48,9 @@ struct Walk {
   int64_t step;
   __device__ __forceinline__ Walk(const Rows<E>& r, int t, int b, uint32_t byte)
       : lane((uint64_t)r.at(t, b) + byte), step(r.st * (int64_t)sizeof(E)) {}
-  __device__ __forceinline__ __attribute__((address_space(1))) E& at(int rows_on) const {
-    return *(__attribute__((address_space(1))) E*)(lane + rows_on * step);
+  __device__ __forceinline__ uint32_t bits(int rows_on) const { return bits_at<E>(lane + rows_on * step); }
+  __device__ __forceinline__ void put(int rows_on, float v) const {
+    *(__attribute__((address_space(1))) E*)(lane + rows_on * step) = static_cast<E>(v);
   }
   __device__ __forceinline__ void move(int rows) { lane += rows * step; }
 };

@@ -11,12 +11,13 @@ using namespace ssm;
 // last one finished beside a pass, so there is one barrier a pass.
 // Bound by issue: a step of four states takes 4 exp (two slots each), 16 products and multiply-adds, two LDS accesses.
 template <typename E, int WAVES, bool SUMMARY, bool GATE>
-__global__ void __launch_bounds__(WAVES * 64)
-scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, const float* __restrict__ coef,
-            const Summary sum, const Spans spans) {
+__global__ void __launch_bounds__(WAVES * 64, WAVES <= 12 ? 6 : 4)      // at least so many waves a SIMD
+scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, const Summary sum,
+            const Spans spans) {
   constexpr int PASS = kKept, ROWS = (PASS + WAVES - 1) / WAVES;   // a wave prepares and finishes ROWS steps
-  constexpr int BATCH = SUMMARY ? 4 : 2;
+  constexpr bool ALL = PASS % WAVES == 0;                          // none has fewer
   __shared__ float2 step_in[2][PASS][kTile];
+  __shared__ alignas(16) float coef[2][PASS][WAVES][2 * kHeld];
   __shared__ float share[SUMMARY ? 1 : 2][SUMMARY ? 1 : WAVES][SUMMARY ? 1 : PASS][kTile];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // neighbours in the grid, which go to different dies, are tiles of a span: spans may lie behind a sample's end
@@ -46,93 +47,97 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   Walk<const E> at_u(l.u, t0 + mine, b, byte), at_dt(l.dt, t0 + mine, b, byte), at_z(l.z, t0 + mine, b, byte);
   Walk<E> at_y(y, t0 + mine, b, byte);
   float* at_states = SUMMARY || !states ? nullptr : states + state_at(t0 / kKept, l.B, b, WAVES, w, l.D, d);
-  E u[ROWS], dt[ROWS], z[ROWS], u_was[ROWS], z_was[ROWS];
+  Coef<E> at_coef(l, WAVES, threadIdx.x, t0, b, g);
+  // What a wave fetches for a pass, two passes ahead: one is not enough for a device that is not full.  The values stay as
+  // they are loaded until they are needed: a conversion here would wait for each load by itself.
+  struct Fetched {
+    uint32_t u[ROWS], dt[ROWS], z[ROWS], coef;
+  } raw0, raw1;
+  uint32_t u_was[ROWS], z_was[ROWS];
   float total = 0.0f;
-  // The values stay as they are loaded until they are needed: a conversion here would wait for each load by itself.
-  auto fetch = [&](int first) {
+  auto fetch = [&](int first, Fetched& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (mine + r < PASS && first + mine + r < stop) {
-        u[r] = at_u.at(r), dt[r] = at_dt.at(r);
-        if (GATE) z[r] = at_z.at(r);
-      } else {
-        u[r] = dt[r] = z[r] = E(0.0f);
+      uint32_t a = 0, b = 0, c = 0;
+      if ((ALL || mine + r < PASS) && first + mine + r < stop) {
+        a = at_u.bits(r), b = at_dt.bits(r);
+        if (GATE) c = at_z.bits(r);
       }
+      x.u[r] = a, x.dt[r] = b, x.z[r] = c;
     }
-    at_u.move(PASS), at_dt.move(PASS);
+    x.coef = at_coef.fetch(stop - first);
+    at_u.move(PASS), at_dt.move(PASS), at_coef.move(1);
     if (GATE) at_z.move(PASS);
   };
-  auto prepare = [&](int first, int buffer) {
+  auto prepare = [&](int first, int buffer, const Fetched& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (mine + r >= PASS) break;
-      float s = softplus<E>((float)dt[r] + bias);
+      if (!ALL && mine + r >= PASS) break;
+      float s = softplus<E>(value<E>(x.dt[r]) + bias);
       s = first + mine + r < stop ? s : 0.0f;            // u is zero there
       if (SUMMARY) total += s;
-      step_in[buffer][mine + r][lane] = make_float2(s, s * (float)u[r]);
+      step_in[buffer][mine + r][lane] = make_float2(s, s * value<E>(x.u[r]));
     }
+    (&coef[buffer][0][0][0])[threadIdx.x] = value<E>(x.coef);
   };
-  auto finish = [&](int first, int buffer) {
+  auto finish = [&](int first, int buffer) __attribute__((always_inline)) {
     float v[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int row = mine + r < PASS ? mine + r : 0;
-      v[r] = skip * (float)u_was[r];
+      const int row = (ALL || mine + r < PASS) ? mine + r : 0;
+      v[r] = skip * value<E>(u_was[r]);
 #pragma unroll
       for (int k = 0; k < WAVES; ++k) v[r] += share[buffer][k][row][lane];
-      if (GATE) v[r] *= (float)z_was[r] * sigmoid<E>((float)z_was[r]);
+      if (GATE) v[r] *= value<E>(z_was[r]) * sigmoid<E>(value<E>(z_was[r]));
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
-      if (mine + r < PASS && first + mine + r < stop && on) at_y.at(r) = static_cast<E>(v[r]);
+      if ((ALL || mine + r < PASS) && first + mine + r < stop && on) at_y.put(r, v[r]);
     at_y.move(PASS);
   };
 
-  const int padded = (l.T + kPad - 1) / kPad * kPad;
   const int passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0;
-  const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + t0) * 2 * kHeld;
-  Coef<BATCH> now, next;
-  if (passes) {
-    fetch(t0);
-    prepare(t0, 0);
-    now.ask(from);
-  }
-  __syncthreads();
-  for (int p = 0; p < passes; ++p) {
-    const int first = t0 + p * PASS, buffer = p & 1;
-    float2 in_[PASS];
-#pragma unroll
-    for (int i = 0; i < PASS; ++i) in_[i] = step_in[buffer][i][lane];
+  auto pass = [&](int p, auto parity) __attribute__((always_inline)) {
+    constexpr int buffer = parity.value;
+    Fetched &here = pick<buffer>(raw0, raw1), &there = pick<buffer>(raw1, raw0);
+    const int first = t0 + p * PASS;
     if (!SUMMARY && p) finish(first - PASS, buffer ^ 1);
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) u_was[r] = u[r], z_was[r] = z[r];
-    if (p + 1 < passes) fetch(first + PASS);
+    for (int r = 0; r < ROWS; ++r) u_was[r] = here.u[r], z_was[r] = here.z[r];
+    fetch(first + 2 * PASS, here);               // nothing, behind the last pass
     if (!SUMMARY && states) {
       if (on) *reinterpret_cast<float4*>(at_states) = make_float4(h[0], h[1], h[2], h[3]);
       at_states += (int64_t)l.B * WAVES * l.D * kHeld;
     }
 #pragma unroll
-    for (int j = 0; j < PASS; j += BATCH) {
-      wait_for_scalars();
-      next.ask(from + (j + BATCH < PASS || p + 1 < passes ? j + BATCH : 0) * 2 * kHeld);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < PASS; ++i) {
+      float Bm[kHeld], Cm[kHeld], v = 0.0f;
+      two_by_two(i);
+      const float2 in_ = step_in[buffer][i][lane];
+      four(coef[buffer][i][w], Bm);
+      if (!SUMMARY) four(coef[buffer][i][w] + kHeld, Cm);
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        float v = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-          h[k] = fmaf(exp2_fast(in_[j + i].x * A2[k]), h[k], in_[j + i].y * now.B(i, k));
-          if (!SUMMARY) v = k ? fmaf(now.C(i, k), h[k], v) : now.C(i, k) * h[k];
-        }
-        if (!SUMMARY) share[buffer][w][j + i][lane] = v;
+      for (int k = 0; k < kHeld; ++k) {
+        h[k] = fmaf(exp2_fast(in_.x * A2[k]), h[k], in_.y * Bm[k]);
+        if (!SUMMARY) v = k ? fmaf(Cm[k], h[k], v) : Cm[k] * h[k];
       }
-      __builtin_amdgcn_sched_barrier(0);
-      now = next;
+      if (!SUMMARY) share[buffer][w][i][lane] = v;
     }
-    from += PASS * 2 * kHeld;
-    if (p + 1 < passes) prepare(first + PASS, buffer ^ 1);
+    now(h);
+    prepare(first + PASS, buffer ^ 1, there);    // a pass that no one walks, behind the last one
     __syncthreads();
+  };
+  if (passes) {
+    fetch(t0, raw0);
+    fetch(t0 + PASS, raw1);
+    prepare(t0, 0, raw0);
   }
+  __syncthreads();
+  constexpr std::integral_constant<int, 0> even;
+  constexpr std::integral_constant<int, 1> odd;
+  int p = 0;
+  for (; p + 1 < passes; p += 2) pass(p, even), pass(p + 1, odd);
+  if (p < passes) pass(p, even);
   if (!SUMMARY && passes) finish(t0 + (passes - 1) * PASS, (passes - 1) & 1);
 
   if constexpr (SUMMARY) {
@@ -156,13 +161,12 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   }
 }
 
-// The workspace of a forward call: Bm and Cm as floats, and the spans' summaries.
+// The workspace of a forward call: the spans' summaries.
 struct Scratch {
-  size_t coef, ends, sums, bytes;
+  size_t ends, sums, bytes;
   Spans spans;
   Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G, 6)) {
     Arena take;
-    coef = take(coef_floats(T, B, N, G));
     const int64_t parts = spans.count > 1 ? (int64_t)spans.count * B * D : 0;
     ends = take(parts * waves_of(N) * kHeld), sums = take(parts);
     bytes = take.at;
@@ -243,7 +247,7 @@ scan_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int slo
 
 extern "C" size_t bppsa_ssm_scan_states_bytes(int T, int B, int D, int N) {
   if (!sizes_ok(T, B, D, N, 1)) return 0;
-  return (kept_coef_floats(T, B, N) + (size_t)bppsa_ceil_div(T, kKept) * B * D * waves_of(N) * kHeld) * sizeof(float);
+  return (size_t)bppsa_ceil_div(T, kKept) * B * D * waves_of(N) * kHeld * sizeof(float);
 }
 
 extern "C" size_t bppsa_ssm_scan_workspace_bytes(int T, int B, int D, int N, int G) {
@@ -261,19 +265,15 @@ extern "C" bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows*
     using E = decltype(e);
     const Layer<E> l = layer_of<E>(*layer);
     auto part = [&](size_t o) { return reinterpret_cast<float*>(static_cast<char*>(workspace) + o); };
-    float* kept = static_cast<float*>(states);
-    float* coef = kept && l.G <= kGroupsKept ? kept : part(at.coef);
-    if (kept) kept += kept_coef_floats(l.T, l.B, l.N);
-    launch_coef(l, coef, s);
     const Summary sum{part(at.ends), part(at.sums)};
     return by_waves(waves_of(l.N), [&](auto waves) {
       constexpr int W = waves.value;
       if (at.spans.count > 1)                  // nothing asks for the last span's summary
         scan_kernel<E, W, true, false><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
-            l, Rows<E>{}, nullptr, nullptr, coef, sum, at.spans);
+            l, Rows<E>{}, nullptr, nullptr, sum, at.spans);
       const auto kernel = l.z.data ? scan_kernel<E, W, false, true> : scan_kernel<E, W, false, false>;
-      kernel<<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(l, rows_of<E>(*y), h_last, kept, coef, sum,
-                                                                        at.spans);
+      kernel<<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(l, rows_of<E>(*y), h_last,
+                                                                        static_cast<float*>(states), sum, at.spans);
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     });

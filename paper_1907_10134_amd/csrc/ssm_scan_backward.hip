@@ -63,11 +63,12 @@ __host__ __device__ __forceinline__ int product_of_lane(int lane) {
 // Where a span's walk from its end with nothing carried in arrives, and the sum of its steps; the cut and the passes are
 // those of the main kernel below.
 template <typename E, int WAVES, bool GATE>
-__global__ void __launch_bounds__(WAVES * 64)
-scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ coef, const Summary sum,
-                             const Spans spans) {
-  constexpr int ROWS = (PASS + WAVES - 1) / WAVES, BATCH = 4;
+__global__ void __launch_bounds__(WAVES * 64, WAVES <= 12 ? 6 : 4)
+scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary sum, const Spans spans) {
+  constexpr int ROWS = (PASS + WAVES - 1) / WAVES;
+  constexpr bool ALL = PASS % WAVES == 0;
   __shared__ float2 step_in[2][PASS][kTile];             // (s, q)
+  __shared__ alignas(16) float coef[2][PASS][WAVES][2 * kHeld];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = blockIdx.x % (l.G * l.tiles), span = blockIdx.x / (l.G * l.tiles) + 1, g = tile / l.tiles, b = blockIdx.y;
   const int in = tile % l.tiles * kTile + lane;
@@ -86,62 +87,65 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const float* __
   const uint32_t byte = (uint32_t)d * sizeof(E);
   const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
   Walk<const E> at_dt(l.dt, last + mine, b, byte), at_dy(dy, last + mine, b, byte), at_z(l.z, last + mine, b, byte);
-  E dt[ROWS], go[ROWS], z[ROWS];
-  auto fetch = [&](int first) {
+  Coef<E> at_coef(l, WAVES, threadIdx.x, last, b, g);
+  struct Fetched {                                       // two passes ahead, as in the forward kernel
+    uint32_t dt[ROWS], go[ROWS], z[ROWS], coef;
+  } raw0, raw1;
+  auto fetch = [&](int first, Fetched& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (mine + r < PASS && first + mine + r < stop) {
-        dt[r] = at_dt.at(r), go[r] = at_dy.at(r);
-        if (GATE) z[r] = at_z.at(r);
-      } else {
-        dt[r] = go[r] = z[r] = E(0.0f);
+      uint32_t a = 0, b = 0, c = 0;
+      if ((ALL || mine + r < PASS) && first >= t0 && first + mine + r < stop) {
+        a = at_dt.bits(r), b = at_dy.bits(r);
+        if (GATE) c = at_z.bits(r);
       }
+      x.dt[r] = a, x.go[r] = b, x.z[r] = c;
     }
-    at_dt.move(-PASS), at_dy.move(-PASS);
+    x.coef = at_coef.fetch(first >= t0 ? stop - first : 0);
+    at_dt.move(-PASS), at_dy.move(-PASS), at_coef.move(-1);
     if (GATE) at_z.move(-PASS);
   };
-  auto prepare = [&](int first, int buffer) {
+  auto prepare = [&](int first, int buffer, const Fetched& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (mine + r >= PASS) break;
-      float s = softplus<E>((float)dt[r] + bias), q = (float)go[r];
-      s = first + mine + r < stop ? s : 0.0f;            // q is zero there
-      if (GATE) q *= (float)z[r] * sigmoid<E>((float)z[r]);
+      if (!ALL && mine + r >= PASS) break;
+      float s = softplus<E>(value<E>(x.dt[r]) + bias), q = value<E>(x.go[r]);
+      s = first >= t0 && first + mine + r < stop ? s : 0.0f;      // q is zero there
+      if (GATE) q *= value<E>(x.z[r]) * sigmoid<E>(value<E>(x.z[r]));
       total += s;
       step_in[buffer][mine + r][lane] = make_float2(s, q);
     }
+    (&coef[buffer][0][0][0])[threadIdx.x] = value<E>(x.coef);
   };
-  const int padded = (l.T + kPad - 1) / kPad * kPad;
-  const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + last) * 2 * kHeld;
-  Coef<BATCH> now, next;
+  auto pass = [&](int k, auto parity) __attribute__((always_inline)) {                  // the k-th from the end
+    constexpr int buffer = parity.value;
+    Fetched &here = pick<buffer>(raw0, raw1), &there = pick<buffer>(raw1, raw0);
+    const int first = last - k * PASS;
+    fetch(first - 2 * PASS, here);               // nothing, in front of the span
+#pragma unroll
+    for (int i = PASS - 1; i >= 0; --i) {
+      float Cm[kHeld];
+      two_by_two(i + 1);
+      const float2 in_ = step_in[buffer][i][lane];
+      four(coef[buffer][i][w] + kHeld, Cm);
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) carry[j] = exp2_fast(in_.x * A2[j]) * fmaf(in_.y, Cm[j], carry[j]);
+    }
+    now(carry);
+    prepare(first - PASS, buffer ^ 1, there);    // a pass that no one walks, in front of it
+    __syncthreads();
+  };
   if (passes) {
-    fetch(last);
-    prepare(last, (passes - 1) & 1);
-    now.ask(from + (PASS - BATCH) * 2 * kHeld);
+    fetch(last, raw0);
+    fetch(last - PASS, raw1);
+    prepare(last, 0, raw0);
   }
   __syncthreads();
-  for (int p = passes - 1; p >= 0; --p) {
-    const int first = t0 + p * PASS, buffer = p & 1;
-    float2 in_[PASS];
-#pragma unroll
-    for (int i = PASS - 1; i >= 0; --i) in_[i] = step_in[buffer][i][lane];
-    if (p) fetch(first - PASS);
-#pragma unroll
-    for (int j = PASS - BATCH; j >= 0; j -= BATCH) {
-      wait_for_scalars();
-      next.ask(from + (j || p ? j - BATCH : 0) * 2 * kHeld);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = BATCH - 1; i >= 0; --i)
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) carry[k] = exp2_fast(in_[j + i].x * A2[k]) * fmaf(in_[j + i].y, now.C(i, k), carry[k]);
-      __builtin_amdgcn_sched_barrier(0);
-      now = next;
-    }
-    from -= PASS * 2 * kHeld;
-    if (p) prepare(first - PASS, buffer ^ 1);
-    __syncthreads();
-  }
+  constexpr std::integral_constant<int, 0> even;
+  constexpr std::integral_constant<int, 1> odd;
+  int k = 0;
+  for (; k + 1 < passes; k += 2) pass(k, even), pass(k + 1, odd);
+  if (k < passes) pass(k, even);
   static_assert(sizeof(step_in) >= WAVES * kTile * sizeof(float));
   float* totals = &step_in[0][0][0].x;
   totals[w * kTile + lane] = total;
@@ -158,12 +162,14 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const float* __
 // of its states, then walks back; the sums over the states go through LDS (s1 = sum g B, s2 = sum w h A, and with a gate
 // sum C h), those over the channels through registers.
 template <typename E, int WAVES, bool GATE>
-__global__ void __launch_bounds__(WAVES * 64)
-scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ states, const float* __restrict__ coef,
-                     const Summary sum, const Spans spans, const Grads<E> o) {
-  constexpr int ROWS = (PASS + WAVES - 1) / WAVES, BATCH = 2, SUMS = GATE ? 3 : 2;
+__global__ void __launch_bounds__(WAVES * 64, WAVES <= 12 ? 3 : 4)
+scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ states, const Summary sum, const Spans spans,
+                     const Grads<E> o) {
+  constexpr int ROWS = (PASS + WAVES - 1) / WAVES, SUMS = GATE ? 3 : 2;
+  constexpr bool ALL = PASS % WAVES == 0;
   __shared__ float2 step_in[2][PASS][kTile];             // (s, s u)
   __shared__ float step_q[2][PASS][kTile];
+  __shared__ alignas(16) float coef[2][PASS][WAVES][2 * kHeld];
   __shared__ float share[SUMS][WAVES][PASS][kTile];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = blockIdx.x % (l.G * l.tiles), span = blockIdx.x / (l.G * l.tiles), g = tile / l.tiles, b = blockIdx.y;
@@ -196,35 +202,37 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   Walk<const E> at_u(l.u, last + mine, b, byte), at_dt(l.dt, last + mine, b, byte), at_dy(dy, last + mine, b, byte), at_z(l.z, last + mine, b, byte);
   Walk<E> at_du(o.du, last + mine, b, byte), at_ddt(o.ddt, last + mine, b, byte), at_dz(o.dz, last + mine, b, byte);
   const float* at_states = states + state_at(last / kKept, l.B, b, WAVES, w, l.D, d);
-  E u[ROWS], dt[ROWS], go[ROWS], z[ROWS];
+  Coef<E> at_coef(l, WAVES, threadIdx.x, last, b, g);
+  uint32_t u[ROWS], dt[ROWS], go[ROWS], z[ROWS], raw_coef;
   struct Row {                                           // of a step: what its outputs are made of
     float s, u, q, slope, gate;                          // slope: sigmoid(raw), gate: dy silu'(z)
   } row[ROWS], was[ROWS];
   float4 kept;
-  auto fetch = [&](int first) {
+  auto fetch = [&](int first) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (mine + r < PASS && first + mine + r < stop) {
-        u[r] = at_u.at(r), dt[r] = at_dt.at(r), go[r] = at_dy.at(r);
-        if (GATE) z[r] = at_z.at(r);
-      } else {
-        u[r] = dt[r] = go[r] = z[r] = E(0.0f);
+      uint32_t a = 0, b = 0, c = 0, e = 0;
+      if ((ALL || mine + r < PASS) && first + mine + r < stop) {
+        a = at_u.bits(r), b = at_dt.bits(r), c = at_dy.bits(r);
+        if (GATE) e = at_z.bits(r);
       }
+      u[r] = a, dt[r] = b, go[r] = c, z[r] = e;
     }
+    raw_coef = at_coef.fetch(stop - first);
     kept = *reinterpret_cast<const float4*>(at_states);
-    at_u.move(-PASS), at_dt.move(-PASS), at_dy.move(-PASS);
+    at_u.move(-PASS), at_dt.move(-PASS), at_dy.move(-PASS), at_coef.move(-1);
     if (GATE) at_z.move(-PASS);
     at_states -= (int64_t)l.B * WAVES * l.D * kHeld;
   };
-  auto prepare = [&](int first, int buffer) {
+  auto prepare = [&](int first, int buffer) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      if (mine + r >= PASS) break;
+      if (!ALL && mine + r >= PASS) break;
       const bool real = on && first + mine + r < stop;
-      const float raw = (float)dt[r] + bias;
-      Row v{softplus<E>(raw), (float)u[r], (float)go[r], sigmoid<E>(raw), 0.0f};
+      const float raw = value<E>(dt[r]) + bias;
+      Row v{softplus<E>(raw), value<E>(u[r]), value<E>(go[r]), sigmoid<E>(raw), 0.0f};
       if (GATE) {
-        const float x = (float)z[r], sg = sigmoid<E>(x);
+        const float x = value<E>(z[r]), sg = sigmoid<E>(x);
         v.gate = v.q * sg * fmaf(x, 1.0f - sg, 1.0f);
         v.q *= x * sg;                                   // silu(z) first, as the forward pass has it
       }
@@ -233,12 +241,13 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       step_in[buffer][mine + r][lane] = make_float2(v.s, v.s * v.u);
       step_q[buffer][mine + r][lane] = v.q;
     }
+    (&coef[buffer][0][0][0])[threadIdx.x] = value<E>(raw_coef);
   };
-  auto finish = [&](int first) {
+  auto finish = [&](int first) __attribute__((always_inline)) {
     float du[ROWS], ddt[ROWS], dz[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int i = mine + r < PASS ? mine + r : 0;
+      const int i = (ALL || mine + r < PASS) ? mine + r : 0;
       const Row v = was[r];
       float s1 = 0.0f, s2 = 0.0f, plain = skip * v.u;
 #pragma unroll
@@ -249,93 +258,69 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       du[r] = fmaf(v.s, s1, skip * v.q);
       ddt[r] = fmaf(v.u, s1, s2) * v.slope;
       dz[r] = v.gate * plain;
-      if (mine + r < PASS && first + mine + r < stop) dbias += ddt[r], dskip = fmaf(v.q, v.u, dskip);
+      if ((ALL || mine + r < PASS) && first + mine + r < stop) dbias += ddt[r], dskip = fmaf(v.q, v.u, dskip);
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
-      if (mine + r < PASS && first + mine + r < stop && on) {
-        at_du.at(r) = static_cast<E>(du[r]), at_ddt.at(r) = static_cast<E>(ddt[r]);
-        if (GATE) at_dz.at(r) = static_cast<E>(dz[r]);
+      if ((ALL || mine + r < PASS) && first + mine + r < stop && on) {
+        at_du.put(r, du[r]), at_ddt.put(r, ddt[r]);
+        if (GATE) at_dz.put(r, dz[r]);
       }
     at_du.move(-PASS), at_ddt.move(-PASS);
     if (GATE) at_dz.move(-PASS);
   };
 
-  const int padded = (l.T + kPad - 1) / kPad * kPad;
-  const float* from = coef + ((((int64_t)b * l.G + g) * WAVES + w) * padded + last) * 2 * kHeld;
-  float* at_bc = o.bc + (((((int64_t)(tile % l.tiles) * l.B + b) * l.G + g) * (padded / PASS) + last / PASS) * WAVES + w) * 64;
-  Coef<BATCH> now, next;
+  float* at_bc = o.bc + (((((int64_t)(tile % l.tiles) * l.B + b) * l.G + g) * ((l.T + PASS - 1) / PASS) + last / PASS) * WAVES + w) * 64;
   if (passes) {
     fetch(last);
     prepare(last, (passes - 1) & 1);
-    now.ask(from);
   }
   __syncthreads();
   for (int p = passes - 1; p >= 0; --p) {
     const int first = t0 + p * PASS, buffer = p & 1;
-    float2 in_[PASS];
-    float q[PASS];
-#pragma unroll
-    for (int i = 0; i < PASS; ++i) in_[i] = step_in[buffer][i][lane], q[i] = step_q[buffer][i][lane];
     float a[PASS][kHeld], h[PASS + 1][kHeld];
     h[0][0] = kept.x, h[0][1] = kept.y, h[0][2] = kept.z, h[0][3] = kept.w;
     if (p + 1 < passes) finish(first + PASS);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) was[r] = row[r];
     if (p) fetch(first - PASS);
-    auto forward = [&](int j) {
 #pragma unroll
-      for (int i = j; i < j + BATCH; ++i)
+    for (int i = 0; i < PASS; ++i) {
+      float Bm[kHeld];
+      two_by_two(i);
+      const float2 in_ = step_in[buffer][i][lane];
+      four(coef[buffer][i][w], Bm);
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-          a[i][k] = exp2_fast(in_[i].x * A2[k]);
-          h[i + 1][k] = fmaf(a[i][k], h[i][k], in_[i].y * now.B(i - j, k));
-        }
-    };
-    float step_sum[PASS];
-    auto backward = [&](int j) {
-#pragma unroll
-      for (int i = j + BATCH - 1; i >= j; --i) {
-        float s1 = 0.0f, s2 = 0.0f, plain = 0.0f, pair[kHeld];
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-          const float gh = fmaf(q[i], now.C(i - j, k), carry[k]);
-          carry[k] = a[i][k] * gh;
-          const float through = carry[k] * h[i][k];
-          s1 = k ? fmaf(gh, now.B(i - j, k), s1) : gh * now.B(i - j, k);
-          s2 = k ? fmaf(through, A[k], s2) : through * A[k];
-          dA[k] = fmaf(through, in_[i].x, dA[k]);
-          if (GATE) plain = k ? fmaf(now.C(i - j, k), h[i + 1][k], plain) : now.C(i - j, k) * h[i + 1][k];
-          pair[k] = swap32_add(gh * in_[i].y, h[i + 1][k] * q[i]);
-        }
-        step_sum[i] = half_row_add(swap16_add(pair[0], pair[1]), swap16_add(pair[2], pair[3]));
-        share[0][w][i][lane] = s1, share[1][w][i][lane] = s2;
-        if (GATE) share[SUMS - 1][w][i][lane] = plain;
+      for (int k = 0; k < kHeld; ++k) {
+        a[i][k] = exp2_fast(in_.x * A2[k]);
+        h[i + 1][k] = fmaf(a[i][k], h[i][k], in_.y * Bm[k]);
       }
-    };
-    // Bm and Cm are asked for in the order 0 2 4 6 4 2 0 of steps: the last two are there when the walk turns
-#pragma unroll
-    for (int j = 0; j < PASS; j += BATCH) {
-      wait_for_scalars();
-      next.ask(from + (j + BATCH < PASS ? j + BATCH : j - BATCH) * 2 * kHeld);
-      __builtin_amdgcn_sched_barrier(0);
-      forward(j);
-      __builtin_amdgcn_sched_barrier(0);
-      if (j + BATCH < PASS) now = next;
     }
     // the last pass's shares have been read: a second barrier a pass instead of a second set of them, whose LDS would let
     // eight waves on a compute unit instead of twelve (1105 us against 925 at T = 4096, B = 4, D = 4096)
     __syncthreads();
+    float step_sum[PASS];
 #pragma unroll
-    for (int j = PASS - BATCH; j >= 0; j -= BATCH) {
-      if (j < PASS - BATCH) {
-        wait_for_scalars();
-        next.ask(from + (j ? j - BATCH : p ? -PASS : 0) * 2 * kHeld);
-        __builtin_amdgcn_sched_barrier(0);
+    for (int i = PASS - 1; i >= 0; --i) {
+      float Bm[kHeld], Cm[kHeld], s1 = 0.0f, s2 = 0.0f, plain = 0.0f, pair[kHeld];
+      two_by_two(i + 1);
+      const float2 in_ = step_in[buffer][i][lane];
+      four(coef[buffer][i][w], Bm), four(coef[buffer][i][w] + kHeld, Cm);
+      const float q = step_q[buffer][i][lane];
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        const float gh = fmaf(q, Cm[k], carry[k]);
+        carry[k] = a[i][k] * gh;
+        const float through = carry[k] * h[i][k];
+        s1 = k ? fmaf(gh, Bm[k], s1) : gh * Bm[k];
+        s2 = k ? fmaf(through, A[k], s2) : through * A[k];
+        dA[k] = fmaf(through, in_.x, dA[k]);
+        if (GATE) plain = k ? fmaf(Cm[k], h[i + 1][k], plain) : Cm[k] * h[i + 1][k];
+        pair[k] = swap32_add(gh * in_.y, h[i + 1][k] * q);
       }
-      backward(j);
-      __builtin_amdgcn_sched_barrier(0);
-      now = next;
+      step_sum[i] = half_row_add(swap16_add(pair[0], pair[1]), swap16_add(pair[2], pair[3]));
+      share[0][w][i][lane] = s1, share[1][w][i][lane] = s2;
+      if (GATE) share[SUMS - 1][w][i][lane] = plain;
     }
     const bool odd = lane & 1, high = lane & 2;
     const float low = in_four_add<0x4E>(four_add(step_sum[0], step_sum[1]), four_add(step_sum[2], step_sum[3]), high);
@@ -343,7 +328,6 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
     const float part = in_four_add<0xB1>(low, top, odd);
     at_bc[lane] = part;
     at_bc -= WAVES * 64;
-    from -= PASS * 2 * kHeld;
     if (p) prepare(first - PASS, buffer ^ 1);
     __syncthreads();
   }
@@ -423,13 +407,12 @@ join_kernel(const Layer<E> l, const Grads<E> o, const Joined to) {
 // bc: parts of dB and dC [tile of the group][b][g][pass][w][64 lanes]; dA, dskip, ddt_bias: one part a span and sample.
 struct Scratch {
   Spans spans;
-  size_t coef, ends, sums, bc, dA, dskip, ddt_bias, bytes;
+  size_t ends, sums, bc, dA, dskip, ddt_bias, bytes;
   int64_t bc_floats;                           // of one tile
   Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G, 8)) {
     const int64_t waves = waves_of(N), tiles = bppsa_ceil_div(D / G, kTile), parts = (int64_t)spans.count * B * D;
-    bc_floats = (int64_t)B * G * ((T + kPad - 1) / kPad * kPad / PASS) * waves * 64;
+    bc_floats = (int64_t)B * G * ((T + PASS - 1) / PASS) * waves * 64;
     Arena take;
-    coef = take(G > kGroupsKept ? coef_floats(T, B, N, G) : 0);
     ends = take(spans.count > 1 ? parts * waves * kHeld : 0), sums = take(spans.count > 1 ? parts : 0);
     bc = take(tiles * bc_floats);
     dA = take(parts * waves * kHeld), dskip = take(parts), ddt_bias = take(parts);
@@ -462,18 +445,14 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
                      part(at.dskip), part(at.ddt_bias), grads->dh0};
     const Summary sum{part(at.ends), part(at.sums)};
     const Rows<const E> out = rows_of<const E>(*dy);
-    const float* kept = static_cast<const float*>(states);
-    const float* coef = kept;
-    kept += kept_coef_floats(l.T, l.B, l.N);
-    if (l.G > kGroupsKept) launch_coef(l, part(at.coef), s), coef = part(at.coef);
     auto walk = [&](auto waves_, auto gate) {
       constexpr int W = waves_.value;
       constexpr bool GATE = gate.value;
       if (at.spans.count > 1)
         scan_backward_summary_kernel<E, W, GATE><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
-            l, out, coef, sum, at.spans);
+            l, out, sum, at.spans);
       scan_backward_kernel<E, W, GATE><<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(
-          l, out, kept, coef, sum, at.spans, o);
+          l, out, static_cast<const float*>(states), sum, at.spans, o);
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     };

@@ -1,11 +1,11 @@
 // What the selective scan's kernels share: how the work is cut, and the arrays between launches.
 //
 // A workgroup takes 64 channels of one group, one a lane, of one sample.  Its waves split the states: wave w holds states
-// 4 w .. 4 w + 3 of all 64 channels, so that Bm and Cm of a step are the same number for a whole wave.  They come through
-// the scalar cache into scalar registers from a float array that a first small launch writes (`coef`), and cost the vector
-// unit nothing; what the waves share, the step's size and the sums over the states, goes through LDS once a channel.
-// The other layout that was thought through, states along the lanes, needs two vector additions a step and four states
-// for the sum over them and 16 bytes of LDS reads a state for Bm and Cm, which by itself would bind the kernel.
+// 4 w .. 4 w + 3 of all 64 channels.  What the waves share goes through LDS: a step's size, made once for a channel, the
+// sums over the states, and Bm and Cm, which are the same number for a whole wave.  (Those were scalar operands first, of
+// no cost to the vector unit; but a scalar load can only be waited for with all others that are out, at every second step,
+// and 32 of them at a time left so few scalar registers that a tenth of the vector instructions moved others out of the
+// way.)  States along the lanes instead would need two vector additions a step for the sum over them.
 #pragma once
 
 #include "ssm_common.h"
@@ -15,7 +15,6 @@ namespace ssm {
 constexpr int kTile = 64;        // channels of a workgroup, one a lane
 constexpr int kHeld = 4;         // states of a channel that a wave holds
 constexpr int kKept = 8;         // steps between two states kept for the backward pass
-constexpr int kPad = kKept;      // `coef` reaches to the next multiple of so many steps: a span's last steps are not tested for
 
 template <typename E>
 struct Layer {
@@ -58,60 +57,42 @@ __host__ __device__ __forceinline__ int64_t state_at(int64_t first, int B, int b
   return (((first * B + b) * waves + w) * D + d) * kHeld;
 }
 
-// coef [b][g][w][t][8]: four Bm, then four Cm, zero beyond the states there are and behind a sample's end.
-static inline int64_t coef_floats(int64_t T, int64_t B, int64_t N, int64_t G) {
-  return B * G * ((T + kPad - 1) / kPad * kPad) * waves_of((int)N) * 2 * kHeld;
-}
-
-// A forward call that keeps states for the backward pass keeps coef in front of them, up to this many groups (the size of
-// the states is asked for without G): one launch less there.
-constexpr int kGroupsKept = 4;
-static inline size_t kept_coef_floats(int64_t T, int64_t B, int64_t N) {
-  return bppsa_align_up((size_t)coef_floats(T, B, N, kGroupsKept), 64);
-}
-
+// Bm and Cm of a pass of kKept steps, for all waves of a workgroup: [step][wave][four Bm, four Cm], one value a thread.
+// A thread fetches its value of a pass ahead, as an element, and leaves it in LDS as a float; a wave reads its eight of a
+// step from one place, 16 bytes an access.  Zero beyond the states there are and behind a sample's end.
 template <typename E>
-static __global__ void __launch_bounds__(256)
-coef_kernel(const Layer<E> l, int waves, int64_t all, float* __restrict__ coef) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= all) return;
-  const int of = (int)(i % 8), padded = (l.T + kPad - 1) / kPad * kPad;
-  const int64_t row = i / 8;
-  const int t = (int)(row % padded), w = (int)(row / padded % waves);
-  const int64_t bg = row / padded / waves;
-  const int g = (int)(bg % l.G), b = (int)(bg / l.G), n = w * kHeld + of % kHeld;
-  const bool in = n < l.N && t < clamp_length(l.lengths, b, l.T);
-  coef[i] = in ? load((of < kHeld ? l.Bm : l.Cm).at(t, b) + g * l.N + n) : 0.0f;
-}
-
-// Bm and Cm of STEPS steps in scalar registers.  Scalar loads come back in any order, so the only wait for one is the wait
-// for all that are out, LDS reads among them: a batch's loads go out together, right behind the wait for the batch
-// before, and have the time of that one's steps.  (Left to the compiler, which asks for one step's at a time, a wave
-// waited for every one: 492 us instead of 344 at T = 30000, D = 2048.)  Batches of four steps, 64 registers for two of them,
-// suit the summaries; in the main kernels they left so few that a quarter of the backward pass's vector instructions moved
-// scalars to and from vector lanes: batches of two there.
-typedef float TwoSteps __attribute__((ext_vector_type(4 * kHeld)));
-typedef const __attribute__((address_space(4))) TwoSteps* ScalarCoef;       // read through the scalar cache
-template <int STEPS>
 struct Coef {
-  TwoSteps at[STEPS / 2];
-  __device__ __forceinline__ void ask(const float* from) {
-#pragma unroll
-    for (int k = 0; k < STEPS / 2; ++k) at[k] = ((ScalarCoef)from)[k];
+  uint64_t at;
+  int64_t step;                    // of a pass
+  int row;                         // of the pass
+  bool real;
+  __device__ __forceinline__ Coef(const Layer<E>& l, int waves, int thread, int first, int b, int g) {
+    const int k = thread % (2 * kHeld), n = thread / (2 * kHeld) % waves * kHeld + k % kHeld;
+    row = thread / (2 * kHeld) / waves, real = n < l.N;
+    const Rows<const E> r{k < kHeld ? l.Bm.data : l.Cm.data, k < kHeld ? l.Bm.st : l.Cm.st, k < kHeld ? l.Bm.sb : l.Cm.sb};
+    at = (uint64_t)(r.at(first + row, b) + g * l.N + (real ? n : 0));
+    step = r.st * (int64_t)sizeof(E) * kKept;
   }
-  __device__ __forceinline__ float B(int i, int k) const { return at[i / 2][i % 2 * 2 * kHeld + k]; }
-  __device__ __forceinline__ float C(int i, int k) const { return at[i / 2][i % 2 * 2 * kHeld + kHeld + k]; }
+  __device__ __forceinline__ uint32_t fetch(int left) const { return real && row < left ? bits_at<E>(at) : 0; }   // left: steps of the pass that there are
+  __device__ __forceinline__ void move(int passes) { at += passes * step; }
 };
-// All scalar loads and LDS accesses of this wave are done; none of what follows is moved in front of it.
-__device__ __forceinline__ void wait_for_scalars() {
-  __builtin_amdgcn_s_waitcnt(0xC07F);        // lgkmcnt(0), nothing else
-  __builtin_amdgcn_sched_barrier(0);
+template <int SECOND, typename X>
+__device__ __forceinline__ X& pick(X& a, X& b) {
+  if constexpr (SECOND) return b;
+  else return a;
 }
 
-template <typename E>
-static void launch_coef(const Layer<E>& l, float* coef, hipStream_t s) {
-  const int64_t all = coef_floats(l.T, l.B, l.N, l.G);
-  coef_kernel<E><<<(unsigned)((all + 255) / 256), 256, 0, s>>>(l, waves_of(l.N), all, coef);
+// Two steps' instructions stay together: without a limit the compiler starts a whole pass's products and exponentials, twice
+// the registers.
+__device__ __forceinline__ void two_by_two(int i) {
+  if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+}
+// The states are computed here and not later: nothing but the next pass needs them, and the compiler keeps the operands of
+// several passes instead.
+__device__ __forceinline__ void now(float (&h)[kHeld]) { asm volatile("" : "+v"(h[0]), "+v"(h[1]), "+v"(h[2]), "+v"(h[3])); }
+__device__ __forceinline__ void four(const float* from, float (&v)[kHeld]) {
+  const float4 x = *reinterpret_cast<const float4*>(from);
+  v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
 }
 
 // A long sequence with few channels is cut into spans, each scanned by workgroups of its own.  A first launch scans each
@@ -148,14 +129,14 @@ __device__ __forceinline__ void join_spans(const Summary& sum, int first, int st
   }
 }
 
-// As many spans as give every SIMD `waves` waves, none shorter than 32 steps (a multiple of kPad), 64 at most.
+// As many spans as give every SIMD `waves` waves, none shorter than 32 steps (a multiple of kKept), 64 at most.
 static inline Spans spans_of(int T, int B, int D, int N, int G, int waves) {
   const int64_t have = (int64_t)G * bppsa_ceil_div(D / G, kTile) * B * waves_of(N);
   int64_t count = (int64_t)bppsa_compute_units() * 4 * waves / have;
   if (count > T / 32) count = T / 32;
   if (count > 64) count = 64;
   if (count < 2) return Spans{1, T};
-  const int steps = bppsa_ceil_div(bppsa_ceil_div(T, (int)count), kPad) * kPad;
+  const int steps = bppsa_ceil_div(bppsa_ceil_div(T, (int)count), kKept) * kKept;
   return Spans{bppsa_ceil_div(T, steps), steps};
 }
 
