@@ -45,14 +45,16 @@ __device__ __forceinline__ float value(uint32_t bits) {
 template <typename E>
 struct Walk {
   uint64_t lane;
-  int64_t step;
-  __device__ __forceinline__ Walk(const Rows<E>& r, int t, int b, uint32_t byte)
-      : lane((uint64_t)r.at(t, b) + byte), step(r.st * (int64_t)sizeof(E)) {}
+  int64_t step, move_by;           // bytes of a row and of a pass
+  __device__ __forceinline__ Walk(const Rows<E>& r, int t, int b, uint32_t byte, int rows_of_pass)
+      : lane((uint64_t)r.at(t, b) + byte), step(r.st * (int64_t)sizeof(E)), move_by(rows_of_pass * step) {
+    asm("" : "+s"(move_by));       // or a pass back is taken off by two instructions instead of added by one
+  }
   __device__ __forceinline__ uint32_t bits(int rows_on) const { return bits_at<E>(lane + rows_on * step); }
   __device__ __forceinline__ void put(int rows_on, float v) const {
     *(__attribute__((address_space(1))) E*)(lane + rows_on * step) = static_cast<E>(v);
   }
-  __device__ __forceinline__ void move(int rows) { lane += rows * step; }
+  __device__ __forceinline__ void move() { lane += move_by; }
 };
 
 // V neighbouring elements by one access of any alignment: the memory path takes 16 bytes from an odd element as well, and a

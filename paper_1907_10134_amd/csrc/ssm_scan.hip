@@ -44,8 +44,8 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f, skip = l.skip ? l.skip[d] : 0.0f;
   const uint32_t byte = (uint32_t)d * sizeof(E);
   const int mine = w * ROWS;                             // this wave's first step of a pass
-  Walk<const E> at_u(l.u, t0 + mine, b, byte), at_dt(l.dt, t0 + mine, b, byte), at_z(l.z, t0 + mine, b, byte);
-  Walk<E> at_y(y, t0 + mine, b, byte);
+  Walk<const E> at_u(l.u, t0 + mine, b, byte, PASS), at_dt(l.dt, t0 + mine, b, byte, PASS), at_z(l.z, t0 + mine, b, byte, PASS);
+  Walk<E> at_y(y, t0 + mine, b, byte, PASS);
   float* at_states = SUMMARY || !states ? nullptr : states + state_at(t0 / kKept, l.B, b, WAVES, w, l.D, d);
   Coef<E> at_coef(l, WAVES, threadIdx.x, t0, b, g);
   // What a wave fetches for a pass, two passes ahead: one is not enough for a device that is not full.  The values stay as
@@ -66,8 +66,8 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
       x.u[r] = a, x.dt[r] = b, x.z[r] = c;
     }
     x.coef = at_coef.fetch(stop - first);
-    at_u.move(PASS), at_dt.move(PASS), at_coef.move(1);
-    if (GATE) at_z.move(PASS);
+    at_u.move(), at_dt.move(), at_coef.move(1);
+    if (GATE) at_z.move();
   };
   auto prepare = [&](int first, int buffer, const Fetched& x) __attribute__((always_inline)) {
 #pragma unroll
@@ -93,7 +93,7 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
       if ((ALL || mine + r < PASS) && first + mine + r < stop && on) at_y.put(r, v[r]);
-    at_y.move(PASS);
+    at_y.move();
   };
 
   const int passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0;

@@ -86,7 +86,7 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary s
   const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f;
   const uint32_t byte = (uint32_t)d * sizeof(E);
   const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
-  Walk<const E> at_dt(l.dt, last + mine, b, byte), at_dy(dy, last + mine, b, byte), at_z(l.z, last + mine, b, byte);
+  Walk<const E> at_dt(l.dt, last + mine, b, byte, -PASS), at_dy(dy, last + mine, b, byte, -PASS), at_z(l.z, last + mine, b, byte, -PASS);
   Coef<E> at_coef(l, WAVES, threadIdx.x, last, b, g);
   struct Fetched {                                       // two passes ahead, as in the forward kernel
     uint32_t dt[ROWS], go[ROWS], z[ROWS], coef;
@@ -102,8 +102,8 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary s
       x.dt[r] = a, x.go[r] = b, x.z[r] = c;
     }
     x.coef = at_coef.fetch(first >= t0 ? stop - first : 0);
-    at_dt.move(-PASS), at_dy.move(-PASS), at_coef.move(-1);
-    if (GATE) at_z.move(-PASS);
+    at_dt.move(), at_dy.move(), at_coef.move(-1);
+    if (GATE) at_z.move();
   };
   auto prepare = [&](int first, int buffer, const Fetched& x) __attribute__((always_inline)) {
 #pragma unroll
@@ -199,8 +199,8 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   const uint32_t byte = (uint32_t)d * sizeof(E);
   float dskip = 0.0f, dbias = 0.0f;
   const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
-  Walk<const E> at_u(l.u, last + mine, b, byte), at_dt(l.dt, last + mine, b, byte), at_dy(dy, last + mine, b, byte), at_z(l.z, last + mine, b, byte);
-  Walk<E> at_du(o.du, last + mine, b, byte), at_ddt(o.ddt, last + mine, b, byte), at_dz(o.dz, last + mine, b, byte);
+  Walk<const E> at_u(l.u, last + mine, b, byte, -PASS), at_dt(l.dt, last + mine, b, byte, -PASS), at_dy(dy, last + mine, b, byte, -PASS), at_z(l.z, last + mine, b, byte, -PASS);
+  Walk<E> at_du(o.du, last + mine, b, byte, -PASS), at_ddt(o.ddt, last + mine, b, byte, -PASS), at_dz(o.dz, last + mine, b, byte, -PASS);
   const float* at_states = states + state_at(last / kKept, l.B, b, WAVES, w, l.D, d);
   Coef<E> at_coef(l, WAVES, threadIdx.x, last, b, g);
   uint32_t u[ROWS], dt[ROWS], go[ROWS], z[ROWS], raw_coef;
@@ -220,8 +220,8 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
     }
     raw_coef = at_coef.fetch(stop - first);
     kept = *reinterpret_cast<const float4*>(at_states);
-    at_u.move(-PASS), at_dt.move(-PASS), at_dy.move(-PASS), at_coef.move(-1);
-    if (GATE) at_z.move(-PASS);
+    at_u.move(), at_dt.move(), at_dy.move(), at_coef.move(-1);
+    if (GATE) at_z.move();
     at_states -= (int64_t)l.B * WAVES * l.D * kHeld;
   };
   auto prepare = [&](int first, int buffer) __attribute__((always_inline)) {
@@ -266,8 +266,8 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
         at_du.put(r, du[r]), at_ddt.put(r, ddt[r]);
         if (GATE) at_dz.put(r, dz[r]);
       }
-    at_du.move(-PASS), at_ddt.move(-PASS);
-    if (GATE) at_dz.move(-PASS);
+    at_du.move(), at_ddt.move();
+    if (GATE) at_dz.move();
   };
 
   float* at_bc = o.bc + (((((int64_t)(tile % l.tiles) * l.B + b) * l.G + g) * ((l.T + PASS - 1) / PASS) + last / PASS) * WAVES + w) * 64;
