@@ -10,14 +10,14 @@ using namespace ssm;
 // the states in LDS, and each wave finishes its ROWS of outputs.  Inputs of the next pass are prepared and outputs of the
 // last one finished beside a pass, so there is one barrier a pass.
 // Bound by issue: a step of four states takes 4 exp (two slots each), 16 products and multiply-adds, two LDS accesses.
-template <typename E, int WAVES, bool SUMMARY, bool GATE>
+template <typename E, int WAVES, int H, bool SUMMARY, bool GATE>
 __global__ void __launch_bounds__(WAVES * 64, WAVES <= 12 ? 6 : 4)      // at least so many waves a SIMD
 scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, const Summary sum,
             const Spans spans) {
   constexpr int PASS = kKept, ROWS = (PASS + WAVES - 1) / WAVES;   // a wave prepares and finishes ROWS steps
   constexpr bool ALL = PASS % WAVES == 0;                          // none has fewer
   __shared__ float2 step_in[2][PASS][kTile];
-  __shared__ alignas(16) float coef[2][PASS][WAVES][2 * kHeld];
+  __shared__ alignas(16) float coef[2][PASS][WAVES][2 * H];
   __shared__ float share[SUMMARY ? 1 : 2][SUMMARY ? 1 : WAVES][SUMMARY ? 1 : PASS][kTile];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // neighbours in the grid, which go to different dies, are tiles of a span: spans may lie behind a sample's end
@@ -31,10 +31,10 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   if (!SUMMARY && on)
     for (int t = (t0 > len ? t0 : len) + w; t < t1; t += WAVES) store(y.at(t, b) + d, 0.0f);
 
-  float A2[kHeld], h[kHeld];
+  float A2[H], h[H];
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    const int n = w * kHeld + i;
+  for (int i = 0; i < H; ++i) {
+    const int n = w * H + i;
     A2[i] = n < l.N ? l.A[(int64_t)d * l.N + n] * kLog2e : 0.0f;
     h[i] = !SUMMARY && n < l.N && l.h0 ? l.h0[((int64_t)b * l.D + d) * l.N + n] : 0.0f;
   }
@@ -46,8 +46,8 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   const int mine = w * ROWS;                             // this wave's first step of a pass
   Walk<const E> at_u(l.u, t0 + mine, b, byte, PASS), at_dt(l.dt, t0 + mine, b, byte, PASS), at_z(l.z, t0 + mine, b, byte, PASS);
   Walk<E> at_y(y, t0 + mine, b, byte, PASS);
-  float* at_states = SUMMARY || !states ? nullptr : states + state_at(t0 / kKept, l.B, b, WAVES, w, l.D, d);
-  Coef<E> at_coef(l, WAVES, threadIdx.x, t0, b, g);
+  float* at_states = SUMMARY || !states ? nullptr : states + state_at(H, t0 / kKept, l.B, b, WAVES, w, l.D, d);
+  Coef<E, H> at_coef(l, WAVES, threadIdx.x, t0, b, g);
   // What a wave fetches for a pass, two passes ahead: one is not enough for a device that is not full.  The values stay as
   // they are loaded until they are needed: a conversion here would wait for each load by itself.
   struct Fetched {
@@ -78,7 +78,7 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
       if (SUMMARY) total += s;
       step_in[buffer][mine + r][lane] = make_float2(s, s * value<E>(x.u[r]));
     }
-    (&coef[buffer][0][0][0])[threadIdx.x] = value<E>(x.coef);
+    if (64 * H >= 256 || threadIdx.x < WAVES * PASS * 2 * H) (&coef[buffer][0][0][0])[threadIdx.x] = value<E>(x.coef);
   };
   auto finish = [&](int first, int buffer) __attribute__((always_inline)) {
     float v[ROWS];
@@ -106,18 +106,18 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
     for (int r = 0; r < ROWS; ++r) u_was[r] = here.u[r], z_was[r] = here.z[r];
     fetch(first + 2 * PASS, here);               // nothing, behind the last pass
     if (!SUMMARY && states) {
-      if (on) *reinterpret_cast<float4*>(at_states) = make_float4(h[0], h[1], h[2], h[3]);
-      at_states += (int64_t)l.B * WAVES * l.D * kHeld;
+      if (on) put(at_states, h);
+      at_states += (int64_t)l.B * WAVES * l.D * H;
     }
 #pragma unroll
     for (int i = 0; i < PASS; ++i) {
-      float Bm[kHeld], Cm[kHeld], v = 0.0f;
+      float Bm[H], Cm[H], v = 0.0f;
       two_by_two(i);
       const float2 in_ = step_in[buffer][i][lane];
-      four(coef[buffer][i][w], Bm);
-      if (!SUMMARY) four(coef[buffer][i][w] + kHeld, Cm);
+      get(coef[buffer][i][w], Bm);
+      if (!SUMMARY) get(coef[buffer][i][w] + H, Cm);
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
+      for (int k = 0; k < H; ++k) {
         h[k] = fmaf(exp2_fast(in_.x * A2[k]), h[k], in_.y * Bm[k]);
         if (!SUMMARY) v = k ? fmaf(Cm[k], h[k], v) : Cm[k] * h[k];
       }
@@ -147,7 +147,7 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
     totals[w * kTile + lane] = total;
     __syncthreads();
     if (!on) return;
-    *reinterpret_cast<float4*>(sum.ends + state_at(span, l.B, b, WAVES, w, l.D, d)) = make_float4(h[0], h[1], h[2], h[3]);
+    put(sum.ends + state_at(H, span, l.B, b, WAVES, w, l.D, d), h);
     if (w == 0) {
       for (int k = 1; k < WAVES; ++k) total += totals[k * kTile + lane];
       sum.sums[((int64_t)span * l.B + b) * l.D + d] = total;
@@ -156,8 +156,8 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
     if (!on) return;
     if (h_last && (len ? t0 < len && len <= t1 : span == 0))
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i)
-        if (w * kHeld + i < l.N) h_last[((int64_t)b * l.D + d) * l.N + w * kHeld + i] = h[i];
+      for (int i = 0; i < H; ++i)
+        if (w * H + i < l.N) h_last[((int64_t)b * l.D + d) * l.N + w * H + i] = h[i];
   }
 }
 
@@ -168,7 +168,7 @@ struct Scratch {
   Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G, 6)) {
     Arena take;
     const int64_t parts = spans.count > 1 ? (int64_t)spans.count * B * D : 0;
-    ends = take(parts * waves_of(N) * kHeld), sums = take(parts);
+    ends = take(parts * padded_of(N)), sums = take(parts);
     bytes = take.at;
   }
 };
@@ -176,7 +176,7 @@ struct Scratch {
 // One token.  A thread holds four states of a channel, 2^LANES neighbouring lanes a channel, for kStreams rows of the batch
 // one after the other, so that A is read once for all of them and their states are on their way together.  Bound by the
 // states' memory: 16 bytes a lane, read and written in place.  VECTOR: N is a multiple of 4 and state and A lie on 16 bytes.
-constexpr int kStreams = 4;
+constexpr int kStreams = 4, kHeld = 4;
 template <typename E, int LANES, bool VECTOR>
 __global__ void __launch_bounds__(256)
 scan_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int slots_in_state, const int32_t* __restrict__ slots) {
@@ -247,7 +247,7 @@ scan_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int slo
 
 extern "C" size_t bppsa_ssm_scan_states_bytes(int T, int B, int D, int N) {
   if (!sizes_ok(T, B, D, N, 1)) return 0;
-  return (size_t)bppsa_ceil_div(T, kKept) * B * D * waves_of(N) * kHeld * sizeof(float);
+  return (size_t)bppsa_ceil_div(T, kKept) * B * D * padded_of(N) * sizeof(float);
 }
 
 extern "C" size_t bppsa_ssm_scan_workspace_bytes(int T, int B, int D, int N, int G) {
@@ -266,12 +266,12 @@ extern "C" bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows*
     const Layer<E> l = layer_of<E>(*layer);
     auto part = [&](size_t o) { return reinterpret_cast<float*>(static_cast<char*>(workspace) + o); };
     const Summary sum{part(at.ends), part(at.sums)};
-    return by_waves(waves_of(l.N), [&](auto waves) {
-      constexpr int W = waves.value;
+    return by_states(l.N, [&](auto waves, auto held) {
+      constexpr int W = waves.value, H = held.value;
       if (at.spans.count > 1)                  // nothing asks for the last span's summary
-        scan_kernel<E, W, true, false><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
+        scan_kernel<E, W, H, true, false><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
             l, Rows<E>{}, nullptr, nullptr, sum, at.spans);
-      const auto kernel = l.z.data ? scan_kernel<E, W, false, true> : scan_kernel<E, W, false, false>;
+      const auto kernel = l.z.data ? scan_kernel<E, W, H, false, true> : scan_kernel<E, W, H, false, false>;
       kernel<<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(l, rows_of<E>(*y), h_last,
                                                                         static_cast<float*>(states), sum, at.spans);
       BPPSA_CHECK_LAUNCH();

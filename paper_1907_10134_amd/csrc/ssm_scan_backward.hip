@@ -20,10 +20,11 @@ struct Grads {
 
 constexpr int PASS = kKept;
 
-// Sums over the wave's 64 lanes of the 8 products of each of 8 steps; lane l is left with product `bits reversed(l)` of the
-// 64, counted 8 step + 2 state + (0: dB, 1: dC).  A level halves the registers and doubles the lanes that are summed: two
-// registers exchange halves and are added, one slot a register and level, 126 in all, where 64 full sums would take 384.
-// Levels one to three run as soon as a step's products are there.
+// Sums over the wave's 64 lanes of the 2 H products (dB and dC of H states) of each of 8 steps.  A level halves the registers
+// and doubles the lanes that are summed: two registers exchange halves and are added, one slot a register and level, 126
+// in all at H = 4, where 64 full sums would take 384.  At the end a lane has one product, at H = 2 the same one as its
+// neighbour: the bits of its number say which, from the highest on dB or dC, state, step (lowest bit first each).
+// The levels of one step run as soon as its products are there.
 __device__ __forceinline__ float swap32_add(float a, float b) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
@@ -56,19 +57,40 @@ __device__ __forceinline__ float in_four_add(float a, float b, bool second) {
   const float keep = second ? b : a, give = second ? a : b;
   return keep + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(give), QUAD_PERM, 0xf, 0xf, true));
 }
-__host__ __device__ __forceinline__ int product_of_lane(int lane) {
-  return (lane & 1) << 5 | (lane & 2) << 3 | (lane & 4) << 1 | (lane & 8) >> 1 | (lane & 16) >> 3 | (lane & 32) >> 5;
+struct Product {
+  int of_C, state, step;
+  bool first;                      // of the lanes that have it
+};
+__device__ __forceinline__ Product product_of_lane(int lane, int held) {
+  auto bit = [&](int k) { return lane >> k & 1; };
+  if (held == 4) return Product{bit(5), bit(4) | bit(3) << 1, bit(2) | bit(1) << 1 | bit(0) << 2, true};
+  return Product{bit(5), bit(4), bit(3) | bit(2) << 1 | bit(1) << 2, !bit(0)};
+}
+// The levels over the steps.
+template <int H>
+__device__ __forceinline__ float over_steps(const float (&x)[PASS], int lane) {
+  const bool odd = lane & 1, high = lane & 2;
+  if constexpr (H == 4) {
+    const float low = in_four_add<0x4E>(four_add(x[0], x[1]), four_add(x[2], x[3]), high);
+    const float top = in_four_add<0x4E>(four_add(x[4], x[5]), four_add(x[6], x[7]), high);
+    return in_four_add<0xB1>(low, top, odd);
+  } else {
+    const float low = four_add(half_row_add(x[0], x[1]), half_row_add(x[2], x[3]));
+    const float top = four_add(half_row_add(x[4], x[5]), half_row_add(x[6], x[7]));
+    const float v = in_four_add<0x4E>(low, top, high);
+    return in_four_add<0xB1>(v, v, odd);
+  }
 }
 
 // Where a span's walk from its end with nothing carried in arrives, and the sum of its steps; the cut and the passes are
 // those of the main kernel below.
-template <typename E, int WAVES, bool GATE>
+template <typename E, int WAVES, int H, bool GATE>
 __global__ void __launch_bounds__(WAVES * 64, WAVES <= 12 ? 6 : 4)
 scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary sum, const Spans spans) {
   constexpr int ROWS = (PASS + WAVES - 1) / WAVES;
   constexpr bool ALL = PASS % WAVES == 0;
   __shared__ float2 step_in[2][PASS][kTile];             // (s, q)
-  __shared__ alignas(16) float coef[2][PASS][WAVES][2 * kHeld];
+  __shared__ alignas(16) float coef[2][PASS][WAVES][2 * H];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = blockIdx.x % (l.G * l.tiles), span = blockIdx.x / (l.G * l.tiles) + 1, g = tile / l.tiles, b = blockIdx.y;
   const int in = tile % l.tiles * kTile + lane;
@@ -76,10 +98,10 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary s
   const int d = g * l.wide + (on ? in : 0);
   const int len = clamp_length(l.lengths, b, l.T), t0 = span * spans.steps;
   const int t1 = t0 + spans.steps < l.T ? t0 + spans.steps : l.T, stop = t1 < len ? t1 : len;
-  float A2[kHeld], carry[kHeld], total = 0.0f;
+  float A2[H], carry[H], total = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    const int n = w * kHeld + i;
+  for (int i = 0; i < H; ++i) {
+    const int n = w * H + i;
     A2[i] = n < l.N ? l.A[(int64_t)d * l.N + n] * kLog2e : 0.0f;
     carry[i] = 0.0f;
   }
@@ -87,7 +109,7 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary s
   const uint32_t byte = (uint32_t)d * sizeof(E);
   const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
   Walk<const E> at_dt(l.dt, last + mine, b, byte, -PASS), at_dy(dy, last + mine, b, byte, -PASS), at_z(l.z, last + mine, b, byte, -PASS);
-  Coef<E> at_coef(l, WAVES, threadIdx.x, last, b, g);
+  Coef<E, H> at_coef(l, WAVES, threadIdx.x, last, b, g);
   struct Fetched {                                       // two passes ahead, as in the forward kernel
     uint32_t dt[ROWS], go[ROWS], z[ROWS], coef;
   } raw0, raw1;
@@ -115,7 +137,7 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary s
       total += s;
       step_in[buffer][mine + r][lane] = make_float2(s, q);
     }
-    (&coef[buffer][0][0][0])[threadIdx.x] = value<E>(x.coef);
+    if (64 * H >= 256 || threadIdx.x < WAVES * PASS * 2 * H) (&coef[buffer][0][0][0])[threadIdx.x] = value<E>(x.coef);
   };
   auto pass = [&](int k, auto parity) __attribute__((always_inline)) {                  // the k-th from the end
     constexpr int buffer = parity.value;
@@ -124,12 +146,12 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary s
     fetch(first - 2 * PASS, here);               // nothing, in front of the span
 #pragma unroll
     for (int i = PASS - 1; i >= 0; --i) {
-      float Cm[kHeld];
+      float Cm[H];
       two_by_two(i + 1);
       const float2 in_ = step_in[buffer][i][lane];
-      four(coef[buffer][i][w] + kHeld, Cm);
+      get(coef[buffer][i][w] + H, Cm);
 #pragma unroll
-      for (int j = 0; j < kHeld; ++j) carry[j] = exp2_fast(in_.x * A2[j]) * fmaf(in_.y, Cm[j], carry[j]);
+      for (int j = 0; j < H; ++j) carry[j] = exp2_fast(in_.x * A2[j]) * fmaf(in_.y, Cm[j], carry[j]);
     }
     now(carry);
     prepare(first - PASS, buffer ^ 1, there);    // a pass that no one walks, in front of it
@@ -151,7 +173,7 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary s
   totals[w * kTile + lane] = total;
   __syncthreads();
   if (!on) return;
-  *reinterpret_cast<float4*>(sum.ends + state_at(span, l.B, b, WAVES, w, l.D, d)) = make_float4(carry[0], carry[1], carry[2], carry[3]);
+  put(sum.ends + state_at(H, span, l.B, b, WAVES, w, l.D, d), carry);
   if (w == 0) {
     for (int k = 1; k < WAVES; ++k) total += totals[k * kTile + lane];
     sum.sums[((int64_t)span * l.B + b) * l.D + d] = total;
@@ -161,15 +183,16 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary s
 // The cut of the work is the forward kernel's; the passes run from the span's end.  In a pass every wave first finds a and h
 // of its states, then walks back; the sums over the states go through LDS (s1 = sum g B, s2 = sum w h A, and with a gate
 // sum C h), those over the channels through registers.
-template <typename E, int WAVES, bool GATE>
+template <typename E, int WAVES, int H, bool GATE>
 __global__ void __launch_bounds__(WAVES * 64, WAVES <= 12 ? 3 : 4)
 scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ states, const Summary sum, const Spans spans,
                      const Grads<E> o) {
-  constexpr int ROWS = (PASS + WAVES - 1) / WAVES, SUMS = GATE ? 3 : 2;
+  // sixteen waves have 128 registers each, not enough for a and h of eight steps: in two halves, the first four steps walked twice
+  constexpr int ROWS = (PASS + WAVES - 1) / WAVES, SUMS = GATE ? 3 : 2, HALVES = WAVES > 12 ? 2 : 1;
   constexpr bool ALL = PASS % WAVES == 0;
   __shared__ float2 step_in[2][PASS][kTile];             // (s, s u)
   __shared__ float step_q[2][PASS][kTile];
-  __shared__ alignas(16) float coef[2][PASS][WAVES][2 * kHeld];
+  __shared__ alignas(16) float coef[2][PASS][WAVES][2 * H];
   __shared__ float share[SUMS][WAVES][PASS][kTile];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = blockIdx.x % (l.G * l.tiles), span = blockIdx.x / (l.G * l.tiles), g = tile / l.tiles, b = blockIdx.y;
@@ -185,10 +208,10 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       if (GATE) store(o.dz.at(t, b) + d, 0.0f);
     }
 
-  float A[kHeld], A2[kHeld], carry[kHeld], dA[kHeld];
+  float A[H], A2[H], carry[H], dA[H];
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    const int n = w * kHeld + i;
+  for (int i = 0; i < H; ++i) {
+    const int n = w * H + i;
     A[i] = n < l.N ? l.A[(int64_t)d * l.N + n] : 0.0f;
     A2[i] = A[i] * kLog2e;
     carry[i] = dA[i] = 0.0f;
@@ -201,13 +224,13 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
   Walk<const E> at_u(l.u, last + mine, b, byte, -PASS), at_dt(l.dt, last + mine, b, byte, -PASS), at_dy(dy, last + mine, b, byte, -PASS), at_z(l.z, last + mine, b, byte, -PASS);
   Walk<E> at_du(o.du, last + mine, b, byte, -PASS), at_ddt(o.ddt, last + mine, b, byte, -PASS), at_dz(o.dz, last + mine, b, byte, -PASS);
-  const float* at_states = states + state_at(last / kKept, l.B, b, WAVES, w, l.D, d);
-  Coef<E> at_coef(l, WAVES, threadIdx.x, last, b, g);
+  const float* at_states = states + state_at(H, last / kKept, l.B, b, WAVES, w, l.D, d);
+  Coef<E, H> at_coef(l, WAVES, threadIdx.x, last, b, g);
   uint32_t u[ROWS], dt[ROWS], go[ROWS], z[ROWS], raw_coef;
   struct Row {                                           // of a step: what its outputs are made of
     float s, u, q, slope, gate;                          // slope: sigmoid(raw), gate: dy silu'(z)
   } row[ROWS], was[ROWS];
-  float4 kept;
+  float kept[H];
   auto fetch = [&](int first) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
@@ -219,10 +242,10 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       u[r] = a, dt[r] = b, go[r] = c, z[r] = e;
     }
     raw_coef = at_coef.fetch(stop - first);
-    kept = *reinterpret_cast<const float4*>(at_states);
+    get(at_states, kept);
     at_u.move(), at_dt.move(), at_dy.move(), at_coef.move(-1);
     if (GATE) at_z.move();
-    at_states -= (int64_t)l.B * WAVES * l.D * kHeld;
+    at_states -= (int64_t)l.B * WAVES * l.D * H;
   };
   auto prepare = [&](int first, int buffer) __attribute__((always_inline)) {
 #pragma unroll
@@ -241,7 +264,7 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       step_in[buffer][mine + r][lane] = make_float2(v.s, v.s * v.u);
       step_q[buffer][mine + r][lane] = v.q;
     }
-    (&coef[buffer][0][0][0])[threadIdx.x] = value<E>(raw_coef);
+    if (64 * H >= 256 || threadIdx.x < WAVES * PASS * 2 * H) (&coef[buffer][0][0][0])[threadIdx.x] = value<E>(raw_coef);
   };
   auto finish = [&](int first) __attribute__((always_inline)) {
     float du[ROWS], ddt[ROWS], dz[ROWS];
@@ -278,55 +301,67 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   __syncthreads();
   for (int p = passes - 1; p >= 0; --p) {
     const int first = t0 + p * PASS, buffer = p & 1;
-    float a[PASS][kHeld], h[PASS + 1][kHeld];
-    h[0][0] = kept.x, h[0][1] = kept.y, h[0][2] = kept.z, h[0][3] = kept.w;
     if (p + 1 < passes) finish(first + PASS);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) was[r] = row[r];
+    float start[H], step_sum[PASS];
+#pragma unroll
+    for (int k = 0; k < H; ++k) start[k] = kept[k];
     if (p) fetch(first - PASS);
 #pragma unroll
-    for (int i = 0; i < PASS; ++i) {
-      float Bm[kHeld];
-      two_by_two(i);
-      const float2 in_ = step_in[buffer][i][lane];
-      four(coef[buffer][i][w], Bm);
+    for (int half = HALVES - 1; half >= 0; --half) {
+      constexpr int STEPS = PASS / HALVES;
+      float a[STEPS][H], h[STEPS + 1][H];
+      auto step = [&](int i, float (&decay)[H], const float (&before)[H], float (&after)[H]) __attribute__((always_inline)) {
+        float Bm[H];
+        two_by_two(i);
+        const float2 in_ = step_in[buffer][i][lane];
+        get(coef[buffer][i][w], Bm);
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
-        a[i][k] = exp2_fast(in_.x * A2[k]);
-        h[i + 1][k] = fmaf(a[i][k], h[i][k], in_.y * Bm[k]);
+        for (int k = 0; k < H; ++k) {
+          decay[k] = exp2_fast(in_.x * A2[k]);
+          after[k] = fmaf(decay[k], before[k], in_.y * Bm[k]);
+        }
+      };
+#pragma unroll
+      for (int k = 0; k < H; ++k) h[0][k] = start[k];
+      if (half)
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+          float decay[H];
+          step(i, decay, h[0], h[0]);
+        }
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) step(half * STEPS + i, a[i], h[i], h[i + 1]);
+      // the last pass's shares have been read: a second barrier a pass instead of a second set of them, whose LDS would let
+      // eight waves on a compute unit instead of twelve (1105 us against 925 at T = 4096, B = 4, D = 4096)
+      if (half == HALVES - 1) __syncthreads();
+#pragma unroll
+      for (int j = STEPS - 1; j >= 0; --j) {
+        const int i = half * STEPS + j;
+        float Bm[H], Cm[H], s1 = 0.0f, s2 = 0.0f, plain = 0.0f, pair[H];
+        two_by_two(i + 1);
+        const float2 in_ = step_in[buffer][i][lane];
+        get(coef[buffer][i][w], Bm), get(coef[buffer][i][w] + H, Cm);
+        const float q = step_q[buffer][i][lane];
+#pragma unroll
+        for (int k = 0; k < H; ++k) {
+          const float gh = fmaf(q, Cm[k], carry[k]);
+          carry[k] = a[j][k] * gh;
+          const float through = carry[k] * h[j][k];
+          s1 = k ? fmaf(gh, Bm[k], s1) : gh * Bm[k];
+          s2 = k ? fmaf(through, A[k], s2) : through * A[k];
+          dA[k] = fmaf(through, in_.x, dA[k]);
+          if (GATE) plain = k ? fmaf(Cm[k], h[j + 1][k], plain) : Cm[k] * h[j + 1][k];
+          pair[k] = swap32_add(gh * in_.y, h[j + 1][k] * q);
+        }
+        if constexpr (H == 4) step_sum[i] = half_row_add(swap16_add(pair[0], pair[1]), swap16_add(pair[2], pair[3]));
+        else step_sum[i] = swap16_add(pair[0], pair[1]);
+        share[0][w][i][lane] = s1, share[1][w][i][lane] = s2;
+        if (GATE) share[SUMS - 1][w][i][lane] = plain;
       }
     }
-    // the last pass's shares have been read: a second barrier a pass instead of a second set of them, whose LDS would let
-    // eight waves on a compute unit instead of twelve (1105 us against 925 at T = 4096, B = 4, D = 4096)
-    __syncthreads();
-    float step_sum[PASS];
-#pragma unroll
-    for (int i = PASS - 1; i >= 0; --i) {
-      float Bm[kHeld], Cm[kHeld], s1 = 0.0f, s2 = 0.0f, plain = 0.0f, pair[kHeld];
-      two_by_two(i + 1);
-      const float2 in_ = step_in[buffer][i][lane];
-      four(coef[buffer][i][w], Bm), four(coef[buffer][i][w] + kHeld, Cm);
-      const float q = step_q[buffer][i][lane];
-#pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
-        const float gh = fmaf(q, Cm[k], carry[k]);
-        carry[k] = a[i][k] * gh;
-        const float through = carry[k] * h[i][k];
-        s1 = k ? fmaf(gh, Bm[k], s1) : gh * Bm[k];
-        s2 = k ? fmaf(through, A[k], s2) : through * A[k];
-        dA[k] = fmaf(through, in_.x, dA[k]);
-        if (GATE) plain = k ? fmaf(Cm[k], h[i + 1][k], plain) : Cm[k] * h[i + 1][k];
-        pair[k] = swap32_add(gh * in_.y, h[i + 1][k] * q);
-      }
-      step_sum[i] = half_row_add(swap16_add(pair[0], pair[1]), swap16_add(pair[2], pair[3]));
-      share[0][w][i][lane] = s1, share[1][w][i][lane] = s2;
-      if (GATE) share[SUMS - 1][w][i][lane] = plain;
-    }
-    const bool odd = lane & 1, high = lane & 2;
-    const float low = in_four_add<0x4E>(four_add(step_sum[0], step_sum[1]), four_add(step_sum[2], step_sum[3]), high);
-    const float top = in_four_add<0x4E>(four_add(step_sum[4], step_sum[5]), four_add(step_sum[6], step_sum[7]), high);
-    const float part = in_four_add<0xB1>(low, top, odd);
-    at_bc[lane] = part;
+    at_bc[lane] = over_steps<H>(step_sum, lane);
     at_bc -= WAVES * 64;
     if (p) prepare(first - PASS, buffer ^ 1);
     __syncthreads();
@@ -345,11 +380,11 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
     for (int k = 1; k < WAVES; ++k) dskip += totals[k * kTile + lane], dbias += totals[(WAVES + k) * kTile + lane];
     o.dskip[part * l.D + d] = dskip, o.ddt_bias[part * l.D + d] = dbias;
   }
-  *reinterpret_cast<float4*>(o.dA + state_at(span, l.B, b, WAVES, w, l.D, d)) = make_float4(dA[0], dA[1], dA[2], dA[3]);
+  put(o.dA + state_at(H, span, l.B, b, WAVES, w, l.D, d), dA);
   if (o.dh0 && span == 0)
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i)
-      if (w * kHeld + i < l.N) o.dh0[((int64_t)b * l.D + d) * l.N + w * kHeld + i] = carry[i];
+    for (int i = 0; i < H; ++i)
+      if (w * H + i < l.N) o.dh0[((int64_t)b * l.D + d) * l.N + w * H + i] = carry[i];
 }
 
 // The sums over parts.  The first workgroups have dB and dC, the tiles' parts in the tiles' order, a thread the place of a lane
@@ -359,7 +394,7 @@ struct Joined {
   void *dBm, *dCm;
   float *dA, *dskip, *ddt_bias;
   int64_t places;                              // of dB and dC: the parts of one tile
-  int first_groups, waves, parts;              // workgroups for dB and dC; waves of the main kernel; samples times spans
+  int first_groups, waves, held, parts;        // workgroups for dB and dC; waves of the main kernel and their states; samples times spans
 };
 template <typename E>
 __global__ void __launch_bounds__(256)
@@ -367,21 +402,22 @@ join_kernel(const Layer<E> l, const Grads<E> o, const Joined to) {
   if ((int)blockIdx.x < to.first_groups) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= to.places) return;
-    const int passes = (l.T + PASS - 1) / PASS, product = product_of_lane((int)(i & 63));
-    const int w = (int)(i / 64 % to.waves), t = (int)(i / 64 / to.waves % passes) * PASS + product / 8;
+    const int passes = (l.T + PASS - 1) / PASS;
+    const Product product = product_of_lane((int)(i & 63), to.held);
+    const int w = (int)(i / 64 % to.waves), t = (int)(i / 64 / to.waves % passes) * PASS + product.step;
     const int64_t bg = i / 64 / to.waves / passes;
-    const int g = (int)(bg % l.G), b = (int)(bg / l.G), n = w * kHeld + product / 2 % kHeld;
-    if (t >= l.T || n >= l.N) return;
+    const int g = (int)(bg % l.G), b = (int)(bg / l.G), n = w * to.held + product.state;
+    if (t >= l.T || n >= l.N || !product.first) return;
     float sum = 0.0f;
     if (t < clamp_length(l.lengths, b, l.T)) {
 #pragma unroll 8
       for (int k = 0; k < l.tiles; ++k) sum += o.bc[k * to.places + i];
     }
-    store(static_cast<E*>(product & 1 ? to.dCm : to.dBm) + (((int64_t)t * l.B + b) * l.G + g) * l.N + n, sum);
+    store(static_cast<E*>(product.of_C ? to.dCm : to.dBm) + (((int64_t)t * l.B + b) * l.G + g) * l.N + n, sum);
     return;
   }
   __shared__ float quarter[4][64];
-  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, of_dA = to.waves * kHeld * l.D;
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, of_dA = to.waves * to.held * l.D;
   const int i = ((int)blockIdx.x - to.first_groups) * 64 + lane, all = of_dA + 2 * l.D;
   const float* from = i < of_dA ? o.dA + i : i < of_dA + l.D ? o.dskip + (i - of_dA) : o.ddt_bias + (i - of_dA - l.D);
   const int64_t step = i < of_dA ? of_dA : l.D;
@@ -395,7 +431,7 @@ join_kernel(const Layer<E> l, const Grads<E> o, const Joined to) {
   if (q || i >= all) return;
   sum = (quarter[0][lane] + quarter[1][lane]) + (quarter[2][lane] + quarter[3][lane]);
   if (i < of_dA) {
-    const int w = i / (kHeld * l.D), d = i / kHeld % l.D, n = w * kHeld + i % kHeld;
+    const int w = i / (to.held * l.D), d = i / to.held % l.D, n = w * to.held + i % to.held;
     if (n < l.N) to.dA[(int64_t)d * l.N + n] = sum;
   } else if (i < of_dA + l.D) {
     if (to.dskip) to.dskip[i - of_dA] = sum;
@@ -413,9 +449,9 @@ struct Scratch {
     const int64_t waves = waves_of(N), tiles = bppsa_ceil_div(D / G, kTile), parts = (int64_t)spans.count * B * D;
     bc_floats = (int64_t)B * G * ((T + PASS - 1) / PASS) * waves * 64;
     Arena take;
-    ends = take(spans.count > 1 ? parts * waves * kHeld : 0), sums = take(spans.count > 1 ? parts : 0);
+    ends = take(spans.count > 1 ? parts * padded_of(N) : 0), sums = take(spans.count > 1 ? parts : 0);
     bc = take(tiles * bc_floats);
-    dA = take(parts * waves * kHeld), dskip = take(parts), ddt_bias = take(parts);
+    dA = take(parts * padded_of(N)), dskip = take(parts), ddt_bias = take(parts);
     bytes = take.at;
   }
 };
@@ -445,22 +481,22 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
                      part(at.dskip), part(at.ddt_bias), grads->dh0};
     const Summary sum{part(at.ends), part(at.sums)};
     const Rows<const E> out = rows_of<const E>(*dy);
-    auto walk = [&](auto waves_, auto gate) {
-      constexpr int W = waves_.value;
+    auto walk = [&](auto waves_, auto held, auto gate) {
+      constexpr int W = waves_.value, H = held.value;
       constexpr bool GATE = gate.value;
       if (at.spans.count > 1)
-        scan_backward_summary_kernel<E, W, GATE><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
+        scan_backward_summary_kernel<E, W, H, GATE><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
             l, out, sum, at.spans);
-      scan_backward_kernel<E, W, GATE><<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(
+      scan_backward_kernel<E, W, H, GATE><<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(
           l, out, static_cast<const float*>(states), sum, at.spans, o);
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     };
-    BPPSA_TRY(by_waves(waves, [&](auto w) { return l.z.data ? walk(w, std::true_type{}) : walk(w, std::false_type{}); }));
+    BPPSA_TRY(by_states(l.N, [&](auto w, auto h) { return l.z.data ? walk(w, h, std::true_type{}) : walk(w, h, std::false_type{}); }));
     const int64_t first = (at.bc_floats + 255) / 256;
-    const Joined to{grads->dBm, grads->dCm, grads->dA, grads->dskip, grads->ddt_bias, at.bc_floats, (int)first, waves,
+    const Joined to{grads->dBm, grads->dCm, grads->dA, grads->dskip, grads->ddt_bias, at.bc_floats, (int)first, waves, held_of(l.N),
                     at.spans.count * l.B};
-    join_kernel<E><<<(unsigned)(first + ((waves * kHeld + 2) * (int64_t)l.D + 63) / 64), 256, 0, s>>>(l, o, to);
+    join_kernel<E><<<(unsigned)(first + ((padded_of(l.N) + 2) * (int64_t)l.D + 63) / 64), 256, 0, s>>>(l, o, to);
     BPPSA_CHECK_LAUNCH();
     return BPPSA_OK;
   });

@@ -1,7 +1,7 @@
 // What the selective scan's kernels share: how the work is cut, and the arrays between launches.
 //
-// A workgroup takes 64 channels of one group, one a lane, of one sample.  Its waves split the states: wave w holds states
-// 4 w .. 4 w + 3 of all 64 channels.  What the waves share goes through LDS: a step's size, made once for a channel, the
+// A workgroup takes 64 channels of one group, one a lane, of one sample.  Its waves split the states: wave w holds H states of all
+// 64 channels, from H w on.  What the waves share goes through LDS: a step's size, made once for a channel, the
 // sums over the states, and Bm and Cm, which are the same number for a whole wave.  (Those were scalar operands first, of
 // no cost to the vector unit; but a scalar load can only be waited for with all others that are out, at every second step,
 // and 32 of them at a time left so few scalar registers that a tenth of the vector instructions moved others out of the
@@ -13,7 +13,6 @@
 namespace ssm {
 
 constexpr int kTile = 64;        // channels of a workgroup, one a lane
-constexpr int kHeld = 4;         // states of a channel that a wave holds
 constexpr int kKept = 8;         // steps between two states kept for the backward pass
 
 template <typename E>
@@ -32,45 +31,61 @@ Layer<E> layer_of(const bppsa_ssm& l) {
                   bppsa_ceil_div(wide, kTile)};
 }
 
-// Waves of a workgroup for N states: the next of 1, 2, 4, 6, 8, 12, 16.
+// The waves of a workgroup for N states and how many of them each holds: four, but two where there are few, or as many rows as
+// eight would be a wave's to prepare (at N = 8 two waves of four states took longer than N = 16 does).
+static inline int held_of(int N) { return N <= 8 ? 2 : 4; }
 static inline int waves_of(int N) {
-  const int need = (N + kHeld - 1) / kHeld;
-  for (int w : {1, 2, 4, 6, 8, 12})
-    if (need <= w) return w;
-  return 16;
+  return N <= 4 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : N <= 48 ? 12 : 16;
 }
+static inline int padded_of(int N) { return waves_of(N) * held_of(N); }
 template <typename F>
-bppsa_status by_waves(int waves, F&& f) {
-  switch (waves) {
-    case 1: return f(std::integral_constant<int, 1>{});
-    case 2: return f(std::integral_constant<int, 2>{});
-    case 4: return f(std::integral_constant<int, 4>{});
-    case 6: return f(std::integral_constant<int, 6>{});
-    case 8: return f(std::integral_constant<int, 8>{});
-    case 12: return f(std::integral_constant<int, 12>{});
-    default: return f(std::integral_constant<int, 16>{});
-  }
+bppsa_status by_states(int N, F&& f) {
+  typedef std::integral_constant<int, 2> Two;
+  typedef std::integral_constant<int, 4> Four;
+  if (N <= 4) return f(std::integral_constant<int, 2>{}, Two{});
+  if (N <= 8) return f(std::integral_constant<int, 4>{}, Two{});
+  if (N <= 16) return f(std::integral_constant<int, 4>{}, Four{});
+  if (N <= 32) return f(std::integral_constant<int, 8>{}, Four{});
+  if (N <= 48) return f(std::integral_constant<int, 12>{}, Four{});
+  return f(std::integral_constant<int, 16>{}, Four{});
 }
 
-// Offsets of an array of states, float4 a channel and wave: [first][b][wave][d][4].
-__host__ __device__ __forceinline__ int64_t state_at(int64_t first, int B, int b, int waves, int w, int D, int d) {
-  return (((first * B + b) * waves + w) * D + d) * kHeld;
+// Offsets of an array of states, `held` floats a channel and wave: [first][b][wave][d][held].
+__host__ __device__ __forceinline__ int64_t state_at(int held, int64_t first, int B, int b, int waves, int w, int D, int d) {
+  return (((first * B + b) * waves + w) * D + d) * held;
+}
+template <int H>
+struct alignas(4 * H) States {
+  float v[H];
+};
+template <int H>
+__device__ __forceinline__ void get(const float* from, float (&v)[H]) {
+  const States<H> x = *reinterpret_cast<const States<H>*>(from);
+#pragma unroll
+  for (int i = 0; i < H; ++i) v[i] = x.v[i];
+}
+template <int H>
+__device__ __forceinline__ void put(float* to, const float (&v)[H]) {
+  States<H> x;
+#pragma unroll
+  for (int i = 0; i < H; ++i) x.v[i] = v[i];
+  *reinterpret_cast<States<H>*>(to) = x;
 }
 
-// Bm and Cm of a pass of kKept steps, for all waves of a workgroup: [step][wave][four Bm, four Cm], one value a thread.
-// A thread fetches its value of a pass ahead, as an element, and leaves it in LDS as a float; a wave reads its eight of a
-// step from one place, 16 bytes an access.  Zero beyond the states there are and behind a sample's end.
-template <typename E>
+// Bm and Cm of a pass of kKept steps, for all waves of a workgroup: [step][wave][H of Bm, H of Cm], one value a thread.
+// A thread fetches its value of a pass ahead, as an element, and leaves it in LDS as a float; a wave reads those of its
+// states of a step from one place, all at once.  Zero beyond the states there are and behind a sample's end.
+template <typename E, int H>
 struct Coef {
   uint64_t at;
   int64_t step;                    // of a pass
   int row;                         // of the pass
   bool real;
   __device__ __forceinline__ Coef(const Layer<E>& l, int waves, int thread, int first, int b, int g) {
-    const int k = thread % (2 * kHeld), n = thread / (2 * kHeld) % waves * kHeld + k % kHeld;
-    row = thread / (2 * kHeld) / waves, real = n < l.N;
-    const Rows<const E> r{k < kHeld ? l.Bm.data : l.Cm.data, k < kHeld ? l.Bm.st : l.Cm.st, k < kHeld ? l.Bm.sb : l.Cm.sb};
-    at = (uint64_t)(r.at(first + row, b) + g * l.N + (real ? n : 0));
+    const int k = thread % (2 * H), n = thread / (2 * H) % waves * H + k % H;
+    row = thread / (2 * H) / waves, real = n < l.N && row < kKept;
+    const Rows<const E> r{k < H ? l.Bm.data : l.Cm.data, k < H ? l.Bm.st : l.Cm.st, k < H ? l.Bm.sb : l.Cm.sb};
+    at = (uint64_t)(r.at(first + (row < kKept ? row : 0), b) + g * l.N + (real ? n : 0));
     step = r.st * (int64_t)sizeof(E) * kKept;
   }
   __device__ __forceinline__ uint32_t fetch(int left) const { return real && row < left ? bits_at<E>(at) : 0; }   // left: steps of the pass that there are
@@ -89,10 +104,10 @@ __device__ __forceinline__ void two_by_two(int i) {
 }
 // The states are computed here and not later: nothing but the next pass needs them, and the compiler keeps the operands of
 // several passes instead.
-__device__ __forceinline__ void now(float (&h)[kHeld]) { asm volatile("" : "+v"(h[0]), "+v"(h[1]), "+v"(h[2]), "+v"(h[3])); }
-__device__ __forceinline__ void four(const float* from, float (&v)[kHeld]) {
-  const float4 x = *reinterpret_cast<const float4*>(from);
-  v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+template <int H>
+__device__ __forceinline__ void now(float (&h)[H]) {
+#pragma unroll
+  for (int i = 0; i < H; ++i) asm volatile("" : "+v"(h[i]));
 }
 
 // A long sequence with few channels is cut into spans, each scanned by workgroups of its own.  A first launch scans each
@@ -103,28 +118,28 @@ struct Spans {
   int count, steps;
 };
 struct Summary {
-  float *ends, *sums;              // [span][b][wave][d][4], [span][b][d]
+  float *ends, *sums;              // [span][b][wave][d][held], [span][b][d]
 };
 
 // Carries h over `count` spans, from `first` on, one after the other by `step`.  Eight of them are asked for together: one at
 // a time, the 47 of T = 30000 took some 20 us.
+template <int H>
 __device__ __forceinline__ void join_spans(const Summary& sum, int first, int step, int count, int B, int b, int waves, int w,
-                                           int D, int d, const float (&A2)[kHeld], float (&h)[kHeld]) {
+                                           int D, int d, const float (&A2)[H], float (&h)[H]) {
   constexpr int AHEAD = 8;
   for (int k = 0; k < count; k += AHEAD) {
-    float4 end[AHEAD];
-    float s[AHEAD];
+    float end[AHEAD][H], s[AHEAD];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       const int at = first + step * (k + j < count ? k + j : count - 1);
-      end[j] = *reinterpret_cast<const float4*>(sum.ends + state_at(at, B, b, waves, w, D, d));
+      get(sum.ends + state_at(H, at, B, b, waves, w, D, d), end[j]);
       s[j] = sum.sums[((int64_t)at * B + b) * D + d];
     }
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       if (k + j >= count) break;
-      h[0] = fmaf(exp2_fast(A2[0] * s[j]), h[0], end[j].x), h[1] = fmaf(exp2_fast(A2[1] * s[j]), h[1], end[j].y);
-      h[2] = fmaf(exp2_fast(A2[2] * s[j]), h[2], end[j].z), h[3] = fmaf(exp2_fast(A2[3] * s[j]), h[3], end[j].w);
+#pragma unroll
+      for (int i = 0; i < H; ++i) h[i] = fmaf(exp2_fast(A2[i] * s[j]), h[i], end[j][i]);
     }
   }
 }
