@@ -61,14 +61,26 @@ __device__ __forceinline__ void input(const Conv<E>& c, int t, int b, int d, int
   for (int i = 0; i < V; ++i) x[i] = (float)s.v[i];
 }
 
+// Which channels and which span a thread has: threads are counted through the channels of a span and on to the next span, so
+// that a row of few or odd channels leaves no lanes idle.
+struct Place {
+  int d, span;
+  bool real;
+};
+__device__ __forceinline__ Place place_of(int64_t thread, int D, int V, int spans) {
+  const int across = (D + V - 1) / V, first = (int)(thread % across) * V;
+  const int64_t span = thread / across;
+  return Place{first + V <= D ? first : D - V, (int)(span < spans ? span : 0), span < spans};
+}
+
 template <typename E, int W, int V>
 __global__ void __launch_bounds__(64)
 conv_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state_last) {
-  const int first = (blockIdx.x * 64 + threadIdx.x) * V, d = first + V <= c.D ? first : c.D - V;
-  const int b = blockIdx.y, t0 = blockIdx.z * c.span;
-  if (first >= c.D) return;
+  const Place at = place_of((int64_t)blockIdx.x * 64 + threadIdx.x, c.D, V, (c.T + c.span - 1) / c.span);
+  const int d = at.d, b = blockIdx.y, t0 = at.span * c.span;
+  if (!at.real) return;
   const int len = clamp_length(c.lengths, b, c.T), t1 = t0 + c.span < c.T ? t0 + c.span : c.T, stop = t1 < len ? t1 : len;
-  if (state_last && blockIdx.z == 0)
+  if (state_last && t0 == 0)
 #pragma unroll
     for (int k = 0; k + 1 < W; ++k) {
       float x[V];
@@ -80,13 +92,14 @@ conv_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state_last) {
     const Taps<V, W> taps(c, d);
 #pragma unroll
     for (int k = 1; k < W; ++k) input<E, W, V>(c, t0 - W + k, b, d, len, seen[k]);
+    const E* from = c.x.at(t0, b) + d;
+    E* to = y.at(t0, b) + d;
     for (int t = t0; t < stop; t += kAhead) {
       Some<E, V> x[kAhead];
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) x[j] = load_some<E, V>(c.x.at(t + j < stop ? t + j : stop - 1, b) + d);
+      for (int j = 0; j < kAhead; ++j) x[j] = load_some<E, V>(from + (t + j < stop ? j : stop - 1 - t) * c.x.st);
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        if (t + j >= stop) break;
         float out[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -96,8 +109,9 @@ conv_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state_last) {
           const float p = taps.sum(seen, i);
           out[i] = c.silu ? p * sigmoid<E>(p) : p;
         }
-        store_some<E, V>(y.at(t + j, b) + d, out);
+        if (t + j < stop) store_some<E, V>(to + j * y.st, out);
       }
+      from += kAhead * c.x.st, to += kAhead * y.st;
     }
   }
   const float zero[V] = {};
@@ -232,9 +246,9 @@ conv_step_kernel(const Conv<E> c, Rows<E> y, E* __restrict__ state, int slots_in
 
 // Steps of a span: 64, or fewer, to 8, while the device would have less than `waves` a SIMD; every span reads W-1 rows twice.
 // Forward at T = 4096, B = 4, D = 4096: 60.8 us in spans of 32 (four waves), 69.5 in spans of 64.
-int span_of(int T, int64_t waves_a_step, int waves) {
+int span_of(int T, int64_t threads_a_step, int waves) {
   int span = 64;
-  while (span > 8 && waves_a_step * bppsa_ceil_div(T, span) < (int64_t)bppsa_compute_units() * 4 * waves) span /= 2;
+  while (span > 8 && threads_a_step * bppsa_ceil_div(T, span) < (int64_t)bppsa_compute_units() * 256 * waves) span /= 2;
   return span;
 }
 // Channels of a thread.
@@ -247,7 +261,7 @@ int backward_width(int D, int type) {
   const int V = type == BPPSA_F32 ? kNarrow<float> : kNarrow<bf16_t>;
   return D >= V ? V : 1;
 }
-int backward_span(int T, int B, int D, int type) { return span_of(T, (int64_t)B * waves_for(D, backward_width(D, type)), 2); }
+int backward_span(int T, int B, int D, int type) { return span_of(T, (int64_t)B * bppsa_ceil_div(D, backward_width(D, type)), 2); }
 
 template <typename F>
 bppsa_status by_width(int W, F&& f) {
@@ -261,7 +275,7 @@ bppsa_status by_width(int W, F&& f) {
 bppsa_status check_conv(const bppsa_conv* c) {
   if (!c || c->T < 1 || c->B < 1 || c->D < 1 || c->W < 1 || !c->x.data || !c->weight) return BPPSA_EINVAL;
   if (c->W < 2 || c->W > BPPSA_SSM_MAX_W || c->type < BPPSA_F32 || c->type > BPPSA_F16) return BPPSA_EUNSUPPORTED;
-  if (bppsa_mul_overflows(c->T, c->B, c->D, 2) || c->B > 65535 || c->T > 65535 * 8) return BPPSA_EOVERFLOW;
+  if (bppsa_mul_overflows(c->T, c->B, c->D, 2) || c->B > 65535 || c->T > 65535 * 64 || c->D > 1 << 24) return BPPSA_EOVERFLOW;
   return BPPSA_OK;
 }
 
@@ -275,8 +289,9 @@ extern "C" bppsa_status bppsa_ssm_conv(const bppsa_conv* conv, const bppsa_rows*
     return by_width(conv->W, [&](auto w) {
       auto run = [&](auto v) {
         constexpr int V = v.value;
-        const int wide = waves_for(conv->D, V), span = span_of(conv->T, (int64_t)conv->B * wide, 4);
-        conv_kernel<E, w.value, V><<<dim3(wide, conv->B, bppsa_ceil_div(conv->T, span)), 64, 0, (hipStream_t)stream>>>(
+        const int across = bppsa_ceil_div(conv->D, V), span = span_of(conv->T, (int64_t)conv->B * across, 4);
+        const int64_t threads = (int64_t)across * bppsa_ceil_div(conv->T, span);
+        conv_kernel<E, w.value, V><<<dim3((unsigned)((threads + 63) / 64), conv->B), 64, 0, (hipStream_t)stream>>>(
             conv_of<E>(*conv, span), rows_of<E>(*y), static_cast<E*>(state_last));
         BPPSA_CHECK_LAUNCH();
         return BPPSA_OK;

@@ -10,6 +10,7 @@ from .binding import _check, _lib, _ptr, _stream
 
 BLOCK = 256                        # BPPSA_ADAMW_BLOCK
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_f32 = torch.float32
 
 _c_int, _c_void_p, _c_double, _c_int64 = ctypes.c_int, ctypes.c_void_p, ctypes.c_double, ctypes.c_int64
 _lib.bppsa_adamw_pieces.restype = _c_int64
@@ -39,6 +40,8 @@ class AdamW:
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(params)
         if len(decay) != len(params) or (copies is not None and len(copies) != len(params)):
             raise ValueError("weight_decay and copies need one entry for each parameter")
+        if not isinstance(params[0], torch.Tensor):
+            raise ValueError("parameters must be float32 tensors")
         if not isinstance(grads[0], torch.Tensor) or grads[0].dtype not in _TYPES:
             raise ValueError("gradients must be float32, bfloat16 or float16 tensors")
         self.params, self.grads, self.copies = params, grads, None if copies is None else list(copies)
@@ -56,19 +59,23 @@ class AdamW:
             raise ValueError("state must hold %s for each parameter" % ", ".join(names))
         self.state = {name: list(x) for name, x in state.items()}
         device, self._grad_type, rows, lengths = params[0].device, _TYPES[grads[0].dtype], [], []
+        kinds = [("params", params, _f32), ("grads", grads, grads[0].dtype)] + [("state[%r]" % name, self.state[name], t) for name, t in names.items()]
+        if copies is not None:
+            kinds.append(("copies", self.copies, torch.bfloat16))
+        pack, blank = struct.Struct("@7Pqd").pack, () if state_bits == 8 else (0, 0)
         for k, p in enumerate(params):
             n = p.numel() if isinstance(p, torch.Tensor) else 0
-            known = [("params[%d]" % k, p, torch.float32, n), ("grads[%d]" % k, grads[k], grads[0].dtype, n)]
-            known += [("state[%r][%d]" % (name, k), self.state[name][k], t, size(p, name) if n else 0) for name, t in names.items()]
-            if copies is not None:
-                known.append(("copies[%d]" % k, copies[k], torch.bfloat16, n))
-            at = {}
-            for name, x, t, count in known:
-                at[name.split("[")[0] if "state" not in name else name.split("'")[1]] = _ptr(x, t, name)
+            counts = (n, n, n, n, -(-n // BLOCK), -(-n // BLOCK), n) if state_bits == 8 else (n, n, n, n, n)
+            at = []
+            for (name, of, t), count in zip(kinds, counts):
+                x = of[k]
+                if type(x) is not torch.Tensor or x.dtype is not t or not x.is_cuda or not x.is_contiguous():
+                    _ptr(x, t, "%s[%d]" % (name, k))       # says what is wrong, if anything is
                 if x is None or x.numel() != count or x.device != device:
-                    raise ValueError("%s must have %d values on %s" % (name, count, device))
-            rows.append(struct.pack("@7Pqd", at["params"], at["grads"], at["m"], at["v"], at.get("m_scale", 0),
-                                    at.get("v_scale", 0), at.get("copies", 0), n, float(decay[k])))
+                    raise ValueError("%s[%d] must have %d values on %s" % (name, k, count, device))
+                at.append(x.data_ptr())
+            copy = at.pop() if copies is not None else 0
+            rows.append(pack(*at, *blank, copy, n, float(decay[k])))
             lengths.append(n)
         n = (ctypes.c_int64 * len(params))(*lengths)
         self._n_pieces = int(_lib.bppsa_adamw_pieces(len(params), n, None))

@@ -307,9 +307,7 @@ def ssm_conv_backward(dy, x, weight, bias=None, silu=True, state0=None, lengths=
                       stream=None):
     """bppsa_ssm_conv_backward: the gradients of sum(y dy), as SsmConvGrads; dstate0 [B, W-1, D] is filled if given."""
     conv, (T, B, D, W) = _conv(x, weight, bias, silu, state0, lengths)
-    dx = torch.empty_like(x)
-    dweight = torch.empty((D, W), dtype=torch.float32, device=x.device)
-    dbias = None if bias is None else torch.empty((D,), dtype=torch.float32, device=x.device)
+    dx, dweight, dbias = torch.empty_like(x), torch.empty_like(weight), None if bias is None else torch.empty_like(bias)
     _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_conv_backward_workspace_bytes(T, B, D, W), x.device, stream)
     _check(_lib.bppsa_ssm_conv_backward(conv, _pack_rows(*_rows(dy, x.shape, x.dtype, "dy")),
                                         _pack_rows(*_rows(dx, x.shape, x.dtype, "dx")), dweight.data_ptr(),
