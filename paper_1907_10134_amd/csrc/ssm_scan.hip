@@ -161,13 +161,14 @@ scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __re
   }
 }
 
+constexpr int kWavesWanted = 6;  // of a SIMD, by spans: as many as fit
 // The workspace of a forward call: the spans' summaries.
 struct Scratch {
   size_t ends, sums, bytes;
-  Spans spans;
-  Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G, 6)) {
+  Scratch(int T, int B, int D, int N, int G) {
     Arena take;
-    const int64_t parts = spans.count > 1 ? (int64_t)spans.count * B * D : 0;
+    const int most = most_spans(T, B, D, N, G, kWavesWanted);
+    const int64_t parts = most > 1 ? (int64_t)most * B * D : 0;
     ends = take(parts * padded_of(N)), sums = take(parts);
     bytes = take.at;
   }
@@ -260,6 +261,7 @@ extern "C" bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows*
   if (!y || !writable(*y, layer->T, layer->B) || (h_last && h_last == layer->h0)) return BPPSA_EINVAL;
   const Scratch at(layer->T, layer->B, layer->D, layer->N, layer->G);
   BPPSA_TRY(check_workspace(workspace, workspace_bytes, at.bytes));
+  const Spans spans = spans_of(layer->T, layer->B, layer->D, layer->N, layer->G, kWavesWanted, layer->lengths != nullptr);
   const hipStream_t s = (hipStream_t)stream;
   return by_type(layer->type, [&](auto e) {
     using E = decltype(e);
@@ -268,12 +270,12 @@ extern "C" bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows*
     const Summary sum{part(at.ends), part(at.sums)};
     return by_states(l.N, [&](auto waves, auto held) {
       constexpr int W = waves.value, H = held.value;
-      if (at.spans.count > 1)                  // nothing asks for the last span's summary
-        scan_kernel<E, W, H, true, false><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
-            l, Rows<E>{}, nullptr, nullptr, sum, at.spans);
+      if (spans.count > 1)                  // nothing asks for the last span's summary
+        scan_kernel<E, W, H, true, false><<<dim3(l.G * l.tiles * (spans.count - 1), l.B), W * 64, 0, s>>>(
+            l, Rows<E>{}, nullptr, nullptr, sum, spans);
       const auto kernel = l.z.data ? scan_kernel<E, W, H, false, true> : scan_kernel<E, W, H, false, false>;
-      kernel<<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(l, rows_of<E>(*y), h_last,
-                                                                        static_cast<float*>(states), sum, at.spans);
+      kernel<<<dim3(l.G * l.tiles * spans.count, l.B), W * 64, 0, s>>>(l, rows_of<E>(*y), h_last,
+                                                                        static_cast<float*>(states), sum, spans);
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     });

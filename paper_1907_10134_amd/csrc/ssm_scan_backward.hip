@@ -441,15 +441,17 @@ join_kernel(const Layer<E> l, const Grads<E> o, const Joined to) {
 }
 
 // bc: parts of dB and dC [tile of the group][b][g][pass][w][64 lanes]; dA, dskip, ddt_bias: one part a span and sample.
+constexpr int kWavesWanted = 8;    // of a SIMD, by spans: T = 4096, B = 4, D = 4096 at 3, 4, 6, 8, 12: 952, 1038, 955, 925, 909 us and
+                                   // 265, 234, 234, 235, 248 for the summaries
 struct Scratch {
-  Spans spans;
   size_t ends, sums, bc, dA, dskip, ddt_bias, bytes;
   int64_t bc_floats;                           // of one tile
-  Scratch(int T, int B, int D, int N, int G) : spans(spans_of(T, B, D, N, G, 8)) {
-    const int64_t waves = waves_of(N), tiles = bppsa_ceil_div(D / G, kTile), parts = (int64_t)spans.count * B * D;
+  Scratch(int T, int B, int D, int N, int G) {
+    const int most = most_spans(T, B, D, N, G, kWavesWanted);
+    const int64_t waves = waves_of(N), tiles = bppsa_ceil_div(D / G, kTile), parts = (int64_t)most * B * D;
     bc_floats = (int64_t)B * G * ((T + PASS - 1) / PASS) * waves * 64;
     Arena take;
-    ends = take(spans.count > 1 ? parts * padded_of(N) : 0), sums = take(spans.count > 1 ? parts : 0);
+    ends = take(most > 1 ? parts * padded_of(N) : 0), sums = take(most > 1 ? parts : 0);
     bc = take(tiles * bc_floats);
     dA = take(parts * padded_of(N)), dskip = take(parts), ddt_bias = take(parts);
     bytes = take.at;
@@ -471,6 +473,7 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
   if (!layer->z.data != !grads->dz.data || (layer->z.data && !writable(grads->dz, layer->T, layer->B))) return BPPSA_EINVAL;
   const Scratch at(layer->T, layer->B, layer->D, layer->N, layer->G);
   BPPSA_TRY(check_workspace(workspace, workspace_bytes, at.bytes));
+  const Spans spans = spans_of(layer->T, layer->B, layer->D, layer->N, layer->G, kWavesWanted, layer->lengths != nullptr);
   const hipStream_t s = (hipStream_t)stream;
   return by_type(layer->type, [&](auto e) {
     using E = decltype(e);
@@ -484,18 +487,18 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
     auto walk = [&](auto waves_, auto held, auto gate) {
       constexpr int W = waves_.value, H = held.value;
       constexpr bool GATE = gate.value;
-      if (at.spans.count > 1)
-        scan_backward_summary_kernel<E, W, H, GATE><<<dim3(l.G * l.tiles * (at.spans.count - 1), l.B), W * 64, 0, s>>>(
-            l, out, sum, at.spans);
-      scan_backward_kernel<E, W, H, GATE><<<dim3(l.G * l.tiles * at.spans.count, l.B), W * 64, 0, s>>>(
-          l, out, static_cast<const float*>(states), sum, at.spans, o);
+      if (spans.count > 1)
+        scan_backward_summary_kernel<E, W, H, GATE><<<dim3(l.G * l.tiles * (spans.count - 1), l.B), W * 64, 0, s>>>(
+            l, out, sum, spans);
+      scan_backward_kernel<E, W, H, GATE><<<dim3(l.G * l.tiles * spans.count, l.B), W * 64, 0, s>>>(
+          l, out, static_cast<const float*>(states), sum, spans, o);
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     };
     BPPSA_TRY(by_states(l.N, [&](auto w, auto h) { return l.z.data ? walk(w, h, std::true_type{}) : walk(w, h, std::false_type{}); }));
     const int64_t first = (at.bc_floats + 255) / 256;
     const Joined to{grads->dBm, grads->dCm, grads->dA, grads->dskip, grads->ddt_bias, at.bc_floats, (int)first, waves, held_of(l.N),
-                    at.spans.count * l.B};
+                    spans.count * l.B};
     join_kernel<E><<<(unsigned)(first + ((padded_of(l.N) + 2) * (int64_t)l.D + 63) / 64), 256, 0, s>>>(l, o, to);
     BPPSA_CHECK_LAUNCH();
     return BPPSA_OK;
