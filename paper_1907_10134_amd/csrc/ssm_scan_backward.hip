@@ -441,13 +441,18 @@ join_kernel(const Layer<E> l, const Grads<E> o, const Joined to) {
 }
 
 // bc: parts of dB and dC [tile of the group][b][g][pass][w][64 lanes]; dA, dskip, ddt_bias: one part a span and sample.
-constexpr int kWavesWanted = 8;    // of a SIMD, by spans: T = 4096, B = 4, D = 4096 at 3, 4, 6, 8, 12: 952, 1038, 955, 925, 909 us and
-                                   // 265, 234, 234, 235, 248 for the summaries
+// Three waves fit a SIMD.  Where that is twelve spans and more, so many at a time do, each with few spans to join (T = 4096, B
+// = 16, D = 64: 122 us, 146 with eight waves a SIMD; T = 2000, B = 4, D = 400: 95 and 107); with fewer, rounds of shorter
+// spans (T = 4096, B = 4, D = 4096 with summaries: 1217 us in three spans, 1160 in eight).
+int waves_wanted(int D, int N, int G, int B) {
+  const int64_t have = (int64_t)G * bppsa_ceil_div(D / G, kTile) * B * waves_of(N);
+  return bppsa_compute_units() * 4 * 3 / have >= 12 ? 3 : 8;
+}
 struct Scratch {
   size_t ends, sums, bc, dA, dskip, ddt_bias, bytes;
   int64_t bc_floats;                           // of one tile
   Scratch(int T, int B, int D, int N, int G) {
-    const int most = most_spans(T, B, D, N, G, kWavesWanted);
+    const int most = most_spans(T, B, D, N, G, waves_wanted(D, N, G, B));
     const int64_t waves = waves_of(N), tiles = bppsa_ceil_div(D / G, kTile), parts = (int64_t)most * B * D;
     bc_floats = (int64_t)B * G * ((T + PASS - 1) / PASS) * waves * 64;
     Arena take;
@@ -473,7 +478,8 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
   if (!layer->z.data != !grads->dz.data || (layer->z.data && !writable(grads->dz, layer->T, layer->B))) return BPPSA_EINVAL;
   const Scratch at(layer->T, layer->B, layer->D, layer->N, layer->G);
   BPPSA_TRY(check_workspace(workspace, workspace_bytes, at.bytes));
-  const Spans spans = spans_of(layer->T, layer->B, layer->D, layer->N, layer->G, kWavesWanted, layer->lengths != nullptr);
+  const Spans spans = spans_of(layer->T, layer->B, layer->D, layer->N, layer->G,
+                               waves_wanted(layer->D, layer->N, layer->G, layer->B), layer->lengths != nullptr);
   const hipStream_t s = (hipStream_t)stream;
   return by_type(layer->type, [&](auto e) {
     using E = decltype(e);
