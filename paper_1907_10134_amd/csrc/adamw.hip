@@ -158,7 +158,8 @@ __device__ __forceinline__ void update(const bppsa_adamw_tensor& t, const Held<G
 }
 
 // A workgroup takes a piece; a wave four blocks of it in a row, four values a lane, and asks for all of a full piece's
-// before it works on the first.  Bound by memory.
+// before it works on the first (a block at a time: 1190 and 854 us instead of 1107 and 638 for 210 M parameters with bf16
+// gradients and copies, moments in 32 and in 8 bits).  Bound by memory, 5.3 TB/s.
 template <typename G, bool EIGHT>
 __global__ void __launch_bounds__(kThreads)
 adamw_kernel(const bppsa_adamw_tensor* __restrict__ tensors, const bppsa_adamw_piece* __restrict__ pieces, const Step c) {

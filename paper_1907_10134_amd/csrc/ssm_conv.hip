@@ -11,6 +11,8 @@ using namespace ssm;
 // window of inputs and one of gradients and the sums of the weights' gradients have to stay in registers too) and a span
 // of steps, the window of the last W inputs in registers.  The last thread of a row starts early enough to have V channels
 // too and repeats some of its neighbour's, with the same results; fewer than V channels go one to a thread.
+// T = 4096, B = 4, D = 4096, W = 4, bf16: forward 50 us (5.3 TB/s) on the same buffers again, 57 on others each time; with 8 bytes a
+// lane 71, with 128 registers, which spills, 84.
 constexpr int kAhead = 4;        // rows that are asked for together
 constexpr int kTogether = 4;     // spans of a workgroup of the backward pass
 
