@@ -141,7 +141,8 @@ __device__ __forceinline__ void join_spans(const Summary& sum, int first, int st
     for (int j = 0; j < AHEAD; ++j) {
       if (k + j >= count) break;
 #pragma unroll
-      for (int i = 0; i < H; ++i) h[i] = fmaf(exp2_fast(A2[i] * s[j]), h[i], end[j][i]);
+      for (int i = 0; i < H; ++i)            // zero stays zero where a positive A lets the factor overflow
+        h[i] = h[i] == 0.0f ? end[j][i] : fmaf(exp2_fast(A2[i] * s[j]), h[i], end[j][i]);
     }
   }
 }

@@ -152,6 +152,26 @@ def test_a_step_that_hardly_moves_and_one_that_forgets():
     _close(h_last, ssm.scan(**ref)[1], "float32", "h_last")
 
 
+def test_states_that_grow():
+    """A positive A: nothing enters for 900 steps, over which the decay's product passes the largest float many times, and
+    the states of the last steps grow from there; the same for the gradient, from the other end."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D, N = 910, 1, 64, 16
+    c, _, dy, _ = _case(12, T, B, D, N, 1, "float32", False, False, False, "tb")
+    c["A"].fill_(2.0)
+    c["dt"].fill_(1.0)
+    c["u"][:900] = 0.0
+    dy[10:] = 0.0
+    states = bp.ssm_scan_states(T, B, D, N)
+    y = bp.ssm_scan(**c, states=states)
+    _close(y, ssm.scan(**{k: _f64(v) for k, v in c.items()})[0], "float32", "y", sums=N)
+    g = bp.ssm_scan_backward(dy, states=states, **c)
+    assert all(bool(torch.isfinite(x).all()) for x in (g.du, g.ddt, g.dA, g.dBm, g.dCm))
+    want = ssm.scan_backward(_f64(dy), **{k: _f64(v) for k, v in c.items()})
+    _close(g.du, want["du"], "float32", "du", sums=2 * N)
+
+
 def test_a_nan_stays_in_its_channel():
     import torch
     import paper_1907_10134_amd as bp
