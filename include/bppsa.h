@@ -533,7 +533,9 @@ typedef struct bppsa_ssm {
 /*
  * Forward over whole sequences.  Writes y [T,B,D]; h_last [B,D,N], the state after each sample's last token, if not
  * NULL; `states`, bppsa_ssm_scan_states_bytes bytes of device memory in a layout of the library's own, if not NULL: what
- * the backward pass reads.  The results are the same bits on every call with the same sizes.
+ * the backward pass reads (N / 2 bytes for each channel and step, N rounded up to 4, 8 or a multiple of 16).  The workspace
+ * may be of size 0.  The results are the same bits on every call with the same sizes; the spans into which time is split,
+ * and so the last bits, may be others where lengths are given than where they are NULL.
  */
 size_t bppsa_ssm_scan_states_bytes(int T, int B, int D, int N);
 size_t bppsa_ssm_scan_workspace_bytes(int T, int B, int D, int N, int G);
@@ -598,7 +600,8 @@ bppsa_status bppsa_ssm_conv_step(const bppsa_conv* conv, const bppsa_rows* y, vo
  * for each BPPSA_ADAMW_BLOCK values of a tensor, the last block being what is left: value = e4m3 * scale, scale = the
  * block's largest magnitude (2^-100 at least) / 448.  m is rounded to the nearest; the root goes up or down by chance, so
  * that steps smaller than its spacing add up, and does not become zero.  The chance of value `place` of tensor number
- * `tensor` comes from hashing them with `seed` (bppsa_adamw_chance in the source; the same bits for the same seed).
+ * `tensor` comes from hashing them with `seed`: x = seed * 0x9E3779B1 + tensor * 0x6A09E667 + place in 32 bits, then
+ * x = (x ^ x >> 16) * k for k = 0xBB67AE85 and then 0x3C6EF373, x ^= x >> 15, and the upper 24 bits of x over 2^24.
  * A gradient that is not finite makes its values, in 8 bits its whole block of moments, not finite.
  *
  * `tensors` [n_tensors] and `pieces` [n_pieces] are DEVICE copies of what the caller fills in on the host once:

@@ -148,7 +148,7 @@ __device__ __forceinline__ void join_spans(const Summary& sum, int first, int st
 }
 
 // As many spans as give every SIMD `waves` waves, none shorter than 32 steps (a multiple of kKept), 64 at most.  Where samples
-// have lengths of their own, half as many again and more: spans behind an end leave units free for others (T = 1000, B =
+// have lengths of their own, three quarters more: spans behind an end leave units free for others (T = 1000, B =
 // 16, D = 640: 76 us with twice the spans, 87 with as many as below; without lengths twice as many cost T = 2048, B =
 // 64, D = 32 a sixth).
 static inline Spans spans_of(int T, int B, int D, int N, int G, int waves, bool ragged) {
