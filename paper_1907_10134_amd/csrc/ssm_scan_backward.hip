@@ -403,20 +403,20 @@ template <typename E>
 __global__ void __launch_bounds__(256)
 join_kernel(const Layer<E> l, const Grads<E> o, const Joined to) {
   if ((int)blockIdx.x < to.first_groups) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= to.places) return;
     const int passes = (l.T + PASS - 1) / PASS;
-    const Product product = product_of_lane((int)(i & 63), to.held);
-    const int w = (int)(i / 64 % to.waves), t = (int)(i / 64 / to.waves % passes) * PASS + product.step;
-    const int64_t bg = i / 64 / to.waves / passes;
-    const int g = (int)(bg % l.G), b = (int)(bg / l.G), n = w * to.held + product.state;
-    if (t >= l.T || n >= l.N || !product.first) return;
-    float sum = 0.0f;
-    if (t < clamp_length(l.lengths, b, l.T)) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < to.places; i += (int64_t)to.first_groups * 256) {
+      const Product product = product_of_lane((int)(i & 63), to.held);
+      const int w = (int)(i / 64 % to.waves), t = (int)(i / 64 / to.waves % passes) * PASS + product.step;
+      const int64_t bg = i / 64 / to.waves / passes;
+      const int g = (int)(bg % l.G), b = (int)(bg / l.G), n = w * to.held + product.state;
+      if (t >= l.T || n >= l.N || !product.first) continue;
+      float sum = 0.0f;
+      if (t < clamp_length(l.lengths, b, l.T)) {
 #pragma unroll 8
-      for (int k = 0; k < l.tiles; ++k) sum += o.bc[k * to.places + i];
+        for (int k = 0; k < l.tiles; ++k) sum += o.bc[k * to.places + i];
+      }
+      store(static_cast<E*>(product.of_C ? to.dCm : to.dBm) + (((int64_t)t * l.B + b) * l.G + g) * l.N + n, sum);
     }
-    store(static_cast<E*>(product.of_C ? to.dCm : to.dBm) + (((int64_t)t * l.B + b) * l.G + g) * l.N + n, sum);
     return;
   }
   __shared__ float quarter[4][64];
@@ -505,7 +505,8 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
       return BPPSA_OK;
     };
     BPPSA_TRY(by_states(l.N, [&](auto w, auto h) { return l.z.data ? walk(w, h, std::true_type{}) : walk(w, h, std::false_type{}); }));
-    const int64_t first = (at.bc_floats + 255) / 256;
+    // a launch has fewer than 2^32 threads: more places than 2^28 are taken in turns
+    const int64_t first = std::min<int64_t>((at.bc_floats + 255) / 256, 1 << 20);
     const Joined to{grads->dBm, grads->dCm, grads->dA, grads->dskip, grads->ddt_bias, at.bc_floats, (int)first, waves, held_of(l.N),
                     spans.count * l.B};
     join_kernel<E><<<(unsigned)(first + ((padded_of(l.N) + 2) * (int64_t)l.D + 63) / 64), 256, 0, s>>>(l, o, to);

@@ -184,9 +184,9 @@ static inline bppsa_status check_layer(const bppsa_ssm* l) {
   if (!l->u.data || !l->dt.data || !l->Bm.data || !l->Cm.data || !l->A) return BPPSA_EINVAL;
   if (l->D % l->G) return BPPSA_ESHAPE;
   if (l->N > BPPSA_SSM_MAX_N || l->type < BPPSA_F32 || l->type > BPPSA_F16) return BPPSA_EUNSUPPORTED;
-  // one grid axis counts the samples; rows are addressed by 32 bits of bytes
+  // one grid axis counts the samples; rows are addressed by 32 bits of bytes; a launch has fewer than 2^32 threads
   if (bppsa_mul_overflows(l->T, l->B, l->D, 2) || bppsa_mul_overflows(l->B, l->D, l->N, 1) || l->B > 65535 || l->D > 1 << 24 ||
-      l->T > 0x7FFFFFFF - 64)
+      l->T > 0x7FFFFFFF - 64 || (int64_t)l->G * bppsa_ceil_div(l->D / l->G, kTile) >= 1 << 22)
     return BPPSA_EOVERFLOW;
   return BPPSA_OK;
 }

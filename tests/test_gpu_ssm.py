@@ -310,6 +310,27 @@ def test_rows_further_apart_than_32_bits_count():
     _close(bp.ssm_conv_backward(dy, u, w).dx, ssm.conv_backward(_f64(dy), ref["u"], _f64(w))["dx"], "bfloat16", "dx")
 
 
+def test_more_tokens_than_one_round_of_the_joining_launch_has():
+    """2^25 tokens of a channel and a state, 2^29 places of dB and dC: the first, a middle and the last sample's."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B = 1 << 14, 2048
+    torch.manual_seed(3)
+    r = lambda *shape: torch.randn(shape, device="cuda")
+    u, dt, bm, cm, dy = r(T, B, 1), 0.5 * r(T, B, 1), r(T, B, 1, 1), r(T, B, 1, 1), r(T, B, 1)
+    A = torch.full((1, 1), -1.0, device="cuda")
+    states = bp.ssm_scan_states(T, B, 1, 1)
+    y = bp.ssm_scan(u, dt, A, bm, cm, states=states)
+    g = bp.ssm_scan_backward(dy, u, dt, A, bm, cm, states)
+    for b in (0, 1000, B - 1):
+        at = slice(b, b + 1)
+        ref = dict(u=_f64(u[:, at]), dt=_f64(dt[:, at]), A=_f64(A), Bm=_f64(bm[:, at]), Cm=_f64(cm[:, at]))
+        _close(y[:, at], ssm.scan(**ref)[0], "float32", "y", sums=3)
+        want = ssm.scan_backward(_f64(dy[:, at]), **ref)
+        for name in ("du", "ddt", "dBm", "dCm"):
+            _close(getattr(g, name)[:, at], want[name], "float32", name, sums=65)
+
+
 def test_inputs_that_repeat_a_row():
     """Broadcast inputs, strides of zero: read as they say; the gradient is that of each place."""
     import torch
