@@ -598,10 +598,13 @@ bppsa_status bppsa_ssm_conv_step(const bppsa_conv* conv, const bppsa_rows* y, vo
  * theta is fp32, grad of grad_type, copy (NULL: none) a bfloat16 copy of the new theta.
  * state_bits 32: m and v are fp32.  state_bits 8: m holds m, and v holds the ROOT of v, in e4m3 (OCP), with one fp32 scale
  * for each BPPSA_ADAMW_BLOCK values of a tensor, the last block being what is left: value = e4m3 * scale, scale = the
- * block's largest magnitude (2^-100 at least) / 448.  m is rounded to the nearest; the root goes up or down by chance, so
+ * block's largest magnitude (2^-100 at least) / 448.  The root goes up or down by chance, so
  * that steps smaller than its spacing add up, and does not become zero.  The chance of value `place` of tensor number
  * `tensor` comes from hashing them with `seed`: x = seed * 0x9E3779B1 + tensor * 0x6A09E667 + place in 32 bits, then
  * x = (x ^ x >> 16) * k for k = 0xBB67AE85 and then 0x3C6EF373, x ^= x >> 15, and the upper 24 bits of x over 2^24.
+ * m is rounded to the nearest, but by chance (the upper 24 bits of x * 0x9E3779B1) where its magnitude has become smaller
+ * and lies below 2^-6 scale: there the nearest would be the old value again, and a weight whose gradient has stopped would
+ * move for ever.  With beta1 > 15/16, where that holds for larger values too, m is always rounded by chance.
  * A gradient that is not finite makes its values, in 8 bits its whole block of moments, not finite.
  *
  * `tensors` [n_tensors] and `pieces` [n_pieces] are DEVICE copies of what the caller fills in on the host once:

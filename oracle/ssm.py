@@ -124,11 +124,32 @@ def e4m3_values():
     return np.concatenate([sub, rest])[:127]
 
 
-def chance(seed, tensor, n):
-    """[0, 1) for places 0..n of a tensor: two rounds of multiply and fold over place, tensor and seed."""
+def _numbers(seed, tensor, n):
     low = 0xFFFFFFFF
     x = (np.arange(n, dtype=np.uint64) + np.uint64((seed * 0x9E3779B1 + tensor * 0x6A09E667) & low)) & np.uint64(low)
     for k in (0xBB67AE85, 0x3C6EF373):
         x = ((x ^ (x >> np.uint64(16))) * np.uint64(k)) & np.uint64(low)
-    x = x ^ (x >> np.uint64(15))
+    return x ^ (x >> np.uint64(15))
+
+
+def chance(seed, tensor, n):
+    """[0, 1) for places 0..n of a tensor: two rounds of multiply and fold over place, tensor and seed."""
+    return (_numbers(seed, tensor, n) >> np.uint64(8)).astype(np.float64) * 2.0 ** -24
+
+
+def chance_of_m(seed, tensor, n):
+    """The same for the first moment, where that is rounded by chance."""
+    x = (_numbers(seed, tensor, n) * np.uint64(0x9E3779B1)) & np.uint64(0xFFFFFFFF)
     return (x >> np.uint64(8)).astype(np.float64) * 2.0 ** -24
+
+
+def held_m(q, shrinks, beta1, by):
+    """e4m3 values of first moments q in units of their scales; `shrinks`: the magnitude has become smaller, `by`: [0, 1) each.
+    Also which of them went by chance."""
+    grid, size = e4m3_values(), np.clip(np.abs(q), 0, 448)
+    above = np.clip(np.searchsorted(grid, size), 1, 126)
+    lo, hi = grid[above - 1], grid[above]
+    share = (size - lo) / (hi - lo)
+    by_chance = (shrinks & (size < 2.0 ** -6)) | (beta1 > 15 / 16)
+    nearest = np.where((share < 0.5) | ((share == 0.5) & (above % 2 == 1)), lo, hi)
+    return np.sign(q) * np.where(by_chance, np.where(share + by >= 1, hi, lo), nearest), by_chance

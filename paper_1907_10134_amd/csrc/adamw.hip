@@ -16,24 +16,41 @@ struct Step {
   float beta1, one_minus_beta1, beta2, one_minus_beta2, per_correct1, per_root_correct2, eps, lr;
   double lr_exact;
   uint32_t seed;
+  bool long_memory;                // beta1 > 15/16, see held_m
 };
 
-// Whether the root of v goes up: [0, 1) for a place of a tensor, two rounds of multiply and fold.
-__device__ __forceinline__ float chance(uint32_t x) {
+// The number that decides which way a place of a tensor is rounded: two rounds of multiply and fold.
+__device__ __forceinline__ uint32_t folded(uint32_t x) {
   x = (x ^ (x >> 16)) * 0xBB67AE85u;
   x = (x ^ (x >> 16)) * 0x3C6EF373u;
-  x ^= x >> 15;
-  return (float)(x >> 8) * 0x1p-24f;
+  return x ^ (x >> 15);
 }
+__device__ __forceinline__ float chance(uint32_t x) { return (float)(x >> 8) * 0x1p-24f; }      // [0, 1)
 
-// q >= 0 in units of its block's scale, on the grid of e4m3 below or above it by chance; above zero stays above zero.
+// q >= 0 in units of its block's scale, on the grid of e4m3 below or above it by chance.
 __device__ __forceinline__ float up_or_down(float q, float up) {
   // 2^(floor(log2 q) - 3), the spacing of e4m3 at q (2^-9 below 2^-6), from the exponent bits
   const uint32_t e = __float_as_uint(fmaxf(q, 0x1p-6f)) & 0x7F800000u;
   const float unit = __uint_as_float(e - (3u << 23)), per = __uint_as_float(0x7F000000u - (e - (3u << 23)));
   const float low = floorf(q * per) * unit;
-  const float chosen = (q - low) * per + up >= 1.0f ? low + unit : low;
+  return (q - low) * per + up >= 1.0f ? low + unit : low;
+}
+// The root of v: above zero stays above zero.
+__device__ __forceinline__ float held_root(float q, uint32_t x) {
+  const float chosen = up_or_down(q, chance(x));
   return q > 0.0f ? fminf(fmaxf(chosen, 0x1p-9f), 448.0f) : q;
+}
+
+// m: to the nearest, which the conversion does, where that cannot stop it from decaying.  A value that nothing feeds loses
+// 1 - beta1 of itself a step.  At beta1 <= 15/16 that is more than half the grid's spacing from 2^-6 on, where a value has 8 to 15
+// spacings; below, where the spacing stays 2^-9, it is not: 4 spacings at 0.9 are 3.6, and 4 again, for ever, over a root
+// that goes on falling, and so a weight without a gradient would move by up to a third of lr a step.  A magnitude that has
+// become smaller there goes up or down by chance instead, and so reaches zero; at a larger beta1 every value does.
+__device__ __forceinline__ bool held_by_chance(float q, float m, float was, bool long_memory) {
+  return long_memory || (fabsf(q) < 0x1p-6f && fabsf(m) < fabsf(was));
+}
+__device__ __forceinline__ float held_m(float q, uint32_t x) {
+  return copysignf(up_or_down(fabsf(q), chance(x * 0x9E3779B1u)), q);
 }
 
 template <typename T, int N>
@@ -112,12 +129,12 @@ struct Held {
 template <typename G, bool EIGHT>
 __device__ __forceinline__ void update(const bppsa_adamw_tensor& t, const Held<G, EIGHT>& x, int64_t i, int n, bool full, int lane,
                                        float keep, uint32_t tensor, const Step& c) {
-  float theta[4], m[4], v[4], root[4];
+  float theta[4], m[4], v[4], root[4], was[4];
   if constexpr (EIGHT) {
     unpack(__builtin_bit_cast(uint32_t, x.m), m);
     unpack(__builtin_bit_cast(uint32_t, x.v), v);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) m[k] *= x.m_scale, v[k] *= x.v_scale, v[k] *= v[k];
+    for (int k = 0; k < 4; ++k) was[k] = m[k] *= x.m_scale, v[k] *= x.v_scale, v[k] *= v[k];
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k) m[k] = x.m[k], v[k] = x.v[k];
@@ -143,11 +160,20 @@ __device__ __forceinline__ void update(const bppsa_adamw_tensor& t, const Held<G
     const float sm = scale_of(wave_largest(m)), sv = scale_of(wave_largest(root));
     const float im = 1.0f / sm, iv = 1.0f / sv;
     const uint32_t place = c.seed * 0x9E3779B1u + tensor * 0x6A09E667u + (uint32_t)i;
+    uint32_t number[4];
+    bool any = false, by_chance[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
+      number[k] = folded(place + k);
+      root[k] = held_root(root[k] * iv, number[k]);
+      by_chance[k] = held_by_chance(m[k] * im, m[k], was[k], c.long_memory);
       m[k] *= im;
-      root[k] = up_or_down(root[k] * iv, chance(place + k));
+      any |= by_chance[k];
     }
+    if (any)                                   // hardly a value of a block is so small
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (by_chance[k]) m[k] = held_m(m[k], number[k]);
     put4(static_cast<uint8_t*>(t.m) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(m)).v);
     put4(static_cast<uint8_t*>(t.v) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(root)).v);
     if (lane == 0) t.m_scale[i / kBlock] = sm, t.v_scale[i / kBlock] = sv;
@@ -212,7 +238,7 @@ extern "C" bppsa_status bppsa_adamw_step(int n_tensors, const bppsa_adamw_tensor
   if (state_bits != 32 && state_bits != 8) return BPPSA_EUNSUPPORTED;
   if (n_pieces > 0x7FFFFFFF) return BPPSA_EOVERFLOW;
   const Step c{(float)beta1, (float)(1 - beta1), (float)beta2, (float)(1 - beta2), (float)(1 / (1 - std::pow(beta1, step))),
-               (float)(1 / std::sqrt(1 - std::pow(beta2, step))), (float)eps, (float)lr, lr, seed};
+               (float)(1 / std::sqrt(1 - std::pow(beta2, step))), (float)eps, (float)lr, lr, seed, beta1 > 0.9375};
   return ssm::by_type(grad_type, [&](auto g) -> bppsa_status {
     using G = decltype(g);
     if (state_bits == 8)
