@@ -76,7 +76,7 @@ __device__ __forceinline__ void store_some(E* p, const float (&x)[V]) {
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp, 2^x
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// exp(a) for a of at most 87.  EXACT: the product with log2(e) loses |x| 2^-24 of the
+// exp(a).  EXACT, for a of at most 87: the product with log2(e) loses |x| 2^-24 of the
 // result; its rounding and the constant's own come back as a first-order term, which leaves v_exp_f32's error.  Without, for
 // activations of 16 bits, whose own rounding is 2^8 times as much.
 template <bool EXACT>
@@ -100,11 +100,17 @@ __device__ __forceinline__ float reciprocal_sum(float c, float e) {
 template <typename E>
 constexpr bool kExact = sizeof(E) == 4;
 
-// 1 / (1 + exp(-x)), exp(-x) of 87 at most, which is finite.  A NaN counts as -87 here: it is a factor elsewhere wherever
-// this is one.
+// 1 / (1 + exp(-x)); nothing is left of it for very negative x, down to the lowest value of a type, of which x times this and
+// its derivative have to be zero.  EXACT: from exp(-|x|), so that no exponential is infinite and needs a correction; without, an
+// infinite one gives zero by itself.
 template <typename E>
 __device__ __forceinline__ float sigmoid(float x) {
-  return reciprocal_sum<kExact<E>>(1.0f, exp_of<kExact<E>>(fminf(-x, 87.0f)));
+  if constexpr (kExact<E>) {
+    const float e = exp_of<true>(-fabsf(x)), r = reciprocal_sum<true>(1.0f, e);
+    return x >= 0.0f ? r : e * r;
+  } else {
+    return reciprocal_sum<false>(1.0f, exp_of<false>(-x));
+  }
 }
 
 // max(x, 0) + log1p(exp(-|x|)).  log1p(e) = 2 atanh(s), s = e / (2 + e) <= 1/3, as an odd polynomial in s: log(1 + e)

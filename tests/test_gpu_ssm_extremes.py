@@ -1,0 +1,62 @@
+"""GPU: the state space layer where values are at the ends of their types."""
+import numpy as np
+import pytest
+
+from oracle import ssm
+from test_gpu_ssm import _act, _case, _close, _f64
+
+pytestmark = pytest.mark.gpu
+
+
+def _lowest(dtype):
+    import torch
+    return float(torch.finfo(getattr(torch, dtype)).min)
+
+
+@pytest.mark.parametrize("dtype", ("float32", "bfloat16", "float16"))
+def test_gates_of_large_negative_values(dtype):
+    """silu and its derivative are zero there: the lowest value of a type is what a mask is filled with."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D, N = 24, 2, 70, 16
+    c, _, dy, dy_ref = _case(21, T, B, D, N, 1, dtype, True, True, False, "tb")
+    low = _lowest(dtype)
+    c["z"][:, 0, ::3] = low
+    c["z"][::2, 1, 1::3] = max(low, -1e30)
+    c["z"][5, 1] = max(low, -90.0)
+    ref = {k: _f64(v) for k, v in c.items()}
+    states = bp.ssm_scan_states(T, B, D, N)
+    y = bp.ssm_scan(**c, states=states)
+    y_ref = ssm.scan(**ref)[0]
+    assert np.all(np.abs(y_ref[:, 0, ::3]) == 0)
+    _close(y, y_ref, dtype, "y", sums=N + 2)
+    g = bp.ssm_scan_backward(dy, states=states, **c)
+    want = ssm.scan_backward(dy_ref, **ref)
+    for name in ("du", "ddt", "dz"):
+        _close(getattr(g, name), want[name], dtype, name, sums=2 * N + 8)
+    for name in ("dBm", "dCm"):
+        _close(getattr(g, name), want[name], dtype, name, sums=66)
+    one = {k: v[0] if k in ("u", "dt", "z", "Bm", "Cm") else v for k, v in c.items() if k != "h0"}
+    state = c["h0"].clone()
+    _close(bp.ssm_scan_step(state=state, **one), y_ref[0], dtype, "the token's y", sums=N + 2)
+
+
+@pytest.mark.parametrize("dtype", ("float32", "bfloat16", "float16"))
+@pytest.mark.parametrize("size", (-1e30, None))
+def test_convolutions_of_large_negative_values(dtype, size):
+    """With weights of one sign p is as large and negative as the input: y is zero, and so is what comes back through it."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D, W = 70, 2, 41, 4
+    rng = np.random.default_rng(4)
+    x, dy = _act(rng, (T, B, D), dtype), _act(rng, (T, B, D), dtype)
+    low = _lowest(dtype)
+    x[3::9, :, ::2] = low if size is None else max(low, size)
+    w = torch.from_numpy(rng.uniform(0.1, 0.9, (D, W)).astype(np.float32)).cuda()
+    y_ref, _, p, _ = ssm.conv(_f64(x), _f64(w))
+    assert float(np.min(p)) < -6000
+    _close(bp.ssm_conv(x, w), y_ref, dtype, "y")
+    want = ssm.conv_backward(_f64(dy), _f64(x), _f64(w))
+    _close(bp.ssm_conv_backward(dy, x, w).dx, want["dx"], dtype, "dx")
+    state = x[:W - 1].transpose(0, 1).contiguous()
+    _close(bp.ssm_conv_step(x[W - 1], w, None, state), y_ref[W - 1], dtype, "the token's y")
