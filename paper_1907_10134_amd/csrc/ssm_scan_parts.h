@@ -125,10 +125,16 @@ struct Summary {
 
 // Carries h over `count` spans, from `first` on, one after the other by `step`.  Eight of them are asked for together: one at
 // a time, the 47 of T = 30000 took some 20 us.
+// Where a state grows (a positive A), a span's factor may pass the largest float though its product with a small state does
+// not: three factors of a third of the exponent, one after the other, are as large as a product of floats can be made.
 template <int H>
 __device__ __forceinline__ void join_spans(const Summary& sum, int first, int step, int count, int B, int b, int waves, int w,
                                            int D, int d, const float (&A2)[H], float (&h)[H]) {
   constexpr int AHEAD = 8;
+  bool grow = false;
+#pragma unroll
+  for (int i = 0; i < H; ++i) grow |= A2[i] > 0.0f;
+  const bool any_grows = __any(grow);
   for (int k = 0; k < count; k += AHEAD) {
     float end[AHEAD][H], s[AHEAD];
 #pragma unroll
@@ -141,8 +147,15 @@ __device__ __forceinline__ void join_spans(const Summary& sum, int first, int st
     for (int j = 0; j < AHEAD; ++j) {
       if (k + j >= count) break;
 #pragma unroll
-      for (int i = 0; i < H; ++i)            // zero stays zero where a positive A lets the factor overflow
-        h[i] = h[i] == 0.0f ? end[j][i] : fmaf(exp2_fast(A2[i] * s[j]), h[i], end[j][i]);
+      for (int i = 0; i < H; ++i) {
+        const float x = A2[i] * s[j];
+        if (any_grows) {
+          const float third = exp2_fast(x * (1.0f / 3.0f));
+          h[i] = h[i] == 0.0f ? end[j][i] : fmaf(h[i] * third * third, third, end[j][i]);      // zero stays zero
+        } else {
+          h[i] = fmaf(exp2_fast(x), h[i], end[j][i]);
+        }
+      }
     }
   }
 }

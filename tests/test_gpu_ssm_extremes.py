@@ -60,3 +60,34 @@ def test_convolutions_of_large_negative_values(dtype, size):
     _close(bp.ssm_conv_backward(dy, x, w).dx, want["dx"], dtype, "dx")
     state = x[:W - 1].transpose(0, 1).contiguous()
     _close(bp.ssm_conv_step(x[W - 1], w, None, state), y_ref[W - 1], dtype, "the token's y")
+
+
+def test_states_that_grow_from_small_ones():
+    """A positive A: over the second of three spans of 32 steps a state of 1e-30 grows by e^93, further than the largest float is from
+    one, and so does the gradient on its way back.  The exponent, 32 steps times A, is off by a rounding each of the step's size (of
+    two, 2^-23), A log2(e), their product and the steps' sum: 93 * 2.5 * 2^-23 = 2.8e-5 of the result; 64 other steps add 2^-23 each."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D, N = 96, 1, 64, 16
+    c, _, dy, _ = _case(13, T, B, D, N, 1, "float32", False, False, False, "tb")
+    c["A"].fill_(2.0)
+    c["dt"].fill_(-20.0)
+    c["dt"][32:64] = 1.19                                # softplus: 1.455
+    c["u"].zero_()
+    c["h0"] = torch.full((B, D, N), 1e-30, device="cuda") * (1 + torch.rand((B, D, N), device="cuda"))
+    dy[:64] = 0.0
+    dy[64:] *= 1e-30
+    ref = {k: _f64(v) for k, v in c.items()}
+    states, h_last = bp.ssm_scan_states(T, B, D, N), torch.empty((B, D, N), device="cuda")
+    off = lambda got, want, what: np.testing.assert_allclose(_f64(got), want, rtol=0, atol=4e-5 * np.max(np.abs(want)), err_msg=what)
+    y_ref, last_ref, _, _ = ssm.scan(**ref)
+    assert 1e9 < np.max(last_ref) < 1e13
+    y = bp.ssm_scan(**c, h_last=h_last, states=states)
+    off(h_last, last_ref, "h_last")
+    off(y, y_ref, "y")
+    dh0 = torch.empty((B, D, N), device="cuda")
+    g = bp.ssm_scan_backward(dy, states=states, dh0=dh0, **c)
+    want = ssm.scan_backward(_f64(dy), **ref)
+    assert np.max(np.abs(want["dh0"])) > 1e8
+    off(dh0, want["dh0"], "dh0")
+    off(g.du[:32], want["du"][:32], "du")
