@@ -2,7 +2,8 @@
 their steps for single tokens, with the names of the C ABI in include/bppsa.h.
 
 Activations are float32, bfloat16 or float16, all of one call the same, [T, B, channels] with the channels contiguous and any
-strides of time and sample; parameters, states and their gradients are contiguous float32.
+strides of time and sample; parameters, states and their gradients are contiguous float32.  A call runs on the current stream
+or on `stream`; the caller orders that stream with the ones that make the inputs and use the results.
 """
 from __future__ import annotations
 
@@ -154,13 +155,26 @@ def _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths):
                        _param(lengths, (B,), "lengths", _i32)), (T, B, D, N, G)
 
 
-def _opaque(workspace, nbytes, device, stream):
+def _opaque(workspace, nbytes, device):
     """(tensor that has to live through the call, pointer, bytes) of a scratch array."""
     if workspace is None:
         if not nbytes:
             return None, None, 0
-        workspace = _workspace(nbytes, device, stream)
+        workspace = _workspace(nbytes, device)
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _aside(stream, call, *args):
+    """A call on a stream of its own: what it makes comes out of that stream's memory, which no one else's pending work still uses
+    and which goes back there behind the call's own, and is not given out again before the caller's stream is done with it."""
+    here = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        made = call(*args)
+    if stream != here:
+        for t in made if isinstance(made, tuple) else (made,):
+            if t is not None:
+                t.record_stream(here)
+    return made
 
 
 def ssm_scan_workspace_bytes(T, B, D, N, G):
@@ -189,13 +203,15 @@ def ssm_scan(u, dt, A, Bm, Cm, skip=None, z=None, dt_bias=None, h0=None, lengths
 
     u, dt, z [T, B, D]; Bm, Cm [T, B, G, N]; A [D, N]; skip, dt_bias [D]; h0 [B, D, N]; lengths [B] int32.  h_last [B, D, N]
     receives the last states, states (see ssm_scan_states) what ssm_scan_backward needs."""
+    if stream is not None:
+        return _aside(stream, ssm_scan, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths, y, h_last, states, workspace)
     layer, dims = _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
     T, B, D, N, G = dims
     if y is None:
         y = torch.empty_like(u)
-    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_workspace_bytes(T, B, D, N, G), u.device, stream)
+    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_workspace_bytes(T, B, D, N, G), u.device)
     _check(_lib.bppsa_ssm_scan(layer, _pack_rows(*_rows(y, u.shape, u.dtype, "y")), _param(h_last, (B, D, N), "h_last"),
-                               _states(states, dims), ws, nbytes, _stream(stream)), "bppsa_ssm_scan")
+                               _states(states, dims), ws, nbytes, _stream()), "bppsa_ssm_scan")
     return y
 
 
@@ -210,6 +226,8 @@ def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=N
                       workspace=None, stream=None):
     """bppsa_ssm_scan_backward: the gradients of sum(y dy), as SsmGrads; the other arguments are those of the ssm_scan call
     that filled `states`.  dskip, dz and ddt_bias are None where there is no such input; dh0 [B, D, N] is filled if given."""
+    if stream is not None:
+        return _aside(stream, ssm_scan_backward, dy, u, dt, A, Bm, Cm, states, skip, z, dt_bias, h0, lengths, dh0, workspace)
     layer, dims = _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
     T, B, D, N, G = dims
     if states is None:
@@ -223,9 +241,9 @@ def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=N
     out = _pack_grads(du.data_ptr(), su[0], su[1], ddt.data_ptr(), sd[0], sd[1], 0 if dz is None else dz.data_ptr(), su[0], su[1],
                       dBm.data_ptr(), dCm.data_ptr(), dA.data_ptr(), 0 if dskip is None else dskip.data_ptr(),
                       0 if dbias is None else dbias.data_ptr(), _param(dh0, (B, D, N), "dh0"))
-    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_backward_workspace_bytes(T, B, D, N, G), dev, stream)
+    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_backward_workspace_bytes(T, B, D, N, G), dev)
     _check(_lib.bppsa_ssm_scan_backward(layer, _pack_rows(*_rows(dy, u.shape, t, "dy")), _states(states, dims), out, ws, nbytes,
-                                        _stream(stream)), "bppsa_ssm_scan_backward")
+                                        _stream()), "bppsa_ssm_scan_backward")
     return SsmGrads(du, ddt, dA, dBm, dCm, dskip, dz, dbias, dh0)
 
 
@@ -261,6 +279,8 @@ def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slot
     """bppsa_ssm_scan_step: y [B, D] of one token of each stream; state [slots, D, N] float32 is advanced in place.
 
     u, dt, z [B, D]; Bm, Cm [B, G, N]; slots [B] int32, a row with one outside the state (-1, say) belongs to no stream."""
+    if stream is not None:
+        return _aside(stream, ssm_scan_step, u, dt, A, Bm, Cm, state, skip, z, dt_bias, slots, y)
     layer, (_, B, D, N, _) = _quick_layer(True, u, dt, A, Bm, Cm, skip, z, dt_bias, None, None) or \
         _token_layer(u, dt, A, Bm, Cm, skip, z, dt_bias)
     at = _ptr(state, _f32, "state")
@@ -270,7 +290,7 @@ def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slot
     if y is None:
         y = torch.empty_like(u)
     _check(_lib.bppsa_ssm_scan_step(layer, _pack_rows(*_token(y, u.shape, u.dtype, "y")), at, slots_in_state,
-                                    _slots(slots, B, slots_in_state), _stream(stream)), "bppsa_ssm_scan_step")
+                                    _slots(slots, B, slots_in_state), _stream()), "bppsa_ssm_scan_step")
     return y
 
 
@@ -292,11 +312,13 @@ def ssm_conv(x, weight, bias=None, silu=True, state0=None, lengths=None, y=None,
     """bppsa_ssm_conv: the causal convolution of x [T, B, D] with weight [D, W], channel by channel, and silu.
 
     state0 [B, W-1, D] holds the inputs in front of the first; state_last, of the same shape, receives the last ones."""
+    if stream is not None:
+        return _aside(stream, ssm_conv, x, weight, bias, silu, state0, lengths, y, state_last)
     conv, (_, B, D, W) = _conv(x, weight, bias, silu, state0, lengths)
     if y is None:
         y = torch.empty_like(x)
     _check(_lib.bppsa_ssm_conv(conv, _pack_rows(*_rows(y, x.shape, x.dtype, "y")),
-                               _param(state_last, (B, W - 1, D), "state_last", x.dtype), _stream(stream)), "bppsa_ssm_conv")
+                               _param(state_last, (B, W - 1, D), "state_last", x.dtype), _stream()), "bppsa_ssm_conv")
     return y
 
 
@@ -306,19 +328,23 @@ SsmConvGrads = namedtuple("SsmConvGrads", "dx dweight dbias dstate0")
 def ssm_conv_backward(dy, x, weight, bias=None, silu=True, state0=None, lengths=None, dstate0=None, workspace=None,
                       stream=None):
     """bppsa_ssm_conv_backward: the gradients of sum(y dy), as SsmConvGrads; dstate0 [B, W-1, D] is filled if given."""
+    if stream is not None:
+        return _aside(stream, ssm_conv_backward, dy, x, weight, bias, silu, state0, lengths, dstate0, workspace)
     conv, (T, B, D, W) = _conv(x, weight, bias, silu, state0, lengths)
     dx, dweight, dbias = torch.empty_like(x), torch.empty_like(weight), None if bias is None else torch.empty_like(bias)
-    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_conv_backward_workspace_bytes(T, B, D, W), x.device, stream)
+    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_conv_backward_workspace_bytes(T, B, D, W), x.device)
     _check(_lib.bppsa_ssm_conv_backward(conv, _pack_rows(*_rows(dy, x.shape, x.dtype, "dy")),
                                         _pack_rows(*_rows(dx, x.shape, x.dtype, "dx")), dweight.data_ptr(),
                                         None if dbias is None else dbias.data_ptr(),
-                                        _param(dstate0, (B, W - 1, D), "dstate0", x.dtype), ws, nbytes, _stream(stream)),
+                                        _param(dstate0, (B, W - 1, D), "dstate0", x.dtype), ws, nbytes, _stream()),
            "bppsa_ssm_conv_backward")
     return SsmConvGrads(dx, dweight, dbias, dstate0)
 
 
 def ssm_conv_step(x, weight, bias, state, silu=True, slots=None, y=None, stream=None):
     """bppsa_ssm_conv_step: y [B, D] of one token of each stream; state [slots, W-1, D] is moved on in place."""
+    if stream is not None:
+        return _aside(stream, ssm_conv_step, x, weight, bias, state, silu, slots, y)
     if not (isinstance(x, torch.Tensor) and isinstance(weight, torch.Tensor)):
         raise TypeError("x and weight must be torch.Tensors")
     if x.dim() != 2 or weight.dim() != 2:
@@ -337,5 +363,5 @@ def ssm_conv_step(x, weight, bias, state, silu=True, slots=None, y=None, stream=
     if y is None:
         y = torch.empty_like(x)
     _check(_lib.bppsa_ssm_conv_step(conv, _pack_rows(*_token(y, shape, t, "y")), at, slots_in_state,
-                                    _slots(slots, B, slots_in_state), _stream(stream)), "bppsa_ssm_conv_step")
+                                    _slots(slots, B, slots_in_state), _stream()), "bppsa_ssm_conv_step")
     return y

@@ -1,0 +1,86 @@
+"""The state space layer's binding: streams of the caller's choice, and what it refuses."""
+import contextlib
+
+import pytest
+
+
+class _Made:
+    def __init__(self):
+        self.recorded = []
+
+    def record_stream(self, stream):
+        self.recorded.append(stream)
+
+
+class _Stream:
+    device = "cuda:0"
+
+
+def test_what_a_call_makes_on_another_stream_is_that_streams(monkeypatch):
+    """Allocated with the stream current, and kept from it until the caller's stream is done: every array of every result."""
+    import torch
+    from paper_1907_10134_amd import ssm
+    here, side, now = _Stream(), _Stream(), []
+
+    @contextlib.contextmanager
+    def on(stream):
+        now.append(stream)
+        yield
+        now.pop()
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[-1] if now else here)
+
+    def call(make):
+        assert torch.cuda.current_stream() is side
+        return make()
+
+    one = ssm._aside(side, call, _Made)
+    assert one.recorded == [here] and not now
+    g = ssm._aside(side, call, lambda: ssm.SsmGrads(*([_Made() for _ in range(8)] + [None])))
+    assert type(g) is ssm.SsmGrads and g.dh0 is None and all(x.recorded == [here] for x in g[:8])
+    now.append(side)                           # already the current one
+    assert ssm._aside(side, call, _Made).recorded == []
+
+
+@pytest.mark.parametrize("name", ("ssm_scan", "ssm_scan_backward", "ssm_scan_step", "ssm_conv", "ssm_conv_backward", "ssm_conv_step"))
+def test_every_call_hands_all_its_arguments_over(monkeypatch, name):
+    import inspect
+    from paper_1907_10134_amd import ssm
+    call, got = getattr(ssm, name), []
+    monkeypatch.setattr(ssm, "_aside", lambda stream, again, *args: got.append((stream, again, args)))
+    names = [k for k in inspect.signature(call).parameters if k != "stream"]
+    assert list(inspect.signature(call).parameters)[-1] == "stream"
+    call(**{k: k for k in names}, stream="side")
+    assert got == [("side", call, tuple(names))]
+
+
+@pytest.mark.gpu
+def test_memory_of_results_on_another_stream_is_not_given_out_again():
+    """One field of the result is kept: the others' memory, still being written there, must not become new arrays here."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D, N = 512, 4, 256, 16
+    r = lambda *shape: torch.randn(shape, device="cuda")
+    u, dt, z, dy, Bm, Cm, A = r(T, B, D), r(T, B, D), r(T, B, D), r(T, B, D), r(T, B, 1, N), r(T, B, 1, N), -torch.rand((D, N), device="cuda")
+    w, bias, one = torch.rand((D, 4), device="cuda") - 0.5, torch.rand(D, device="cuda"), torch.ones(D, device="cuda")
+    states = bp.ssm_scan_states(T, B, D, N)
+    call = lambda stream: (bp.ssm_scan(u, dt, A, Bm, Cm, one, z, bias, states=states, stream=stream),
+                           *bp.ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, one, z, bias, stream=stream)[:8],
+                           bp.ssm_conv(u, w, bias, stream=stream), *bp.ssm_conv_backward(dy, u, w, bias, stream=stream)[:3],
+                           bp.ssm_scan_step(u[0], dt[0], A, Bm[0], Cm[0], torch.zeros((B, D, N), device="cuda"), stream=stream),
+                           bp.ssm_conv_step(u[0], w, bias, torch.zeros((B, 3, D), device="cuda"), stream=stream))
+    want = call(None)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = call(side)
+    shapes, places = [x.shape for x in got], {x.data_ptr() for x in got}
+    kept = got[1]
+    del got
+    new = [torch.empty(shape, device="cuda") for shape in shapes for _ in range(2)]
+    assert not places & {x.data_ptr() for x in new}
+    side.synchronize()
+    assert torch.equal(kept, want[1])
+    for a, b in zip(call(side), want):
+        side.synchronize()
+        assert torch.equal(a, b)
