@@ -59,6 +59,7 @@ class AdamW:
             raise ValueError("state must hold %s for each parameter" % ", ".join(names))
         self.state = {name: list(x) for name, x in state.items()}
         device, self._grad_type, rows, lengths = params[0].device, _TYPES[grads[0].dtype], [], []
+        self._device = device.index
         kinds = [("params", params, _f32), ("grads", grads, grads[0].dtype)] + [("state[%r]" % name, self.state[name], t) for name, t in names.items()]
         if copies is not None:
             kinds.append(("copies", self.copies, torch.bfloat16))
@@ -90,6 +91,9 @@ class AdamW:
         """One update.  With 8-bit moments `seed` (the number of the step unless given) decides which roots go up."""
         t = self.t + 1
         seed = t if seed is None else int(seed)
+        now = torch.cuda.current_device() if stream is None else stream.device.index
+        if now != self._device:
+            raise ValueError("AdamW: the tensors are on cuda:%d, the stream is cuda:%d's" % (self._device, now))
         _check(_lib.bppsa_adamw_step(len(self.params), self._tensors.data_ptr(), self._n_pieces, self._pieces.data_ptr(),
                                      self._grad_type, self.state_bits, t, self.lr, self.beta1, self.beta2, self.eps,
                                      seed & 0xFFFFFFFF, _stream(stream)), "bppsa_adamw_step")

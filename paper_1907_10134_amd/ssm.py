@@ -13,7 +13,7 @@ from collections import namedtuple
 
 import torch
 
-from .binding import _check, _lib, _ptr, _stream, _workspace
+from .binding import _check, _lib, _ptr, _raw_stream, _workspace
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _i32, _f32, _plain = torch.int32, torch.float32, torch.contiguous_format
@@ -40,12 +40,19 @@ _pack_grads = struct.Struct("@" + "Pqq" * 3 + "P" * 6).pack
 _pack_conv = struct.Struct("@6iPqq" + "P" * 4).pack
 
 
-def _rows(t, shape, dtype, name, groups=False):
-    """(pointer, time stride, sample stride) of an activation [T, B, channels] or [T, B, G, N]."""
+def _on(t, device, name):
+    """Refuses what is no tensor on the GPU, or on another one than the first argument."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
     if not t.is_cuda:
         raise ValueError("%s must live on the GPU" % name)
+    if t.get_device() != device:
+        raise ValueError("%s must be on cuda:%d like the first argument, not on %s" % (name, device, t.device))
+
+
+def _rows(t, shape, dtype, name, device, groups=False):
+    """(pointer, time stride, sample stride) of an activation [T, B, channels] or [T, B, G, N]."""
+    _on(t, device, name)
     if t.dtype is not dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
     if t.shape != shape:
@@ -59,40 +66,44 @@ def _rows(t, shape, dtype, name, groups=False):
     return t.data_ptr(), s[0], s[1]
 
 
-def _token(t, shape, dtype, name, groups=False):
-    """The same of one token of each stream, [B, channels] or [B, G, N]: (pointer, 0, sample stride)."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError("%s must be a torch.Tensor" % name)
-    if t.dtype is dtype and t.is_cuda and t.shape == shape:
+def _token(t, shape, dtype, name, device):
+    """The same of one token of each stream, [B, channels]: (pointer, 0, sample stride)."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == device and t.shape == shape:
         s = t.stride()
-        if groups:
-            if (s[2] == 1 or shape[2] == 1) and (s[1] == shape[2] or shape[1] == 1):
-                return t.data_ptr(), 0, s[0]
-        elif s[1] == 1 or shape[1] == 1:
+        if s[1] == 1 or shape[1] == 1:
             return t.data_ptr(), 0, s[0]
-    p, _, b = _rows(t.unsqueeze(0), (1,) + tuple(shape), dtype, name, groups)      # names what is wrong
+    p, _, b = _rows(t.unsqueeze(0) if isinstance(t, torch.Tensor) else t, (1,) + tuple(shape), dtype, name, device)   # names what is wrong
     return p, 0, b
 
 
-def _param(t, shape, name, dtype=torch.float32):
+def _param(t, shape, name, device, dtype=torch.float32):
     if t is None:
         return 0
-    if type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous():
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous():
         return t.data_ptr()
+    _on(t, device, name)
     p = _ptr(t, dtype, name)
     if t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
     return p
 
 
+def _whole(t, dtype, name, device):
+    """The address of a contiguous array whose shape the caller looks at."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    _on(t, device, name)
+    return _ptr(t, dtype, name)
+
+
 _NONE = (0, 0, 0)
 
 
-def _own(t, shape):
+def _own(t, shape, device):
     """The address of an optional fp32 parameter if it is what it has to be, None if that has to be looked at closer."""
     if t is None:
         return 0
-    if t.dtype is _f32 and t.is_cuda and t.shape == shape and t.is_contiguous():
+    if t.dtype is _f32 and t.get_device() == device and t.shape == shape and t.is_contiguous():
         return t.data_ptr()
     return None
 
@@ -100,14 +111,15 @@ def _own(t, shape):
 def _quick_layer(token, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths):
     """_layer in one go where every tensor is as it should be with nothing odd about it (6 us instead of 11); None otherwise."""
     try:
-        t, wide, narrow = u.dtype, u.shape, Bm.shape
+        t, wide, narrow, at = u.dtype, u.shape, Bm.shape, u.get_device()
         if token:
             (B, D), T, (_, G, N) = wide, 1, narrow
         else:
             (T, B, D), (_, _, G, N) = wide, narrow
         if not (dt.dtype is t and Bm.dtype is t and Cm.dtype is t and A.dtype is _f32 and dt.shape == wide and Cm.shape == narrow and
-                narrow[:-2] == wide[:-1] and A.shape == (D, N) and u.is_cuda and dt.is_cuda and Bm.is_cuda and Cm.is_cuda and
-                A.is_cuda and A.is_contiguous()):
+                narrow[:-2] == wide[:-1] and A.shape == (D, N) and
+                at >= 0 and dt.get_device() == at and Bm.get_device() == at and Cm.get_device() == at and
+                A.get_device() == at and A.is_contiguous()):
             return None
         su, sd, sb, sc = u.stride(), dt.stride(), Bm.stride(), Cm.stride()
         if not (su[-1] == sd[-1] == sb[-1] == sc[-1] == 1 and sb[-2] == sc[-2] == N):
@@ -115,44 +127,61 @@ def _quick_layer(token, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths):
         pz, sz = 0, su
         if z is not None:
             sz = z.stride()
-            if not (z.dtype is t and z.is_cuda and z.shape == wide and sz[-1] == 1):
+            if not (z.dtype is t and z.get_device() == at and z.shape == wide and sz[-1] == 1):
                 return None
             pz = z.data_ptr()
-        params = (A.data_ptr(), _own(skip, (D,)), _own(dt_bias, (D,)), _own(h0, (B, D, N)))
+        params = (A.data_ptr(), _own(skip, (D,), at), _own(dt_bias, (D,), at), _own(h0, (B, D, N), at))
         if None in params:
             return None
-        at = 0 if lengths is None else _param(lengths, (B,), "lengths", _i32)
+        ends = 0 if lengths is None else _param(lengths, (B,), "lengths", at, _i32)
         kind = _TYPES[t]
         if token:
             return _pack_layer(1, B, D, N, G, kind, u.data_ptr(), 0, su[0], dt.data_ptr(), 0, sd[0], pz, 0, sz[0], Bm.data_ptr(), 0,
-                               sb[0], Cm.data_ptr(), 0, sc[0], *params, at), (1, B, D, N, G)
+                               sb[0], Cm.data_ptr(), 0, sc[0], *params, ends), (1, B, D, N, G), at
         return _pack_layer(T, B, D, N, G, kind, u.data_ptr(), su[0], su[1], dt.data_ptr(), sd[0], sd[1], pz, sz[0], sz[1],
-                           Bm.data_ptr(), sb[0], sb[1], Cm.data_ptr(), sc[0], sc[1], *params, at), (T, B, D, N, G)
+                           Bm.data_ptr(), sb[0], sb[1], Cm.data_ptr(), sc[0], sc[1], *params, ends), (T, B, D, N, G), at
     except (AttributeError, KeyError, TypeError, ValueError):
         return None
 
 
-def _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths):
-    """The bytes of bppsa_ssm and (T, B, D, N, G)."""
-    quick = _quick_layer(False, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
+def _layer(token, u, dt, A, Bm, Cm, skip, z, dt_bias, h0=None, lengths=None):
+    """The bytes of bppsa_ssm, (T, B, D, N, G) and the device's number; token: of [B, channels], T = 1."""
+    quick = _quick_layer(token, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
     if quick is not None:
         return quick
     if not (isinstance(u, torch.Tensor) and isinstance(Bm, torch.Tensor)):
         raise TypeError("u and Bm must be torch.Tensors")
+    if token:
+        if u.dim() != 2 or Bm.dim() != 3:
+            raise ValueError("u must be [B, D] and Bm [B, G, N]")
+        one = lambda t: t.unsqueeze(0) if isinstance(t, torch.Tensor) else t
+        return _layer(False, one(u), one(dt), A, one(Bm), one(Cm), skip, one(z), dt_bias)
     if u.dim() != 3 or Bm.dim() != 4:
         raise ValueError("u must be [T, B, D] and Bm [T, B, G, N]")
     T, B, D = u.shape
     G, N = Bm.shape[2], Bm.shape[3]
-    t, wide, narrow = u.dtype, u.shape, (T, B, G, N)
+    t, wide, narrow, at = u.dtype, u.shape, (T, B, G, N), u.get_device()
     if t not in _TYPES:
         raise ValueError("activations must be float32, bfloat16 or float16, got %s" % t)
     if A is None:
         raise TypeError("A must be a torch.Tensor")
-    return _pack_layer(T, B, D, N, G, _TYPES[t], *_rows(u, wide, t, "u"), *_rows(dt, wide, t, "dt"),
-                       *(_NONE if z is None else _rows(z, wide, t, "z")), *_rows(Bm, narrow, t, "Bm", True),
-                       *_rows(Cm, narrow, t, "Cm", True), _param(A, (D, N), "A"), _param(skip, (D,), "skip"),
-                       _param(dt_bias, (D,), "dt_bias"), _param(h0, (B, D, N), "h0"),
-                       _param(lengths, (B,), "lengths", _i32)), (T, B, D, N, G)
+    return _pack_layer(T, B, D, N, G, _TYPES[t], *_rows(u, wide, t, "u", at), *_rows(dt, wide, t, "dt", at),
+                       *(_NONE if z is None else _rows(z, wide, t, "z", at)), *_rows(Bm, narrow, t, "Bm", at, True),
+                       *_rows(Cm, narrow, t, "Cm", at, True), _param(A, (D, N), "A", at), _param(skip, (D,), "skip", at),
+                       _param(dt_bias, (D,), "dt_bias", at), _param(h0, (B, D, N), "h0", at),
+                       _param(lengths, (B,), "lengths", at, _i32)), (T, B, D, N, G), at
+
+
+# without what torch.cuda.current_device does for a program that has not used the GPU yet
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _here(device):
+    """The current stream, which has to be one of the tensors' device: a kernel started elsewhere would use them from there."""
+    now = _current_device()
+    if now != device:
+        raise ValueError("the tensors are on cuda:%d, the current device is cuda:%d" % (device, now))
+    return _raw_stream(now) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _opaque(workspace, nbytes, device):
@@ -189,12 +218,13 @@ def ssm_scan_states(T, B, D, N, device="cuda"):
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _states(states, dims):
+def _states(states, dims, device):
     if states is None:
         return None
-    if states.numel() * states.element_size() < _lib.bppsa_ssm_scan_states_bytes(*dims[:4]):
+    at = _whole(states, torch.uint8, "states", device)
+    if states.numel() < _lib.bppsa_ssm_scan_states_bytes(*dims[:4]):
         raise ValueError("states is too small for these sizes")
-    return _ptr(states, torch.uint8, "states")
+    return at
 
 
 def ssm_scan(u, dt, A, Bm, Cm, skip=None, z=None, dt_bias=None, h0=None, lengths=None, y=None, h_last=None, states=None,
@@ -205,13 +235,13 @@ def ssm_scan(u, dt, A, Bm, Cm, skip=None, z=None, dt_bias=None, h0=None, lengths
     receives the last states, states (see ssm_scan_states) what ssm_scan_backward needs."""
     if stream is not None:
         return _aside(stream, ssm_scan, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths, y, h_last, states, workspace)
-    layer, dims = _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
+    layer, dims, at = _layer(False, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
     T, B, D, N, G = dims
     if y is None:
         y = torch.empty_like(u)
     _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_workspace_bytes(T, B, D, N, G), u.device)
-    _check(_lib.bppsa_ssm_scan(layer, _pack_rows(*_rows(y, u.shape, u.dtype, "y")), _param(h_last, (B, D, N), "h_last"),
-                               _states(states, dims), ws, nbytes, _stream()), "bppsa_ssm_scan")
+    _check(_lib.bppsa_ssm_scan(layer, _pack_rows(*_rows(y, u.shape, u.dtype, "y", at)), _param(h_last, (B, D, N), "h_last", at),
+                               _states(states, dims, at), ws, nbytes, _here(at)), "bppsa_ssm_scan")
     return y
 
 
@@ -228,7 +258,7 @@ def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=N
     that filled `states`.  dskip, dz and ddt_bias are None where there is no such input; dh0 [B, D, N] is filled if given."""
     if stream is not None:
         return _aside(stream, ssm_scan_backward, dy, u, dt, A, Bm, Cm, states, skip, z, dt_bias, h0, lengths, dh0, workspace)
-    layer, dims = _layer(u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
+    layer, dims, at = _layer(False, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
     T, B, D, N, G = dims
     if states is None:
         raise TypeError("states must be the array that ssm_scan filled")
@@ -240,39 +270,19 @@ def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=N
     su, sd = du.stride(), ddt.stride()
     out = _pack_grads(du.data_ptr(), su[0], su[1], ddt.data_ptr(), sd[0], sd[1], 0 if dz is None else dz.data_ptr(), su[0], su[1],
                       dBm.data_ptr(), dCm.data_ptr(), dA.data_ptr(), 0 if dskip is None else dskip.data_ptr(),
-                      0 if dbias is None else dbias.data_ptr(), _param(dh0, (B, D, N), "dh0"))
+                      0 if dbias is None else dbias.data_ptr(), _param(dh0, (B, D, N), "dh0", at))
     _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_backward_workspace_bytes(T, B, D, N, G), dev)
-    _check(_lib.bppsa_ssm_scan_backward(layer, _pack_rows(*_rows(dy, u.shape, t, "dy")), _states(states, dims), out, ws, nbytes,
-                                        _stream()), "bppsa_ssm_scan_backward")
+    _check(_lib.bppsa_ssm_scan_backward(layer, _pack_rows(*_rows(dy, u.shape, t, "dy", at)), _states(states, dims, at), out, ws,
+                                        nbytes, _here(at)), "bppsa_ssm_scan_backward")
     return SsmGrads(du, ddt, dA, dBm, dCm, dskip, dz, dbias, dh0)
 
 
-def _slots(slots, B, slots_in_state):
+def _slots(slots, B, slots_in_state, device):
     if slots is None:
         if slots_in_state < B:
             raise ValueError("state has fewer slots than the batch has rows")
         return None
-    return _param(slots, (B,), "slots", _i32)
-
-
-def _token_layer(u, dt, A, Bm, Cm, skip, z, dt_bias):
-    if not (isinstance(u, torch.Tensor) and isinstance(Bm, torch.Tensor)):
-        raise TypeError("u and Bm must be torch.Tensors")
-    if u.dim() != 2 or Bm.dim() != 3:
-        raise ValueError("u must be [B, D] and Bm [B, G, N]")
-    wide, narrow, t = u.shape, Bm.shape, u.dtype
-    B, D = wide
-    if t not in _TYPES:
-        raise ValueError("activations must be float32, bfloat16 or float16, got %s" % t)
-    if narrow[0] != B:
-        raise ValueError("Bm must have %d rows, got %d" % (B, narrow[0]))
-    if A is None:
-        raise TypeError("A must be a torch.Tensor")
-    _, G, N = narrow
-    return _pack_layer(1, B, D, N, G, _TYPES[t], *_token(u, wide, t, "u"), *_token(dt, wide, t, "dt"),
-                        *(_NONE if z is None else _token(z, wide, t, "z")), *_token(Bm, narrow, t, "Bm", True),
-                        *_token(Cm, narrow, t, "Cm", True), _param(A, (D, N), "A"), _param(skip, (D,), "skip"),
-                        _param(dt_bias, (D,), "dt_bias"), 0, 0), (1, B, D, N, G)
+    return _param(slots, (B,), "slots", device, _i32)
 
 
 def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slots=None, y=None, stream=None):
@@ -281,16 +291,16 @@ def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slot
     u, dt, z [B, D]; Bm, Cm [B, G, N]; slots [B] int32, a row with one outside the state (-1, say) belongs to no stream."""
     if stream is not None:
         return _aside(stream, ssm_scan_step, u, dt, A, Bm, Cm, state, skip, z, dt_bias, slots, y)
-    layer, (_, B, D, N, _) = _quick_layer(True, u, dt, A, Bm, Cm, skip, z, dt_bias, None, None) or \
-        _token_layer(u, dt, A, Bm, Cm, skip, z, dt_bias)
-    at = _ptr(state, _f32, "state")
+    layer, (_, B, D, N, _), at = _quick_layer(True, u, dt, A, Bm, Cm, skip, z, dt_bias, None, None) or \
+        _layer(True, u, dt, A, Bm, Cm, skip, z, dt_bias)
+    states = _whole(state, _f32, "state", at)
     slots_in_state = state.shape[0]
     if state.shape != (slots_in_state, D, N):
         raise ValueError("state must be [slots, %d, %d], got %s" % (D, N, tuple(state.shape)))
     if y is None:
         y = torch.empty_like(u)
-    _check(_lib.bppsa_ssm_scan_step(layer, _pack_rows(*_token(y, u.shape, u.dtype, "y")), at, slots_in_state,
-                                    _slots(slots, B, slots_in_state), _stream()), "bppsa_ssm_scan_step")
+    _check(_lib.bppsa_ssm_scan_step(layer, _pack_rows(*_token(y, u.shape, u.dtype, "y", at)), states, slots_in_state,
+                                    _slots(slots, B, slots_in_state, at), _here(at)), "bppsa_ssm_scan_step")
     return y
 
 
@@ -300,12 +310,12 @@ def _conv(x, weight, bias, silu, state0, lengths):
     if x.dim() != 3 or weight.dim() != 2:
         raise ValueError("x must be [T, B, D] and weight [D, W]")
     T, B, D = x.shape
-    W = weight.shape[1]
+    W, at = weight.shape[1], x.get_device()
     if x.dtype not in _TYPES:
         raise ValueError("activations must be float32, bfloat16 or float16, got %s" % x.dtype)
-    return _pack_conv(T, B, D, W, _TYPES[x.dtype], bool(silu), *_rows(x, x.shape, x.dtype, "x"), _param(weight, (D, W), "weight"),
-                      _param(bias, (D,), "bias"), _param(state0, (B, W - 1, D), "state0", x.dtype),
-                      _param(lengths, (B,), "lengths", _i32)), (T, B, D, W)
+    return _pack_conv(T, B, D, W, _TYPES[x.dtype], bool(silu), *_rows(x, x.shape, x.dtype, "x", at),
+                      _param(weight, (D, W), "weight", at), _param(bias, (D,), "bias", at),
+                      _param(state0, (B, W - 1, D), "state0", at, x.dtype), _param(lengths, (B,), "lengths", at, _i32)), (T, B, D, W), at
 
 
 def ssm_conv(x, weight, bias=None, silu=True, state0=None, lengths=None, y=None, state_last=None, stream=None):
@@ -314,11 +324,11 @@ def ssm_conv(x, weight, bias=None, silu=True, state0=None, lengths=None, y=None,
     state0 [B, W-1, D] holds the inputs in front of the first; state_last, of the same shape, receives the last ones."""
     if stream is not None:
         return _aside(stream, ssm_conv, x, weight, bias, silu, state0, lengths, y, state_last)
-    conv, (_, B, D, W) = _conv(x, weight, bias, silu, state0, lengths)
+    conv, (_, B, D, W), at = _conv(x, weight, bias, silu, state0, lengths)
     if y is None:
         y = torch.empty_like(x)
-    _check(_lib.bppsa_ssm_conv(conv, _pack_rows(*_rows(y, x.shape, x.dtype, "y")),
-                               _param(state_last, (B, W - 1, D), "state_last", x.dtype), _stream()), "bppsa_ssm_conv")
+    _check(_lib.bppsa_ssm_conv(conv, _pack_rows(*_rows(y, x.shape, x.dtype, "y", at)),
+                               _param(state_last, (B, W - 1, D), "state_last", at, x.dtype), _here(at)), "bppsa_ssm_conv")
     return y
 
 
@@ -330,13 +340,13 @@ def ssm_conv_backward(dy, x, weight, bias=None, silu=True, state0=None, lengths=
     """bppsa_ssm_conv_backward: the gradients of sum(y dy), as SsmConvGrads; dstate0 [B, W-1, D] is filled if given."""
     if stream is not None:
         return _aside(stream, ssm_conv_backward, dy, x, weight, bias, silu, state0, lengths, dstate0, workspace)
-    conv, (T, B, D, W) = _conv(x, weight, bias, silu, state0, lengths)
+    conv, (T, B, D, W), at = _conv(x, weight, bias, silu, state0, lengths)
     dx, dweight, dbias = torch.empty_like(x), torch.empty_like(weight), None if bias is None else torch.empty_like(bias)
     _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_conv_backward_workspace_bytes(T, B, D, W), x.device)
-    _check(_lib.bppsa_ssm_conv_backward(conv, _pack_rows(*_rows(dy, x.shape, x.dtype, "dy")),
-                                        _pack_rows(*_rows(dx, x.shape, x.dtype, "dx")), dweight.data_ptr(),
+    _check(_lib.bppsa_ssm_conv_backward(conv, _pack_rows(*_rows(dy, x.shape, x.dtype, "dy", at)),
+                                        _pack_rows(*_rows(dx, x.shape, x.dtype, "dx", at)), dweight.data_ptr(),
                                         None if dbias is None else dbias.data_ptr(),
-                                        _param(dstate0, (B, W - 1, D), "dstate0", x.dtype), ws, nbytes, _stream()),
+                                        _param(dstate0, (B, W - 1, D), "dstate0", at, x.dtype), ws, nbytes, _here(at)),
            "bppsa_ssm_conv_backward")
     return SsmConvGrads(dx, dweight, dbias, dstate0)
 
@@ -349,19 +359,19 @@ def ssm_conv_step(x, weight, bias, state, silu=True, slots=None, y=None, stream=
         raise TypeError("x and weight must be torch.Tensors")
     if x.dim() != 2 or weight.dim() != 2:
         raise ValueError("x must be [B, D] and weight [D, W]")
-    shape, t = x.shape, x.dtype
+    shape, t, at = x.shape, x.dtype, x.get_device()
     B, D = shape
     W = weight.shape[1]
     if t not in _TYPES:
         raise ValueError("activations must be float32, bfloat16 or float16, got %s" % t)
-    conv = _pack_conv(1, B, D, W, _TYPES[t], bool(silu), *_token(x, shape, t, "x"), _param(weight, (D, W), "weight"),
-                      _param(bias, (D,), "bias"), 0, 0)
-    at = _ptr(state, t, "state")
+    conv = _pack_conv(1, B, D, W, _TYPES[t], bool(silu), *_token(x, shape, t, "x", at), _param(weight, (D, W), "weight", at),
+                      _param(bias, (D,), "bias", at), 0, 0)
+    states = _whole(state, t, "state", at)
     slots_in_state = state.shape[0]
     if state.shape != (slots_in_state, W - 1, D):
         raise ValueError("state must be [slots, %d, %d], got %s" % (W - 1, D, tuple(state.shape)))
     if y is None:
         y = torch.empty_like(x)
-    _check(_lib.bppsa_ssm_conv_step(conv, _pack_rows(*_token(y, shape, t, "y")), at, slots_in_state,
-                                    _slots(slots, B, slots_in_state), _stream()), "bppsa_ssm_conv_step")
+    _check(_lib.bppsa_ssm_conv_step(conv, _pack_rows(*_token(y, shape, t, "y", at)), states, slots_in_state,
+                                    _slots(slots, B, slots_in_state, at), _here(at)), "bppsa_ssm_conv_step")
     return y

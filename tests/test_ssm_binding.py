@@ -84,3 +84,55 @@ def test_memory_of_results_on_another_stream_is_not_given_out_again():
     for a, b in zip(call(side), want):
         side.synchronize()
         assert torch.equal(a, b)
+
+
+def test_a_current_device_that_is_not_the_tensors_is_refused(monkeypatch):
+    import torch
+    import paper_1907_10134_amd as bp
+    from paper_1907_10134_amd import ssm
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(ssm, "_current_device", lambda: 1)
+    with pytest.raises(ValueError, match="cuda:0, the current device is cuda:1"):
+        ssm._here(0)
+    opt = object.__new__(bp.AdamW)             # no GPU is needed to be refused
+    opt._device, opt.t = 0, 0
+    with pytest.raises(ValueError, match="cuda:0"):
+        opt.step()
+    _Stream.device, was = torch.device("cuda:2"), _Stream.device
+    try:
+        with pytest.raises(ValueError, match="cuda:2"):
+            opt.step(stream=_Stream())
+    finally:
+        _Stream.device = was
+    assert opt.t == 0
+
+
+@pytest.mark.gpu
+def test_tensors_of_several_devices_are_refused(monkeypatch):
+    import torch
+    import paper_1907_10134_amd as bp
+    from paper_1907_10134_amd import ssm
+    x, w = torch.zeros((4, 2, 8), device="cuda"), torch.zeros((8, 4), device="cuda")
+    for check in (lambda: ssm._rows(x, x.shape, x.dtype, "dt", 1), lambda: ssm._param(w, w.shape, "A", 1),
+                  lambda: ssm._token(x[0], x[0].shape, x.dtype, "u", 1), lambda: ssm._on(x, 1, "states")):
+        with pytest.raises(ValueError, match="cuda:1 like the first argument"):
+            check()
+    n = torch.zeros((4, 2, 1, 4), device="cuda")
+    for cpu in ("dt", "A", "Bm", "Cm", "skip", "z", "dt_bias", "h0", "lengths", "y", "h_last", "states"):
+        c = {"u": x, "dt": x, "A": w, "Bm": n, "Cm": n, "skip": w[:, 0].contiguous(), "z": x, "dt_bias": w[:, 0].contiguous(),
+             "h0": torch.zeros((2, 8, 4), device="cuda"), "lengths": torch.ones(2, dtype=torch.int32, device="cuda"),
+             "y": torch.empty_like(x), "h_last": torch.zeros((2, 8, 4), device="cuda"), "states": bp.ssm_scan_states(4, 2, 8, 4)}
+        c[cpu] = c[cpu].cpu()
+        with pytest.raises(ValueError, match="%s must live on the GPU" % cpu):
+            bp.ssm_scan(**c)
+    with pytest.raises(ValueError, match="state must live on the GPU"):
+        bp.ssm_scan_step(x[0], x[0], w, n[0], n[0], torch.zeros((2, 8, 4)))
+    with pytest.raises(TypeError):
+        bp.ssm_conv_step(x[0], w, None, None)
+    with pytest.raises(ValueError, match=r"\[B, D\] and Bm"):
+        bp.ssm_scan_step(x, x[0], w, n[0], n[0], torch.zeros((2, 8, 4), device="cuda"))
+    with pytest.raises(ValueError, match="Cm must have shape"):
+        bp.ssm_scan_step(x[0], x[0], w, n[0], n[0, :1], torch.zeros((2, 8, 4), device="cuda"))
+    monkeypatch.setattr(ssm, "_current_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device is cuda:1"):
+        bp.ssm_conv(x, w)
