@@ -532,10 +532,11 @@ typedef struct bppsa_ssm {
 
 /*
  * Forward over whole sequences.  Writes y [T,B,D]; h_last [B,D,N], the state after each sample's last token, if not
- * NULL; `states`, bppsa_ssm_scan_states_bytes bytes of device memory in a layout of the library's own, if not NULL: what
- * the backward pass reads (N / 2 bytes for each channel and step, N rounded up to 4, 8 or a multiple of 16).  The workspace
- * may be of size 0.  The results are the same bits on every call with the same sizes; the spans into which time is split,
- * and so the last bits, may be others where lengths are given than where they are NULL.
+ * NULL; `states`, bppsa_ssm_scan_states_bytes bytes of device memory on a multiple of 16 (BPPSA_EINVAL otherwise) in a
+ * layout of the library's own, if not NULL: what the backward pass reads (N / 2 bytes for each channel and step, N rounded
+ * up to 4, 8 or a multiple of 16).  The workspace may be of size 0.  The results are the same bits on every call with the
+ * same sizes; the spans into which time is split, and so the last bits, may be others where lengths are given than where
+ * they are NULL.
  */
 size_t bppsa_ssm_scan_states_bytes(int T, int B, int D, int N);
 size_t bppsa_ssm_scan_workspace_bytes(int T, int B, int D, int N, int G);

@@ -260,7 +260,7 @@ extern "C" size_t bppsa_ssm_scan_workspace_bytes(int T, int B, int D, int N, int
 extern "C" bppsa_status bppsa_ssm_scan(const bppsa_ssm* layer, const bppsa_rows* y, float* h_last, void* states,
                                        void* workspace, size_t workspace_bytes, void* stream) {
   BPPSA_TRY(check_layer(layer));
-  if (!y || !writable(*y, layer->T, layer->B) || (h_last && h_last == layer->h0)) return BPPSA_EINVAL;
+  if (!y || !writable(*y, layer->T, layer->B) || (h_last && h_last == layer->h0) || !states_ok(states)) return BPPSA_EINVAL;
   const Scratch at(layer->T, layer->B, layer->D, layer->N, layer->G);
   BPPSA_TRY(check_workspace(workspace, workspace_bytes, at.bytes));
   const Spans spans = spans_of(layer->T, layer->B, layer->D, layer->N, layer->G, kWavesWanted, layer->lengths != nullptr);

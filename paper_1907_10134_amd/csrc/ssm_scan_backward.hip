@@ -476,7 +476,7 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
                                                 const bppsa_ssm_grads* grads, void* workspace, size_t workspace_bytes,
                                                 void* stream) {
   BPPSA_TRY(check_layer(layer));
-  if (!dy || !dy->data || !states || !grads || !grads->dBm || !grads->dCm || !grads->dA) return BPPSA_EINVAL;
+  if (!dy || !dy->data || !states || !states_ok(states) || !grads || !grads->dBm || !grads->dCm || !grads->dA) return BPPSA_EINVAL;
   if (!writable(grads->du, layer->T, layer->B) || !writable(grads->ddt, layer->T, layer->B)) return BPPSA_EINVAL;
   if (!layer->z.data != !grads->dz.data || (layer->z.data && !writable(grads->dz, layer->T, layer->B))) return BPPSA_EINVAL;
   const Scratch at(layer->T, layer->B, layer->D, layer->N, layer->G);

@@ -204,6 +204,9 @@ static inline bppsa_status check_layer(const bppsa_ssm* l) {
   return BPPSA_OK;
 }
 
+// The kept states are read and written by 8 and 16 bytes.
+static inline bool states_ok(const void* states) { return ((uintptr_t)states & 15) == 0; }
+
 static inline bppsa_status check_workspace(const void* workspace, size_t have, size_t need) {
   if (need && (!workspace || have < need)) return BPPSA_EWORKSPACE;
   return need && ((uintptr_t)workspace & 255) ? BPPSA_EINVAL : BPPSA_OK;

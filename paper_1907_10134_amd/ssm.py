@@ -190,6 +190,9 @@ def _opaque(workspace, nbytes, device):
         if not nbytes:
             return None, None, 0
         workspace = _workspace(nbytes, device)
+    else:
+        _on(workspace, device, "workspace")
+        _ptr(workspace, workspace.dtype, "workspace")          # contiguous
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
@@ -239,7 +242,7 @@ def ssm_scan(u, dt, A, Bm, Cm, skip=None, z=None, dt_bias=None, h0=None, lengths
     T, B, D, N, G = dims
     if y is None:
         y = torch.empty_like(u)
-    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_workspace_bytes(T, B, D, N, G), u.device)
+    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_workspace_bytes(T, B, D, N, G), at)
     _check(_lib.bppsa_ssm_scan(layer, _pack_rows(*_rows(y, u.shape, u.dtype, "y", at)), _param(h_last, (B, D, N), "h_last", at),
                                _states(states, dims, at), ws, nbytes, _here(at)), "bppsa_ssm_scan")
     return y
@@ -262,7 +265,7 @@ def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=N
     T, B, D, N, G = dims
     if states is None:
         raise TypeError("states must be the array that ssm_scan filled")
-    t, dev, like = u.dtype, u.device, torch.empty_like
+    t, like = u.dtype, torch.empty_like
     du, ddt = like(u), like(dt)
     dz = None if z is None else like(u)
     dBm, dCm = like(Bm, memory_format=_plain), like(Cm, memory_format=_plain)
@@ -271,7 +274,7 @@ def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=N
     out = _pack_grads(du.data_ptr(), su[0], su[1], ddt.data_ptr(), sd[0], sd[1], 0 if dz is None else dz.data_ptr(), su[0], su[1],
                       dBm.data_ptr(), dCm.data_ptr(), dA.data_ptr(), 0 if dskip is None else dskip.data_ptr(),
                       0 if dbias is None else dbias.data_ptr(), _param(dh0, (B, D, N), "dh0", at))
-    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_backward_workspace_bytes(T, B, D, N, G), dev)
+    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_backward_workspace_bytes(T, B, D, N, G), at)
     _check(_lib.bppsa_ssm_scan_backward(layer, _pack_rows(*_rows(dy, u.shape, t, "dy", at)), _states(states, dims, at), out, ws,
                                         nbytes, _here(at)), "bppsa_ssm_scan_backward")
     return SsmGrads(du, ddt, dA, dBm, dCm, dskip, dz, dbias, dh0)
@@ -342,7 +345,7 @@ def ssm_conv_backward(dy, x, weight, bias=None, silu=True, state0=None, lengths=
         return _aside(stream, ssm_conv_backward, dy, x, weight, bias, silu, state0, lengths, dstate0, workspace)
     conv, (T, B, D, W), at = _conv(x, weight, bias, silu, state0, lengths)
     dx, dweight, dbias = torch.empty_like(x), torch.empty_like(weight), None if bias is None else torch.empty_like(bias)
-    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_conv_backward_workspace_bytes(T, B, D, W), x.device)
+    _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_conv_backward_workspace_bytes(T, B, D, W), at)
     _check(_lib.bppsa_ssm_conv_backward(conv, _pack_rows(*_rows(dy, x.shape, x.dtype, "dy", at)),
                                         _pack_rows(*_rows(dx, x.shape, x.dtype, "dx", at)), dweight.data_ptr(),
                                         None if dbias is None else dbias.data_ptr(),

@@ -136,3 +136,50 @@ def test_tensors_of_several_devices_are_refused(monkeypatch):
     monkeypatch.setattr(ssm, "_current_device", lambda: 1)
     with pytest.raises(ValueError, match="current device is cuda:1"):
         bp.ssm_conv(x, w)
+
+
+def test_kept_states_off_16_bytes_are_refused():
+    """The kernels read and write them by 8 and 16 bytes."""
+    import ctypes
+    from test_oracle_ssm import EINVAL, EWORKSPACE, ONE, Grads, Rows, _rows, _ssm
+    import paper_1907_10134_amd as bp
+    from paper_1907_10134_amd import ssm
+    lib = ctypes.CDLL(bp.binding.lib_path())
+    p, n = ctypes.c_void_p, ctypes.c_size_t
+    need = ssm.ssm_scan_workspace_bytes(4000, 1, 32, 16, 1)
+    assert need                                # so that a call with good states ends at the missing workspace
+    g = Grads(_rows(), _rows(), Rows(), ONE, ONE, ONE, None, None, None)
+    for states, want in ((ONE + 8, EINVAL), (ONE + 1, EINVAL), (ONE + 16, EWORKSPACE)):
+        l = ctypes.byref(_ssm(T=4000, B=1))
+        assert lib.bppsa_ssm_scan(l, ctypes.byref(_rows()), None, p(states), None, n(0), None) == want
+        assert lib.bppsa_ssm_scan_backward(l, ctypes.byref(_rows()), p(states), ctypes.byref(g), None, n(0), None) == want
+
+
+def test_a_workspace_that_is_not_the_gpus_is_refused():
+    import torch
+    from paper_1907_10134_amd import ssm
+    with pytest.raises(ValueError, match="workspace must live on the GPU"):
+        ssm._opaque(torch.empty(1 << 20, dtype=torch.uint8), 4096, 0)
+    with pytest.raises(TypeError, match="workspace"):
+        ssm._opaque(1 << 20, 4096, 0)
+
+
+@pytest.mark.gpu
+def test_a_workspace_with_gaps_is_refused():
+    import torch
+    import paper_1907_10134_amd as bp
+    from paper_1907_10134_amd import ssm
+    T, D, N = 4000, 32, 16
+    r = lambda *shape: torch.randn(shape, device="cuda")
+    u, dt, Bm, Cm, A = r(T, 1, D), r(T, 1, D), r(T, 1, 1, N), r(T, 1, 1, N), -torch.rand((D, N), device="cuda")
+    need = ssm.ssm_scan_workspace_bytes(T, 1, D, N, 1)
+    for bad in (torch.empty((need, 2), dtype=torch.uint8, device="cuda")[:, 0], torch.empty(4, device="cuda").expand(need, 4)):
+        with pytest.raises(ValueError, match="workspace must be contiguous"):
+            bp.ssm_scan(u, dt, A, Bm, Cm, workspace=bad)
+    with pytest.raises(bp.BppsaError):
+        bp.ssm_scan(u, dt, A, Bm, Cm, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+    whole = torch.empty(-(-need // 4), device="cuda")
+    assert torch.equal(bp.ssm_scan(u, dt, A, Bm, Cm, workspace=whole), bp.ssm_scan(u, dt, A, Bm, Cm))
+    states = torch.empty(bp.ssm_scan_states(T, 1, D, N).numel() + 8, dtype=torch.uint8, device="cuda")
+    with pytest.raises(bp.BppsaError):
+        bp.ssm_scan(u, dt, A, Bm, Cm, states=states[8:])
