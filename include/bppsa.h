@@ -517,7 +517,9 @@ typedef struct bppsa_rows {
  * [D], h0 [B,D,N] fp32.  z.data, skip, dt_bias, h0 and lengths may be NULL (no gate, 0, 0, zeros, all of T).
  * lengths [B]: sample b has lengths[b] tokens (clamped to 0..T).  What lies behind them is never read; outputs and
  * gradients there are zero, and the last state is the one after the sample's own last token.
- * D has to be a multiple of G, N at most BPPSA_SSM_MAX_N (BPPSA_EUNSUPPORTED beyond).
+ * D has to be a multiple of G, N at most BPPSA_SSM_MAX_N (BPPSA_EUNSUPPORTED beyond).  Sizes that no launch can hold are
+ * BPPSA_EOVERFLOW, before anything is launched (B over 65535, D over 2^24; the backward pass also D (N + 2) of about 2^30 and
+ * more, N rounded up to 4, 8 or a multiple of 16); the byte counts of such sizes are 0.
  * The struct is host memory, its pointers device memory.  Here and in all calls of this section an output may not overlap
  * an input or another output (h_last = h0 and state_last = state0 are refused: BPPSA_EINVAL), except what is said to be
  * changed in place.
@@ -610,7 +612,8 @@ bppsa_status bppsa_ssm_conv_step(const bppsa_conv* conv, const bppsa_rows* y, vo
  *
  * `tensors` [n_tensors] and `pieces` [n_pieces] are DEVICE copies of what the caller fills in on the host once:
  * bppsa_adamw_pieces writes the list of pieces of lengths n[0..n_tensors) (host memory) and returns how many there are
- * (pieces NULL: only counts; 0: invalid), each a tensor's number and the first of its at most BPPSA_ADAMW_PIECE values.
+ * (pieces NULL: only counts; 0: invalid), each a tensor's number and the number of a piece of BPPSA_ADAMW_PIECE of its
+ * values, the last one of what is left.  2^24 pieces and more are BPPSA_EOVERFLOW.
  */
 #define BPPSA_ADAMW_BLOCK 256
 #define BPPSA_ADAMW_PIECE 4096

@@ -236,7 +236,7 @@ extern "C" bppsa_status bppsa_adamw_step(int n_tensors, const bppsa_adamw_tensor
   if (n_tensors < 1 || !tensors || n_pieces < 1 || !pieces || step < 1) return BPPSA_EINVAL;
   if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps > 0) || !std::isfinite(lr)) return BPPSA_EINVAL;
   if (state_bits != 32 && state_bits != 8) return BPPSA_EUNSUPPORTED;
-  if (n_pieces > 0x7FFFFFFF) return BPPSA_EOVERFLOW;
+  if (n_pieces >= 1 << 24) return BPPSA_EOVERFLOW;       // a launch has fewer than 2^32 threads
   const Step c{(float)beta1, (float)(1 - beta1), (float)beta2, (float)(1 - beta2), (float)(1 / (1 - std::pow(beta1, step))),
                (float)(1 / std::sqrt(1 - std::pow(beta2, step))), (float)eps, (float)lr, lr, seed, beta1 > 0.9375};
   return ssm::by_type(grad_type, [&](auto g) -> bppsa_status {

@@ -274,11 +274,14 @@ bppsa_status by_width(int W, F&& f) {
   }
 }
 
+bool too_large(int T, int B, int D) {
+  return bppsa_mul_overflows(T, B, D, 2) || B > 65535 || T > 65535 * 64 || D > 1 << 24;
+}
+
 bppsa_status check_conv(const bppsa_conv* c) {
   if (!c || c->T < 1 || c->B < 1 || c->D < 1 || c->W < 1 || !c->x.data || !c->weight) return BPPSA_EINVAL;
   if (c->W < 2 || c->W > BPPSA_SSM_MAX_W || c->type < BPPSA_F32 || c->type > BPPSA_F16) return BPPSA_EUNSUPPORTED;
-  if (bppsa_mul_overflows(c->T, c->B, c->D, 2) || c->B > 65535 || c->T > 65535 * 64 || c->D > 1 << 24) return BPPSA_EOVERFLOW;
-  return BPPSA_OK;
+  return too_large(c->T, c->B, c->D) ? BPPSA_EOVERFLOW : BPPSA_OK;
 }
 
 }  // namespace
@@ -304,7 +307,7 @@ extern "C" bppsa_status bppsa_ssm_conv(const bppsa_conv* conv, const bppsa_rows*
 }
 
 extern "C" size_t bppsa_ssm_conv_backward_workspace_bytes(int T, int B, int D, int W) {
-  if (T < 1 || B < 1 || D < 1 || W < 2 || W > BPPSA_SSM_MAX_W) return 0;
+  if (T < 1 || B < 1 || D < 1 || W < 2 || W > BPPSA_SSM_MAX_W || too_large(T, B, D)) return 0;
   // the type is not asked for: the shorter spans of the two
   const int span = std::min(backward_span(T, B, D, BPPSA_F32), backward_span(T, B, D, BPPSA_BF16));
   return (size_t)bppsa_ceil_div(T, span * kTogether) * B * (W + 1) * D * sizeof(float);

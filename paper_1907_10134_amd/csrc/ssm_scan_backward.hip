@@ -480,6 +480,10 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
   if (!writable(grads->du, layer->T, layer->B) || !writable(grads->ddt, layer->T, layer->B)) return BPPSA_EINVAL;
   if (!layer->z.data != !grads->dz.data || (layer->z.data && !writable(grads->dz, layer->T, layer->B))) return BPPSA_EINVAL;
   const Scratch at(layer->T, layer->B, layer->D, layer->N, layer->G);
+  // the joining launch: more places of dB and dC than 2^28 are taken in turns, the parameters' sums are not
+  const int64_t first = std::min<int64_t>((at.bc_floats + 255) / 256, 1 << 20);
+  const int64_t groups = first + ((padded_of(layer->N) + 2) * (int64_t)layer->D + 63) / 64;
+  if (groups >= 1 << 24) return BPPSA_EOVERFLOW;
   BPPSA_TRY(check_workspace(workspace, workspace_bytes, at.bytes));
   const Spans spans = spans_of(layer->T, layer->B, layer->D, layer->N, layer->G,
                                waves_wanted(layer->D, layer->N, layer->G, layer->B), layer->lengths != nullptr);
@@ -505,11 +509,9 @@ extern "C" bppsa_status bppsa_ssm_scan_backward(const bppsa_ssm* layer, const bp
       return BPPSA_OK;
     };
     BPPSA_TRY(by_states(l.N, [&](auto w, auto h) { return l.z.data ? walk(w, h, std::true_type{}) : walk(w, h, std::false_type{}); }));
-    // a launch has fewer than 2^32 threads: more places than 2^28 are taken in turns
-    const int64_t first = std::min<int64_t>((at.bc_floats + 255) / 256, 1 << 20);
     const Joined to{grads->dBm, grads->dCm, grads->dA, grads->dskip, grads->ddt_bias, at.bc_floats, (int)first, waves, held_of(l.N),
                     spans.count * l.B};
-    join_kernel<E><<<(unsigned)(first + ((padded_of(l.N) + 2) * (int64_t)l.D + 63) / 64), 256, 0, s>>>(l, o, to);
+    join_kernel<E><<<(unsigned)groups, 256, 0, s>>>(l, o, to);
     BPPSA_CHECK_LAUNCH();
     return BPPSA_OK;
   });

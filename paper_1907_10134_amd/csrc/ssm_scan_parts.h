@@ -188,8 +188,14 @@ struct Arena {
   }
 };
 
+// One grid axis counts the samples, rows are addressed by 32 bits of bytes, and a launch has fewer than 2^32 threads.
+static inline bool too_large(int T, int B, int D, int N, int G) {
+  return bppsa_mul_overflows(T, B, D, 2) || bppsa_mul_overflows(B, D, N, 1) || B > 65535 || D > 1 << 24 || T > 0x7FFFFFFF - 64 ||
+         (int64_t)G * bppsa_ceil_div(D / G, kTile) >= 1 << 22;
+}
+
 static inline bool sizes_ok(int T, int B, int D, int N, int G) {
-  return T > 0 && B > 0 && D > 0 && N > 0 && G > 0 && N <= BPPSA_SSM_MAX_N && D % G == 0;
+  return T > 0 && B > 0 && D > 0 && N > 0 && G > 0 && N <= BPPSA_SSM_MAX_N && D % G == 0 && !too_large(T, B, D, N, G);
 }
 
 static inline bppsa_status check_layer(const bppsa_ssm* l) {
@@ -197,11 +203,7 @@ static inline bppsa_status check_layer(const bppsa_ssm* l) {
   if (!l->u.data || !l->dt.data || !l->Bm.data || !l->Cm.data || !l->A) return BPPSA_EINVAL;
   if (l->D % l->G) return BPPSA_ESHAPE;
   if (l->N > BPPSA_SSM_MAX_N || l->type < BPPSA_F32 || l->type > BPPSA_F16) return BPPSA_EUNSUPPORTED;
-  // one grid axis counts the samples; rows are addressed by 32 bits of bytes; a launch has fewer than 2^32 threads
-  if (bppsa_mul_overflows(l->T, l->B, l->D, 2) || bppsa_mul_overflows(l->B, l->D, l->N, 1) || l->B > 65535 || l->D > 1 << 24 ||
-      l->T > 0x7FFFFFFF - 64 || (int64_t)l->G * bppsa_ceil_div(l->D / l->G, kTile) >= 1 << 22)
-    return BPPSA_EOVERFLOW;
-  return BPPSA_OK;
+  return too_large(l->T, l->B, l->D, l->N, l->G) ? BPPSA_EOVERFLOW : BPPSA_OK;
 }
 
 // The kept states are read and written by 8 and 16 bytes.
