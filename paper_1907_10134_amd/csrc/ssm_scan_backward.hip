@@ -19,6 +19,9 @@ struct Grads {
 };
 
 constexpr int PASS = kKept;
+// Passes after which the sums over time go to their totals and start again: 512 steps in a row, then the totals, keep a span of any
+// length as exact as fp32 sums of that many terms.
+constexpr int kRun = 64;
 
 // Sums over the wave's 64 lanes of the 2 H products (dB and dC of H states) of each of 8 steps.  A level halves the registers
 // and doubles the lanes that are summed: two registers exchange halves and are added, one slot a register and level, 126
@@ -197,6 +200,7 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   __shared__ float step_q[2][PASS][kTile];
   __shared__ alignas(16) float coef[2][PASS][WAVES][2 * H];
   __shared__ float share[SUMS][WAVES][PASS][kTile];
+  __shared__ float2 totals[WAVES][kTile];                // of dskip and ddt_bias, every wave those of its rows
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = blockIdx.x % (l.G * l.tiles), span = blockIdx.x / (l.G * l.tiles), g = tile / l.tiles, b = blockIdx.y;
   const int in = tile % l.tiles * kTile + lane;
@@ -224,6 +228,7 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
   const float bias = l.dt_bias ? l.dt_bias[d] : 0.0f, skip = l.skip ? l.skip[d] : 0.0f;
   const uint32_t byte = (uint32_t)d * sizeof(E);
   float dskip = 0.0f, dbias = 0.0f;
+  totals[w][lane] = make_float2(0.0f, 0.0f);
   const int mine = w * ROWS, passes = stop > t0 ? (stop - t0 + PASS - 1) / PASS : 0, last = t0 + (passes - 1) * PASS;
   Walk<const E> at_u(l.u, last + mine, b, byte, -PASS), at_dt(l.dt, last + mine, b, byte, -PASS), at_dy(dy, last + mine, b, byte, -PASS), at_z(l.z, last + mine, b, byte, -PASS);
   Walk<E> at_du(o.du, last + mine, b, byte, -PASS), at_ddt(o.ddt, last + mine, b, byte, -PASS), at_dz(o.dz, last + mine, b, byte, -PASS);
@@ -294,6 +299,21 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
       }
     at_du.move(), at_ddt.move();
     if (GATE) at_dz.move();
+  };
+
+  // adds the sums so far to their totals, of dA in memory that no one else has (in LDS they would cost N = 8 a workgroup a
+  // compute unit: 726 us instead of 654 at T = 4096, B = 4, D = 4096)
+  auto total = [&](bool first) __attribute__((always_inline)) {
+    if (on) {
+      float before[H] = {}, *at_dA = o.dA + state_at(H, span, l.B, b, WAVES, w, l.D, d);
+      if (!first) get(at_dA, before);
+#pragma unroll
+      for (int i = 0; i < H; ++i) before[i] += dA[i], dA[i] = 0.0f;
+      put(at_dA, before);
+    }
+    const float2 before = totals[w][lane];
+    totals[w][lane] = make_float2(before.x + dskip, before.y + dbias);
+    dskip = dbias = 0.0f;
   };
 
   float* at_bc = o.bc + (((((int64_t)(tile % l.tiles) * l.B + b) * l.G + g) * ((l.T + PASS - 1) / PASS) + last / PASS) * WAVES + w) * 64;
@@ -367,23 +387,21 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
     at_bc[lane] = over_steps<H>(step_sum, lane);
     at_bc -= WAVES * 64;
     if (p) prepare(first - PASS, buffer ^ 1);
+    // here: beside finish() the kernels of sixteen waves would spill 66 values, not 15 (T = 2048, B = 4, D = 2048, N = 64: 1041 us,
+    // 1663 without this branch and 46)
+    if (p && p % kRun == 0) total(p == (passes - 1) / kRun * kRun);
     __syncthreads();
   }
   if (passes) finish(t0);
-
-  // dskip and ddt_bias: every wave has the steps of its rows
-  __syncthreads();
-  float* totals = &share[0][0][0][0];
-  static_assert(sizeof(share) >= 2 * WAVES * kTile * sizeof(float));
-  totals[w * kTile + lane] = dskip, totals[(WAVES + w) * kTile + lane] = dbias;
+  total(passes <= kRun);
   __syncthreads();
   if (!on) return;
-  const int64_t part = (int64_t)span * l.B + b;
   if (w == 0) {
-    for (int k = 1; k < WAVES; ++k) dskip += totals[k * kTile + lane], dbias += totals[(WAVES + k) * kTile + lane];
-    o.dskip[part * l.D + d] = dskip, o.ddt_bias[part * l.D + d] = dbias;
+    float2 sum = totals[0][lane];
+    for (int k = 1; k < WAVES; ++k) sum.x += totals[k][lane].x, sum.y += totals[k][lane].y;
+    const int64_t part = (int64_t)span * l.B + b;
+    o.dskip[part * l.D + d] = sum.x, o.ddt_bias[part * l.D + d] = sum.y;
   }
-  put(o.dA + state_at(H, span, l.B, b, WAVES, w, l.D, d), dA);
   if (o.dh0 && span == 0)
 #pragma unroll
     for (int i = 0; i < H; ++i)
