@@ -176,6 +176,35 @@ def _layer(token, u, dt, A, Bm, Cm, skip, z, dt_bias, h0=None, lengths=None):
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
+def _like(t):
+    """A new array of t's shape and order of dimensions, its channels side by side also where t is windows of one array, whose order
+    torch cannot tell."""
+    new = torch.empty_like(t)
+    return new if new.stride(-1) == 1 else torch.empty_like(t, memory_format=_plain)
+
+
+def _output(y, x, name, device):
+    """(the array, the bytes of bppsa_rows) of an output like x [T, B, D], made here unless given."""
+    if y is None:
+        y = torch.empty_like(x)
+        s = y.stride()
+        if s[2] == 1:
+            return y, _pack_rows(y.data_ptr(), s[0], s[1])
+        y = torch.empty_like(x, memory_format=_plain)          # see _like
+    return y, _pack_rows(*_rows(y, x.shape, x.dtype, name, device))
+
+
+def _token_output(y, x, device):
+    """The same of one token of each stream, like x [B, D]."""
+    if y is None:
+        y = torch.empty_like(x)
+        s = y.stride()
+        if s[1] == 1:
+            return y, _pack_rows(y.data_ptr(), 0, s[0])
+        y = torch.empty_like(x, memory_format=_plain)
+    return y, _pack_rows(*_token(y, x.shape, x.dtype, "y", device))
+
+
 def _here(device):
     """The current stream, which has to be one of the tensors' device: a kernel started elsewhere would use them from there."""
     now = _current_device()
@@ -240,10 +269,9 @@ def ssm_scan(u, dt, A, Bm, Cm, skip=None, z=None, dt_bias=None, h0=None, lengths
         return _aside(stream, ssm_scan, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths, y, h_last, states, workspace)
     layer, dims, at = _layer(False, u, dt, A, Bm, Cm, skip, z, dt_bias, h0, lengths)
     T, B, D, N, G = dims
-    if y is None:
-        y = torch.empty_like(u)
+    y, out = _output(y, u, "y", at)
     _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_scan_workspace_bytes(T, B, D, N, G), at)
-    _check(_lib.bppsa_ssm_scan(layer, _pack_rows(*_rows(y, u.shape, u.dtype, "y", at)), _param(h_last, (B, D, N), "h_last", at),
+    _check(_lib.bppsa_ssm_scan(layer, out, _param(h_last, (B, D, N), "h_last", at),
                                _states(states, dims, at), ws, nbytes, _here(at)), "bppsa_ssm_scan")
     return y
 
@@ -266,8 +294,8 @@ def ssm_scan_backward(dy, u, dt, A, Bm, Cm, states, skip=None, z=None, dt_bias=N
     if states is None:
         raise TypeError("states must be the array that ssm_scan filled")
     t, like = u.dtype, torch.empty_like
-    du, ddt = like(u), like(dt)
-    dz = None if z is None else like(u)
+    du, ddt = _like(u), _like(dt)
+    dz = None if z is None else like(du)
     dBm, dCm = like(Bm, memory_format=_plain), like(Cm, memory_format=_plain)
     dA, dskip, dbias = like(A), None if skip is None else like(skip), None if dt_bias is None else like(dt_bias)
     su, sd = du.stride(), ddt.stride()
@@ -300,10 +328,9 @@ def ssm_scan_step(u, dt, A, Bm, Cm, state, skip=None, z=None, dt_bias=None, slot
     slots_in_state = state.shape[0]
     if state.shape != (slots_in_state, D, N):
         raise ValueError("state must be [slots, %d, %d], got %s" % (D, N, tuple(state.shape)))
-    if y is None:
-        y = torch.empty_like(u)
-    _check(_lib.bppsa_ssm_scan_step(layer, _pack_rows(*_token(y, u.shape, u.dtype, "y", at)), states, slots_in_state,
-                                    _slots(slots, B, slots_in_state, at), _here(at)), "bppsa_ssm_scan_step")
+    y, out = _token_output(y, u, at)
+    _check(_lib.bppsa_ssm_scan_step(layer, out, states, slots_in_state, _slots(slots, B, slots_in_state, at), _here(at)),
+           "bppsa_ssm_scan_step")
     return y
 
 
@@ -328,10 +355,8 @@ def ssm_conv(x, weight, bias=None, silu=True, state0=None, lengths=None, y=None,
     if stream is not None:
         return _aside(stream, ssm_conv, x, weight, bias, silu, state0, lengths, y, state_last)
     conv, (_, B, D, W), at = _conv(x, weight, bias, silu, state0, lengths)
-    if y is None:
-        y = torch.empty_like(x)
-    _check(_lib.bppsa_ssm_conv(conv, _pack_rows(*_rows(y, x.shape, x.dtype, "y", at)),
-                               _param(state_last, (B, W - 1, D), "state_last", at, x.dtype), _here(at)), "bppsa_ssm_conv")
+    y, out = _output(y, x, "y", at)
+    _check(_lib.bppsa_ssm_conv(conv, out, _param(state_last, (B, W - 1, D), "state_last", at, x.dtype), _here(at)), "bppsa_ssm_conv")
     return y
 
 
@@ -344,10 +369,10 @@ def ssm_conv_backward(dy, x, weight, bias=None, silu=True, state0=None, lengths=
     if stream is not None:
         return _aside(stream, ssm_conv_backward, dy, x, weight, bias, silu, state0, lengths, dstate0, workspace)
     conv, (T, B, D, W), at = _conv(x, weight, bias, silu, state0, lengths)
-    dx, dweight, dbias = torch.empty_like(x), torch.empty_like(weight), None if bias is None else torch.empty_like(bias)
+    dx, out = _output(None, x, "dx", at)
+    dweight, dbias = torch.empty_like(weight), None if bias is None else torch.empty_like(bias)
     _ws, ws, nbytes = _opaque(workspace, _lib.bppsa_ssm_conv_backward_workspace_bytes(T, B, D, W), at)
-    _check(_lib.bppsa_ssm_conv_backward(conv, _pack_rows(*_rows(dy, x.shape, x.dtype, "dy", at)),
-                                        _pack_rows(*_rows(dx, x.shape, x.dtype, "dx", at)), dweight.data_ptr(),
+    _check(_lib.bppsa_ssm_conv_backward(conv, _pack_rows(*_rows(dy, x.shape, x.dtype, "dy", at)), out, dweight.data_ptr(),
                                         None if dbias is None else dbias.data_ptr(),
                                         _param(dstate0, (B, W - 1, D), "dstate0", at, x.dtype), ws, nbytes, _here(at)),
            "bppsa_ssm_conv_backward")
@@ -373,8 +398,7 @@ def ssm_conv_step(x, weight, bias, state, silu=True, slots=None, y=None, stream=
     slots_in_state = state.shape[0]
     if state.shape != (slots_in_state, W - 1, D):
         raise ValueError("state must be [slots, %d, %d], got %s" % (W - 1, D, tuple(state.shape)))
-    if y is None:
-        y = torch.empty_like(x)
-    _check(_lib.bppsa_ssm_conv_step(conv, _pack_rows(*_token(y, shape, t, "y", at)), states, slots_in_state,
-                                    _slots(slots, B, slots_in_state, at), _here(at)), "bppsa_ssm_conv_step")
+    y, out = _token_output(y, x, at)
+    _check(_lib.bppsa_ssm_conv_step(conv, out, states, slots_in_state, _slots(slots, B, slots_in_state, at), _here(at)),
+           "bppsa_ssm_conv_step")
     return y

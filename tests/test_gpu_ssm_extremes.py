@@ -114,3 +114,25 @@ def test_sums_over_many_steps_in_one_span():
     for name in ("dA", "dskip", "ddt_bias"):
         off = abs(float(getattr(g, name)) / (float(want[name].item()) * B) - 1)
         assert off <= 1156 * 2.0 ** -24 + 2 * 2.0 ** -21, (name, off)
+
+
+@pytest.mark.parametrize("way", ("time", "samples"))
+def test_windows_of_one_array_as_inputs(way):
+    """Rows that overlap, [t] or [b] one element behind the last: the gradients come back with their channels side by side."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D, N = 12, 3, 20, 8
+    c, _, dy, dy_ref = _case(14, T, B, D, N, 1, "float32", True, True, False, "tb")
+    of = lambda x: x.as_strided((T, B, D), (1, 40, 1) if way == "time" else (40, 1, 1))
+    for name in ("u", "dt", "z"):
+        c[name] = of(c[name].contiguous().flatten())
+    ref = {k: _f64(v) for k, v in c.items()}
+    states = bp.ssm_scan_states(T, B, D, N)
+    _close(bp.ssm_scan(**c, states=states), ssm.scan(**ref)[0], "float32", "y", sums=N + 2)
+    g = bp.ssm_scan_backward(dy, states=states, **c)
+    want = ssm.scan_backward(dy_ref, **ref)
+    for name in ("du", "ddt", "dz"):
+        _close(getattr(g, name), want[name], "float32", name, sums=2 * N + 8)
+    w = torch.rand((D, 4), device="cuda") - 0.5
+    _close(bp.ssm_conv(c["u"], w), ssm.conv(ref["u"], _f64(w))[0], "float32", "conv")
+    _close(bp.ssm_conv_backward(dy, c["u"], w).dx, ssm.conv_backward(dy_ref, ref["u"], _f64(w))["dx"], "float32", "dx")

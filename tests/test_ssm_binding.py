@@ -183,3 +183,18 @@ def test_a_workspace_with_gaps_is_refused():
     states = torch.empty(bp.ssm_scan_states(T, 1, D, N).numel() + 8, dtype=torch.uint8, device="cuda")
     with pytest.raises(bp.BppsaError):
         bp.ssm_scan(u, dt, A, Bm, Cm, states=states[8:])
+
+
+def test_new_arrays_have_their_channels_side_by_side():
+    import torch
+    from paper_1907_10134_amd.ssm import _like
+    x = torch.empty(1000)
+    for shape, strides in (((12, 3, 20), (1, 40, 1)), ((12, 3, 20), (40, 1, 1)), ((12, 3, 20), (0, 20, 1)), ((12, 3, 20), (20, 0, 1)),
+                           ((12, 3, 20), (0, 0, 1)), ((12, 20), (1, 1)), ((12, 3, 20), (20, 300, 1)), ((1, 3, 20), (1, 20, 1))):
+        new = _like(x.as_strided(shape, strides))
+        assert new.shape == shape and new.stride(-1) == 1 and new.numel() == len({i for i in _offsets(new)}), strides
+
+
+def _offsets(x):
+    import itertools
+    return (sum(i * s for i, s in zip(at, x.stride())) for at in itertools.product(*map(range, x.shape)))
