@@ -136,3 +136,12 @@ def test_windows_of_one_array_as_inputs(way):
     w = torch.rand((D, 4), device="cuda") - 0.5
     _close(bp.ssm_conv(c["u"], w), ssm.conv(ref["u"], _f64(w))[0], "float32", "conv")
     _close(bp.ssm_conv_backward(dy, c["u"], w).dx, ssm.conv_backward(dy_ref, ref["u"], _f64(w))["dx"], "float32", "dx")
+
+
+@pytest.mark.parametrize("N", (49, 64))
+@pytest.mark.parametrize("dtype", ("float32", "bfloat16"))
+@pytest.mark.parametrize("gate,given,ragged", [(False, True, False), (True, True, True)])
+def test_sixteen_waves_and_many_spans(N, dtype, gate, given, ragged):
+    """The widest workgroups with time in spans: their summaries and joins."""
+    from test_gpu_ssm import test_scan_and_gradients as whole
+    whole((1100, 2, 40, N, 1), dtype, gate, given, ragged, "bt")
