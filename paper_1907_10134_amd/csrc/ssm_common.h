@@ -24,8 +24,6 @@ Rows<E> rows_of(const bppsa_rows& r) {
 
 // Activations are computed in fp32 and rounded once, to the nearest even, when they are stored.
 template <typename E>
-__device__ __forceinline__ float load(const E* p) { return static_cast<float>(*p); }
-template <typename E>
 __device__ __forceinline__ void store(E* p, float v) { *p = static_cast<E>(v); }
 
 // An element as it was loaded, in a register of its own, and its value.
