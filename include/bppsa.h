@@ -609,6 +609,7 @@ bppsa_status bppsa_ssm_conv_step(const bppsa_conv* conv, const bppsa_rows* y, vo
  * and lies below 2^-6 scale: there the nearest would be the old value again, and a weight whose gradient has stopped would
  * move for ever.  With beta1 > 15/16, where that holds for larger values too, m is always rounded by chance.
  * A gradient that is not finite makes its values, in 8 bits its whole block of moments, not finite.
+ * lr and eps have to be finite in fp32, and eps at least 2^-126 (BPPSA_EINVAL otherwise).
  *
  * `tensors` [n_tensors] and `pieces` [n_pieces] are DEVICE copies of what the caller fills in on the host once:
  * bppsa_adamw_pieces writes the list of pieces of lengths n[0..n_tensors) (host memory) and returns how many there are

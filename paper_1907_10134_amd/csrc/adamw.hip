@@ -1,4 +1,5 @@
 // One AdamW update of many tensors by one launch, moments in 32 or in 8 bits.
+#include <cfloat>
 #include <cmath>
 
 #include "ssm_common.h"
@@ -234,7 +235,8 @@ extern "C" bppsa_status bppsa_adamw_step(int n_tensors, const bppsa_adamw_tensor
                                          const bppsa_adamw_piece* pieces, int grad_type, int state_bits, int step, double lr,
                                          double beta1, double beta2, double eps, uint32_t seed, void* stream) {
   if (n_tensors < 1 || !tensors || n_pieces < 1 || !pieces || step < 1) return BPPSA_EINVAL;
-  if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps > 0) || !std::isfinite(lr)) return BPPSA_EINVAL;
+  if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !std::isfinite((float)lr)) return BPPSA_EINVAL;
+  if (!((float)eps >= FLT_MIN) || !std::isfinite((float)eps)) return BPPSA_EINVAL;       // v_rcp_f32 takes no less
   if (state_bits != 32 && state_bits != 8) return BPPSA_EUNSUPPORTED;
   if (n_pieces >= 1 << 24) return BPPSA_EOVERFLOW;       // a launch has fewer than 2^32 threads
   const Step c{(float)beta1, (float)(1 - beta1), (float)beta2, (float)(1 - beta2), (float)(1 / (1 - std::pow(beta1, step))),

@@ -102,3 +102,18 @@ def test_8_bits_with_float16_gradients_and_copies(shift):
         assert torch.equal(a, b)
     for name in run[0][1]:
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(run[0][1][name], run[1][1][name])), name
+
+
+@pytest.mark.parametrize("bits", (8, 32))
+def test_the_smallest_eps_leaves_values_without_gradients_as_they_are(bits):
+    import torch
+    import paper_1907_10134_amd as bp
+    p, g = torch.linspace(-1, 1, 600, device="cuda"), torch.zeros(600, device="cuda")
+    was = p.clone()
+    opt = bp.AdamW([p], [g], state_bits=bits, eps=2.0 ** -126, weight_decay=0.0)
+    opt.step()
+    assert torch.equal(p, was)
+    opt.eps = 2.0 ** -127
+    with pytest.raises(bp.BppsaError):
+        opt.step()
+    assert opt.t == 1

@@ -1,7 +1,7 @@
 """CPU: sizes that no launch or no count of bytes can hold are refused before anything is launched."""
 import ctypes
 
-from test_oracle_ssm import EOVERFLOW, EWORKSPACE, ONE, Grads, Rows, _rows, _ssm, lib  # noqa: F401 (a fixture)
+from test_oracle_ssm import EINVAL, EOVERFLOW, EWORKSPACE, ONE, Grads, Rows, _rows, _ssm, lib  # noqa: F401 (a fixture)
 
 MOST = 0x7FFFFFFF
 
@@ -35,3 +35,11 @@ def test_sizes_of_which_the_bytes_do_not_fit_have_none(lib):  # noqa: F811
     assert lib.bppsa_ssm_conv_backward_workspace_bytes(MOST, MOST, MOST, 4) == 0
     assert lib.bppsa_ssm_conv_backward_workspace_bytes(1 << 20, 64, 8192, 4) > 1 << 32
     assert lib.bppsa_ssm_scan_backward_workspace_bytes(1 << 18, 4, 8192, 16, 1) > 1 << 30
+
+
+def test_an_eps_or_lr_that_fp32_does_not_hold(lib):  # noqa: F811
+    """The update divides by root + eps: a value that has had no gradient yet would become 0 / 0."""
+    one, d = ctypes.c_void_p(ONE), ctypes.c_double
+    for lr, eps in ((1e-3, 1e-40), (1e-3, 1e-50), (1e-3, float("nan")), (1e-3, 1e39), (1e39, 1e-8), (float("inf"), 1e-8)):
+        assert lib.bppsa_adamw_step(1, one, ctypes.c_int64(1), one, 0, 32, 1, d(lr), d(0.9), d(0.999), d(eps), ctypes.c_uint32(0),
+                                    None) == EINVAL, (lr, eps)
