@@ -216,14 +216,25 @@ def _check(code, where):
         raise BppsaError(code, where)
 
 
-def _workspace(nbytes, device, stream=None):
-    # 256-byte aligned by the caching allocator (its blocks are 512-byte aligned).  A workspace
-    # made here for a stream other than the current one is tied to that stream, so the allocator
-    # does not hand its memory out again while the call is still running there.
-    ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
-    if stream is not None and stream != torch.cuda.current_stream(device):
-        ws.record_stream(stream)
-    return ws
+def _workspace(nbytes, device):
+    # 256-byte aligned by the caching allocator (its blocks are 512-byte aligned)
+    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+
+
+def _aside(stream, call, *args):
+    """A call on a stream of its own: what it makes comes out of that stream's memory, which no one else's pending work still uses
+    and which goes back there behind the call's own, and is not given out again before the caller's stream is done with it."""
+    here = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        made = call(*args)
+    if stream != here:
+        for t in made if isinstance(made, (tuple, list)) else (made,):
+            if isinstance(t, CsrMatrix):
+                for x in (t.indptr, t.indices, t.data):
+                    x.record_stream(here)
+            elif t is not None:
+                t.record_stream(here)
+    return made
 
 
 _last_h20_workspace = None      # the workspace of the latest H = 20 scan that allocated its own
@@ -252,6 +263,8 @@ def forward(cell, x, w_ih, w_hh, b_ih, b_hh, h, stream=None):
 
 def head_seed(h_last, w_out, b_out, labels, seed=None, loss=None, stream=None):
     """bppsa_head_seed: seed[B,H] = dL/dh_T of the softmax cross-entropy head."""
+    if stream is not None:
+        return _aside(stream, head_seed, h_last, w_out, b_out, labels, seed, loss)
     B, H = h_last.shape
     C = w_out.shape[0]
     if seed is None:
@@ -267,6 +280,8 @@ def head_seed(h_last, w_out, b_out, labels, seed=None, loss=None, stream=None):
 def build_jacobians(cell, h, x=None, w_ih=None, w_hh=None, b_ih=None, b_hh=None, Jt=None,
                     stream=None):
     """bppsa_build_jacobians: Jt[T,B,H,H], Jt[t] = (dh[t+1]/dh[t])^T."""
+    if stream is not None:
+        return _aside(stream, build_jacobians, cell, h, x, w_ih, w_hh, b_ih, b_hh, Jt)
     T1, B, H = h.shape
     T = T1 - 1
     I = x.shape[2] if x is not None else 1
@@ -284,11 +299,13 @@ def scan_workspace_bytes(T, B, H):
 
 def scan(Jt, seed, G=None, g0=None, workspace=None, stream=None):
     """bppsa_scan: G[t-1] = dL/dh[t], t = 1..T; optional g0 = dL/dh[0]."""
+    if stream is not None:
+        return _aside(stream, scan, Jt, seed, G, g0, workspace)
     T, B, H, _ = Jt.shape
     if G is None:
         G = torch.empty((T, B, H), dtype=torch.float32, device=Jt.device)
     if workspace is None:
-        workspace = _workspace(scan_workspace_bytes(T, B, H), Jt.device, stream)
+        workspace = _workspace(scan_workspace_bytes(T, B, H), Jt.device)
         if H == 20:
             global _last_h20_workspace
             _last_h20_workspace = workspace
@@ -302,6 +319,9 @@ def scan_h20_diag(Jt, seed, G=None, g0=None, workspace=None, stream=None, absent
                   lookback_stats=None):
     """bppsa_scan_h20_diag: the H = 20 scan with chosen dies standing aside / a forced unit length;
     lookback_stats, if given, is an int64 tensor of 3 that receives (hops, look-backs, max hops)."""
+    if stream is not None:
+        return _aside(stream, scan_h20_diag, Jt, seed, G, g0, workspace,
+                      None, absent_dies, unit_halves, lookback_stats)
     T, B, H, _ = Jt.shape
     if G is None:
         G = torch.empty((T, B, H), dtype=torch.float32, device=Jt.device)
@@ -318,11 +338,14 @@ def scan_h128_diag(Jt, seed, G=None, g0=None, workspace=None, stream=None, chain
                    last_slab_steps=0):
     """bppsa_scan_h128_diag: the H = 128 scan with a forced schedule (segments walked by the serial
     chain, segments per slab of totals, segment length inside the last slab)."""
+    if stream is not None:
+        return _aside(stream, scan_h128_diag, Jt, seed, G, g0, workspace,
+                      None, chain_segments, slab_segments, last_slab_steps)
     T, B, H, _ = Jt.shape
     if G is None:
         G = torch.empty((T, B, H), dtype=torch.float32, device=Jt.device)
     if workspace is None:
-        workspace = _workspace(scan_workspace_bytes(T, B, H), Jt.device, stream)
+        workspace = _workspace(scan_workspace_bytes(T, B, H), Jt.device)
     _check(_lib.bppsa_scan_h128_diag(T, B, _ptr(Jt), _ptr(seed), _ptr(G), _ptr(g0), workspace.data_ptr(),
                                      workspace.numel() * workspace.element_size(), _stream(stream),
                                      int(chain_segments), int(slab_segments), int(last_slab_steps)),
@@ -333,11 +356,13 @@ def scan_h128_diag(Jt, seed, G=None, g0=None, workspace=None, stream=None, chain
 def scan_h128_relay_diag(Jt, seed, G=None, g0=None, workspace=None, stream=None, workers=4, patience=20000):
     """bppsa_scan_h128_relay_diag: the H = 128 scan as one serial chain per sample, walked by `workers`
     compute units in turn that wait `patience` times 10 ns for each other."""
+    if stream is not None:
+        return _aside(stream, scan_h128_relay_diag, Jt, seed, G, g0, workspace, None, workers, patience)
     T, B, H, _ = Jt.shape
     if G is None:
         G = torch.empty((T, B, H), dtype=torch.float32, device=Jt.device)
     if workspace is None:
-        workspace = _workspace(scan_workspace_bytes(T, B, H), Jt.device, stream)
+        workspace = _workspace(scan_workspace_bytes(T, B, H), Jt.device)
     _check(_lib.bppsa_scan_h128_relay_diag(T, B, _ptr(Jt), _ptr(seed), _ptr(G), _ptr(g0), workspace.data_ptr(),
                                            workspace.numel() * workspace.element_size(), _stream(stream),
                                            int(workers), int(patience)),
@@ -372,12 +397,14 @@ def scan_static(Jt, seed, G, g0=None, stream=None):
 
 def rnn_scan_fused(h, w_hh, seed, G=None, g0=None, workspace=None, stream=None):
     """bppsa_rnn_scan_fused: the tanh-RNN scan with the Jacobians generated in the kernel."""
+    if stream is not None:
+        return _aside(stream, rnn_scan_fused, h, w_hh, seed, G, g0, workspace)
     T1, B, H = h.shape
     T = T1 - 1
     if G is None:
         G = torch.empty((T, B, H), dtype=torch.float32, device=h.device)
     if workspace is None:
-        workspace = _workspace(scan_workspace_bytes(T, B, H), h.device, stream)
+        workspace = _workspace(scan_workspace_bytes(T, B, H), h.device)
         global _last_h20_workspace
         _last_h20_workspace = workspace
     _check(_lib.bppsa_rnn_scan_fused(T, B, H, _ptr(h, name="h"), _ptr(w_hh, name="w_hh"), _ptr(seed, name="seed"),
@@ -393,6 +420,8 @@ def gru_scan_fused_workspace_bytes(T, B, H):
 
 def gru_scan_fused(h, x, w_ih, w_hh, b_ih, b_hh, seed, G=None, g0=None, workspace=None, stream=None):
     """bppsa_gru_scan_fused: the H = 128 GRU scan with the Jacobians generated inside its kernels."""
+    if stream is not None:
+        return _aside(stream, gru_scan_fused, h, x, w_ih, w_hh, b_ih, b_hh, seed, G, g0, workspace)
     T1, B, H = h.shape
     T = T1 - 1
     I = x.shape[2]
@@ -410,6 +439,9 @@ def gru_scan_fused(h, x, w_ih, w_hh, b_ih, b_hh, seed, G=None, g0=None, workspac
 def gru_scan_fused_relay_diag(h, x, w_ih, w_hh, b_ih, b_hh, seed, G=None, g0=None, workspace=None, stream=None, workers=4,
                               patience=20000):
     """bppsa_gru_scan_fused_relay_diag: scan_h128_relay_diag with the Jacobians generated."""
+    if stream is not None:
+        return _aside(stream, gru_scan_fused_relay_diag, h, x, w_ih, w_hh, b_ih, b_hh, seed,
+                      G, g0, workspace, None, workers, patience)
     T1, B, H = h.shape
     T = T1 - 1
     if G is None:
@@ -431,6 +463,8 @@ def param_grads_workspace_bytes(cell, T, B, H, I):
 def param_grads(cell, h, x, G, w_ih=None, w_hh=None, b_ih=None, b_hh=None, out=None,
                 workspace=None, stream=None):
     """bppsa_param_grads: returns (dW_ih, dW_hh, db_ih, db_hh)."""
+    if stream is not None:
+        return _aside(stream, param_grads, cell, h, x, G, w_ih, w_hh, b_ih, b_hh, out, workspace)
     T1, B, H = h.shape
     T = T1 - 1
     I = x.shape[2]
@@ -458,6 +492,8 @@ def param_grads(cell, h, x, G, w_ih=None, w_hh=None, b_ih=None, b_hh=None, out=N
 
 def head_backward(h_last, w_out, b_out, labels, seed=None, loss=None, dW_out=None, db_out=None, stream=None):
     """bppsa_head_backward: (seed, loss, dW_out, db_out) of the softmax cross-entropy head."""
+    if stream is not None:
+        return _aside(stream, head_backward, h_last, w_out, b_out, labels, seed, loss, dW_out, db_out)
     B, H = h_last.shape
     C = w_out.shape[0]
     dev = h_last.device
@@ -599,6 +635,8 @@ def _two_call(rows, cols, dev, call_indptr, call_fill):
 
 def csr_conv3x3(weight, mask, h, w, stream=None):
     """bppsa_csr_conv3x3_indptr + _fill.  weight [co,ci,3,3] fp32, mask same shape uint8 or None."""
+    if stream is not None:
+        return _aside(stream, csr_conv3x3, weight, mask, h, w)
     co, ci = weight.shape[:2]
     st = _stream(stream)
     wp, mp = _ptr(weight), _ptr(mask, torch.uint8, "mask")
@@ -612,6 +650,8 @@ def csr_conv3x3(weight, mask, h, w, stream=None):
 
 def csr_conv2d(weight, mask, h, w, stride=(1, 1), padding=(0, 0), dilation=(1, 1), stream=None):
     """bppsa_csr_conv2d_indptr + _fill.  weight [co,ci,kh,kw] fp32, mask same shape uint8 or None."""
+    if stream is not None:
+        return _aside(stream, csr_conv2d, weight, mask, h, w, stride, padding, dilation)
     co, ci, kh, kw = weight.shape
     g = Conv2dGeometry(kh, kw, stride[0], stride[1], padding[0], padding[1], dilation[0], dilation[1])
     oh = (h + 2 * padding[0] - dilation[0] * (kh - 1) - 1) // stride[0] + 1
@@ -628,6 +668,8 @@ def csr_conv2d(weight, mask, h, w, stride=(1, 1), padding=(0, 0), dilation=(1, 1
 
 def csr_linear(weight, mask, stream=None):
     """bppsa_csr_linear_indptr + _fill.  weight [out,in]."""
+    if stream is not None:
+        return _aside(stream, csr_linear, weight, mask)
     out, inn = weight.shape
     st = _stream(stream)
     wp, mp = _ptr(weight), _ptr(mask, torch.uint8, "mask")
@@ -639,6 +681,8 @@ def csr_linear(weight, mask, stream=None):
 
 
 def csr_relu(x, stream=None):
+    if stream is not None:
+        return _aside(stream, csr_relu, x)
     d = x.numel()
     dev = x.device
     indptr = torch.empty(d + 1, dtype=_int32, device=dev)
@@ -650,6 +694,8 @@ def csr_relu(x, stream=None):
 
 
 def csr_maxpool2x2(x, stream=None):
+    if stream is not None:
+        return _aside(stream, csr_maxpool2x2, x)
     c, h, w = x.shape
     dev = x.device
     n_out = c * (h // 2) * (w // 2)
@@ -662,6 +708,8 @@ def csr_maxpool2x2(x, stream=None):
 
 
 def spmv(A, x, y=None, stream=None):
+    if stream is not None:
+        return _aside(stream, spmv, A, x, y)
     if y is None:
         y = torch.empty((A.rows,), dtype=torch.float32, device=x.device)
     d = A.desc()

@@ -13,7 +13,7 @@ from collections import namedtuple
 
 import torch
 
-from .binding import _check, _lib, _ptr, _raw_stream, _workspace
+from .binding import _aside, _check, _lib, _ptr, _raw_stream, _workspace
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _i32, _f32, _plain = torch.int32, torch.float32, torch.contiguous_format
@@ -223,19 +223,6 @@ def _opaque(workspace, nbytes, device):
         _on(workspace, device, "workspace")
         _ptr(workspace, workspace.dtype, "workspace")          # contiguous
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
-
-
-def _aside(stream, call, *args):
-    """A call on a stream of its own: what it makes comes out of that stream's memory, which no one else's pending work still uses
-    and which goes back there behind the call's own, and is not given out again before the caller's stream is done with it."""
-    here = torch.cuda.current_stream(stream.device)
-    with torch.cuda.stream(stream):
-        made = call(*args)
-    if stream != here:
-        for t in made if isinstance(made, tuple) else (made,):
-            if t is not None:
-                t.record_stream(here)
-    return made
 
 
 def ssm_scan_workspace_bytes(T, B, D, N, G):
