@@ -9,6 +9,7 @@ import torch
 from .binding import _check, _lib, _ptr, _stream
 
 BLOCK = 256                        # BPPSA_ADAMW_BLOCK
+_ROW = 9                           # words of a bppsa_adamw_tensor, the second the gradient's address
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _f32 = torch.float32
 
@@ -28,7 +29,8 @@ class AdamW:
     None.  weight_decay: one number or one for each tensor.  `state` (made here unless given) is a dict of lists, a tensor for
     each parameter: "m" and "v", float32; with state_bits=8 float8_e4m3fn, with "m_scale" and "v_scale", float32 of one value
     for each 256, and "v" then stands for the root of the second moment.  The tensors' addresses are taken once, here: replace
-    their values, not the tensors.  `t` counts the steps; lr, beta1, beta2 and eps are read at every step."""
+    their values, not the tensors, but for gradients that a program makes anew, see read_gradients().  `t` counts the steps;
+    lr, beta1, beta2 and eps are read at every step."""
 
     def __init__(self, params, grads, state_bits=32, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, copies=None,
                  state=None):
@@ -82,18 +84,38 @@ class AdamW:
         self._n_pieces = int(_lib.bppsa_adamw_pieces(len(params), n, None))
         if self._n_pieces < 1:
             raise ValueError("AdamW: nothing to update")
+        self._table = bytearray(b"".join(rows))              # what the device has a copy of
         pieces = torch.empty((self._n_pieces, 2), dtype=torch.int32)
         _lib.bppsa_adamw_pieces(len(params), n, pieces.data_ptr())
         self._pieces = pieces.to(device)
-        self._tensors = torch.frombuffer(bytearray(b"".join(rows)), dtype=torch.uint8).to(device)
+        self._tensors = torch.frombuffer(self._table, dtype=torch.uint8).to(device)
+
+    def read_gradients(self, grads):
+        """Reads the gradients from these tensors from now on, of the sizes and the type of those before."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError("AdamW needs as many gradients as parameters")
+        kind, device, at = self.grads[0].dtype, self.params[0].device, []
+        for k, (g, p) in enumerate(zip(grads, self.params)):
+            where = _ptr(g, kind, "grads[%d]" % k)
+            if where is None or g.numel() != p.numel() or g.device != device:
+                raise ValueError("grads[%d] must have %d values on %s" % (k, p.numel(), device))
+            at.append(where)
+        table = memoryview(self._table).cast("q")
+        table[1::_ROW] = memoryview(bytearray(struct.pack("@%dq" % len(at), *at))).cast("q")
+        self.grads = grads
+        self._tensors = torch.frombuffer(self._table, dtype=torch.uint8).to(device)
 
     def step(self, seed=None, stream=None):
-        """One update.  With 8-bit moments `seed` (the number of the step unless given) decides which roots go up."""
+        """One update.  With 8-bit moments `seed` (the number of the step unless given) decides which values that are
+        rounded by chance go up."""
         t = self.t + 1
         seed = t if seed is None else int(seed)
         now = torch.cuda.current_device() if stream is None else stream.device.index
         if now != self._device:
             raise ValueError("AdamW: the tensors are on cuda:%d, the stream is cuda:%d's" % (self._device, now))
+        if stream is not None:
+            self._tensors.record_stream(stream)        # read_gradients() lets the table go
         _check(_lib.bppsa_adamw_step(len(self.params), self._tensors.data_ptr(), self._n_pieces, self._pieces.data_ptr(),
                                      self._grad_type, self.state_bits, t, self.lr, self.beta1, self.beta2, self.eps,
                                      seed & 0xFFFFFFFF, _stream(stream)), "bppsa_adamw_step")

@@ -117,3 +117,37 @@ def test_the_smallest_eps_leaves_values_without_gradients_as_they_are(bits):
     with pytest.raises(bp.BppsaError):
         opt.step()
     assert opt.t == 1
+
+
+@pytest.mark.parametrize("bits", (8, 32))
+def test_gradients_of_other_tensors(bits):
+    """A program that makes its gradients anew at every step gives them to the optimiser; the old ones are not read again."""
+    import torch
+    import paper_1907_10134_amd as bp
+    torch.manual_seed(4)
+    lengths = (1, 300, 5000)
+    steps = [[torch.randn(n, device="cuda").bfloat16() for n in lengths] for _ in range(4)]
+    held, anew = [[torch.linspace(-1, 1, n, device="cuda") for n in lengths] for _ in range(2)]
+    g = [x.clone() for x in steps[0]]
+    one, two = bp.AdamW(held, g, state_bits=bits), bp.AdamW(anew, steps[0], state_bits=bits)
+    for k, now in enumerate(steps):
+        for a, b in zip(g, now):
+            a.copy_(b)
+        one.step()
+        if k:
+            two.read_gradients(now)
+            for x in steps[k - 1]:
+                x.fill_(float("nan"))
+        two.step(stream=torch.cuda.current_stream())
+    assert two.grads == steps[-1] and all(torch.equal(a, b) for a, b in zip(held, anew)) and bool(torch.isfinite(held[2]).all())
+    bad = lambda grads, error=ValueError: pytest.raises(error, two.read_gradients, grads)
+    bad(steps[-1][:2])
+    bad([x.float() for x in steps[-1]])
+    bad(steps[-1][::-1])
+    bad([None] + steps[-1][1:])
+    bad([x.cpu() for x in steps[-1]])
+    bad([7] + steps[-1][1:], TypeError)
+    was = [x.clone() for x in anew]
+    two.step()                                 # a refusal has changed nothing
+    one.step()
+    assert all(torch.equal(a, b) for a, b in zip(held, anew)) and not torch.equal(was[2], anew[2])
