@@ -17,7 +17,6 @@ struct Step {
   float beta1, one_minus_beta1, beta2, one_minus_beta2, per_correct1, per_root_correct2, eps, lr;
   double lr_exact;
   uint32_t seed;
-  bool long_memory;                // beta1 > 15/16, see held_m
 };
 
 // The number that decides which way a place of a tensor is rounded: two rounds of multiply and fold.
@@ -46,12 +45,11 @@ __device__ __forceinline__ float held_root(float q, uint32_t x) {
 // 1 - beta1 of itself a step.  At beta1 <= 15/16 that is more than half the grid's spacing from 2^-6 on, where a value has 8 to 15
 // spacings; below, where the spacing stays 2^-9, it is not: 4 spacings at 0.9 are 3.6, and 4 again, for ever, over a root
 // that goes on falling, and so a weight without a gradient would move by up to a third of lr a step.  A magnitude that has
-// become smaller there goes up or down by chance instead, and so reaches zero; at a larger beta1 every value does.
-__device__ __forceinline__ bool held_by_chance(float q, float m, float was, bool long_memory) {
-  return long_memory || (fabsf(q) < 0x1p-6f && fabsf(m) < fabsf(was));
-}
-__device__ __forceinline__ float held_m(float q, uint32_t x) {
-  return copysignf(up_or_down(fabsf(q), chance(x * 0x9E3779B1u)), q);
+// become smaller there goes up or down by chance instead, and so reaches zero; at a larger beta1 (LONG) every value does.
+__device__ __forceinline__ float chance_of_m(uint32_t x) { return chance(x * 0x9E3779B1u); }
+__device__ __forceinline__ float held_m(float q, uint32_t x) { return copysignf(up_or_down(fabsf(q), chance_of_m(x)), q); }
+__device__ __forceinline__ float held_small_m(float q, uint32_t x) {     // below 2^-6
+  return copysignf(floorf(fmaf(fabsf(q), 0x1p9f, chance_of_m(x))) * 0x1p-9f, q);
 }
 
 template <typename T, int N>
@@ -127,7 +125,7 @@ struct Held {
 };
 
 // One block by one wave.
-template <typename G, bool EIGHT>
+template <typename G, bool EIGHT, bool LONG>
 __device__ __forceinline__ void update(const bppsa_adamw_tensor& t, const Held<G, EIGHT>& x, int64_t i, int n, bool full, int lane,
                                        float keep, uint32_t tensor, const Step& c) {
   float theta[4], m[4], v[4], root[4], was[4];
@@ -167,14 +165,14 @@ __device__ __forceinline__ void update(const bppsa_adamw_tensor& t, const Held<G
     for (int k = 0; k < 4; ++k) {
       number[k] = folded(place + k);
       root[k] = held_root(root[k] * iv, number[k]);
-      by_chance[k] = held_by_chance(m[k] * im, m[k], was[k], c.long_memory);
+      by_chance[k] = fabsf(m[k]) < fminf(fabsf(was[k]), 0x1p-6f * sm);
       m[k] *= im;
       any |= by_chance[k];
     }
-    if (any)                                   // hardly a value of a block is so small
+    // hardly a value of a block is so small.  19 layers of width 76: 11.86 us, 11.65 without, 12.3 with held_m() here for both
+    if (LONG || any)
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (by_chance[k]) m[k] = held_m(m[k], number[k]);
+      for (int k = 0; k < 4; ++k) m[k] = LONG ? held_m(m[k], number[k]) : by_chance[k] ? held_small_m(m[k], number[k]) : m[k];
     put4(static_cast<uint8_t*>(t.m) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(m)).v);
     put4(static_cast<uint8_t*>(t.v) + i, n, full, __builtin_bit_cast(Pack<uint8_t, 4>, pack(root)).v);
     if (lane == 0) t.m_scale[i / kBlock] = sm, t.v_scale[i / kBlock] = sv;
@@ -187,7 +185,7 @@ __device__ __forceinline__ void update(const bppsa_adamw_tensor& t, const Held<G
 // A workgroup takes a piece; a wave four blocks of it in a row, four values a lane, and asks for all of a full piece's
 // before it works on the first (a block at a time: 1190 and 854 us instead of 1107 and 638 for 210 M parameters with bf16
 // gradients and copies, moments in 32 and in 8 bits).  Bound by memory, 5.3 TB/s.
-template <typename G, bool EIGHT>
+template <typename G, bool EIGHT, bool LONG>
 __global__ void __launch_bounds__(kThreads)
 adamw_kernel(const bppsa_adamw_tensor* __restrict__ tensors, const bppsa_adamw_piece* __restrict__ pieces, const Step c) {
   const bppsa_adamw_piece piece = pieces[blockIdx.x];
@@ -206,7 +204,7 @@ adamw_kernel(const bppsa_adamw_tensor* __restrict__ tensors, const bppsa_adamw_p
     for (int j = 0; j < BLOCKS; ++j) x[j].get(t, first + start + j * kBlock + lane * 4, 4, true);
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j)
-      update(t, x[j], first + start + j * kBlock + lane * 4, 4, true, lane, keep, (uint32_t)piece.tensor, c);
+      update<G, EIGHT, LONG>(t, x[j], first + start + j * kBlock + lane * 4, 4, true, lane, keep, (uint32_t)piece.tensor, c);
     return;
   }
   for (int at = start; at < count && at < start + BLOCKS * kBlock; at += kBlock) {
@@ -214,7 +212,7 @@ adamw_kernel(const bppsa_adamw_tensor* __restrict__ tensors, const bppsa_adamw_p
     const int n = count - at - lane * 4;       // values that are left for this lane
     Held<G, EIGHT> x;
     x.get(t, i, n, aligned && n >= 4);
-    update(t, x, i, n, aligned && n >= 4, lane, keep, (uint32_t)piece.tensor, c);
+    update<G, EIGHT, LONG>(t, x, i, n, aligned && n >= 4, lane, keep, (uint32_t)piece.tensor, c);
   }
 }
 
@@ -240,13 +238,11 @@ extern "C" bppsa_status bppsa_adamw_step(int n_tensors, const bppsa_adamw_tensor
   if (state_bits != 32 && state_bits != 8) return BPPSA_EUNSUPPORTED;
   if (n_pieces >= 1 << 24) return BPPSA_EOVERFLOW;       // a launch has fewer than 2^32 threads
   const Step c{(float)beta1, (float)(1 - beta1), (float)beta2, (float)(1 - beta2), (float)(1 / (1 - std::pow(beta1, step))),
-               (float)(1 / std::sqrt(1 - std::pow(beta2, step))), (float)eps, (float)lr, lr, seed, beta1 > 0.9375};
+               (float)(1 / std::sqrt(1 - std::pow(beta2, step))), (float)eps, (float)lr, lr, seed};
   return ssm::by_type(grad_type, [&](auto g) -> bppsa_status {
     using G = decltype(g);
-    if (state_bits == 8)
-      adamw_kernel<G, true><<<(unsigned)n_pieces, kThreads, 0, (hipStream_t)stream>>>(tensors, pieces, c);
-    else
-      adamw_kernel<G, false><<<(unsigned)n_pieces, kThreads, 0, (hipStream_t)stream>>>(tensors, pieces, c);
+    const auto kernel = state_bits == 32 ? adamw_kernel<G, false, false> : beta1 > 0.9375 ? adamw_kernel<G, true, true> : adamw_kernel<G, true, false>;
+    kernel<<<(unsigned)n_pieces, kThreads, 0, (hipStream_t)stream>>>(tensors, pieces, c);
     BPPSA_CHECK_LAUNCH();
     return BPPSA_OK;
   });
