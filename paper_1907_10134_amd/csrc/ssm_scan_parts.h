@@ -127,14 +127,30 @@ struct Summary {
 // a time, the 47 of T = 30000 took some 20 us.
 // Where a state grows (a positive A), a span's factor may pass the largest float though its product with a small state does
 // not: three factors of a third of the exponent, one after the other, are as large as a product of floats can be made.
+// Such states go one span at a time, by a loop that is short: both ways eight at a time cost a kernel that joins one span
+// 15.6 us instead of 14.5 (T = 64, B = 24, D = 254, N = 64).
 template <int H>
 __device__ __forceinline__ void join_spans(const Summary& sum, int first, int step, int count, int B, int b, int waves, int w,
                                            int D, int d, const float (&A2)[H], float (&h)[H]) {
   constexpr int AHEAD = 8;
-  bool grow = false;
+  bool grows = false;
 #pragma unroll
-  for (int i = 0; i < H; ++i) grow |= A2[i] > 0.0f;
-  const bool any_grows = __any(grow);
+  for (int i = 0; i < H; ++i) grows |= A2[i] > 0.0f;
+  if (__any(grows)) {
+#pragma unroll 1
+    for (int k = 0; k < count; ++k) {
+      const int at = first + step * k;
+      float end[H];
+      get(sum.ends + state_at(H, at, B, b, waves, w, D, d), end);
+      const float third = sum.sums[((int64_t)at * B + b) * D + d] * (1.0f / 3.0f);
+#pragma unroll
+      for (int i = 0; i < H; ++i) {
+        const float factor = exp2_fast(A2[i] * third);
+        h[i] = h[i] == 0.0f ? end[i] : fmaf(h[i] * factor * factor, factor, end[i]);      // zero stays zero
+      }
+    }
+    return;
+  }
   for (int k = 0; k < count; k += AHEAD) {
     float end[AHEAD][H], s[AHEAD];
 #pragma unroll
@@ -147,15 +163,7 @@ __device__ __forceinline__ void join_spans(const Summary& sum, int first, int st
     for (int j = 0; j < AHEAD; ++j) {
       if (k + j >= count) break;
 #pragma unroll
-      for (int i = 0; i < H; ++i) {
-        const float x = A2[i] * s[j];
-        if (any_grows) {
-          const float third = exp2_fast(x * (1.0f / 3.0f));
-          h[i] = h[i] == 0.0f ? end[j][i] : fmaf(h[i] * third * third, third, end[j][i]);      // zero stays zero
-        } else {
-          h[i] = fmaf(exp2_fast(x), h[i], end[j][i]);
-        }
-      }
+      for (int i = 0; i < H; ++i) h[i] = fmaf(exp2_fast(A2[i] * s[j]), h[i], end[j][i]);
     }
   }
 }
