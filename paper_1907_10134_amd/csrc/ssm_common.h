@@ -39,7 +39,8 @@ __device__ __forceinline__ float value(uint32_t bits) {
 }
 
 // The rows of an array that a wave walks through: a lane's address in vector registers, moved on by a stride in scalar ones.
-// (Both in scalar registers, with the lane's offset added by the access, left too few of them for Bm and Cm.)
+// (Both in scalar registers, with the lane's offset added by the access, left too few of them while Bm and Cm were scalars too; not
+// tried since those are in LDS.)
 template <typename E>
 struct Walk {
   uint64_t lane;

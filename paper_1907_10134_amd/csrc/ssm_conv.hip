@@ -7,12 +7,14 @@ namespace {
 
 using namespace ssm;
 
-// All kernels here are bound by memory.  A thread takes V neighbouring channels (16 bytes forward, 8 backward, where a
-// window of inputs and one of gradients and the sums of the weights' gradients have to stay in registers too) and a span
-// of steps, the window of the last W inputs in registers.  The last thread of a row starts early enough to have V channels
-// too and repeats some of its neighbour's, with the same results; fewer than V channels go one to a thread.
-// T = 4096, B = 4, D = 4096, W = 4, bf16: forward 50 us (5.3 TB/s) on the same buffers again, 57 on others each time; with 8 bytes a
-// lane 71, with 128 registers, which spills, 84.
+// The forward kernels are bound by memory; the backward one is not: 25 us at T = 1000, B = 16, D = 641, W = 4, f16, whose bytes
+// would take 10, with 706 vector instructions for 16 values, of which 147 move the windows on and 61 make row addresses.
+// A thread takes V neighbouring channels (16 bytes forward, 8 backward, where a window of inputs and one of gradients and the
+// sums of the weights' gradients have to stay in registers too) and a span of steps, the window of the last W inputs in
+// registers.  The last thread of a row starts early enough to have V channels too and repeats some of its neighbour's, with
+// the same results; fewer than V channels go one to a thread.
+// T = 4096, B = 4, D = 4096, W = 4, bf16: forward 49 us (5.4 TB/s) on the same buffers again, 57 on others each time; with 8
+// bytes a lane 71, with 128 registers, which spills, 84.
 constexpr int kAhead = 4;        // rows that are asked for together
 constexpr int kTogether = 4;     // spans of a workgroup of the backward pass
 

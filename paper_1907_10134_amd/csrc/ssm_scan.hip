@@ -10,8 +10,9 @@ using namespace ssm;
 // the states in LDS, and each wave finishes its ROWS of outputs.  Inputs of the next pass are prepared and outputs of the
 // last one finished beside a pass, so there is one barrier a pass.
 // Bound by issue: a step of four states takes 4 exp (two slots each) and 16 products and multiply-adds, a step and channel some
-// 45 slots beside them for softplus, gate and sums.  T = 30000, B = 1, D = 2048, N = 16, bf16, gated: 311 us with the
-// vector unit 88 % busy (and 230 us, 83 %, for the summaries); 0.49 GB of inputs and outputs would take 96 us.
+// 45 slots beside them for softplus, gate and sums.  T = 30000, B = 1, D = 2048, N = 16, bf16, gated: 310 us with the
+// vector unit 88 % busy (and 228 us, 84 %, for the summaries) by a counter that shows 94 % for nothing but one exp and four
+// multiply-adds in turn; 0.49 GB of inputs and outputs would take 96 us.
 template <typename E, int WAVES, int H, bool SUMMARY, bool GATE>
 __global__ void __launch_bounds__(WAVES * 64, WAVES <= 12 ? 6 : 4)      // at least so many waves a SIMD
 scan_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, const Summary sum,

@@ -187,8 +187,8 @@ scan_backward_summary_kernel(const Layer<E> l, Rows<const E> dy, const Summary s
 // of its states, then walks back; the sums over the states go through LDS (s1 = sum g B, s2 = sum w h A, and with a gate
 // sum C h), those over the channels through registers.
 // Bound by issue: a step of four states takes 20 slots to find a and h again, 36 for the walk back and 16 for the sums over
-// channels, a step and channel some 130 beside them.  T = 4096, B = 4, D = 4096, N = 16, bf16, gated: 879 us with the vector
-// unit 89 % busy (and 221 us, 88 %, for the summaries); its 1.6 GB would take 0.31 ms.
+// channels, a step and channel some 130 beside them.  T = 4096, B = 4, D = 4096, N = 16, bf16, gated: 874 us with the vector
+// unit 88 % busy (and 218 us, 87 %, for the summaries); its 1.6 GB would take 0.31 ms.
 template <typename E, int WAVES, int H, bool GATE>
 __global__ void __launch_bounds__(WAVES * 64, WAVES <= 12 ? 3 : 4)
 scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ states, const Summary sum, const Spans spans,
@@ -387,8 +387,8 @@ scan_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict
     at_bc[lane] = over_steps<H>(step_sum, lane);
     at_bc -= WAVES * 64;
     if (p) prepare(first - PASS, buffer ^ 1);
-    // here: beside finish() the kernels of sixteen waves would spill 66 values, not 15 (T = 2048, B = 4, D = 2048, N = 64: 1041 us,
-    // 1663 without this branch and 46)
+    // here: beside finish() the kernels of sixteen waves would spill 66 values, not 13 (T = 2048, B = 4, D = 2048, N = 64: 1034 us,
+    // 1663 without this branch and with 46)
     if (p && p % kRun == 0) total(p == (passes - 1) / kRun * kRun);
     __syncthreads();
   }
