@@ -145,3 +145,26 @@ def test_sixteen_waves_and_many_spans(N, dtype, gate, given, ragged):
     """The widest workgroups with time in spans: their summaries and joins."""
     from test_gpu_ssm import test_scan_and_gradients as whole
     whole((1100, 2, 40, N, 1), dtype, gate, given, ragged, "bt")
+
+
+@pytest.mark.parametrize("T", (504, 513, 520, 1032))
+@pytest.mark.parametrize("N,gate", [(1, True), (20, False)])
+def test_sums_in_runs_of_512_steps(T, N, gate):
+    """One span of 63 to 129 passes of eight steps, ragged: the runs' ends, a sample that ends inside one and an empty one."""
+    import torch
+    import paper_1907_10134_amd as bp
+    B = 4100 if N == 1 else 1040                         # samples enough for the device without spans of time
+    c, ref, dy, dy_ref = _case(T, T, B, 1, N, 1, "float32", gate, True, True, "tb")
+    c["lengths"][1], c["lengths"][2], c["lengths"][3] = T, min(T, 513), min(T, 520)
+    for k in ("u", "dt", "Bm", "Cm") + (("z",) if gate else ()):
+        c[k].nan_to_num_(nan=0.25)
+    dy.nan_to_num_(nan=0.25)
+    ref = {k: _f64(v) for k, v in c.items()}
+    states, dh0 = bp.ssm_scan_states(T, B, 1, N), torch.empty((B, 1, N), device="cuda")
+    bp.ssm_scan(**c, states=states)
+    g = bp.ssm_scan_backward(dy, states=states, dh0=dh0, **c)
+    want = ssm.scan_backward(_f64(dy), **ref)
+    along = 512 + T // 512 + B // 4                      # a run, the runs, a quarter of the samples
+    for name in ("dA", "dskip", "ddt_bias"):
+        _close(getattr(g, name), want[name], "float32", name, sums=along)
+    _close(dh0, want["dh0"], "float32", "dh0")
