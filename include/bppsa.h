@@ -595,6 +595,53 @@ bppsa_status bppsa_ssm_conv_step(const bppsa_conv* conv, const bppsa_rows* y, vo
                                  const int32_t* slots, void* stream);
 
 /*
+ * A gated linear recurrence, one state a channel.  With rho = sigmoid(r[t,b,d] + r_bias[d]), iota = sigmoid(i[t,b,d] +
+ * i_bias[d]) and a = exp(-decay[d] rho), for every sample b and channel d
+ *     h[t] = a h[t-1] + sqrt(1 - a^2) iota x[t,b,d],     y[t,b,d] = h[t] * ( z ? silu(z[t,b,d]) : 1 )
+ * x, r, i, z are [T,B,D]; decay [D] (not negative), r_bias, i_bias [D], h0 [B,D] fp32.  z.data, r_bias, i_bias, h0 and
+ * lengths may be NULL (no gate, 0, 0, zeros, all of T); lengths, outputs behind an end and the last state as in bppsa_ssm.
+ * The state is held in fp32.  Sizes that no launch can hold are BPPSA_EOVERFLOW before anything is launched (D over 2^24, 2^23
+ * and more tiles of 64 steps and 64 channels over all samples); the byte counts of such sizes are 0.
+ */
+typedef struct bppsa_gated {
+  int32_t T, B, D, type;
+  bppsa_rows x, r, i, z;
+  const float *decay, *r_bias, *i_bias, *h0;
+  const int32_t* lengths;
+} bppsa_gated;
+
+/*
+ * Forward over whole sequences.  Writes y [T,B,D]; h_last [B,D], the state after each sample's last token, if not NULL;
+ * `states`, bppsa_gated_scan_states_bytes bytes of device memory on a multiple of 16 in a layout of the library's own, if
+ * not NULL: what the backward pass reads (4 bytes for each channel and 64 steps).  The workspace may be of size 0.  The
+ * results are the same bits on every call with the same sizes.
+ */
+size_t bppsa_gated_scan_states_bytes(int T, int B, int D);
+size_t bppsa_gated_scan_workspace_bytes(int T, int B, int D);
+bppsa_status bppsa_gated_scan(const bppsa_gated* layer, const bppsa_rows* y, float* h_last, void* states,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of sum(y dy) + sum(h_last dh_last); dh_last [B,D] may be NULL (zero).  layer and states are those of the forward
+ * call.  dx, dr, di, dz are [T,B,D] of the activations' type, written in full; dz.data is NULL where there is no gate.
+ * ddecay, dr_bias, di_bias [D] are overwritten; the biases' may be NULL, and dh0 [B,D] too.  Where 1 - a^2 is zero (a decay
+ * of zero) the root's derivative, which is infinite, counts as zero.  Sums over samples and time run in a fixed order: the
+ * same bits on every call.
+ */
+typedef struct bppsa_gated_grads {
+  bppsa_rows dx, dr, di, dz;
+  float *ddecay, *dr_bias, *di_bias, *dh0;
+} bppsa_gated_grads;
+size_t bppsa_gated_scan_backward_workspace_bytes(int T, int B, int D);
+bppsa_status bppsa_gated_scan_backward(const bppsa_gated* layer, const bppsa_rows* dy, const float* dh_last, const void* states,
+                                       const bppsa_gated_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token of each of B streams (layer->T = 1; h0 and lengths NULL): state [slots_in_state,D] is advanced in place; slots as
+ * in bppsa_ssm_scan_step. */
+bppsa_status bppsa_gated_scan_step(const bppsa_gated* layer, const bppsa_rows* y, float* state, int slots_in_state,
+                                   const int32_t* slots, void* stream);
+
+/*
  * One AdamW update (decoupled weight decay) of many tensors by one launch:
  *     m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
  *     theta <- theta (1 - lr decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps).

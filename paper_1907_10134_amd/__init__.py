@@ -17,4 +17,8 @@ from .ssm import (  # noqa: F401
     SsmGrads, SsmConvGrads, ssm_scan, ssm_scan_states, ssm_scan_workspace_bytes, ssm_scan_backward,
     ssm_scan_backward_workspace_bytes, ssm_scan_step, ssm_conv, ssm_conv_backward, ssm_conv_step,
 )
+from .gated import (  # noqa: F401
+    GatedGrads, gated_scan, gated_scan_states, gated_scan_workspace_bytes, gated_scan_backward,
+    gated_scan_backward_workspace_bytes, gated_scan_step,
+)
 from .optim import AdamW  # noqa: F401

@@ -1,0 +1,416 @@
+"""GPU: the gated linear recurrence against the fp64 oracle."""
+import numpy as np
+import pytest
+
+from oracle import gated
+
+pytestmark = pytest.mark.gpu
+
+TYPES = ("float32", "bfloat16", "float16")
+
+
+def _bound(ref, dtype, memory, sums):
+    """Half a step of the output's type relative to the value, and fp32 arithmetic relative to the largest of the tensor: a
+    step's decay and input are good to 6 roundings of 2^-24 each (two sigmoids, an exponential whose argument is rounded, the
+    root and two products), each kept over a state's memory of `memory` steps, and `sums` of so many fp32 parts in a row."""
+    import torch
+    half = torch.finfo(getattr(torch, dtype)).eps / 2
+    return half * np.abs(ref) + (6 * memory + sums) * 2.0 ** -24 * max(np.max(np.abs(ref), initial=0.0), 2.0 ** -14)
+
+
+def _close(got, ref, dtype, what, memory=50, sums=8):
+    got = got.detach().double().cpu().numpy()
+    assert got.shape == ref.shape, (what, got.shape, ref.shape)
+    assert np.all(np.isfinite(got)), what
+    off = np.abs(got - ref)
+    worst = np.max(off - _bound(ref, dtype, memory, sums), initial=0.0)
+    assert worst <= 0, (what, float(np.max(off)), float(np.max(np.abs(ref), initial=0.0)))
+
+
+def _act(rng, shape, dtype, order="tb", wide=0, at=0, scale=1.0):
+    """A tensor [T, B, C] on the GPU, as a column slice of a wider one if `wide`."""
+    import torch
+    T, B, C = shape
+    full = (B, T, wide or C) if order == "bt" else (T, B, wide or C)
+    x = torch.from_numpy(rng.standard_normal(full) * scale).to(getattr(torch, dtype)).cuda()
+    if order == "bt":
+        x = x.transpose(0, 1)
+    return x[:, :, at:at + C]
+
+
+def _f64(x):
+    return x.detach().double().cpu().numpy()
+
+
+def _f32(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda()
+
+
+def _case(seed, T, B, D, dtype, gate, given, ragged, order):
+    """Decays of 0.04 to 2 and gates near one half: a state's memory, 1 / (1 - a), is 50 steps or fewer."""
+    import torch
+    rng = np.random.default_rng(seed)
+    gates = _act(rng, (T, B, 2 * D + 1), dtype, order, scale=0.5)
+    c = {"x": _act(rng, (T, B, D), dtype, order), "r": gates[..., :D], "i": gates[..., D + 1:],
+         "decay": _f32(np.exp(rng.uniform(np.log(0.04), np.log(2.0), D)))}
+    if gate:
+        c["z"] = _act(rng, (T, B, D), dtype, order, wide=2 * D + 1, at=D)
+    if given:
+        c.update(r_bias=_f32(0.5 * rng.standard_normal(D)), i_bias=_f32(rng.standard_normal(D)), h0=_f32(rng.standard_normal((B, D))))
+    dy = _act(rng, (T, B, D), dtype, order)
+    dh_last = _f32(rng.standard_normal((B, D))) if given else None
+    if ragged:
+        n = rng.integers(0, T + 1, B)
+        n[0] = T // 2
+        n[-1] = 0 if B > 1 else 1
+        c["lengths"] = torch.from_numpy(n.astype(np.int32)).cuda()
+    ref = {k: _f64(v) for k, v in c.items()}
+    dy_ref = _f64(dy)
+    if ragged:                                 # what lies behind a sample's end must not be read: NaN there
+        for b, k in enumerate(ref["lengths"].astype(int)):
+            for name in ("x", "r", "i") + (("z",) if gate else ()):
+                c[name][k:, b] = float("nan")
+                ref[name][k:, b] = 0.0
+            dy[k:, b] = float("nan")
+            dy_ref[k:, b] = 0.0
+    return c, ref, dy, dy_ref, dh_last
+
+
+SIZES = [(1, 1, 1), (1, 3, 2), (2, 3, 5), (7, 1, 64), (8, 2, 65), (16, 2, 127), (17, 4, 130), (63, 3, 66), (64, 2, 128), (65, 2, 129),
+         (127, 1, 3), (128, 2, 40), (129, 2, 256), (257, 1, 129), (1000, 2, 41), (700, 1, 320), (2111, 1, 33), (515, 5, 8), (4100, 1, 2)]
+
+
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gate,given,ragged,order", [(False, False, False, "tb"), (True, True, False, "bt"),
+                                                     (True, False, True, "tb"), (False, True, True, "bt")])
+def test_scan_and_gradients(size, dtype, gate, given, ragged, order):
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D = size
+    c, ref, dy, dy_ref, dh_last = _case(sum(size) + len(dtype), T, B, D, dtype, gate, given, ragged, order)
+    y_ref, last_ref, _ = gated.scan(**ref)
+    h_last = torch.full((B, D), float("nan"), device="cuda")
+    y = bp.gated_scan(**c, h_last=h_last)
+    _close(y, y_ref, dtype, "y")
+    _close(h_last, last_ref, "float32", "h_last")
+    states = bp.gated_scan_states(T, B, D)
+    y2 = bp.gated_scan(**c, states=states)
+    assert torch.equal(y, y2)
+    dh0 = torch.full((B, D), float("nan"), device="cuda")
+    g = bp.gated_scan_backward(dy, states=states, dh_last=dh_last, dh0=dh0, **c)
+    want = gated.scan_backward(dy_ref, **ref, dh_last=None if dh_last is None else _f64(dh_last))
+    for name in ("dx", "dr", "di") + (("dz",) if gate else ()):
+        _close(getattr(g, name), want[name], dtype, name)
+    _close(dh0, want["dh0"], "float32", "dh0")
+    assert (g.dz is None) == (not gate) and (g.dr_bias is None) == (not given) and (g.di_bias is None) == (not given)
+    # sums over time and samples, whose parts are up to 64 steps in a row
+    for name in ("ddecay",) + (("dr_bias", "di_bias") if given else ()):
+        _close(getattr(g, name), want[name], "float32", name, sums=64 * max(1.0, _spread(c, ref, dy_ref, want, name)))
+    again = bp.gated_scan_backward(dy, states=states, dh_last=dh_last, dh0=torch.empty_like(dh0), **c)
+    assert all(torch.equal(a, b) for a, b in zip(g[:7], again[:7]) if a is not None), "the same bits on every call"
+
+
+def _spread(c, ref, dy_ref, want, name):
+    """How much larger than the largest sum the largest sum of magnitudes is: roundings are relative to the terms, which cancel."""
+    terms = {"ddecay": "dr", "dr_bias": "dr", "di_bias": "di"}[name]
+    t = np.abs(want[terms])
+    if name == "ddecay":
+        sig = 1 / (1 + np.exp(ref["r"] + (ref["r_bias"] if "r_bias" in ref else 0.0)))       # 1 - rho
+        t = t / (ref["decay"] * sig)
+    return float(np.max(t.sum((0, 1))) / max(np.max(np.abs(want[name])), 2.0 ** -14))
+
+
+def test_gradients_against_differences():
+    """Central differences of the kernels' own forward pass in float32: the loss is a sum of 6144 terms of order one, good to
+    1e-6 of its 100 or so, over 2e-2: 1e-2 of the largest gradient of each input."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D = 96, 2, 32
+    c, _, dy, _, dh_last = _case(11, T, B, D, "float32", True, True, False, "tb")
+    states = bp.gated_scan_states(T, B, D)
+    bp.gated_scan(**c, states=states)
+    g = bp.gated_scan_backward(dy, states=states, dh_last=dh_last, dh0=torch.empty((B, D), device="cuda"), **c)
+
+    def loss():
+        last = torch.empty((B, D), device="cuda")
+        return float((bp.gated_scan(**c, h_last=last).double() * dy.double()).sum() + (last.double() * dh_last.double()).sum())
+
+    for name, grad in (("x", g.dx), ("r", g.dr), ("i", g.di), ("z", g.dz), ("decay", g.ddecay), ("r_bias", g.dr_bias),
+                       ("i_bias", g.di_bias), ("h0", g.dh0)):
+        at = tuple(int(k) for k in np.unravel_index(int(grad.abs().argmax()), grad.shape))
+        was = float(c[name][at])
+        h = 1e-2 if name != "decay" else 1e-2 * was
+        c[name][at] = was + h
+        up = loss()
+        c[name][at] = was - h
+        down = loss()
+        c[name][at] = was
+        want = float(grad[at])
+        assert abs((up - down) / (2 * h) - want) <= 1e-2 * abs(want) + 1e-2, (name, (up - down) / (2 * h), want)
+
+
+def test_gates_at_their_ends():
+    """Decays of 0, of 1e-6 and of 100, gate inputs of -200 to 200 and the lowest value of the type: nothing is lost or infinite."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D = 80, 2, 64
+    c, _, dy, _, dh_last = _case(5, T, B, D, "float32", True, True, False, "tb")
+    c["decay"][:16], c["decay"][16:32], c["decay"][32:40] = 0.0, 1e-6, 100.0
+    c["r"][:, :, ::5], c["r"][:, :, 1::5] = -200.0, 200.0
+    c["i"][:, :, ::3], c["i"][:, :, 1::7] = -200.0, 200.0
+    c["z"][:, :, 3], c["z"][:, :, 4], c["z"][:, :, 5] = -80.0, 200.0, torch.finfo(torch.float32).min
+    c["r"][:, :, 6] = torch.finfo(torch.float32).min
+    ref = {k: _f64(v) for k, v in c.items()}
+    states, h_last = bp.gated_scan_states(T, B, D), torch.empty((B, D), device="cuda")
+    y_ref, last, _ = gated.scan(**ref)
+    # a memory of T steps here
+    _close(bp.gated_scan(**c, states=states, h_last=h_last), y_ref, "float32", "y", memory=T)
+    _close(h_last, last, "float32", "h_last", memory=T)
+    g = bp.gated_scan_backward(dy, states=states, dh_last=dh_last, dh0=torch.empty((B, D), device="cuda"), **c)
+    want = gated.scan_backward(_f64(dy), **ref, dh_last=_f64(dh_last))
+    for name in ("dx", "di", "dr", "dz"):
+        _close(getattr(g, name), want[name], "float32", name, memory=T)
+    # the derivative of the root grows as 1 / m where the decay is small: each channel by itself
+    for k in range(D):
+        _close(g.ddecay[k:k + 1], want["ddecay"][k:k + 1], "float32", "ddecay[%d]" % k, memory=T,
+               sums=64 * T * B)
+
+
+def test_long_memory_from_a_state():
+    """Decays of 1e-5: the state of 3000 steps before is still there."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D = 3000, 1, 130
+    c, ref, _, _, _ = _case(12, T, B, D, "bfloat16", False, True, False, "tb")
+    c["decay"].fill_(1e-5)
+    ref["decay"] = _f64(c["decay"])
+    h_last = torch.empty((B, D), device="cuda")
+    y = bp.gated_scan(**c, h_last=h_last)
+    want, last, _ = gated.scan(**ref)
+    # the products of 3000 decays, each rounded once: 3000 of 2^-24, and as many additions
+    _close(y, want, "bfloat16", "y", memory=T)
+    _close(h_last, last, "float32", "h_last", memory=T)
+
+
+def test_a_nan_stays_in_its_channel():
+    """From its step on, over the ends of tiles, also where decays have become zero in between."""
+    import torch
+    import paper_1907_10134_amd as bp
+    c, _, _, _, _ = _case(6, 700, 2, 96, "float32", False, True, False, "tb")
+    c["decay"][70:72] = 60.0
+    c["x"][50, 1, 70], c["x"][50, 1, 60] = float("nan"), float("inf")
+    y = bp.gated_scan(**c)
+    bad = ~torch.isfinite(y)
+    assert bool(torch.isnan(y[50:, 1, 70]).all()) and int(bad[:, :, 70].sum()) == 650
+    assert float(y[50, 1, 60]) in (float("inf"), float("-inf")) and int(bad[:, 0].sum()) == 0 and int(bad.sum() - bad[:, :, 60].sum()) == 650
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,D,gate,slots", [(1, 1, False, 1), (3, 70, True, 9), (5, 64, True, 5), (2, 130, False, 4), (67, 96, True, 70),
+                                            (4, 2049, False, 8)])
+def test_scan_step(dtype, B, D, gate, slots):
+    import torch
+    import paper_1907_10134_amd as bp
+    c, ref, _, _, _ = _case(B + D, 1, B, D, dtype, gate, True, False, "tb")
+    del c["h0"], ref["h0"]
+    rng = np.random.default_rng(1)
+    state = _f32(rng.standard_normal((slots, D)))
+    at = rng.permutation(slots)[:B].astype(np.int32)
+    if B > 2:
+        at[1], at[2] = -1, slots                  # rows of no stream
+    on = (at >= 0) & (at < slots)
+    before = _f64(state)
+    one = {k: v[0] if k in ("x", "r", "i", "z") else v for k, v in c.items()}
+    y = bp.gated_scan_step(state=state, slots=torch.from_numpy(at).cuda(), **one)
+    ref["h0"] = np.zeros((B, D))
+    ref["h0"][on] = before[at[on]]
+    y_ref, last, _ = gated.scan(**ref)
+    y_ref[0, ~on] = 0.0
+    want = before.copy()
+    want[at[on]] = last[on]
+    _close(y, y_ref[0], dtype, "y", memory=1)
+    _close(state, want, "float32", "state", memory=1)
+    untouched = np.setdiff1d(np.arange(slots), at[on])
+    assert np.array_equal(_f64(state)[untouched], before[untouched])
+
+
+def test_tokens_one_by_one_are_the_sequence():
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D = 70, 3, 48
+    c, _, _, _, _ = _case(21, T, B, D, "float32", True, True, False, "tb")
+    want_last = torch.empty((B, D), device="cuda")
+    want = bp.gated_scan(**c, h_last=want_last)
+    state = c.pop("h0").clone()
+    for t in range(T):
+        y = bp.gated_scan_step(state=state, **{k: v[t] if k in ("x", "r", "i", "z") else v for k, v in c.items()})
+        assert float((y - want[t]).abs().max()) < 6 * 50 * 2.0 ** -24 * float(want.abs().max())
+    assert float((state - want_last).abs().max()) < 6 * 50 * 2.0 ** -24 * float(want_last.abs().max())
+
+
+def test_pieces_are_differentiated_through_their_seam():
+    """A sequence in two pieces, the second's dh0 the first's dh_last: the gradients of the whole."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D, cut = 200, 2, 40, 90
+    c, _, dy, _, dh_last = _case(22, T, B, D, "float32", True, True, False, "tb")
+    part = lambda a, b: {k: v[a:b] if k in ("x", "r", "i", "z") else v for k, v in c.items()}
+    states = bp.gated_scan_states(T, B, D)
+    bp.gated_scan(**c, states=states)
+    dh0 = torch.empty((B, D), device="cuda")
+    want = bp.gated_scan_backward(dy, states=states, dh_last=dh_last, dh0=dh0, **c)
+    s1, s2 = bp.gated_scan_states(cut, B, D), bp.gated_scan_states(T - cut, B, D)
+    mid, dmid, d0 = (torch.empty((B, D), device="cuda") for _ in range(3))
+    bp.gated_scan(**part(0, cut), states=s1, h_last=mid)
+    second = dict(part(cut, T), h0=mid)
+    bp.gated_scan(**second, states=s2)
+    g2 = bp.gated_scan_backward(dy[cut:], states=s2, dh_last=dh_last, dh0=dmid, **second)
+    g1 = bp.gated_scan_backward(dy[:cut], states=s1, dh_last=dmid, dh0=d0, **part(0, cut))
+    tol = 6 * 50 * 2.0 ** -24
+    for name in ("dx", "dr", "di", "dz"):
+        a, b = torch.cat((getattr(g1, name), getattr(g2, name))), getattr(want, name)
+        assert float((a - b).abs().max()) <= tol * float(b.abs().max()), name
+    assert float((d0 - dh0).abs().max()) <= tol * float(dh0.abs().max())
+    assert float((g1.ddecay + g2.ddecay - want.ddecay).abs().max()) <= 64 * tol * float(want.ddecay.abs().max())
+
+
+def test_rows_further_apart_than_32_bits_count():
+    """Rows 2^28 elements apart, nine of them: the last lies 2^31 elements behind the first."""
+    import torch
+    import paper_1907_10134_amd as bp
+    rng = np.random.default_rng(2)
+    T, D = 9, 64
+    wide = torch.empty((T, 1, 1 << 28), dtype=torch.bfloat16, device="cuda")
+    put = lambda at: wide[:, :, at:at + D].copy_(_act(rng, (T, 1, D), "bfloat16"))
+    x, r, i, dy = put(0), put(64), put(128), put(192)
+    decay = torch.rand(D, device="cuda") + 0.1
+    out = wide[:, :, 256:320]
+    states = bp.gated_scan_states(T, 1, D)
+    bp.gated_scan(x, r, i, decay, y=out, states=states)
+    ref = dict(x=_f64(x), r=_f64(r), i=_f64(i), decay=_f64(decay))
+    _close(out, gated.scan(**ref)[0], "bfloat16", "y")
+    g = bp.gated_scan_backward(dy, x, r, i, decay, states)
+    want = gated.scan_backward(_f64(dy), **ref)
+    for name in ("dx", "dr", "di"):
+        _close(getattr(g, name), want[name], "bfloat16", name)
+
+
+def test_inputs_that_repeat_a_row():
+    """Broadcast inputs, strides of zero: read as they say; the gradient is that of each place.  An output may not be one."""
+    import torch
+    import paper_1907_10134_amd as bp
+    c, ref, dy, dy_ref, _ = _case(8, 20, 3, 40, "float32", False, False, False, "tb")
+    c["r"], c["x"] = c["r"][:1].expand(20, 3, 40), c["x"][:, :1].expand(20, 3, 40)
+    ref["r"], ref["x"] = _f64(c["r"]), _f64(c["x"])
+    states = bp.gated_scan_states(20, 3, 40)
+    _close(bp.gated_scan(**c, states=states), gated.scan(**ref)[0], "float32", "y")
+    g = bp.gated_scan_backward(dy, states=states, **c)
+    want = gated.scan_backward(dy_ref, **ref)
+    _close(g.dx, want["dx"], "float32", "dx")
+    _close(g.dr, want["dr"], "float32", "dr")
+    with pytest.raises(bp.BppsaError):
+        bp.gated_scan(**c, y=torch.empty((1, 3, 40), device="cuda").expand(20, 3, 40))
+
+
+def test_rows_behind_an_end_of_an_output_with_gaps():
+    """The output as a column slice of a wider array: zeros behind each sample's end, and nothing beside the slice."""
+    import torch
+    import paper_1907_10134_amd as bp
+    c, ref, _, _, _ = _case(9, 150, 3, 33, "bfloat16", True, True, True, "bt")
+    wide = torch.full((3, 150, 80), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = wide.transpose(0, 1)[:, :, 20:53]
+    bp.gated_scan(**c, y=out)
+    _close(out, gated.scan(**ref)[0], "bfloat16", "y")
+    assert bool((wide[:, :, :20] == 7).all()) and bool((wide[:, :, 53:] == 7).all())
+
+
+def test_another_stream_and_two_graphs():
+    """The training calls on a stream of their own, then two captured graphs that are replayed in turn between eager calls: the
+    eager bits each time."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D = 900, 2, 200
+    cases = [_case(s, T, B, D, "bfloat16", True, True, True, "tb") for s in (31, 32)]
+    held = [(bp.gated_scan_states(T, B, D), torch.empty((B, D), device="cuda"), torch.empty((B, D), device="cuda")) for _ in cases]
+
+    def work(k, stream=None):
+        c, _, dy, _, dh_last = cases[k]
+        states, last, dh0 = held[k]
+        y = bp.gated_scan(**c, states=states, h_last=last, stream=stream)
+        g = bp.gated_scan_backward(dy, states=states, dh_last=dh_last, dh0=dh0, stream=stream, **c)
+        return [y, last, *g]
+
+    want = [[x.clone() for x in work(k)] for k in (0, 1)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = work(0, side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want[0]))
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work(0), work(1)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, outs = [], []
+    for k in (0, 1):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(work(k))
+        graphs.append(graph)
+    for _ in range(4):
+        for k in (0, 1):
+            for x in outs[k]:
+                x.zero_()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            assert all(torch.equal(a, b) for a, b in zip(outs[k], want[k]))
+            assert all(torch.equal(a, b) for a, b in zip(work(k), want[k]))
+
+
+def test_two_streams_at_once():
+    """Long sequences on two streams side by side: neither waits for the other, both are right."""
+    import torch
+    import paper_1907_10134_amd as bp
+    T, B, D = 6000, 1, 256
+    c, _, _, _, _ = _case(41, T, B, D, "bfloat16", True, True, False, "tb")
+    want = bp.gated_scan(**c)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[bp.gated_scan(**c, stream=s) for s in streams] for _ in range(5)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for pair in got for y in pair)
+
+
+def test_refusals():
+    import torch
+    import paper_1907_10134_amd as bp
+    c, _, dy, _, _ = _case(10, 8, 2, 16, "float32", True, True, False, "tb")
+    bad = lambda **k: pytest.raises(ValueError, bp.gated_scan, **dict(c, **k))
+    bad(x=c["x"].double())
+    bad(r=c["r"].half())
+    bad(r=c["r"][:4])
+    bad(decay=c["decay"][:8])
+    bad(decay=c["decay"].double())
+    bad(h0=c["h0"][:1])
+    bad(z=c["z"][:, :1])
+    bad(lengths=torch.ones(2, dtype=torch.int64, device="cuda"))
+    bad(lengths=torch.ones(3, dtype=torch.int32, device="cuda"))
+    bad(states=torch.empty(8, dtype=torch.uint8, device="cuda"))
+    bad(x=torch.empty((8, 2, 32), device="cuda")[:, :, ::2])
+    bad(x=c["x"].cpu())
+    bad(i_bias=c["i_bias"].cpu())
+    with pytest.raises(bp.BppsaError):
+        bp.gated_scan(c["x"][:0], c["r"][:0], c["i"][:0], c["decay"])
+    with pytest.raises(bp.BppsaError):
+        bp.gated_scan(**c, h_last=c["h0"])
+    with pytest.raises(TypeError):
+        bp.gated_scan(c["x"], c["r"], c["i"], None)
+    with pytest.raises(TypeError):
+        bp.gated_scan_backward(dy, c["x"], c["r"], c["i"], c["decay"], None)
+    with pytest.raises(ValueError):
+        bp.gated_scan_step(c["x"][0], c["r"][0], c["i"][0], c["decay"], torch.empty((1, 16), device="cuda"))
+    with pytest.raises(ValueError):
+        bp.gated_scan_step(c["x"][0], c["r"][0], c["i"][0], c["decay"], torch.empty((4, 17), device="cuda"))
