@@ -682,6 +682,87 @@ bppsa_status bppsa_adamw_step(int n_tensors, const bppsa_adamw_tensor* tensors, 
                               const bppsa_adamw_piece* pieces, int grad_type, int state_bits, int step, double lr,
                               double beta1, double beta2, double eps, uint32_t seed, void* stream);
 
+/*
+ * The loss of a student against a teacher's top logits, and its gradient for the student's logits.  For every row (t,b), with
+ * q = softmax(logits / temperature) over the V tokens and the K entries (index c_k, logit t_k) of the teacher, of which one
+ * with an index outside [0, V) or a logit of minus infinity does not count:
+ *     p_k = exp(t_k / temperature) / sum of those        where top_norm is NULL (the entries are all there is),
+ *     p_k = exp(t_k / temperature - top_norm[t,b])       otherwise: the teacher's logarithm of the sum over ITS vocabulary;
+ *                                                        p_0 = max(0, 1 - sum p_k) is the share of all other tokens,
+ *     soft = sum_k p_k log(p_k / q[c_k]) + p_0 log(p_0 / q_0),   q_0 the sum of q over the tokens that are no entry
+ *     loss = weight * ( (1 - hard) temperature^2 soft  -  hard log softmax(logits)[target] ).
+ * A term with p = 0 is 0, and so is that of p_0 where the other tokens' sum is below 2^-126 of the largest term.  An index may
+ * come twice: its shares add up in the gradient.  A target outside [0, V) has no second term; a row without entries no first.
+ * Rows of weight 0 are not read: their loss and gradient are zero.  Otherwise infinities and NaN mean what the formulas say
+ * (a student's logit of minus infinity is a token that has no share).
+ * logits and dlogits are [T,B,V] with strides as above, dlogits of the logits' type, or the logits themselves (same address and
+ * strides: the gradient takes their place), or NULL: the loss alone.  top_logits [T,B,K] of top_type and top_index [T,B,K]
+ * int32, top_norm, weight (NULL: 1), targets (may be NULL where hard is 0) and loss [T,B] are contiguous.
+ * temperature lies between 2^-20 and 2^20, hard in [0, 1]; K at most BPPSA_DISTIL_MAX_K and V at most BPPSA_DISTIL_MAX_V, fewer than 2^22 rows.
+ */
+#define BPPSA_DISTIL_MAX_K 256
+#define BPPSA_DISTIL_MAX_V (1 << 20)
+typedef struct bppsa_distil_rows {
+  int32_t T, B, V, K, type, top_type;
+  bppsa_rows logits;
+  const void* top_logits;
+  const int32_t* top_index;
+  const float *top_norm, *weight;
+  const int32_t* targets;
+  float temperature, hard;
+} bppsa_distil_rows;
+bppsa_status bppsa_distil(const bppsa_distil_rows* rows, float* loss, const bppsa_rows* dlogits, void* stream);
+
+/*
+ * One step of a beam search.  Of B sequences with W beams each, whose running scores are scores [B,W], the W best of the W V
+ * candidates  scores[b,w] + log softmax(logits[b,w])[v]  become the new beams, best first: choice->scores, parents (the beam
+ * w that a candidate continues) and tokens (v), [B,W] each.  A beam's candidates are in the order of its logits, of equal ones
+ * the lower token first; between beams the sums decide in 64 bits, of equal ones the lower beam.
+ * finished [B,W] (bytes, may be NULL): a finished beam has the one candidate `end`, at its score as it is; its other tokens
+ * count as minus infinity, as do all of a beam whose score or whose logarithm of the sum is not finite.  choice->finished (may
+ * be NULL if finished is) tells the beams whose parent was or whose token is `end`.  end is a token, or -1 where there is none
+ * and finished is NULL.  Logits of beams that are finished or whose score is not finite are not read.
+ * slots [B,W] (may be NULL): where the beams keep their states, no slot twice.  The first child of a beam goes on in its slot, the
+ * others take the slots of beams without a child, in order: choice->slots; choice->sources has the slot that a child's states are
+ * copied from by bppsa_beam_move, -1 where they are in place.
+ * logits: stride_t is that of a sequence, stride_b that of a beam, in elements; the V logits lie side by side.
+ * W is at most BPPSA_BEAM_MAX_W and V at most BPPSA_BEAM_MAX_V, 2^24 rows of 8192 logits at most.  Outputs are other arrays than inputs.
+ */
+#define BPPSA_BEAM_MAX_W 32
+#define BPPSA_BEAM_MAX_V (1 << 19)
+typedef struct bppsa_beam {
+  int32_t B, W, V, type, end;
+  bppsa_rows logits;
+  const float* scores;
+  const uint8_t* finished;
+  const int32_t* slots;
+} bppsa_beam;
+typedef struct bppsa_beam_choice {
+  float* scores;
+  int32_t *parents, *tokens;
+  uint8_t* finished;
+  int32_t *slots, *sources;
+} bppsa_beam_choice;
+size_t bppsa_beam_select_workspace_bytes(int B, int W, int V);
+bppsa_status bppsa_beam_select(const bppsa_beam* beams, const bppsa_beam_choice* choice, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/*
+ * Copies states from slot sources[i] to slot slots[i] of every tensor, in place, for each of `rows` rows i whose two slots lie in
+ * [0, slots_in_state) and differ.  No slot may be written twice, or read and written: those of bppsa_beam_select are not.
+ * `tensors` and `pieces` [n_pieces] are DEVICE copies of what the caller fills in on the host once: a tensor's first slot and
+ * the bytes of one slot (slots side by side), and the list that bppsa_beam_pieces writes for the bytes of n_tensors
+ * tensors (host memory) and counts (pieces NULL: only counts; 0: invalid, or more than 2^22).
+ */
+#define BPPSA_BEAM_PIECE 16384
+typedef struct bppsa_beam_tensor {
+  void* data;
+  int64_t bytes;
+} bppsa_beam_tensor;
+int64_t bppsa_beam_pieces(int n_tensors, const int64_t* bytes, bppsa_adamw_piece* pieces);
+bppsa_status bppsa_beam_move(const bppsa_beam_tensor* tensors, int64_t n_pieces, const bppsa_adamw_piece* pieces, int rows,
+                             const int32_t* sources, const int32_t* slots, int slots_in_state, void* stream);
+
 /* ------------------------------------------------------------------------
  * Measurement aid (not part of the method).
  * ---------------------------------------------------------------------- */

@@ -21,4 +21,6 @@ from .gated import (  # noqa: F401
     GatedGrads, gated_scan, gated_scan_states, gated_scan_workspace_bytes, gated_scan_backward,
     gated_scan_backward_workspace_bytes, gated_scan_step,
 )
+from .loss import DistilLoss, distil  # noqa: F401
+from .search import BeamChoice, BeamStates, beam_select, beam_select_workspace_bytes  # noqa: F401
 from .optim import AdamW  # noqa: F401

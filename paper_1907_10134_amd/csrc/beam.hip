@@ -1,0 +1,343 @@
+// One step of a beam search: the selection over beams and vocabulary, and the move of the beams' states.
+//
+// A beam's candidates are its score plus log softmax of its logits.  Within a beam the logits alone decide the order (larger
+// first, of equal ones the lower token); the beams' lists are merged by their sums in 64 bits (of equal ones the lower beam): sums
+// of different beams may lie next to each other, and a selection that turned on a rounding would differ from run to run of a
+// model with other sizes of a batch.
+#include <algorithm>
+
+#include "ssm_common.h"
+
+namespace {
+
+using namespace ssm;
+
+constexpr int kThreads = 256, kEach = 32, kPiece = kThreads * kEach;
+constexpr int kMostBeams = BPPSA_BEAM_MAX_W, kMostPieces = 64;
+static_assert(kMostPieces * kPiece == BPPSA_BEAM_MAX_V);
+
+// What a piece of a row leaves: its largest value, the sum of exponentials relative to that and its first W logits.
+struct Pieces {
+  float* largest;                  // [row][piece]
+  double* sum;
+  uint64_t* key;                   // [row][piece][W], 0 where there are fewer
+  int count;
+};
+
+// Ascending with the value, and of equal values descending with the place; never 0.
+__device__ __forceinline__ uint64_t key_of(float v, int place) {
+  const uint32_t u = __float_as_uint(v);
+  return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~place;
+}
+__device__ __forceinline__ float value_of(uint64_t key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+__device__ __forceinline__ int place_of(uint64_t key) { return (int)~(uint32_t)key; }
+
+template <typename T, typename F>
+__device__ __forceinline__ T over_lanes(T v, F&& f) {
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) v = f(v, __shfl_xor(v, k));
+  return v;
+}
+
+template <typename E>
+struct Beams {
+  Rows<const E> logits;            // [B][W][V], the sequences' stride first
+  const float* scores;
+  const uint8_t* finished;
+  const int32_t* slots;
+  int B, W, V, end;
+};
+template <typename E>
+__device__ __forceinline__ bool alive(const Beams<E>& s, int row) {
+  return fabsf(s.scores[row]) < INFINITY && !(s.finished && s.finished[row]);
+}
+
+// One workgroup a piece of a row, whose values stay in registers.  The W-th largest of a piece is no smaller than the smallest
+// of the largest values of W groups of threads; so few values reach that bound (22 of 8192 normal ones at W = 8) that
+// each can count those in front of it.  Where more than kThreads do, they are taken one after the other.
+template <typename E>
+__global__ void __launch_bounds__(kThreads)
+beam_piece_kernel(const Beams<E> s, const Pieces out) {
+  constexpr int V = 16 / sizeof(E), LOADS = kEach / V;
+  __shared__ float group[kThreads / 64][kMostBeams];
+  __shared__ double sums[kThreads / 64];
+  __shared__ uint64_t found[kThreads];
+  __shared__ int n_found;
+  const int piece = blockIdx.x % out.count, row = blockIdx.x / out.count, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (!alive(s, row)) return;
+  const E* const from = s.logits.at(row / s.W, row % s.W);
+  const int first = piece * kPiece + (int)threadIdx.x * V;
+  float v[kEach], m = -INFINITY, e = 0.0f;
+#pragma unroll
+  for (int k = 0; k < LOADS; ++k) {
+    const int at = first + k * kThreads * V;
+    if (at + V <= s.V) {
+      const Some<E, V> x = load_some<E, V>(from + at);
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[k * V + j] = (float)x.v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[k * V + j] = at + j < s.V ? (float)from[at + j] : -INFINITY;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) v[k] += 0.0f, m = fmaxf(m, v[k]);        // no -0, which is equal to 0
+  const int groups = s.W <= 1 ? 1 : 1 << (32 - __builtin_clz(s.W - 1));
+  if (threadIdx.x == 0) n_found = 0;
+  for (int k = groups; k < 64; k <<= 1) m = fmaxf(m, __shfl_xor(m, k));
+  if (lane < groups) group[wave][lane] = m;
+  __syncthreads();
+  for (int k = 0; k < kThreads / 64; ++k) m = fmaxf(m, group[k][lane & (groups - 1)]);
+  float bound = m;
+  for (int k = 1; k < groups; k <<= 1) bound = fminf(bound, __shfl_xor(bound, k)), m = fmaxf(m, __shfl_xor(m, k));
+  const float zero = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    e += exp2_fast((v[k] - zero) * kLog2e);
+    const int place = first + k / V * kThreads * V + k % V;
+    if (v[k] >= bound && place < s.V) {
+      const int at = atomicAdd(&n_found, 1);
+      if (at < kThreads) found[at] = key_of(v[k], place);
+    }
+  }
+  const double sum = over_lanes((double)e, [](double a, double b) { return a + b; });
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  const int n = n_found;
+  const int64_t at = (int64_t)row * out.count + piece;
+  if (threadIdx.x == 0) {
+    double all = sums[0];
+    for (int k = 1; k < kThreads / 64; ++k) all += sums[k];
+    out.largest[at] = zero, out.sum[at] = all;
+  }
+  uint64_t* const to = out.key + at * s.W;
+  if (n <= kThreads) {
+    const uint64_t mine = threadIdx.x < n ? found[threadIdx.x] : 0;
+    int before = 0;
+    for (int k = 0; k < n; ++k) before += found[k] > mine;
+    if (threadIdx.x < n && before < s.W) to[before] = mine;
+    if (threadIdx.x >= n && threadIdx.x < s.W) to[threadIdx.x] = 0;
+    return;
+  }
+  uint64_t last = ~(uint64_t)0;
+  for (int i = 0; i < s.W; ++i) {
+    uint64_t best = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int place = first + k / V * kThreads * V + k % V;
+      const uint64_t key = place < s.V ? key_of(v[k], place) : 0;
+      if (key < last && key > best) best = key;
+    }
+    best = over_lanes(best, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+    __syncthreads();
+    if (lane == 0) found[wave] = best;
+    __syncthreads();
+    for (int k = 0; k < kThreads / 64; ++k) best = found[k] > best ? found[k] : best;
+    if (threadIdx.x == 0) to[i] = best;
+    last = best;
+  }
+}
+
+// One workgroup a sequence: a wave merges the pieces' lists of a beam, then the first one the beams' lists.
+struct Choice {
+  float* scores;
+  int32_t *parents, *tokens, *slots, *sources;
+  uint8_t* finished;
+};
+template <typename E>
+__global__ void __launch_bounds__(1024)
+beam_join_kernel(const Beams<E> s, const Pieces in, const Choice out) {
+  extern __shared__ uint64_t lists[];          // of each wave, [piece][W]
+  __shared__ double total[kMostBeams][kMostBeams];
+  __shared__ int token[kMostBeams][kMostBeams], parent[kMostBeams];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, W = s.W;
+  uint64_t* const list = lists + (int64_t)wave * in.count * W;
+  for (int w = wave; w < W; w += waves) {
+    const int row = blockIdx.x * W + w;
+    const float score = s.scores[row];
+    double norm = NAN;
+    if (alive(s, row)) {
+      const int64_t at = (int64_t)row * in.count;
+      const float largest = lane < in.count ? in.largest[at + lane] : -INFINITY;
+      const double sum = lane < in.count ? in.sum[at + lane] : 0.0;
+      const float m = over_lanes(sum > 0.0 ? largest : -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+      const double all = over_lanes(sum == 0.0 ? 0.0 : sum * exp((double)largest - (double)m), [](double a, double b) { return a + b; });
+      norm = (double)m + log(all);
+      for (int k = lane; k < in.count * W; k += 64) list[k] = in.key[at * W + k];
+    }
+    if (!(fabs(norm) < INFINITY)) {            // only a finished beam's end counts; of equal candidates the first tokens
+      const bool ends = s.finished && s.finished[row] && fabsf(score) < INFINITY;
+      if (lane < W) {
+        int k = lane;
+        double v = -INFINITY;
+        if (ends) {
+          k = lane == 0 ? s.end : lane - 1 < s.end ? lane - 1 : lane;
+          if (lane == 0) v = (double)score;
+        }
+        total[w][lane] = v, token[w][lane] = k < s.V ? k : -1;
+      }
+      continue;
+    }
+    // a lane has the first of a piece's list that is not yet taken
+    int next = 0;
+    __builtin_amdgcn_wave_barrier();
+    for (int i = 0; i < W; ++i) {
+      const uint64_t mine = lane < in.count && next < W ? list[lane * W + next] : 0;
+      const uint64_t best = over_lanes(mine, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+      if (mine == best) ++next;
+      if (lane == 0) {
+        const double v = (double)score + ((double)value_of(best) - norm);
+        total[w][i] = v, token[w][i] = best ? place_of(best) : -1;
+      }
+    }
+  }
+  __syncthreads();
+  if (wave) return;
+  int next = 0;
+  for (int i = 0; i < W; ++i) {
+    const bool any = lane < W && next < W && token[lane][next] >= 0;
+    double v = any ? total[lane][next] : 0.0;
+    int who = any ? lane : 64;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+      const double u = __shfl_xor(v, k);
+      const int other = __shfl_xor(who, k);
+      if (other < 64 && (who == 64 || u > v || (u == v && other < who))) v = u, who = other;
+    }
+    if (lane == who) {
+      const int at = blockIdx.x * W + i, t = token[lane][next];
+      out.scores[at] = (float)v, out.parents[at] = lane, out.tokens[at] = t;
+      if (out.finished) out.finished[at] = (s.finished && s.finished[blockIdx.x * W + lane]) || t == s.end;
+      ++next;
+      parent[i] = lane;
+    }
+  }
+  if (!s.slots) return;
+  __builtin_amdgcn_wave_barrier();
+  // the first child of a beam goes on in its slot, the others take those of beams without one, in order
+  if (lane < W) {
+    const int32_t* const slots = s.slots + (int64_t)blockIdx.x * W;
+    const int p = parent[lane];
+    int more = 0, mine = 0;
+    for (int i = 0; i <= lane; ++i) {
+      bool first = true;
+      for (int k = 0; k < i; ++k) first &= parent[k] != parent[i];
+      if (!first) ++more;
+      if (i == lane) mine = !first;
+    }
+    int home = p;
+    if (mine)
+      for (int k = 0; k < W; ++k) {
+        bool childless = true;
+        for (int i = 0; i < W; ++i) childless &= parent[i] != k;
+        if (childless && --more == 0) home = k;
+      }
+    const int at = blockIdx.x * W + lane, to = slots[home], of = slots[p];
+    out.slots[at] = to, out.sources[at] = mine ? of : -1;
+  }
+}
+
+struct Scratch {
+  size_t largest, sum, key, bytes;
+  int pieces;
+  Scratch(int B, int W, int V) {
+    pieces = bppsa_ceil_div(V, kPiece);
+    const size_t n = (size_t)B * W * pieces;
+    largest = 0, sum = bppsa_align_up(n * sizeof(float), 256);
+    key = sum + bppsa_align_up(n * sizeof(double), 256);
+    bytes = key + bppsa_align_up(n * W * sizeof(uint64_t), 256);
+  }
+};
+
+static inline bool beam_sizes_ok(int B, int W, int V) {
+  return B > 0 && W > 0 && V > 0 && W <= kMostBeams && V <= BPPSA_BEAM_MAX_V &&
+         (int64_t)B * W * bppsa_ceil_div(V, kPiece) < 1 << 24;
+}
+
+// A workgroup takes a piece of a tensor's slots for every so many rows, which it looks through 64 at a time.
+template <typename U>
+__device__ __forceinline__ void copy_bytes(char* to, const char* from, int n) {
+  for (int k = threadIdx.x; k < n / (int)sizeof(U); k += kThreads) reinterpret_cast<U*>(to)[k] = reinterpret_cast<const U*>(from)[k];
+}
+__global__ void __launch_bounds__(kThreads)
+beam_move_kernel(const bppsa_beam_tensor* __restrict__ tensors, const bppsa_adamw_piece* __restrict__ pieces, int rows,
+                 const int32_t* __restrict__ sources, const int32_t* __restrict__ slots, int slots_in_state) {
+  const bppsa_beam_tensor x = tensors[pieces[blockIdx.x].tensor];
+  const int64_t at = (int64_t)pieces[blockIdx.x].piece * BPPSA_BEAM_PIECE;
+  const int n = (int)(x.bytes - at < BPPSA_BEAM_PIECE ? x.bytes - at : BPPSA_BEAM_PIECE);
+  const uint64_t odd = (uint64_t)x.data | (uint64_t)x.bytes;
+  for (int row = blockIdx.y; row < rows; row += gridDim.y) {
+    const int from = sources[row], to = slots[row];
+    if (from < 0 || to < 0 || from >= slots_in_state || to >= slots_in_state || from == to) continue;
+    char* const d = static_cast<char*>(x.data) + at;
+    if ((odd & 15) == 0) copy_bytes<uint4>(d + to * x.bytes, d + from * x.bytes, n);
+    else if ((odd & 3) == 0) copy_bytes<uint32_t>(d + to * x.bytes, d + from * x.bytes, n);
+    else copy_bytes<uint8_t>(d + to * x.bytes, d + from * x.bytes, n);
+  }
+}
+
+}  // namespace
+
+extern "C" size_t bppsa_beam_select_workspace_bytes(int B, int W, int V) {
+  return beam_sizes_ok(B, W, V) ? Scratch(B, W, V).bytes : 0;
+}
+
+extern "C" bppsa_status bppsa_beam_select(const bppsa_beam* beams, const bppsa_beam_choice* choice, void* workspace,
+                                          size_t workspace_bytes, void* stream) {
+  if (!beams || beams->B < 1 || beams->W < 1 || beams->V < 1 || !beams->logits.data || !beams->scores) return BPPSA_EINVAL;
+  if (!choice || !choice->scores || !choice->parents || !choice->tokens || choice->scores == beams->scores) return BPPSA_EINVAL;
+  if (choice->finished && choice->finished == beams->finished) return BPPSA_EINVAL;
+  if (beams->finished && (beams->end < 0 || beams->end >= beams->V || !choice->finished)) return BPPSA_EINVAL;
+  if (beams->slots && (!choice->slots || !choice->sources || choice->slots == beams->slots || choice->sources == beams->slots))
+    return BPPSA_EINVAL;
+  if (beams->W > kMostBeams || beams->V > BPPSA_BEAM_MAX_V || beams->type < BPPSA_F32 || beams->type > BPPSA_F16)
+    return BPPSA_EUNSUPPORTED;
+  if (!beam_sizes_ok(beams->B, beams->W, beams->V)) return BPPSA_EOVERFLOW;
+  const Scratch at(beams->B, beams->W, beams->V);
+  if (!workspace || workspace_bytes < at.bytes) return BPPSA_EWORKSPACE;
+  if ((uintptr_t)workspace & 255) return BPPSA_EINVAL;
+  char* const base = static_cast<char*>(workspace);
+  const Pieces pieces{reinterpret_cast<float*>(base + at.largest), reinterpret_cast<double*>(base + at.sum),
+                      reinterpret_cast<uint64_t*>(base + at.key), at.pieces};
+  const Choice out{choice->scores, choice->parents, choice->tokens, choice->slots, choice->sources, choice->finished};
+  const hipStream_t q = (hipStream_t)stream;
+  const size_t list = (size_t)at.pieces * beams->W * sizeof(uint64_t);         // 16 KB at most
+  const int waves = std::max<int>(1, std::min<int64_t>({16, beams->W, (int64_t)((64 << 10) / list)}));
+  return by_type(beams->type, [&](auto e) {
+    using E = decltype(e);
+    const Beams<E> s{rows_of<const E>(beams->logits), beams->scores, beams->finished, beams->slots, beams->B, beams->W, beams->V, beams->end};
+    beam_piece_kernel<E><<<(unsigned)(beams->B * beams->W * at.pieces), kThreads, 0, q>>>(s, pieces);
+    BPPSA_CHECK_LAUNCH();
+    beam_join_kernel<E><<<beams->B, 64 * waves, waves * list, q>>>(s, pieces, out);
+    BPPSA_CHECK_LAUNCH();
+    return BPPSA_OK;
+  });
+}
+
+extern "C" int64_t bppsa_beam_pieces(int n_tensors, const int64_t* bytes, bppsa_adamw_piece* pieces) {
+  if (n_tensors < 1 || !bytes) return 0;
+  int64_t n = 0;
+  for (int t = 0; t < n_tensors; ++t) {
+    if (bytes[t] < 1) return 0;
+    const int64_t here = (bytes[t] + BPPSA_BEAM_PIECE - 1) / BPPSA_BEAM_PIECE;
+    if (here > 0x7FFFFFFF || n + here > 1 << 22) return 0;
+    if (pieces)
+      for (int64_t k = 0; k < here; ++k) pieces[n + k] = bppsa_adamw_piece{t, (int32_t)k};
+    n += here;
+  }
+  return n;
+}
+
+extern "C" bppsa_status bppsa_beam_move(const bppsa_beam_tensor* tensors, int64_t n_pieces, const bppsa_adamw_piece* pieces, int rows,
+                                        const int32_t* sources, const int32_t* slots, int slots_in_state, void* stream) {
+  if (!tensors || !pieces || n_pieces < 1 || rows < 1 || !sources || !slots || slots_in_state < 1) return BPPSA_EINVAL;
+  if (n_pieces > 1 << 22) return BPPSA_EOVERFLOW;
+  const int64_t want = std::max<int64_t>(1, 4096 / n_pieces);
+  beam_move_kernel<<<dim3((unsigned)n_pieces, (unsigned)std::min<int64_t>(rows, want)), kThreads, 0, (hipStream_t)stream>>>(
+      tensors, pieces, rows, sources, slots, slots_in_state);
+  BPPSA_CHECK_LAUNCH();
+  return BPPSA_OK;
+}
