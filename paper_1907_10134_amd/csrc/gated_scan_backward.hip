@@ -117,7 +117,7 @@ extern "C" bppsa_status bppsa_gated_scan_backward(const bppsa_gated* layer, cons
   float* const parts = static_cast<float*>(workspace);
   BPPSA_TRY(by_type(layer->type, [&](auto e) {
     using E = decltype(e);
-    return by_width(layer->D, [&](auto width) {
+    return by_width<E>(layer->D, [&](auto width) {
       constexpr int V = width.value;
       const Layer<E> l = layer_of<E>(*layer, 64 * V);
       const Grads<E> o{rows_of<E>(grads->dx), rows_of<E>(grads->dr), rows_of<E>(grads->di), rows_of<E>(grads->dz), parts, grads->dh0};
