@@ -82,7 +82,7 @@ __device__ __forceinline__ Gates gates_of(float r, float i, float decay) {
   return g;
 }
 
-// One grid axis counts tiles, samples and columns; a launch has fewer than 2^32 threads.
+// One grid axis counts tiles, samples and columns; a launch has fewer than 2^32 threads, 512 a tile.
 static inline int64_t workgroups(int T, int B, int D) {
   return (int64_t)bppsa_ceil_div(T, kKept) * B * bppsa_ceil_div(D, 64);
 }

@@ -16,63 +16,176 @@ struct Grads {
   float *parts, *dh0;              // parts: of ddecay, dr_bias and di_bias, [part][3][D]
 };
 
-// One thread a lane's channels of a sample, the states of kKept steps found again from the one kept before them.
-template <typename E, int V, bool GATE>
-__global__ void __launch_bounds__(64)
+// The tiles run from the end, kKept steps each, joined as those of the forward pass are: a word says what a tile does to the
+// gradient that comes in from behind.  A run's states are found again from the one kept before its tile and the shares of the
+// runs in front of it, so a tile's inputs are read once.  The gates are made twice, before the tile is joined and behind: kept
+// over it they would be twice the registers.
+template <typename E, int V, bool GATE, bool JOINED>
+__global__ void __launch_bounds__(kWaves * 64, 4)
 gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ dh_last, const float* __restrict__ states,
-                      const Grads<E> o) {
-  const Own<V> own(blockIdx.x, threadIdx.x, l.D);
-  const int b = blockIdx.y, d = own.d, len = clamp_length(l.lengths, b, l.T);
-  if (!own.on) return;
-  float decay[V], rb[V], ib[V], w[V], sums[3][V] = {}, zero[V] = {};
-  parameter(l.decay, d, decay), parameter(l.r_bias, d, rb), parameter(l.i_bias, d, ib);
-  parameter(dh_last ? dh_last + (int64_t)b * l.D : nullptr, d, w);
-  for (int t = len; t < l.T; ++t) {
-    store_some<E, V>(o.dx.at(t, b) + d, zero), store_some<E, V>(o.dr.at(t, b) + d, zero), store_some<E, V>(o.di.at(t, b) + d, zero);
-    if (GATE) store_some<E, V>(o.dz.at(t, b) + d, zero);
+                      const Grads<E> o, int* ticket, uint64_t* words, int total) {
+  constexpr int R = kRunBack;
+  __shared__ float4 runs[2][kWaves][64 * V];             // product of the decays, state from zero, gradient from zero
+  __shared__ float2 border[2][64 * V];                   // the state before the tile, the gradient behind it
+  __shared__ float sums[2][3][kWaves][64 * V];
+  __shared__ int taken[2];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int id = blockIdx.x;
+  if (JOINED) {
+    if (threadIdx.x == 0) taken[1] = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    id = __builtin_amdgcn_readfirstlane(taken[1]);
   }
-  for (int tile = (len + kKept - 1) / kKept - 1; tile >= 0; --tile) {
-    const int first = tile * kKept, end = first + kKept < len ? first + kKept : len;
-    float before[kKept][V], h[V];
-    parameter(states + ((int64_t)tile * l.B + b) * l.D, d, h);
-    for (int t = first; t < end; ++t) {
-      const auto x = load_some<E, V>(l.x.at(t, b) + d), r = load_some<E, V>(l.r.at(t, b) + d), i = load_some<E, V>(l.i.at(t, b) + d);
-      for (int c = 0; c < V; ++c) {
-        before[t - first][c] = h[c];
-        const Gates g = gates_of<E>((float)r.v[c] + rb[c], (float)i.v[c] + ib[c], decay[c]);
-        h[c] = fmaf(g.a, h[c], __builtin_amdgcn_sqrtf(g.m2) * g.iota * (float)x.v[c]);
+  const int tiles = (l.T + kKept - 1) / kKept;
+  for (int parity = 0; id < total; parity ^= 1) {
+    int next = total;
+    if (JOINED && threadIdx.x == 0) next = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int column = id % l.columns, b = id / l.columns % l.B, tile = tiles - 1 - id / l.columns / l.B;
+    const Own<V> own(column, lane, l.D);
+    const int d = own.d, len = clamp_length(l.lengths, b, l.T), t0 = tile * kKept, first = t0 + w * R;
+    const int last_tile = (len + kKept - 1) / kKept - 1;
+    // behind an end
+    if (own.on)
+      for (int t = first > len ? first : len; t < first + R && t < l.T; ++t) {
+        const float zero[V] = {};
+        store_some<E, V>(o.dx.at(t, b) + d, zero), store_some<E, V>(o.dr.at(t, b) + d, zero), store_some<E, V>(o.di.at(t, b) + d, zero);
+        if (GATE) store_some<E, V>(o.dz.at(t, b) + d, zero);
       }
-    }
-    for (int t = end - 1; t >= first; --t) {
-      const auto x_ = load_some<E, V>(l.x.at(t, b) + d), r = load_some<E, V>(l.r.at(t, b) + d), i = load_some<E, V>(l.i.at(t, b) + d);
-      const auto go = load_some<E, V>(dy.at(t, b) + d);
-      Some<E, V> z_ = {};
-      if (GATE) z_ = load_some<E, V>(l.z.at(t, b) + d);
-      float dx[V], dr[V], di[V], dz[V];
-      for (int c = 0; c < V; ++c) {
-        const Gates g = gates_of<E>((float)r.v[c] + rb[c], (float)i.v[c] + ib[c], decay[c]);
-        const float x = (float)x_.v[c], root = g.m2 > 0x1p-120f ? __builtin_amdgcn_rsqf(g.m2) : 0.0f, m = g.m2 * root;
-        float q = (float)go.v[c];
-        if (GATE) {
-          const float z = (float)z_.v[c], sg = sigmoid<E>(z), now = fmaf(g.a, before[t - first][c], m * g.iota * x);
-          dz[c] = q * now * sg * fmaf(z, 1.0f - sg, 1.0f);
-          q *= z * sg;
+    if (len == 0 && tile == 0 && w == 0 && o.dh0 && own.on)
+      for (int c = 0; c < V; ++c) o.dh0[(int64_t)b * l.D + d + c] = dh_last ? dh_last[(int64_t)b * l.D + d + c] : 0.0f;
+
+    Some<E, V> x[R], r[R], i[R], go[R], z[GATE ? R : 1];
+    float a[R][V], e[R][V], q[R][V], decay[V], rb[V], ib[V], sum[3][V] = {};
+    float product[V], end[V], back[V];
+    parameter(l.decay, d, decay), parameter(l.r_bias, d, rb), parameter(l.i_bias, d, ib);
+#pragma unroll
+    for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = back[c] = 0.0f;
+    if (first < len) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        const int t = first + j < len ? first + j : len - 1;
+        r[j] = load_some<E, V>(l.r.at(t, b) + d), i[j] = load_some<E, V>(l.i.at(t, b) + d), x[j] = load_some<E, V>(l.x.at(t, b) + d);
+        go[j] = load_some<E, V>(dy.at(t, b) + d);
+        if (GATE) z[j] = load_some<E, V>(l.z.at(t, b) + d);
+      }
+#pragma unroll
+      for (int j = 0; j < R; ++j)
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          const Gates g = gates_of<E>((float)r[j].v[c] + rb[c], (float)i[j].v[c] + ib[c], decay[c]);
+          const bool real = first + j < len;
+          a[j][c] = real ? g.a : 1.0f;
+          e[j][c] = real ? __builtin_amdgcn_sqrtf(g.m2) * g.iota * (float)x[j].v[c] : 0.0f;
+          q[j][c] = (float)go[j].v[c];
+          if (GATE) q[j][c] *= (float)z[j].v[c] * sigmoid<E>((float)z[j].v[c]);
+          if (!real) q[j][c] = 0.0f;
+          product[c] *= a[j][c], end[c] = fmaf(a[j][c], end[c], e[j][c]);
         }
-        const float gh = q + w[c];
-        w[c] = g.a * gh;
-        const float s = w[c] * g.rho * (g.a * g.iota * x * root - before[t - first][c]);
-        dx[c] = gh * m * g.iota;
-        di[c] = dx[c] * x * (1.0f - g.iota);
-        dr[c] = decay[c] * (1.0f - g.rho) * s;
-        sums[0][c] += s, sums[1][c] += dr[c], sums[2][c] += di[c];
-      }
-      store_some<E, V>(o.dx.at(t, b) + d, dx), store_some<E, V>(o.dr.at(t, b) + d, dr), store_some<E, V>(o.di.at(t, b) + d, di);
-      if (GATE) store_some<E, V>(o.dz.at(t, b) + d, dz);
+#pragma unroll
+      for (int j = R - 1; j >= 0; --j)
+#pragma unroll
+        for (int c = 0; c < V; ++c) back[c] = a[j][c] * (q[j][c] + back[c]);
     }
+#pragma unroll
+    for (int c = 0; c < V; ++c) runs[parity][w][lane * V + c] = make_float4(product[c], end[c], back[c], 0.0f);
+    lds_barrier();
+    if (w < V && t0 < len) {                   // the tile's own share, a channel a lane
+      const int at = w * 64 + lane;
+      float p = 1.0f, s = 0.0f, in = 0.0f;
+#pragma unroll
+      for (int k = kWaves - 1; k >= 0; --k) {
+        const float4 run = runs[parity][k][at];
+        p *= run.x, s = fmaf(run.x, s, run.z);
+      }
+      const int channel = channel_of<V>(column, at, l.D);
+      const bool on = channel < l.D;
+      if (tile == last_tile && dh_last && on) in = dh_last[(int64_t)b * l.D + channel];
+      if (JOINED) {
+        const int64_t step = (int64_t)l.B * l.columns * 64 * V;
+        uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V + at;
+        if (tile < last_tile) leave(mine, word_of(p, s)), in = look_back(mine, -step, last_tile - tile);
+        leave(mine, settled(through(word_of(p, s), in)));
+      }
+      border[parity][at] = make_float2(on ? states[((int64_t)tile * l.B + b) * l.D + channel] : 0.0f, in);
+    }
+    if (JOINED && threadIdx.x == 0) taken[parity] = next;
+    lds_barrier();
+    if (first < len) {
+      float h[V], g[V];
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        const float2 both = border[parity][lane * V + c];
+        h[c] = both.x, g[c] = both.y;
+      }
+      for (int k = 0; k < w; ++k)
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          const float4 run = runs[parity][k][lane * V + c];
+          h[c] = fmaf(run.x, h[c], run.y);
+        }
+      for (int k = kWaves - 1; k > w; --k)
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          const float4 run = runs[parity][k][lane * V + c];
+          g[c] = fmaf(run.x, g[c], run.z);
+        }
+      // the states before each step, in the place of what enters
+#pragma unroll
+      for (int j = 0; j < R; ++j)
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          const float before = h[c];
+          h[c] = fmaf(a[j][c], h[c], e[j][c]), e[j][c] = before;
+        }
+#pragma unroll
+      for (int j = 0; j < R; ++j) as_loaded(x[j]), as_loaded(r[j]), as_loaded(i[j]);
+#pragma unroll
+      for (int j = R - 1; j >= 0; --j) {
+        float dx[V], dr[V], di[V], dz[V];
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          const float rho = sigmoid<E>((float)r[j].v[c] + rb[c]), iota = sigmoid<E>((float)i[j].v[c] + ib[c]), of_x = (float)x[j].v[c];
+          const float m2 = one_minus(a[j][c] * a[j][c], 2.0f * decay[c] * rho);
+          const float root = m2 > 0x1p-120f ? __builtin_amdgcn_rsqf(m2) : 0.0f, m = m2 * root;
+          if (GATE) {
+            const float of_z = (float)z[j].v[c], sg = sigmoid<E>(of_z);
+            dz[c] = (float)go[j].v[c] * h[c] * sg * fmaf(of_z, 1.0f - sg, 1.0f);
+          }
+          const float gh = q[j][c] + g[c];
+          g[c] = a[j][c] * gh;
+          const float s = g[c] * rho * fmaf(a[j][c] * iota * of_x, root, -e[j][c]);
+          dx[c] = gh * m * iota;
+          di[c] = dx[c] * of_x * (1.0f - iota);
+          dr[c] = decay[c] * (1.0f - rho) * s;
+          h[c] = e[j][c];
+          if (first + j < len) sum[0][c] += s, sum[1][c] += dr[c], sum[2][c] += di[c];
+        }
+        if (first + j < len && own.on) {
+          store_some<E, V>(o.dx.at(first + j, b) + d, dx), store_some<E, V>(o.dr.at(first + j, b) + d, dr), store_some<E, V>(o.di.at(first + j, b) + d, di);
+          if (GATE) store_some<E, V>(o.dz.at(first + j, b) + d, dz);
+        }
+      }
+      if (o.dh0 && first == 0 && own.on)
+#pragma unroll
+        for (int c = 0; c < V; ++c) o.dh0[(int64_t)b * l.D + d + c] = g[c];
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int c = 0; c < V; ++c) sums[parity][k][w][lane * V + c] = sum[k][c];
+    lds_barrier();
+    for (int at = threadIdx.x; at < 3 * 64 * V; at += kWaves * 64) {
+      const int k = at / (64 * V), place = at % (64 * V), channel = channel_of<V>(column, place, l.D);
+      float all = 0.0f;
+#pragma unroll
+      for (int n = 0; n < kWaves; ++n) all += sums[parity][k][n][place];
+      if (channel < l.D) o.parts[(((int64_t)tile * l.B + b) * 3 + k) * l.D + channel] = all;
+    }
+    id = JOINED ? __builtin_amdgcn_readfirstlane(taken[parity]) : total;
   }
-  if (o.dh0) store_some<float, V>(o.dh0 + (int64_t)b * l.D + d, w);
-  for (int k = 0; k < 3; ++k) store_some<float, V>(o.parts + ((int64_t)b * 3 + k) * l.D + d, sums[k]);
 }
+
+constexpr int kResident = 2;     // workgroups of a compute unit
 
 // The sums over parts, in order: sixteen waves a sixteenth each, then those.  In 64 bits, which cost nothing beside the loads.
 struct Joined {
@@ -99,8 +212,11 @@ gated_join_kernel(const float* __restrict__ parts, int D, int64_t n, const Joine
 
 }  // namespace
 
+// The words of the widest workgroups, or of one channel a lane, whichever are more, then the parts.
 extern "C" size_t bppsa_gated_scan_backward_workspace_bytes(int T, int B, int D) {
-  return sizes_ok(T, B, D) ? bppsa_align_up((size_t)B * 3 * D * sizeof(float), 256) : 0;
+  if (!sizes_ok(T, B, D)) return 0;
+  const int tiles = bppsa_ceil_div(T, kKept);
+  return words_bytes(tiles, B, bppsa_ceil_div(D, 128), 2) + bppsa_align_up((size_t)tiles * B * 3 * D * sizeof(float), 256);
 }
 
 extern "C" bppsa_status bppsa_gated_scan_backward(const bppsa_gated* layer, const bppsa_rows* dy, const float* dh_last,
@@ -114,21 +230,37 @@ extern "C" bppsa_status bppsa_gated_scan_backward(const bppsa_gated* layer, cons
   if (dh_last && dh_last == grads->dh0) return BPPSA_EINVAL;
   BPPSA_TRY(check_workspace(workspace, workspace_bytes, bppsa_gated_scan_backward_workspace_bytes(layer->T, layer->B, layer->D)));
   const hipStream_t s = (hipStream_t)stream;
-  float* const parts = static_cast<float*>(workspace);
+  const int tiles = bppsa_ceil_div(layer->T, kKept);
+  char* const base = static_cast<char*>(workspace);
+  float* const parts = reinterpret_cast<float*>(base + words_bytes(tiles, layer->B, bppsa_ceil_div(layer->D, 128), 2));
   BPPSA_TRY(by_type(layer->type, [&](auto e) {
     using E = decltype(e);
     return by_width<E>(layer->D, [&](auto width) {
       constexpr int V = width.value;
       const Layer<E> l = layer_of<E>(*layer, 64 * V);
       const Grads<E> o{rows_of<E>(grads->dx), rows_of<E>(grads->dr), rows_of<E>(grads->di), rows_of<E>(grads->dz), parts, grads->dh0};
-      const auto kernel = l.z.data ? gated_backward_kernel<E, V, true> : gated_backward_kernel<E, V, false>;
-      kernel<<<dim3(l.columns, l.B), 64, 0, s>>>(l, rows_of<const E>(*dy), dh_last, static_cast<const float*>(states), o);
+      const int total = tiles * l.B * l.columns;
+      const auto run = [&](auto gate, auto joined) {
+        constexpr bool GATE = gate.value, JOINED = joined.value;
+        const int groups = JOINED ? std::min(total, bppsa_compute_units() * kResident) : total;
+        gated_backward_kernel<E, V, GATE, JOINED><<<groups, kWaves * 64, 0, s>>>(
+            l, rows_of<const E>(*dy), dh_last, static_cast<const float*>(states), o, reinterpret_cast<int*>(base),
+            reinterpret_cast<uint64_t*>(base + kTicketBytes), total);
+      };
+      constexpr std::true_type yes;
+      constexpr std::false_type no;
+      if (tiles > 1) {
+        empty_words(workspace, words_bytes(tiles, l.B, l.columns, V), s);
+        l.z.data ? run(yes, yes) : run(no, yes);
+      } else {
+        l.z.data ? run(yes, no) : run(no, no);
+      }
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     });
   }));
   gated_join_kernel<<<bppsa_ceil_div(3 * layer->D, 64), kJoining * 64, 0, s>>>(
-      parts, layer->D, layer->B, Joined{grads->ddecay, grads->dr_bias, grads->di_bias});
+      parts, layer->D, (int64_t)tiles * layer->B, Joined{grads->ddecay, grads->dr_bias, grads->di_bias});
   BPPSA_CHECK_LAUNCH();
   return BPPSA_OK;
 }
