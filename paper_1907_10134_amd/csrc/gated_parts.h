@@ -40,47 +40,97 @@ struct Own {                     // a lane's channels, of which the first `repea
     if (d > D - V) d = D - V;
   }
 };
-// Values stay as they were loaded up to here: the compiler would widen them as soon as it can and hold twice the registers.
-template <typename E, int V>
-__device__ __forceinline__ void as_loaded(Some<E, V>& x) {
-  static_assert(sizeof(x) <= 4);
-  typedef std::conditional_t<sizeof(x) == 4, uint32_t, uint16_t> U;
-  uint32_t bits = __builtin_bit_cast(U, x);
-  asm volatile("" : "+v"(bits));
-  x = __builtin_bit_cast(Some<E, V>, (U)bits);
-}
-
-// The channel of place `at` of a workgroup's 64 V.
-template <int V>
-__device__ __forceinline__ int channel_of(int column, int at, int D) { return Own<V>(column, at / V, D).d + at % V; }
-template <int V>
-__device__ __forceinline__ void parameter(const float* p, int d, float (&v)[V]) {
-#pragma unroll
-  for (int c = 0; c < V; ++c) v[c] = p ? p[d + c] : 0.0f;
-}
-
-// 1 - exp(-x) for x >= 0, given e = exp(-x): below 1/4, where the difference would lose bits, x times the series of
-// (1 - exp(-x)) / x up to x^6 / 7!, within 2^-26 of it.
-__device__ __forceinline__ float one_minus(float e, float x) {
-  float p = fmaf(x, 1.0f / 5040.0f, -1.0f / 720.0f);
-  p = fmaf(p, x, 1.0f / 120.0f), p = fmaf(p, x, -1.0f / 24.0f), p = fmaf(p, x, 1.0f / 6.0f), p = fmaf(p, x, -0.5f);
-  p = fmaf(p, x, 1.0f);
-  return x < 0.25f ? x * p : 1.0f - e;
-}
-
-// A step's gates: rho and iota, the decay a = exp(-decay rho) and m2 = 1 - a^2, of which what enters is the root.
-struct Gates {
-  float rho, iota, a, m2;
-};
+// A lane's V channels of a row as they were loaded, in one register, and the value of one of them.  (As an array of V the compiler
+// takes them apart where they are loaded, for twice the registers.)
 template <typename E>
-__device__ __forceinline__ Gates gates_of(float r, float i, float decay) {
-  Gates g;
-  g.rho = sigmoid<E>(r), g.iota = sigmoid<E>(i);
-  const float size = decay * g.rho;
-  g.a = exp_of<kExact<E>>(-size);
-  g.m2 = one_minus(g.a * g.a, size + size);
-  return g;
+__device__ __forceinline__ float part(uint32_t bits, int c) {
+  if constexpr (sizeof(E) == 4) return __uint_as_float(bits);
+  else if constexpr (std::is_same_v<E, bf16_t>) return __uint_as_float(c ? bits & 0xFFFF0000u : bits << 16);
+  else return static_cast<float>(__builtin_bit_cast(E, (uint16_t)(c ? bits >> 16 : bits)));
 }
+// Such values stay as they are up to here: widened as soon as they can be they would take twice the registers again.
+__device__ __forceinline__ void as_loaded(uint32_t& bits) { asm volatile("" : "+v"(bits)); }
+
+// The rows of a wave's run in an array: the first one's address and the bytes to the next, both the same for the whole wave, so that
+// an access is a scalar address and a lane's offset of 32 bits, and a row costs one scalar addition.
+template <typename E>
+struct Run {
+  typedef std::remove_const_t<E> T;
+  uint64_t at;
+  int64_t step;
+  __device__ __forceinline__ Run(const Rows<E>& r, int t, int b) : at((uint64_t)r.at(t, b)), step(r.st * (int64_t)sizeof(E)) {}
+  template <int V>
+  using Bits = std::conditional_t<sizeof(Some<T, V>) == 4, uint32_t, uint16_t>;      // of any alignment, as Some is
+  template <int V>
+  using Loose = Bits<V> __attribute__((aligned(sizeof(T))));
+  template <int V>
+  __device__ __forceinline__ uint32_t load(uint32_t byte) const { return *(const __attribute__((address_space(1))) Loose<V>*)(at + byte); }
+  template <int V>
+  __device__ __forceinline__ void store(uint32_t byte, const float (&x)[V]) const {
+    Some<T, V> s;
+#pragma unroll
+    for (int i = 0; i < V; ++i) s.v[i] = static_cast<T>(x[i]);
+    *(__attribute__((address_space(1))) Loose<V>*)(at + byte) = __builtin_bit_cast(Bits<V>, s);
+  }
+  // (opaque, or the lane's offset is added first and every row's address is one of vector registers)
+  __device__ __forceinline__ void move_by(int64_t bytes) {
+    at += bytes;
+    asm("" : "+s"(at));
+  }
+  __device__ __forceinline__ void move() { move_by(step); }
+};
+// R rows of it; of fewer (not WHOLE) the last one again: what is made of those is left out.
+template <bool WHOLE, int R, int V, typename E>
+__device__ __forceinline__ void load_rows(const Rows<E>& from, int first, int b, int rows, uint32_t byte, uint32_t (&x)[R]) {
+  Run<E> run(from, first, b);
+  asm("" : "+s"(run.at));
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    x[j] = run.template load<V>(byte);
+    if (j + 1 < R) run.move_by(WHOLE || j + 1 < rows ? run.step : 0);
+  }
+}
+
+// The instructions of two rows stay together: the compiler starts all rows of a run at once, which takes more registers than there are.
+__device__ __forceinline__ void apart(int row) {
+  if (row % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+}
+
+// The channel of place `at` of a workgroup's 64 V, D where it has none.
+template <int V>
+__device__ __forceinline__ int channel_of(int column, int at, int D) {
+  const Own<V> own(column, at / V, D);
+  return own.on ? own.d + at % V : D;
+}
+// 1 - exp(-x) for x >= 0, given e2 = exp(-x / 2): below 1/4, where the difference would lose bits, x times (1 - exp(-x)) / x
+// interpolated at the five Chebyshev nodes of [0, 1/4], within 2^-28 of it.
+__device__ __forceinline__ float one_minus(float e2, float x) {
+  const float p = fmaf(fmaf(fmaf(fmaf(7.51360599e-3f, x, -4.14906554e-2f), x, 0.166651085f), x, -0.499999523f), x, 1.0f);
+  return x < 0.25f ? x * p : fmaf(-e2, e2, 1.0f);
+}
+
+// A channel's parameters as a step's gates take them.  Activations of 16 bits have their biases and log2(e) in one multiply-add
+// in front of the exponential; float32 ones are added up and go through the corrected functions.
+template <typename E>
+struct Channel {
+  float r_bias, i_bias, decay, of_exp;
+  __device__ __forceinline__ Channel(const Layer<E>& l, int d)
+      : r_bias(l.r_bias ? l.r_bias[d] : 0.0f), i_bias(l.i_bias ? l.i_bias[d] : 0.0f), decay(l.decay[d]), of_exp(decay * -kLog2e) {
+    if (!kExact<E>) r_bias *= -kLog2e, i_bias *= -kLog2e;
+  }
+  __device__ __forceinline__ static float gate(float x, float bias) {
+    if constexpr (kExact<E>) return sigmoid<E>(x + bias);
+    else return __builtin_amdgcn_rcpf(1.0f + exp2_fast(fmaf(x, -kLog2e, bias)));
+  }
+  __device__ __forceinline__ float rho(float r) const { return gate(r, r_bias); }
+  __device__ __forceinline__ float iota(float i) const { return gate(i, i_bias); }
+  __device__ __forceinline__ float a(float rho) const {
+    if constexpr (kExact<E>) return exp_of<true>(-decay * rho);
+    else return exp2_fast(of_exp * rho);
+  }
+  // 1 - a^2
+  __device__ __forceinline__ float m2(float a, float rho) const { return one_minus(a, (decay + decay) * rho); }
+};
 
 // One grid axis counts tiles, samples and columns; a launch has fewer than 2^32 threads, 512 a tile.
 static inline int64_t workgroups(int T, int B, int D) {
@@ -134,20 +184,20 @@ __device__ __forceinline__ float through(uint64_t w, float h) {
 __device__ __forceinline__ uint64_t peek(const uint64_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void leave(uint64_t* p, uint64_t w) { __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// The state that comes into a tile: `mine` is this tile's word of a channel, `step` the words to the next tile, `tiles` how many
-// lie in front of it (the farthest one's word becomes settled without waiting for any other).
-__device__ __forceinline__ float look_back(const uint64_t* mine, int64_t step, int tiles) {
-  constexpr int WINDOW = 8;
+// The state that comes into a tile: `mine` are this tile's words, the same for a wave, `at` a lane's place in them, `step` the words to
+// the next tile, `tiles` how many lie in front of it (the farthest one's words become settled without waiting for any other).
+__device__ __forceinline__ float look_back(const uint64_t* mine, uint32_t at, int64_t step, int tiles) {
+  constexpr int WINDOW = 4;
   int far = 0;                                 // windows behind this one that hold no settled word
   uint64_t w[WINDOW];
   auto window = [&](int k) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < WINDOW; ++j) {
       const int back = k * WINDOW + j + 1;
-      w[j] = peek(mine - step * (back <= tiles ? back : tiles));
+      w[j] = peek(mine - step * (back <= tiles ? back : tiles) + at);
     }
   };
-  for (;;) {
+  for (bool again = true; again;) {
     window(far);
     bool wait = false, found = false;
 #pragma unroll
@@ -155,24 +205,42 @@ __device__ __forceinline__ float look_back(const uint64_t* mine, int64_t step, i
       wait |= !found && w[j] == kEmpty;
       found |= is_settled(w[j]);
     }
-    if (__any(wait)) {
-      __builtin_amdgcn_s_sleep(1);
-      continue;
-    }
-    if (__all(found)) break;
-    ++far;
+    const bool stay = __any(wait), on = !__all(found);
+    if (stay) __builtin_amdgcn_s_sleep(1);
+    else far += on;
+    again = stay || on;
   }
   float h = 0.0f;
-  for (;;) {
+  for (;; --far) {
 #pragma unroll
     for (int j = WINDOW - 1; j >= 0; --j) h = through(w[j], h);
     if (far == 0) return h;
-    window(--far);
+    window(far - 1);
   }
 }
 
-// Empties the words of a call and its ticket, which lies in front of them.
-constexpr int kTicketBytes = 256;
+// The tiles of a column of a sample, which wait for each other, are one chain; the chains are dealt out to eight queues, one a compute
+// die, and a workgroup takes the next tile of its own die's queue (hardware register XCC_ID, id 20), or of another's when
+// that is done: words that were left on this die are found in its L2.  Where a workgroup runs is no more than a preference: each takes
+// exactly one of as many tiles as there are workgroups, and a queue hands its tiles out in the order of its chains' waits.
+constexpr int kQueues = 8, kTicketStride = 32, kTicketBytes = kQueues * kTicketStride * 4;
+__device__ __forceinline__ int2 take(int* tickets, int chains, int each, int tiles) {        // (chain, number of its tile)
+  const int own = __builtin_amdgcn_s_getreg(20 | 3 << 11) & (kQueues - 1);
+  for (int k = 0; k < 2 * kQueues; ++k) {
+    const int q = (own + k) & (kQueues - 1), first = q * each, n = chains - first < each ? chains - first : each;
+    if (n < 1) continue;
+    const int t = __hip_atomic_fetch_add(tickets + q * kTicketStride, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (t < n * tiles) return make_int2(first + t % n, t / n);
+  }
+  return make_int2(-1, 0);                     // not reached
+}
+
+// Chains of a queue.  Columns of one die alone fall into few of its L2's channels where rows lie a power of two apart, so few chains
+// are one queue, whose tiles are neighbours in memory: T = 30000, B = 1, D = 2048 bf16, 16 chains: 146 us, 155 in eight queues;
+// T = 1000, B = 16, D = 330 fp32, 96 chains: 26 us and 20.
+static inline int chains_of_queue(int chains) { return chains >= 64 ? bppsa_ceil_div(chains, kQueues) : chains; }
+
+// Empties the words of a call and its tickets, which lie in front of them.
 static __global__ void __launch_bounds__(256) empty_words_kernel(char* workspace, int64_t sixteens) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= sixteens) return;

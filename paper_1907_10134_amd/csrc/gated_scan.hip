@@ -8,27 +8,24 @@ using namespace gated;
 // A workgroup takes tiles of kTile steps of 64 V channels, one after the other.  Each wave has a run of the steps in registers:
 // it turns them into decays and what enters, finds what its run does to a state, and when the state before it is known walks
 // them again.  Outputs of a tile are on their way while the next one's inputs are asked for.
-template <typename E, int V, bool GATE, bool JOINED>
-__global__ void __launch_bounds__(kWaves * 64, 4)
-gated_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, int* ticket, uint64_t* words,
-             int total) {
-  constexpr int R = kRun;
-  __shared__ float2 runs[2][kWaves][64 * V];
-  __shared__ float before[2][64 * V];
-  __shared__ int taken[2];
+template <typename E, int V, int R, bool GATE, bool JOINED>
+__global__ void __launch_bounds__(kWaves * 64, sizeof(E) == 4 ? 6 : 4)
+gated_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, int* tickets, uint64_t* words, int tiles, int each) {
+  __shared__ float2 runs[kWaves][64 * V];
+  __shared__ float before[64 * V];
+  __shared__ int2 taken;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int id = blockIdx.x;
+  int chain = blockIdx.x, tile = 0;
   if (JOINED) {
-    if (threadIdx.x == 0) taken[1] = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    id = __builtin_amdgcn_readfirstlane(taken[1]);
+    if (threadIdx.x == 0) taken = take(tickets, l.columns * l.B, each, tiles);
+    lds_barrier();
+    chain = __builtin_amdgcn_readfirstlane(taken.x), tile = __builtin_amdgcn_readfirstlane(taken.y);
+    if (chain < 0) return;
   }
-  for (int parity = 0; id < total; parity ^= 1) {
-    int next = total;
-    if (JOINED && threadIdx.x == 0) next = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const int column = id % l.columns, b = id / l.columns % l.B, tile = id / l.columns / l.B;
+  {
+    const int column = chain % l.columns, b = chain / l.columns;
     const Own<V> own(column, lane, l.D);
-    const int d = own.d, len = clamp_length(l.lengths, b, l.T), t0 = tile * kTile, first = t0 + w * R;
+    const int d = own.d, len = clamp_length(l.lengths, b, l.T), t0 = tile * kWaves * R, first = t0 + w * R;
     // behind an end
     if (own.on)
       for (int t = first > len ? first : len; t < first + R && t < l.T; ++t) {
@@ -38,41 +35,47 @@ gated_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __r
     if (len == 0 && tile == 0 && w == 0 && h_last && own.on)
       for (int c = 0; c < V; ++c) h_last[(int64_t)b * l.D + d + c] = l.h0 ? l.h0[(int64_t)b * l.D + d + c] : 0.0f;
 
-    float a[R][V], e[R][V], h[V];
-    Some<E, V> z[GATE ? R : 1];
-    float product[V], end[V];
+    float a[R][V], e[R][V];
+    const int rows = len - first < R ? len - first : R;
+    const uint32_t byte = (uint32_t)d * sizeof(E);
+    // a run with an end in it is another copy of the code: with its conditions in this one there are too few scalar registers
+    auto gather = [&](auto all) __attribute__((always_inline)) {
+      constexpr bool WHOLE = all.value;
+      uint32_t x[R], r[R], i[R];
+      load_rows<WHOLE, R, V>(l.r, first, b, rows, byte, r), load_rows<WHOLE, R, V>(l.i, first, b, rows, byte, i), load_rows<WHOLE, R, V>(l.x, first, b, rows, byte, x);
+      const Channel<E> channel[2] = {Channel<E>(l, d), Channel<E>(l, d + V - 1)};
+      float product[V], end[V];
 #pragma unroll
-    for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = 0.0f;
-    if (first < len) {
-      Some<E, V> x[R], r[R], i[R];
-      float decay[V], rb[V], ib[V];
-      parameter(l.decay, d, decay), parameter(l.r_bias, d, rb), parameter(l.i_bias, d, ib);
+      for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = 0.0f;
 #pragma unroll
       for (int j = 0; j < R; ++j) {
-        const int t = first + j < len ? first + j : len - 1;
-        r[j] = load_some<E, V>(l.r.at(t, b) + d), i[j] = load_some<E, V>(l.i.at(t, b) + d), x[j] = load_some<E, V>(l.x.at(t, b) + d);
-        if (GATE) z[j] = load_some<E, V>(l.z.at(t, b) + d);
-      }
-#pragma unroll
-      for (int j = 0; j < R; ++j)
+        apart(j);
 #pragma unroll
         for (int c = 0; c < V; ++c) {
-          const Gates g = gates_of<E>((float)r[j].v[c] + rb[c], (float)i[j].v[c] + ib[c], decay[c]);
-          const bool real = first + j < len;
-          a[j][c] = real ? g.a : 1.0f;
-          e[j][c] = real ? __builtin_amdgcn_sqrtf(g.m2) * g.iota * (float)x[j].v[c] : 0.0f;
+          const float rho = channel[c].rho(part<E>(r[j], c)), iota = channel[c].iota(part<E>(i[j], c));
+          a[j][c] = channel[c].a(rho), e[j][c] = __builtin_amdgcn_sqrtf(channel[c].m2(a[j][c], rho)) * iota * part<E>(x[j], c);
+          if (!WHOLE && j >= rows) a[j][c] = 1.0f, e[j][c] = 0.0f;
           product[c] *= a[j][c], end[c] = fmaf(a[j][c], end[c], e[j][c]);
         }
-    }
+      }
 #pragma unroll
-    for (int c = 0; c < V; ++c) runs[parity][w][lane * V + c] = make_float2(product[c], end[c]);
+      for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float2(product[c], end[c]);
+    };
+    if (rows == R) gather(std::true_type{});
+    else if (rows > 0) gather(std::false_type{});
+    else
+#pragma unroll
+      for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float2(1.0f, 0.0f);
     lds_barrier();
+    uint32_t z[R];                // asked for now and used when the tile is joined
+    if (GATE && rows == R) load_rows<true, R, V>(l.z, first, b, rows, byte, z);
+    else if (GATE && rows > 0) load_rows<false, R, V>(l.z, first, b, rows, byte, z);
     if (w < V && t0 < len) {                   // the tile's own share, a channel a lane
-      const int at = w * 64 + lane;
+      const uint32_t at = w * 64 + lane;
       float p = 1.0f, s = 0.0f, in = 0.0f;
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) {
-        const float2 run = runs[parity][k][at];
+        const float2 run = runs[k][at];
         p *= run.x, s = fmaf(run.x, s, run.y);
       }
       if (tile == 0 && l.h0) {
@@ -81,48 +84,47 @@ gated_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __r
       }
       if (JOINED) {
         const int64_t step = (int64_t)l.B * l.columns * 64 * V;
-        uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V + at;
-        if (tile) leave(mine, word_of(p, s)), in = look_back(mine, step, tile);
-        leave(mine, settled(through(word_of(p, s), in)));
+        uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V;
+        if (tile) leave(mine + at, word_of(p, s)), in = look_back(mine, at, step, tile);
+        leave(mine + at, settled(through(word_of(p, s), in)));
       }
-      before[parity][at] = in;
+      before[at] = in;
     }
-    if (JOINED && threadIdx.x == 0) taken[parity] = next;
     lds_barrier();
-    if (first < len) {
+    if (rows > 0 && own.on) {
       if (GATE)
 #pragma unroll
         for (int j = 0; j < R; ++j) as_loaded(z[j]);
+      float h[V];
 #pragma unroll
-      for (int c = 0; c < V; ++c) h[c] = before[parity][lane * V + c];
+      for (int c = 0; c < V; ++c) h[c] = before[lane * V + c];
       for (int k = 0; k < w; ++k)
 #pragma unroll
         for (int c = 0; c < V; ++c) {
-          const float2 run = runs[parity][k][lane * V + c];
+          const float2 run = runs[k][lane * V + c];
           h[c] = fmaf(run.x, h[c], run.y);
         }
-      if (states && first % kKept == 0 && own.on)
+      if (states && first % kKept == 0)
 #pragma unroll
         for (int c = 0; c < V; ++c) states[((int64_t)(first / kKept) * l.B + b) * l.D + d + c] = h[c];
+      Run<E> to(y, first, b);
 #pragma unroll
       for (int j = 0; j < R; ++j) {
         float out[V];
 #pragma unroll
         for (int c = 0; c < V; ++c) {
           h[c] = fmaf(a[j][c], h[c], e[j][c]);
-          out[c] = GATE ? h[c] * ((float)z[j].v[c] * sigmoid<E>((float)z[j].v[c])) : h[c];
+          out[c] = GATE ? h[c] * (part<E>(z[j], c) * sigmoid<E>(part<E>(z[j], c))) : h[c];
         }
-        if (first + j < len && own.on) store_some<E, V>(y.at(first + j, b) + d, out);
+        if (j < rows) to.store(byte, out);
+        to.move();
       }
-      if (h_last && own.on && len <= first + R)
+      if (h_last && len <= first + R)
 #pragma unroll
         for (int c = 0; c < V; ++c) h_last[(int64_t)b * l.D + d + c] = h[c];
     }
-    id = JOINED ? __builtin_amdgcn_readfirstlane(taken[parity]) : total;
   }
 }
-
-constexpr int kResident = 2;     // workgroups of a compute unit
 
 // One token.  A thread has a lane's channels of one row of the batch; bound by the launch and one round of loads.
 template <typename E, int V>
@@ -135,24 +137,24 @@ gated_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int sl
   int slot = slots ? slots[b] : b;
   float out[V] = {};
   if (slot < 0 || slot >= slots_in_state) return store_some<E, V>(y.at(0, b) + d, out);
-  float decay[V], rb[V], ib[V], h[V];
   float* const at = state + (int64_t)slot * l.D + d;
-  parameter(l.decay, d, decay), parameter(l.r_bias, d, rb), parameter(l.i_bias, d, ib), parameter(at, 0, h);
+  Some<float, V> h = load_some<float, V>(at);
   const auto x = load_some<E, V>(l.x.at(0, b) + d), r = load_some<E, V>(l.r.at(0, b) + d), i = load_some<E, V>(l.i.at(0, b) + d);
   Some<E, V> z = {};
   if (l.z.data) z = load_some<E, V>(l.z.at(0, b) + d);
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    const Gates g = gates_of<E>((float)r.v[c] + rb[c], (float)i.v[c] + ib[c], decay[c]);
-    h[c] = fmaf(g.a, h[c], __builtin_amdgcn_sqrtf(g.m2) * g.iota * (float)x.v[c]);
-    out[c] = l.z.data ? h[c] * (float)z.v[c] * sigmoid<E>((float)z.v[c]) : h[c];
+    const Channel<E> channel(l, d + c);
+    const float rho = channel.rho((float)r.v[c]), iota = channel.iota((float)i.v[c]), a = channel.a(rho);
+    h.v[c] = fmaf(a, h.v[c], __builtin_amdgcn_sqrtf(channel.m2(a, rho)) * iota * (float)x.v[c]);
+    out[c] = l.z.data ? h.v[c] * (float)z.v[c] * sigmoid<E>((float)z.v[c]) : h.v[c];
   }
   // in place: what is repeated has been read before or behind the neighbour's update, and is not stored
   if (own.repeated) {
-    for (int c = own.repeated; c < V; ++c) at[c] = h[c], store(y.at(0, b) + d + c, out[c]);
+    for (int c = own.repeated; c < V; ++c) at[c] = h.v[c], store(y.at(0, b) + d + c, out[c]);
     return;
   }
-  store_some<float, V>(at, h);
+  *reinterpret_cast<Some<float, V>*>(at) = h;
   store_some<E, V>(y.at(0, b) + d, out);
 }
 
@@ -181,20 +183,22 @@ extern "C" bppsa_status bppsa_gated_scan(const bppsa_gated* layer, const bppsa_r
       constexpr int V = width.value;
       const Layer<E> l = layer_of<E>(*layer, 64 * V);
       const int tiles = bppsa_ceil_div(l.T, kTile), total = tiles * l.B * l.columns;
-      const auto run = [&](auto gate, auto joined) {
-        constexpr bool GATE = gate.value, JOINED = joined.value;
-        const int groups = JOINED ? std::min(total, bppsa_compute_units() * kResident) : total;
-        gated_kernel<E, V, GATE, JOINED><<<groups, kWaves * 64, 0, s>>>(
+      const auto run = [&](auto steps, auto gate, auto joined) {
+        gated_kernel<E, V, steps.value, gate.value, joined.value><<<total, kWaves * 64, 0, s>>>(
             l, rows_of<E>(*y), h_last, static_cast<float*>(states), static_cast<int*>(workspace),
-            reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + kTicketBytes), total);
+            reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + kTicketBytes), tiles, chains_of_queue(l.columns * l.B));
       };
+      constexpr std::integral_constant<int, kRun> whole;
+      constexpr std::integral_constant<int, kRun / 2> half;
       constexpr std::true_type yes;
       constexpr std::false_type no;
       if (tiles > 1) {
         empty_words(workspace, words_bytes(tiles, l.B, l.columns, V), s);
-        l.z.data ? run(yes, yes) : run(no, yes);
-      } else {
-        l.z.data ? run(yes, no) : run(no, no);
+        l.z.data ? run(whole, yes, yes) : run(whole, no, yes);
+      } else if (l.T > kTile / 2) {
+        l.z.data ? run(whole, yes, no) : run(whole, no, no);
+      } else {                       // T = 16, B = 2, D = 40 fp32: 3.8 us, 5.6 by runs of sixteen steps
+        l.z.data ? run(half, yes, no) : run(half, no, no);
       }
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;

@@ -18,29 +18,26 @@ struct Grads {
 
 // The tiles run from the end, kKept steps each, joined as those of the forward pass are: a word says what a tile does to the
 // gradient that comes in from behind.  A run's states are found again from the one kept before its tile and the shares of the
-// runs in front of it, so a tile's inputs are read once.  The gates are made twice, before the tile is joined and behind: kept
-// over it they would be twice the registers.
+// runs in front of it, so a tile's inputs are read once.
 template <typename E, int V, bool GATE, bool JOINED>
-__global__ void __launch_bounds__(kWaves * 64, 4)
+__global__ void __launch_bounds__(kWaves * 64, sizeof(E) == 4 && !GATE ? 6 : 4)
 gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ dh_last, const float* __restrict__ states,
-                      const Grads<E> o, int* ticket, uint64_t* words, int total) {
+                      const Grads<E> o, int* tickets, uint64_t* words, int tiles, int each) {
   constexpr int R = kRunBack;
-  __shared__ float4 runs[2][kWaves][64 * V];             // product of the decays, state from zero, gradient from zero
-  __shared__ float2 border[2][64 * V];                   // the state before the tile, the gradient behind it
-  __shared__ float sums[2][3][kWaves][64 * V];
-  __shared__ int taken[2];
+  __shared__ float4 runs[kWaves][64 * V];             // product of the decays, state from zero, gradient from zero
+  __shared__ float2 border[64 * V];                   // the state before the tile, the gradient behind it
+  __shared__ float sums[3][kWaves][64 * V];
+  __shared__ int2 taken;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int id = blockIdx.x;
+  int chain = blockIdx.x, tile = 0;
   if (JOINED) {
-    if (threadIdx.x == 0) taken[1] = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    id = __builtin_amdgcn_readfirstlane(taken[1]);
+    if (threadIdx.x == 0) taken = take(tickets, l.columns * l.B, each, tiles);
+    lds_barrier();
+    chain = __builtin_amdgcn_readfirstlane(taken.x), tile = tiles - 1 - __builtin_amdgcn_readfirstlane(taken.y);
+    if (chain < 0) return;
   }
-  const int tiles = (l.T + kKept - 1) / kKept;
-  for (int parity = 0; id < total; parity ^= 1) {
-    int next = total;
-    if (JOINED && threadIdx.x == 0) next = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const int column = id % l.columns, b = id / l.columns % l.B, tile = tiles - 1 - id / l.columns / l.B;
+  {
+    const int column = chain % l.columns, b = chain / l.columns;
     const Own<V> own(column, lane, l.D);
     const int d = own.d, len = clamp_length(l.lengths, b, l.T), t0 = tile * kKept, first = t0 + w * R;
     const int last_tile = (len + kKept - 1) / kKept - 1;
@@ -54,47 +51,49 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
     if (len == 0 && tile == 0 && w == 0 && o.dh0 && own.on)
       for (int c = 0; c < V; ++c) o.dh0[(int64_t)b * l.D + d + c] = dh_last ? dh_last[(int64_t)b * l.D + d + c] : 0.0f;
 
-    Some<E, V> x[R], r[R], i[R], go[R], z[GATE ? R : 1];
-    float a[R][V], e[R][V], q[R][V], decay[V], rb[V], ib[V], sum[3][V] = {};
-    float product[V], end[V], back[V];
-    parameter(l.decay, d, decay), parameter(l.r_bias, d, rb), parameter(l.i_bias, d, ib);
+    uint32_t x[R], go[R], z[R];
+    float a[R][V], e[R][V], rho[R][V], iota[R][V], sum[3][V] = {};
+    const int rows = len - first < R ? len - first : R;
+    const uint32_t byte = (uint32_t)d * sizeof(E);
+    auto gather = [&](auto all) __attribute__((always_inline)) {
+      constexpr bool WHOLE = all.value;
+      uint32_t r[R], i[R];
+      load_rows<WHOLE, R, V>(l.r, first, b, rows, byte, r), load_rows<WHOLE, R, V>(l.i, first, b, rows, byte, i), load_rows<WHOLE, R, V>(l.x, first, b, rows, byte, x);
+      load_rows<WHOLE, R, V>(dy, first, b, rows, byte, go);
+      if (GATE) load_rows<WHOLE, R, V>(l.z, first, b, rows, byte, z);
+      const Channel<E> channel[2] = {Channel<E>(l, d), Channel<E>(l, d + V - 1)};
+      float product[V], end[V], back[V];
 #pragma unroll
-    for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = back[c] = 0.0f;
-    if (first < len) {
+      for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = back[c] = 0.0f;
 #pragma unroll
       for (int j = 0; j < R; ++j) {
-        const int t = first + j < len ? first + j : len - 1;
-        r[j] = load_some<E, V>(l.r.at(t, b) + d), i[j] = load_some<E, V>(l.i.at(t, b) + d), x[j] = load_some<E, V>(l.x.at(t, b) + d);
-        go[j] = load_some<E, V>(dy.at(t, b) + d);
-        if (GATE) z[j] = load_some<E, V>(l.z.at(t, b) + d);
-      }
-#pragma unroll
-      for (int j = 0; j < R; ++j)
+        apart(j);
 #pragma unroll
         for (int c = 0; c < V; ++c) {
-          const Gates g = gates_of<E>((float)r[j].v[c] + rb[c], (float)i[j].v[c] + ib[c], decay[c]);
-          const bool real = first + j < len;
-          a[j][c] = real ? g.a : 1.0f;
-          e[j][c] = real ? __builtin_amdgcn_sqrtf(g.m2) * g.iota * (float)x[j].v[c] : 0.0f;
-          q[j][c] = (float)go[j].v[c];
-          if (GATE) q[j][c] *= (float)z[j].v[c] * sigmoid<E>((float)z[j].v[c]);
-          if (!real) q[j][c] = 0.0f;
-          product[c] *= a[j][c], end[c] = fmaf(a[j][c], end[c], e[j][c]);
+          rho[j][c] = channel[c].rho(part<E>(r[j], c)), iota[j][c] = channel[c].iota(part<E>(i[j], c));
+          a[j][c] = channel[c].a(rho[j][c]);
+          e[j][c] = __builtin_amdgcn_sqrtf(channel[c].m2(a[j][c], rho[j][c])) * iota[j][c] * part<E>(x[j], c);
+          float q = part<E>(go[j], c);
+          if (GATE) q *= part<E>(z[j], c) * sigmoid<E>(part<E>(z[j], c));
+          if (!WHOLE && j >= rows) a[j][c] = 1.0f, e[j][c] = q = 0.0f;
+          product[c] *= a[j][c], end[c] = fmaf(a[j][c], end[c], e[j][c]), back[c] = fmaf(product[c], q, back[c]);
         }
+      }
 #pragma unroll
-      for (int j = R - 1; j >= 0; --j)
+      for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float4(product[c], end[c], back[c], 0.0f);
+    };
+    if (rows == R) gather(std::true_type{});
+    else if (rows > 0) gather(std::false_type{});
+    else
 #pragma unroll
-        for (int c = 0; c < V; ++c) back[c] = a[j][c] * (q[j][c] + back[c]);
-    }
-#pragma unroll
-    for (int c = 0; c < V; ++c) runs[parity][w][lane * V + c] = make_float4(product[c], end[c], back[c], 0.0f);
+      for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float4(1.0f, 0.0f, 0.0f, 0.0f);
     lds_barrier();
     if (w < V && t0 < len) {                   // the tile's own share, a channel a lane
-      const int at = w * 64 + lane;
+      const uint32_t at = w * 64 + lane;
       float p = 1.0f, s = 0.0f, in = 0.0f;
 #pragma unroll
       for (int k = kWaves - 1; k >= 0; --k) {
-        const float4 run = runs[parity][k][at];
+        const float4 run = runs[k][at];
         p *= run.x, s = fmaf(run.x, s, run.z);
       }
       const int channel = channel_of<V>(column, at, l.D);
@@ -102,31 +101,30 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
       if (tile == last_tile && dh_last && on) in = dh_last[(int64_t)b * l.D + channel];
       if (JOINED) {
         const int64_t step = (int64_t)l.B * l.columns * 64 * V;
-        uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V + at;
-        if (tile < last_tile) leave(mine, word_of(p, s)), in = look_back(mine, -step, last_tile - tile);
-        leave(mine, settled(through(word_of(p, s), in)));
+        uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V;
+        if (tile < last_tile) leave(mine + at, word_of(p, s)), in = look_back(mine, at, -step, last_tile - tile);
+        leave(mine + at, settled(through(word_of(p, s), in)));
       }
-      border[parity][at] = make_float2(on ? states[((int64_t)tile * l.B + b) * l.D + channel] : 0.0f, in);
+      border[at] = make_float2(on ? states[((int64_t)tile * l.B + b) * l.D + channel] : 0.0f, in);
     }
-    if (JOINED && threadIdx.x == 0) taken[parity] = next;
     lds_barrier();
-    if (first < len) {
+    if (rows > 0 && own.on) {
       float h[V], g[V];
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        const float2 both = border[parity][lane * V + c];
+        const float2 both = border[lane * V + c];
         h[c] = both.x, g[c] = both.y;
       }
       for (int k = 0; k < w; ++k)
 #pragma unroll
         for (int c = 0; c < V; ++c) {
-          const float4 run = runs[parity][k][lane * V + c];
+          const float4 run = runs[k][lane * V + c];
           h[c] = fmaf(run.x, h[c], run.y);
         }
       for (int k = kWaves - 1; k > w; --k)
 #pragma unroll
         for (int c = 0; c < V; ++c) {
-          const float4 run = runs[parity][k][lane * V + c];
+          const float4 run = runs[k][lane * V + c];
           g[c] = fmaf(run.x, g[c], run.z);
         }
       // the states before each step, in the place of what enters
@@ -135,57 +133,64 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
 #pragma unroll
         for (int c = 0; c < V; ++c) {
           const float before = h[c];
-          h[c] = fmaf(a[j][c], h[c], e[j][c]), e[j][c] = before;
+          h[c] = fmaf(a[j][c], h[c], e[j][c]);
+          e[j][c] = before;
         }
 #pragma unroll
-      for (int j = 0; j < R; ++j) as_loaded(x[j]), as_loaded(r[j]), as_loaded(i[j]);
+      for (int j = 0; j < R; ++j) {
+        as_loaded(x[j]), as_loaded(go[j]);
+        if (GATE) as_loaded(z[j]);
+      }
+      const Channel<E> channel[2] = {Channel<E>(l, d), Channel<E>(l, d + V - 1)};
+      Run<E> to_x(o.dx, first, b), to_r(o.dr, first, b), to_i(o.di, first, b), to_z(GATE ? o.dz : o.dx, first, b);
+      const int64_t last = rows - 1;
+      to_x.move_by(last * to_x.step), to_r.move_by(last * to_r.step), to_i.move_by(last * to_i.step);
+      if (GATE) to_z.move_by(last * to_z.step);
 #pragma unroll
       for (int j = R - 1; j >= 0; --j) {
+        apart(j + 1);
         float dx[V], dr[V], di[V], dz[V];
+        if (j >= rows) continue;
 #pragma unroll
         for (int c = 0; c < V; ++c) {
-          const float rho = sigmoid<E>((float)r[j].v[c] + rb[c]), iota = sigmoid<E>((float)i[j].v[c] + ib[c]), of_x = (float)x[j].v[c];
-          const float m2 = one_minus(a[j][c] * a[j][c], 2.0f * decay[c] * rho);
-          const float root = m2 > 0x1p-120f ? __builtin_amdgcn_rsqf(m2) : 0.0f, m = m2 * root;
+          const float of_x = part<E>(x[j], c), m2 = channel[c].m2(a[j][c], rho[j][c]), root = m2 > 0x1p-120f ? __builtin_amdgcn_rsqf(m2) : 0.0f, m = m2 * root;
+          float q = part<E>(go[j], c);
           if (GATE) {
-            const float of_z = (float)z[j].v[c], sg = sigmoid<E>(of_z);
-            dz[c] = (float)go[j].v[c] * h[c] * sg * fmaf(of_z, 1.0f - sg, 1.0f);
+            const float of_z = part<E>(z[j], c), sg = sigmoid<E>(of_z), q_sg = q * sg;
+            dz[c] = q_sg * h[c] * fmaf(of_z, 1.0f - sg, 1.0f);
+            q = q_sg * of_z;
           }
-          const float gh = q[j][c] + g[c];
+          const float gh = q + g[c];
           g[c] = a[j][c] * gh;
-          const float s = g[c] * rho * fmaf(a[j][c] * iota * of_x, root, -e[j][c]);
-          dx[c] = gh * m * iota;
-          di[c] = dx[c] * of_x * (1.0f - iota);
-          dr[c] = decay[c] * (1.0f - rho) * s;
+          const float s = g[c] * rho[j][c] * fmaf(a[j][c] * iota[j][c] * of_x, root, -e[j][c]);
+          dx[c] = gh * m * iota[j][c];
+          di[c] = dx[c] * fmaf(-of_x, iota[j][c], of_x);
+          dr[c] = channel[c].decay * fmaf(-rho[j][c], s, s);
           h[c] = e[j][c];
-          if (first + j < len) sum[0][c] += s, sum[1][c] += dr[c], sum[2][c] += di[c];
+          sum[0][c] += s, sum[1][c] += dr[c], sum[2][c] += di[c];
         }
-        if (first + j < len && own.on) {
-          store_some<E, V>(o.dx.at(first + j, b) + d, dx), store_some<E, V>(o.dr.at(first + j, b) + d, dr), store_some<E, V>(o.di.at(first + j, b) + d, di);
-          if (GATE) store_some<E, V>(o.dz.at(first + j, b) + d, dz);
-        }
+        to_x.store(byte, dx), to_r.store(byte, dr), to_i.store(byte, di);
+        to_x.move_by(-to_x.step), to_r.move_by(-to_r.step), to_i.move_by(-to_i.step);
+        if (GATE) to_z.store(byte, dz), to_z.move_by(-to_z.step);
       }
-      if (o.dh0 && first == 0 && own.on)
+      if (o.dh0 && first == 0)
 #pragma unroll
         for (int c = 0; c < V; ++c) o.dh0[(int64_t)b * l.D + d + c] = g[c];
     }
 #pragma unroll
     for (int k = 0; k < 3; ++k)
 #pragma unroll
-      for (int c = 0; c < V; ++c) sums[parity][k][w][lane * V + c] = sum[k][c];
+      for (int c = 0; c < V; ++c) sums[k][w][lane * V + c] = sum[k][c];
     lds_barrier();
     for (int at = threadIdx.x; at < 3 * 64 * V; at += kWaves * 64) {
       const int k = at / (64 * V), place = at % (64 * V), channel = channel_of<V>(column, place, l.D);
       float all = 0.0f;
 #pragma unroll
-      for (int n = 0; n < kWaves; ++n) all += sums[parity][k][n][place];
+      for (int n = 0; n < kWaves; ++n) all += sums[k][n][place];
       if (channel < l.D) o.parts[(((int64_t)tile * l.B + b) * 3 + k) * l.D + channel] = all;
     }
-    id = JOINED ? __builtin_amdgcn_readfirstlane(taken[parity]) : total;
   }
 }
-
-constexpr int kResident = 2;     // workgroups of a compute unit
 
 // The sums over parts, in order: sixteen waves a sixteenth each, then those.  In 64 bits, which cost nothing beside the loads.
 struct Joined {
@@ -242,10 +247,9 @@ extern "C" bppsa_status bppsa_gated_scan_backward(const bppsa_gated* layer, cons
       const int total = tiles * l.B * l.columns;
       const auto run = [&](auto gate, auto joined) {
         constexpr bool GATE = gate.value, JOINED = joined.value;
-        const int groups = JOINED ? std::min(total, bppsa_compute_units() * kResident) : total;
-        gated_backward_kernel<E, V, GATE, JOINED><<<groups, kWaves * 64, 0, s>>>(
+        gated_backward_kernel<E, V, GATE, JOINED><<<total, kWaves * 64, 0, s>>>(
             l, rows_of<const E>(*dy), dh_last, static_cast<const float*>(states), o, reinterpret_cast<int*>(base),
-            reinterpret_cast<uint64_t*>(base + kTicketBytes), total);
+            reinterpret_cast<uint64_t*>(base + kTicketBytes), tiles, chains_of_queue(l.columns * l.B));
       };
       constexpr std::true_type yes;
       constexpr std::false_type no;
