@@ -6,6 +6,7 @@
 // M = sum p + p0, p0 / q0 = 0 without the normaliser.  The other part, -log softmax(x)[target], has the gradient
 // softmax(x) - 1[target].  What is made of the K entries alone is made in 64 bits: there are few of them, and the parts of a
 // divergence cancel.
+#include "lanes.h"
 #include "ssm_common.h"
 
 namespace {
@@ -37,24 +38,67 @@ struct Loss {
 
 constexpr int kMost = BPPSA_DISTIL_MAX_K;
 
-// exp(d scale), to_log2 = scale log2(e).  The difference to the largest is exact or nearly so; float32 logits take the corrected exponential.
+// exp((x - m) scale) for logits of which m is the largest.  float32 logits take the corrected exponential.  For 16-bit ones it is one
+// multiply-add in front of the exponential, 2^(k x - k m) with k = scale log2(e): what the rounding of k m leaves is the same factor
+// 2^off in all of a row's, and is taken from the logarithm of their sum.  Where k m passes 2^20 the next smaller logit of 16
+// bits has no share left, with a k of 2^20 / m either: so nothing overflows.
 template <typename E>
-__device__ __forceinline__ float exponential(float d, float scale, float to_log2) {
-  if constexpr (kExact<E>) return exp_of<true>(d * scale);
-  else return exp2_fast(d * to_log2);
-}
+struct Exponential {
+  float m, scale, k, km, off;
+  __device__ __forceinline__ Exponential(float largest, float scale)
+      : m(largest), scale(scale), k(fminf(scale * kLog2e, 0x1p20f / fabsf(largest))), km(largest * k), off(fmaf(largest, k, -km)) {}
+  __device__ __forceinline__ float operator()(float x) const {
+    if constexpr (kExact<E>) return exp_of<true>((x - m) * scale);
+    else return exp2_fast(fmaf(x, k, -km));
+  }
+  // what comes off the logarithm of a sum of such
+  __device__ __forceinline__ double log_off() const { return kExact<E> ? 0.0 : 0.69314718055994531 * (double)off; }
+};
 
 // Eight 16-bit or four 32-bit logits as they were loaded, and the value of one.
 template <typename E>
 struct Chunk {
   static constexpr int N = 16 / sizeof(E);
   uint32_t w[4];
+  // the first n become minus infinity
+  __device__ __forceinline__ void leave_out(int n) {
+    constexpr uint32_t none = sizeof(E) == 4 ? 0xFF800000u : std::is_same_v<E, bf16_t> ? 0xFF80u : 0xFC00u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(E) == 4) {
+        if (i < n) w[i] = none;
+      } else {
+        if (2 * i < n) w[i] = (w[i] & 0xFFFF0000u) | none;
+        if (2 * i + 1 < n) w[i] = (w[i] & 0xFFFFu) | none << 16;
+      }
+    }
+  }
   __device__ __forceinline__ float operator[](int k) const {
     if constexpr (sizeof(E) == 4) return __uint_as_float(w[k]);
     else if constexpr (std::is_same_v<E, bf16_t>) return __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
     else return static_cast<float>(__builtin_bit_cast(E, (uint16_t)(k & 1 ? w[k / 2] >> 16 : w[k / 2])));
   }
 };
+typedef uint32_t Four __attribute__((ext_vector_type(4)));
+typedef Four Loose __attribute__((aligned(2)));
+// A whole chunk at a place that is the same for all threads and a thread's offset of 32 bits: one address of scalar registers for
+// each, where sixteen of vector registers would push the row out.
+template <typename E>
+__device__ __forceinline__ Chunk<E> load_whole(const E* place, uint32_t byte) {
+  uint64_t at = (uint64_t)place;
+  asm("" : "+s"(at));
+  const Four w = *(const __attribute__((address_space(1))) Loose*)(at + byte);
+  return Chunk<E>{{w.x, w.y, w.z, w.w}};
+}
+template <typename E>
+__device__ __forceinline__ void store_whole(E* place, uint32_t byte, const float (&v)[Chunk<E>::N]) {
+  uint64_t at = (uint64_t)place;
+  asm("" : "+s"(at));
+  Some<E, Chunk<E>::N> s;
+#pragma unroll
+  for (int k = 0; k < Chunk<E>::N; ++k) s.v[k] = static_cast<E>(v[k]);
+  *(__attribute__((address_space(1))) Loose*)(at + byte) = __builtin_bit_cast(Four, s);
+}
 // What lies behind the row's end counts as minus infinity, which has no share.
 template <typename E>
 __device__ __forceinline__ Chunk<E> load_chunk(const E* x, int at, int V) {
@@ -74,47 +118,31 @@ __device__ __forceinline__ void store_chunk(E* x, int at, int V, const float (&v
     if (at + k < V) store(x + at + k, v[k]);
 }
 
-template <int WAVES, int N>
-struct Share {                     // of the waves, N values each
-  double v[N][WAVES];
+// What the waves of a row tell each other, each by its first lane.
+template <int WAVES>
+struct Share {
+  float largest[WAVES], sums[3][WAVES];
+  float top[WAVES];
+  double shares[WAVES], terms[WAVES];
 };
-// Sums of N values over the workgroup, in the same order for all of its threads.
-template <int WAVES, int N>
-__device__ __forceinline__ void sum_over_threads(double (&v)[N], Share<WAVES, N>& share) {
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) v[i] += __shfl_xor(v[i], k);
-  if constexpr (WAVES > 1) {
-    if ((threadIdx.x & 63) < N) {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if ((threadIdx.x & 63) == i) share.v[i][threadIdx.x >> 6] = v[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = share.v[i][0];
-#pragma unroll
-      for (int k = 1; k < WAVES; ++k) v[i] += share.v[i][k];
-    }
-  }
-}
-
 // One workgroup a row.  CHUNKS > 0: the row is read once, into registers (16 bytes a lane and chunk), and its largest value, its sums
 // and its gradient are made of those; 0: a row too long for that is read three times.  SECOND: the data's own token has a
 // softmax of its own, at another temperature.
 template <typename E, int WAVES, int CHUNKS, bool SECOND>
-__global__ void __launch_bounds__(WAVES * 64)
+__global__ void __launch_bounds__(WAVES * 64, WAVES * CHUNKS <= 64 ? 6 : 4)
 distil_kernel(const Loss<E> l) {
   constexpr int N = Chunk<E>::N, THREADS = WAVES * 64, STEP = THREADS * N, HELD = CHUNKS ? CHUNKS : 1;
   extern __shared__ uint32_t is_entry[];       // a bit a token, where the other tokens are a class
-  __shared__ Share<WAVES, 2> of_max;
-  __shared__ Share<WAVES, 5> of_sum;
+  __shared__ Share<WAVES> of;
+  // of the entries: the place (-1: does not count), the student's logit there, the teacher's, the share
   __shared__ int place[kMost];
-  __shared__ float p[kMost], at_place[kMost];
+  __shared__ float at_place[kMost], logit[kMost], p[kMost];
   const int64_t row = blockIdx.x;
   const int t = (int)(row / l.B), b = (int)(row % l.B), K = l.top.K, first = threadIdx.x * N;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // the entries are dealt out to the first threads; what is made in 64 bits is left to waves that have some
+  const int with_entries = (K + 63) / 64 < WAVES ? (K + 63) / 64 : WAVES;
+  const bool entries = wave < with_entries;
   const float weight = l.weight ? l.weight[row] : 1.0f;
   E* const dx = l.dx.data ? l.dx.at(t, b) : nullptr;
   if (weight == 0.0f) {
@@ -126,140 +154,182 @@ distil_kernel(const Loss<E> l) {
   }
   const E* const x = l.x.at(t, b);
   const bool tail = l.top_norm != nullptr;
-  const float scale = 1.0f / l.tau, to_log2 = scale * kLog2e;
-  // the entries' indices and logits are asked for first, then the row, then the row's logits of the entries
-  constexpr int ENTRIES = (kMost + THREADS - 1) / THREADS;
-  int c[ENTRIES];
-  double logit[ENTRIES];
-#pragma unroll
-  for (int i = 0; i < ENTRIES; ++i) {
-    const int k = threadIdx.x + i * THREADS;
-    c[i] = -1, logit[i] = -INFINITY;
-    if (k < K) c[i] = l.top.index[row * K + k], logit[i] = (double)entry_logit(l.top, row * K + k);
-  }
+  const float scale = 1.0f / l.tau;
   const int target = l.targets && l.hard != 0.0f ? l.targets[row] : -1;
   const bool known = target >= 0 && target < l.V;
-  Chunk<E> held[HELD];
+  // the entries are asked for first, then the row, then the row's logits of the entries
+  constexpr int ENTRIES = (kMost + THREADS - 1) / THREADS;
+  int c[ENTRIES];
+  float raw[ENTRIES];
+  if (entries)
+#pragma unroll
+    for (int i = 0; i < ENTRIES; ++i) {
+      const int k = threadIdx.x + i * THREADS;
+      c[i] = k < K ? l.top.index[row * K + k] : -1, raw[i] = k < K ? entry_logit(l.top, row * K + k) : -INFINITY;
+    }
+  // f(chunk, its first token less the thread's, how many of its tokens are a neighbour's, whether the step is whole).  A step in which not all of the
+  // workgroup's chunks are whole is apart from the others: there is code for its ends but once.  The last chunk of a row begins early
+  // enough to be loaded whole, and what it shares with the one before it is made minus infinity.
+  Chunk<E> held[HELD], end;
+  const int steps = l.V / STEP, end_at = first + steps * STEP, last = l.V - N, end_from = end_at < last ? end_at : last;
+  const bool ends = CHUNKS > 0 && steps * STEP < l.V;
   auto each = [&](auto&& f) __attribute__((always_inline)) {
     if constexpr (CHUNKS > 0) {
 #pragma unroll
-      for (int k = 0; k < CHUNKS; ++k)
-        if (k * STEP < l.V) f(held[k], first + k * STEP);
+      for (int k = 0; k < CHUNKS; ++k) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (k < steps) f(held[k], k * STEP, 0, std::true_type{});
+      }
+      if (ends) f(end, end_from - first, end_at - end_from, std::false_type{});
     } else {
-      for (int v = first; v < l.V; v += STEP) f(load_chunk(x, v, l.V), v);
+      for (int v = 0; first + v < l.V; v += STEP) f(load_chunk(x, first + v, l.V), v, 0, std::true_type{});
     }
   };
-  if constexpr (CHUNKS > 0)
+  if constexpr (CHUNKS > 0) {
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k)
-      if (k * STEP < l.V) held[k] = load_chunk(x, first + k * STEP, l.V);
-  float at_c[ENTRIES];
-  const float at_target = known ? (float)x[target] : 0.0f;
-  double top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < ENTRIES; ++i) {
-    const int k = threadIdx.x + i * THREADS;
-    if (c[i] >= l.V || logit[i] == -INFINITY) c[i] = -1;
-    at_c[i] = c[i] >= 0 ? (float)x[c[i]] : 0.0f;
-    logit[i] = c[i] >= 0 ? logit[i] / (double)l.tau : -INFINITY;
-    top = fmax(top, logit[i]);
-    if (k < K) place[k] = c[i], at_place[k] = at_c[i];
+      if (k < steps) held[k] = load_whole(x + k * STEP, first * sizeof(E));
+    if (ends) {
+      end = __builtin_bit_cast(Chunk<E>, load_some<E, N>(x + end_from));
+      end.leave_out(end_at - end_from);
+    }
   }
-  if (tail) {
-    for (int v = threadIdx.x; v < (l.V + 31) / 32; v += THREADS) is_entry[v] = 0;
-    __syncthreads();
+  // between two passes: the compiler would keep what the first made of the row for the second, in several times the registers
+  auto forget = [&]() __attribute__((always_inline)) {
+    if constexpr (CHUNKS > 0)
 #pragma unroll
-    for (int i = 0; i < ENTRIES; ++i)
-      if (c[i] >= 0) atomicOr(&is_entry[c[i] / 32], 1u << c[i] % 32);
+      for (int k = 0; k < CHUNKS; ++k) asm volatile("" : "+v"(held[k].w[0]), "+v"(held[k].w[1]), "+v"(held[k].w[2]), "+v"(held[k].w[3]));
+    asm volatile("" : "+v"(end.w[0]), "+v"(end.w[1]), "+v"(end.w[2]), "+v"(end.w[3]));
+  };
+  const float at_target = known ? (float)x[target] : 0.0f;
+  float top = -INFINITY;
+  if (entries)
+#pragma unroll
+    for (int i = 0; i < ENTRIES; ++i) {
+      const int k = threadIdx.x + i * THREADS;
+      if (c[i] >= l.V || raw[i] == -INFINITY) c[i] = -1;
+      if (c[i] >= 0) top = fmaxf(top, raw[i]);
+      if (k < K) place[k] = c[i], logit[k] = raw[i], at_place[k] = c[i] >= 0 ? (float)x[c[i]] : 0.0f;
+    }
+  if (tail) {
+    for (int v = threadIdx.x; v <= (l.V + 31) / 32; v += THREADS) is_entry[v] = 0;
+    __syncthreads();
+    for (int k = threadIdx.x; k < K; k += THREADS)
+      if (place[k] >= 0) atomicOr(&is_entry[place[k] / 32], 1u << place[k] % 32);
   }
   float m = -INFINITY;
-  each([&](const Chunk<E>& x, int) __attribute__((always_inline)) {
+  each([&](const Chunk<E>& x, int, int, auto) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < N; ++k) m = fmaxf(m, x[k]);
   });
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) m = fmaxf(m, __shfl_xor(m, k)), top = fmax(top, __shfl_xor(top, k));
-  if constexpr (WAVES > 1) {
-    if ((threadIdx.x & 63) == 0) of_max.v[0][threadIdx.x >> 6] = (double)m, of_max.v[1][threadIdx.x >> 6] = top;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < WAVES; ++k) m = fmaxf(m, (float)of_max.v[0][k]), top = fmax(top, of_max.v[1][k]);
-  } else {
-    __syncthreads();
+  m = lanes::largest(m);
+  if (entries) top = lanes::largest(top);
+  if (lane == 0) of.largest[wave] = m, of.top[wave] = top;
+  __syncthreads();
+  if (WAVES > 1) {
+    m = lanes::largest(lane < WAVES ? of.largest[lane % WAVES] : -INFINITY);
+    if (entries) top = lanes::largest(lane < with_entries ? of.top[lane % WAVES] : -INFINITY);
   }
-  const double norm = tail ? (double)l.top_norm[row] : top;
 
-  float s = 0.0f, s1 = 0.0f, rest = 0.0f;
-  each([&](const Chunk<E>& x, int at) __attribute__((always_inline)) {
-    float e[N], sum = 0.0f, sum1 = 0.0f;
+  {
+    forget();
+    const Exponential<E> of_tau(m, scale), of_one(m, 1.0f);
+    float s = 0.0f, s1 = 0.0f, rest = 0.0f;
+    each([&](const Chunk<E>& x, int at, int, auto) __attribute__((always_inline)) {
+      float e[N], sum = 0.0f, sum1 = 0.0f;
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      e[k] = exponential<E>(x[k] - m, scale, to_log2), sum += e[k];
-      if (SECOND) sum1 += exponential<E>(x[k] - m, 1.0f, kLog2e);
+      for (int k = 0; k < N; ++k) {
+        e[k] = of_tau(x[k]), sum += e[k];
+        if (SECOND) sum1 += of_one(x[k]);
+      }
+      s += sum, s1 += sum1;
+      if (tail) {
+        const int from = first + at;
+        const uint32_t bits = (uint32_t)(((uint64_t)is_entry[from / 32 + 1] << 32 | is_entry[from / 32]) >> from % 32);
+        float others = 0.0f;
+#pragma unroll
+        for (int k = 0; k < N; ++k) others += bits >> k & 1 ? 0.0f : e[k];
+        rest += others;
+      }
+    });
+    s = lanes::sum(s);
+    if (SECOND) s1 = lanes::sum(s1);
+    if (tail) rest = lanes::sum(rest);
+    // the entries' shares, before they are divided by their sum where they are all there is, and what they leave of the divergence
+    double shares = 0.0, terms = 0.0;
+    if (entries) {
+      for (int k = threadIdx.x; k < K; k += THREADS) {
+        if (place[k] < 0) continue;
+        // the difference in 64 bits, its exponential in 32, corrected by what the difference loses there
+        const double over = tail ? (double)logit[k] / (double)l.tau - (double)l.top_norm[row] : ((double)logit[k] - (double)top) / (double)l.tau;
+        const float near = (float)over, e = exp_of<true>(near), share = e > 0.0f ? fmaf(e, (float)(over - (double)near), e) : 0.0f;
+        shares += (double)share, p[k] = share;
+        if (share > 0.0f) terms += (double)share * (over - ((double)at_place[k] - (double)m) * (double)scale);
+      }
+      shares = lanes::sum(shares), terms = lanes::sum(terms);
     }
-    s += sum, s1 += sum1;
-    if (tail) {
-      const uint32_t bits = at < l.V ? is_entry[at / 32] >> at % 32 : 0;
-      float others = 0.0f;
-#pragma unroll
-      for (int k = 0; k < N; ++k) others += bits >> k & 1 ? 0.0f : e[k];
-      rest += others;
+    if (lane == 0) of.sums[0][wave] = s, of.sums[1][wave] = s1, of.sums[2][wave] = rest, of.shares[wave] = shares, of.terms[wave] = terms;
+    __syncthreads();
+    if (WAVES > 1) {               // a lane a wave
+      s = lanes::sum(lane < WAVES ? of.sums[0][lane % WAVES] : 0.0f);
+      if (SECOND) s1 = lanes::sum(lane < WAVES ? of.sums[1][lane % WAVES] : 0.0f);
+      if (tail) rest = lanes::sum(lane < WAVES ? of.sums[2][lane % WAVES] : 0.0f);
+      shares = lanes::sum(lane < with_entries ? of.shares[lane % WAVES] : 0.0);
+      if (wave == 0) terms = lanes::sum(lane < with_entries ? of.terms[lane % WAVES] : 0.0);
     }
-  });
-  // the entries' shares, before they are divided by their sum where they are all there is, and what they leave of the divergence
-  double share[ENTRIES], sums[5] = {(double)s, (double)s1, (double)rest, 0.0, 0.0};
+    const bool any = shares > 0.0;
+    const double p0 = tail && rest > 0.0f ? fmax(0.0, 1.0 - shares) : 0.0;
+    const float over = any && !tail ? (float)(1.0 / shares) : 1.0f;
+    if (dx) {
+    const float of_soft = weight * (1.0f - l.hard) * l.tau, hard = known ? weight * l.hard : 0.0f;
+    const float one = 1.0f / s, of_e1 = SECOND ? hard / s1 : 0.0f, of_e = SECOND ? 0.0f : hard * one;
+    const float M = (tail ? (float)shares : any ? 1.0f : 0.0f) + (float)p0, ratio = p0 > 0.0 ? (float)p0 * (s / rest) : 0.0f;
+    const float elsewhere = fmaf(of_soft * (M - ratio), one, of_e), inside = fmaf(of_soft * M, one, of_e);
+    forget();
+    each([&](const Chunk<E>& x, int at, int shared, auto whole) __attribute__((always_inline)) {
+      float g[N];
 #pragma unroll
-  for (int i = 0; i < ENTRIES; ++i) {
-    share[i] = c[i] >= 0 ? exp(logit[i] - norm) : 0.0;
-    sums[3] += share[i];
-    if (share[i] > 0.0) sums[4] += share[i] * ((logit[i] - norm) - ((double)at_c[i] - (double)m) * (double)scale);
-  }
-  sum_over_threads<WAVES, 5>(sums, of_sum);
-  const double all = sums[3], over = tail || !(all > 0.0) ? 1.0 : 1.0 / all, total = all * over;
-  const double p0 = tail && sums[2] > 0.0 ? fmax(0.0, 1.0 - all) : 0.0;
-  if (threadIdx.x < 64) {
-    const double log_s = log(sums[0]);
-    double soft = sums[4] * over + total * log_s;
-    if (!tail && all > 0.0) soft -= log(all);
-    if (p0 > 0.0) soft += p0 * (log(p0) - log(sums[2]) + log_s);
-    const double ce = known ? (double)m - (double)at_target + (SECOND ? log(sums[1]) : log_s) : 0.0;
-    if (threadIdx.x == 0)
-      l.loss[row] = (float)((double)weight * ((1.0 - (double)l.hard) * (double)l.tau * (double)l.tau * soft + (double)l.hard * ce));
-  }
-  if (!dx) return;
-  const float of_soft = weight * (1.0f - l.hard) * l.tau, hard = known ? weight * l.hard : 0.0f;
-  const float one = (float)(1.0 / sums[0]), of_e1 = SECOND ? (float)((double)hard / sums[1]) : 0.0f, of_e = SECOND ? 0.0f : hard * one;
-  const float M = (float)(total + p0), ratio = p0 > 0.0 ? (float)(p0 * sums[0] / sums[2]) : 0.0f;
-  const float elsewhere = fmaf(of_soft * (M - ratio), one, of_e), inside = fmaf(of_soft * M, one, of_e);
-  each([&](const Chunk<E>& x, int at) __attribute__((always_inline)) {
-    float g[N];
+      for (int k = 0; k < N; ++k) {
+        g[k] = elsewhere * of_tau(x[k]);
+        if (SECOND) g[k] = fmaf(of_e1, of_one(x[k]), g[k]);
+      }
+      if constexpr (CHUNKS == 0) store_chunk<E>(dx, first + at, l.V, g);
+      else if constexpr (whole.value) store_whole(dx + at, first * sizeof(E), g);
+      else
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      g[k] = elsewhere * exponential<E>(x[k] - m, scale, to_log2);
-      if (SECOND) g[k] = fmaf(of_e1, exponential<E>(x[k] - m, 1.0f, kLog2e), g[k]);
+        for (int k = 0; k < N; ++k)
+          if (k >= shared) store(dx + first + at + k, g[k]);
+    });
+    __syncthreads();               // behind it the places of the entries and of the target are written again
+    auto again = [&](int at, float value, float coefficient, float own) __attribute__((always_inline)) {
+      float g = coefficient * of_tau(value) - own;
+      if (SECOND) g = fmaf(of_e1, of_one(value), g);
+      store(dx + at, g);
+    };
+    if (entries)
+      for (int k = threadIdx.x; k < K; k += THREADS) {
+        const int c = place[k];
+        if (c < 0) continue;
+        float own = 0.0f;          // an index may come twice
+        for (int i = 0; i < K; ++i) own += place[i] == c ? p[i] : 0.0f;
+        again(c, at_place[k], inside, of_soft * (own * over) + (c == target ? hard : 0.0f));
+      }
+    if (threadIdx.x == THREADS - 1 && known) {
+      bool entry = false;
+      for (int k = 0; k < K; ++k) entry |= place[k] == target;
+      if (!entry) again(target, at_target, elsewhere, hard);
     }
-    if (at < l.V) store_chunk<E>(dx, at, l.V, g);
-  });
-#pragma unroll
-  for (int i = 0; i < ENTRIES; ++i)
-    if (threadIdx.x + i * THREADS < K) p[threadIdx.x + i * THREADS] = (float)(share[i] * over);
-  __syncthreads();                 // behind it the places of the entries and of the target are written again
-  auto again = [&](int at, float value, float coefficient, float own) __attribute__((always_inline)) {
-    float g = coefficient * exponential<E>(value - m, scale, to_log2) - own;
-    if (SECOND) g = fmaf(of_e1, exponential<E>(value - m, 1.0f, kLog2e), g);
-    store(dx + at, g);
-  };
-#pragma unroll
-  for (int i = 0; i < ENTRIES; ++i)
-    if (c[i] >= 0) {
-      float own = c[i] == target ? hard : 0.0f;
-      for (int k = 0; k < K; ++k) own += place[k] == c[i] ? of_soft * p[k] : 0.0f;
-      again(c[i], at_c[i], inside, own);
     }
-  if (threadIdx.x == THREADS - 1 && known) {
-    bool entry = false;
-    for (int k = 0; k < K; ++k) entry |= place[k] == target;
-    if (!entry) again(target, at_target, elsewhere, hard);
+    // last, when the row's registers are free
+    if (wave == 0) {
+      double soft = 0.0, ce = 0.0, log_s = 0.0;
+      if (tail || (known && !SECOND)) log_s = log((double)s) - of_tau.log_off();
+      if (tail) soft = terms + (shares + p0) * log_s + (p0 > 0.0 ? p0 * (log(p0 / (double)rest) + of_tau.log_off()) : 0.0);
+      else if (any) soft = terms / shares + log((double)s / shares) - of_tau.log_off();
+      if (known) ce = (double)m - (double)at_target + (SECOND ? log((double)s1) - of_one.log_off() : log_s);
+      if (threadIdx.x == 0)
+        l.loss[row] = (float)((double)weight * ((1.0 - (double)l.hard) * (double)l.tau * (double)l.tau * soft + (double)l.hard * ce));
+    }
   }
 }
 
@@ -281,7 +351,7 @@ extern "C" bppsa_status bppsa_distil(const bppsa_distil_rows* r, float* loss, co
     const Loss<E> l{rows_of<const E>(r->logits), dlogits ? rows_of<E>(*dlogits) : Rows<E>{}, Entries{r->top_logits, r->top_index, r->K, r->top_type},
                     r->top_norm, r->weight, r->targets, loss, r->B, r->V, r->temperature, r->hard};
     const auto run = [&](auto waves, auto chunks) {
-      const size_t bits = l.top_norm ? (size_t)bppsa_ceil_div(l.V, 32) * sizeof(uint32_t) : 0;
+      const size_t bits = l.top_norm ? ((size_t)bppsa_ceil_div(l.V, 32) + 1) * sizeof(uint32_t) : 0;
       const auto kernel = l.hard != 0.0f && l.tau != 1.0f ? distil_kernel<E, waves.value, chunks.value, true>
                                                           : distil_kernel<E, waves.value, chunks.value, false>;
       kernel<<<(unsigned)(r->T * r->B), waves.value * 64, bits, (hipStream_t)stream>>>(l);
@@ -294,8 +364,9 @@ extern "C" bppsa_status bppsa_distil(const bppsa_distil_rows* r, float* loss, co
     typedef std::integral_constant<int, 4> Four;
     typedef std::integral_constant<int, 8> Eight;
     typedef std::integral_constant<int, 16> Sixteen;
-    if (fits(1, 1)) run(One{}, One{});
-    else if (fits(4, 2)) run(Four{}, Two{});
+    if (l.V < N) run(One{}, None{});
+    else if (fits(1, 1)) run(One{}, One{});
+    else if (fits(2, 4)) run(Two{}, Four{});
     else if (fits(4, 8)) run(Four{}, Eight{});
     else if (fits(8, 8)) run(Eight{}, Eight{});
     else if (fits(16, 8)) run(Sixteen{}, Eight{});
