@@ -366,6 +366,7 @@ extern "C" bppsa_status bppsa_distil(const bppsa_distil_rows* r, float* loss, co
     typedef std::integral_constant<int, 16> Sixteen;
     if (l.V < N) run(One{}, None{});
     else if (fits(1, 1)) run(One{}, One{});
+    else if (fits(1, 4)) run(One{}, Four{});
     else if (fits(2, 4)) run(Two{}, Four{});
     else if (fits(4, 8)) run(Four{}, Eight{});
     else if (fits(8, 8)) run(Eight{}, Eight{});
