@@ -6,13 +6,14 @@
 // model with other sizes of a batch.
 #include <algorithm>
 
-#include "ssm_common.h"
+#include "chunks.h"
+#include "lanes.h"
 
 namespace {
 
-using namespace ssm;
+using namespace chunks;
 
-constexpr int kThreads = 256, kEach = 32, kPiece = kThreads * kEach;
+constexpr int kThreads = 256, kEach = 32, kPiece = kThreads * kEach, kFound = 1024;
 constexpr int kMostBeams = BPPSA_BEAM_MAX_W, kMostPieces = 64;
 static_assert(kMostPieces * kPiece == BPPSA_BEAM_MAX_V);
 
@@ -26,7 +27,7 @@ struct Pieces {
 
 // Ascending with the value, and of equal values descending with the place; never 0.
 __device__ __forceinline__ uint64_t key_of(float v, int place) {
-  const uint32_t u = __float_as_uint(v);
+  const uint32_t u = __float_as_uint(v + 0.0f);          // no -0, which is equal to 0
   return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~place;
 }
 __device__ __forceinline__ float value_of(uint64_t key) {
@@ -35,11 +36,10 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 }
 __device__ __forceinline__ int place_of(uint64_t key) { return (int)~(uint32_t)key; }
 
-template <typename T, typename F>
-__device__ __forceinline__ T over_lanes(T v, F&& f) {
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) v = f(v, __shfl_xor(v, k));
-  return v;
+// Ascending with the value; 0 for none.
+__device__ __forceinline__ uint64_t order_of(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v + 0.0);
+  return u >> 63 ? ~u : u | (uint64_t)1 << 63;
 }
 
 template <typename E>
@@ -57,53 +57,64 @@ __device__ __forceinline__ bool alive(const Beams<E>& s, int row) {
 
 // One workgroup a piece of a row, whose values stay in registers.  The W-th largest of a piece is no smaller than the smallest
 // of the largest values of W groups of threads; so few values reach that bound (22 of 8192 normal ones at W = 8) that
-// each can count those in front of it.  Where more than kThreads do, they are taken one after the other.
+// each can count those in front of it.  Where more than kFound do, equal ones that is, they are taken one after the other.
 template <typename E>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 8)
 beam_piece_kernel(const Beams<E> s, const Pieces out) {
-  constexpr int V = 16 / sizeof(E), LOADS = kEach / V;
+  constexpr int N = Chunk<E>::N, LOADS = kEach / N, STEP = kThreads * N;
   __shared__ float group[kThreads / 64][kMostBeams];
   __shared__ double sums[kThreads / 64];
-  __shared__ uint64_t found[kThreads];
+  __shared__ uint64_t found[kFound];
   __shared__ int n_found;
   const int piece = blockIdx.x % out.count, row = blockIdx.x / out.count, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (!alive(s, row)) return;
-  const E* const from = s.logits.at(row / s.W, row % s.W);
-  const int first = piece * kPiece + (int)threadIdx.x * V;
-  float v[kEach], m = -INFINITY, e = 0.0f;
+  const E* const from = s.logits.at(row / s.W, row % s.W) + (int64_t)piece * kPiece;
+  const int left = s.V - piece * kPiece, first = threadIdx.x * N;           // tokens from the piece's first on
+  Chunk<E> held[LOADS];
+  if (left >= kPiece) {
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) held[k] = load_whole(from + k * STEP, first * sizeof(E));
+  } else {
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) held[k] = load_chunk(from, first + k * STEP, left);
+  }
+  float of_chunk[LOADS], m = -INFINITY;
 #pragma unroll
   for (int k = 0; k < LOADS; ++k) {
-    const int at = first + k * kThreads * V;
-    if (at + V <= s.V) {
-      const Some<E, V> x = load_some<E, V>(from + at);
+    of_chunk[k] = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[k * V + j] = (float)x.v[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[k * V + j] = at + j < s.V ? (float)from[at + j] : -INFINITY;
-    }
+    for (int j = 0; j < N; ++j) of_chunk[k] = fmaxf(of_chunk[k], held[k][j]);
+    m = fmaxf(m, of_chunk[k]);
   }
-#pragma unroll
-  for (int k = 0; k < kEach; ++k) v[k] += 0.0f, m = fmaxf(m, v[k]);        // no -0, which is equal to 0
   const int groups = s.W <= 1 ? 1 : 1 << (32 - __builtin_clz(s.W - 1));
   if (threadIdx.x == 0) n_found = 0;
-  for (int k = groups; k < 64; k <<= 1) m = fmaxf(m, __shfl_xor(m, k));
-  if (lane < groups) group[wave][lane] = m;
+  float of_group = m;
+  for (int k = groups; k < 64; k <<= 1) of_group = fmaxf(of_group, __shfl_xor(of_group, k));
+  if (lane < groups) group[wave][lane] = of_group;
   __syncthreads();
-  for (int k = 0; k < kThreads / 64; ++k) m = fmaxf(m, group[k][lane & (groups - 1)]);
-  float bound = m;
-  for (int k = 1; k < groups; k <<= 1) bound = fminf(bound, __shfl_xor(bound, k)), m = fmaxf(m, __shfl_xor(m, k));
-  const float zero = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-  for (int k = 0; k < kEach; ++k) {
-    e += exp2_fast((v[k] - zero) * kLog2e);
-    const int place = first + k / V * kThreads * V + k % V;
-    if (v[k] >= bound && place < s.V) {
-      const int at = atomicAdd(&n_found, 1);
-      if (at < kThreads) found[at] = key_of(v[k], place);
-    }
+  for (int k = 0; k < kThreads / 64; ++k) of_group = fmaxf(of_group, group[k][lane & (groups - 1)]);
+  const float bound = -lanes::largest(-of_group), top = lanes::largest(of_group), zero = top == -INFINITY ? 0.0f : top;
+  float e = 0.0f;
+#pragma unroll
+  for (int k = 0; k < LOADS; ++k) {
+    float part = 0.0f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) part += exp2_fast((held[k][j] - zero) * kLog2e);
+    e += part;
   }
-  const double sum = over_lanes((double)e, [](double a, double b) { return a + b; });
+  if (m >= bound)
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) {
+      if (of_chunk[k] < bound) continue;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (held[k][j] >= bound && first + k * STEP + j < left) {
+          const int at = atomicAdd(&n_found, 1);
+          if (at < kFound) found[at] = key_of(held[k][j], piece * kPiece + first + k * STEP + j);
+        }
+    }
+  const double sum = lanes::sum((double)e);
   if (lane == 0) sums[wave] = sum;
   __syncthreads();
   const int n = n_found;
@@ -114,11 +125,14 @@ beam_piece_kernel(const Beams<E> s, const Pieces out) {
     out.largest[at] = zero, out.sum[at] = all;
   }
   uint64_t* const to = out.key + at * s.W;
-  if (n <= kThreads) {
-    const uint64_t mine = threadIdx.x < n ? found[threadIdx.x] : 0;
-    int before = 0;
-    for (int k = 0; k < n; ++k) before += found[k] > mine;
-    if (threadIdx.x < n && before < s.W) to[before] = mine;
+  if (n <= kFound) {
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const uint64_t mine = found[i];
+      int before = 0;
+#pragma unroll 8
+      for (int k = 0; k < n; ++k) before += found[k] > mine;
+      if (before < s.W) to[before] = mine;
+    }
     if (threadIdx.x >= n && threadIdx.x < s.W) to[threadIdx.x] = 0;
     return;
   }
@@ -126,12 +140,13 @@ beam_piece_kernel(const Beams<E> s, const Pieces out) {
   for (int i = 0; i < s.W; ++i) {
     uint64_t best = 0;
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const int place = first + k / V * kThreads * V + k % V;
-      const uint64_t key = place < s.V ? key_of(v[k], place) : 0;
-      if (key < last && key > best) best = key;
-    }
-    best = over_lanes(best, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+    for (int k = 0; k < LOADS; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const uint64_t key = first + k * STEP + j < left ? key_of(held[k][j], piece * kPiece + first + k * STEP + j) : 0;
+        if (key < last && key > best) best = key;
+      }
+    best = lanes::largest(best);
     __syncthreads();
     if (lane == 0) found[wave] = best;
     __syncthreads();
@@ -163,8 +178,8 @@ beam_join_kernel(const Beams<E> s, const Pieces in, const Choice out) {
       const int64_t at = (int64_t)row * in.count;
       const float largest = lane < in.count ? in.largest[at + lane] : -INFINITY;
       const double sum = lane < in.count ? in.sum[at + lane] : 0.0;
-      const float m = over_lanes(sum > 0.0 ? largest : -INFINITY, [](float a, float b) { return fmaxf(a, b); });
-      const double all = over_lanes(sum == 0.0 ? 0.0 : sum * exp((double)largest - (double)m), [](double a, double b) { return a + b; });
+      const float m = lanes::largest(sum > 0.0 ? largest : -INFINITY);
+      const double all = lanes::sum(sum == 0.0 ? 0.0 : sum * exp((double)largest - (double)m));
       norm = (double)m + log(all);
       for (int k = lane; k < in.count * W; k += 64) list[k] = in.key[at * W + k];
     }
@@ -186,7 +201,7 @@ beam_join_kernel(const Beams<E> s, const Pieces in, const Choice out) {
     __builtin_amdgcn_wave_barrier();
     for (int i = 0; i < W; ++i) {
       const uint64_t mine = lane < in.count && next < W ? list[lane * W + next] : 0;
-      const uint64_t best = over_lanes(mine, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+      const uint64_t best = lanes::largest(mine);
       if (mine == best) ++next;
       if (lane == 0) {
         const double v = (double)score + ((double)value_of(best) - norm);
@@ -199,14 +214,9 @@ beam_join_kernel(const Beams<E> s, const Pieces in, const Choice out) {
   int next = 0;
   for (int i = 0; i < W; ++i) {
     const bool any = lane < W && next < W && token[lane][next] >= 0;
-    double v = any ? total[lane][next] : 0.0;
-    int who = any ? lane : 64;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-      const double u = __shfl_xor(v, k);
-      const int other = __shfl_xor(who, k);
-      if (other < 64 && (who == 64 || u > v || (u == v && other < who))) v = u, who = other;
-    }
+    const double v = any ? total[lane][next] : 0.0;
+    const uint64_t mine = any ? order_of(v) : 0;
+    const int who = __builtin_ctzll(__ballot(mine == lanes::largest(mine)));         // the lowest beam of equal ones
     if (lane == who) {
       const int at = blockIdx.x * W + i, t = token[lane][next];
       out.scores[at] = (float)v, out.parents[at] = lane, out.tokens[at] = t;
