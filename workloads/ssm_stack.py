@@ -1,12 +1,14 @@
 """A small stack of selective state space layers, trained and served with the library's operators.
 
 A layer: root-mean-square norm, a projection to two halves, the short convolution and the selective scan of the first half
-gated by the second, a projection back that is added to the stream.  The projections, norms and the loss are plain torch;
-the convolution, the scan, their gradients, their single-token steps and the optimiser are the library's.  Activations are
-bfloat16, the stream between the layers and all parameters float32; the projections use the bfloat16 copies that the
-optimiser keeps.
+gated by the second, a projection back that is added to the stream.  A gated layer has the gated linear recurrence in the
+scan's place, whose two gates come out of one projection.  The projections, norms and the loss on tokens are plain torch;
+the convolution, the recurrences, their gradients, their single-token steps, the loss against another stack's top logits, the
+selection of a beam search with the move of its states and the optimiser are the library's.  Activations are bfloat16, the
+stream between the layers and all parameters float32; the projections use the bfloat16 copies that the optimiser keeps.
 
-    python -m workloads.ssm_stack        trains on sequences with a delayed rule and continues some token by token
+    python -m workloads.ssm_stack        trains on sequences with a delayed rule, continues some token by token, and lets a
+                                         smaller stack with a gated layer learn from the first one's top logits
 """
 from __future__ import annotations
 
@@ -17,7 +19,7 @@ import torch
 import paper_1907_10134_amd as bp
 
 BF16 = torch.bfloat16
-DECAYED = ("embed", "in_proj", "x_proj", "dt_proj", "out_proj")
+DECAYED = ("embed", "in_proj", "x_proj", "dt_proj", "gate_proj", "out_proj")
 
 
 def _norm(x, weight):
@@ -38,14 +40,23 @@ def _mm(x, w):
 
 
 class SsmStack:
-    def __init__(self, vocabulary=16, width=64, layers=2, states=16, taps=4, state_bits=8, lr=3e-3, seed=0, device="cuda"):
+    def __init__(self, vocabulary=16, width=64, layers=2, states=16, taps=4, state_bits=8, lr=3e-3, seed=0, device="cuda",
+                 gated=()):
+        """gated: the numbers of the layers that have the gated linear recurrence."""
         gen = torch.Generator().manual_seed(seed)
         normal = lambda scale, *shape: torch.randn(shape, generator=gen) * scale
         uniform = lambda lo, hi, *shape: lo + (hi - lo) * torch.rand(shape, generator=gen)
         d, D, N, R = width, 2 * width, states, -(-width // 16)
-        self.sizes, self.layers, self.taps = (d, D, N, R), layers, taps
+        self.sizes, self.layers, self.taps, self.gated = (d, D, N, R), layers, taps, frozenset(gated)
         p = {"embed": normal(0.3, vocabulary, d), "last_norm": torch.ones(d)}
         for l in range(layers):
+            if l in self.gated:                # decays of 0.002 to 0.7: gates of one half remember one to 1000 steps
+                p.update({"norm%d" % l: torch.ones(d), "in_proj%d" % l: normal(d ** -0.5, 2 * D, d),
+                          "conv_w%d" % l: uniform(-0.5, 0.5, D, taps), "conv_b%d" % l: torch.zeros(D),
+                          "gate_proj%d" % l: normal(D ** -0.5, 2 * D, D), "r_bias%d" % l: torch.zeros(D),
+                          "i_bias%d" % l: torch.zeros(D), "decay_log%d" % l: uniform(math.log(2e-3), math.log(0.7), D),
+                          "out_proj%d" % l: normal(D ** -0.5, d, D)})
+                continue
             step = torch.exp(uniform(math.log(1e-3), math.log(0.1), D))
             p.update({"norm%d" % l: torch.ones(d), "in_proj%d" % l: normal(d ** -0.5, 2 * D, d),
                       "conv_w%d" % l: uniform(-0.5, 0.5, D, taps), "conv_b%d" % l: torch.zeros(D),
@@ -66,7 +77,8 @@ class SsmStack:
 
     def forward(self, tokens, lengths=None, keep=None, caches=None):
         """Logits [T, B, vocabulary] of tokens [T, B].  keep: a list that receives what backward() reads.  caches: (scan
-        states [B, D, N], last inputs [B, taps - 1, D]) of each layer, filled with the state after each sample."""
+        states [B, D, N], of a gated layer [B, D], last inputs [B, taps - 1, D]) of each layer, filled with the state after each
+        sample."""
         p, w = self.p, self.w
         D = self.sizes[1]
         T, B = tokens.shape
@@ -78,6 +90,15 @@ class SsmStack:
             u, z = xz[..., :D], xz[..., D:]
             h_last, last = caches[l] if caches is not None else (None, None)
             c = bp.ssm_conv(u, p["conv_w%d" % l], p["conv_b%d" % l], lengths=lengths, state_last=last)
+            if l in self.gated:
+                gates, decay = _mm(c, w["gate_proj%d" % l]), torch.exp(p["decay_log%d" % l])
+                states = bp.gated_scan_states(T, B, D, device=x.device) if keep is not None else None
+                y = bp.gated_scan(c, gates[..., :D], gates[..., D:], decay, z=z, r_bias=p["r_bias%d" % l], i_bias=p["i_bias%d" % l],
+                                  lengths=lengths, h_last=h_last, states=states)
+                if keep is not None:
+                    keep.append((x, r, n, u, z, c, gates, decay, states, y))
+                x = x + _mm(y, w["out_proj%d" % l]).float()
+                continue
             proj = _mm(c, w["x_proj%d" % l])
             low, Bm, Cm = self._cut(proj)
             dt = _mm(low, w["dt_proj%d" % l])
@@ -96,18 +117,37 @@ class SsmStack:
 
     def train_step(self, tokens, targets, lengths=None):
         """One iteration on tokens and targets [T, B]; the mean loss over the real tokens, before the update."""
-        p, w, g, keep = self.p, self.w, self.g, []
-        D = self.sizes[1]
+        keep = []
         T, B = tokens.shape
         logits = self.forward(tokens, lengths, keep)
         logp = torch.log_softmax(logits, -1)
-        real = torch.ones((T, B), device=logits.device) if lengths is None else \
-            (torch.arange(T, device=logits.device)[:, None] < lengths).float()
-        real = real / real.sum()
+        real = self._real(T, B, lengths)
         loss = -(logp.gather(-1, targets[..., None])[..., 0] * real).sum()
         dlogits = torch.exp(logp)
         dlogits.scatter_add_(-1, targets[..., None], torch.full((T, B, 1), -1.0, device=logits.device))
-        dlogits = (dlogits * real[..., None]).to(BF16)
+        self._backward((dlogits * real[..., None]).to(BF16), tokens, lengths, keep)
+        return loss
+
+    def distil_step(self, tokens, top_logits, top_index, lengths=None, **how):
+        """One iteration on tokens [T, B] against a teacher's top logits and their indices [T, B, K]; the mean loss over the real
+        tokens, before the update.  how: what bp.distil takes besides."""
+        keep = []
+        T, B = tokens.shape
+        logits = self.forward(tokens, lengths, keep)
+        made = bp.distil(logits, top_logits, top_index, weight=self._real(T, B, lengths), dlogits=logits, **how)
+        self._backward(made.dlogits.to(BF16), tokens, lengths, keep)
+        return made.loss.sum()
+
+    def _real(self, T, B, lengths):
+        """[T, B]: each real token's share of them all."""
+        device = self.p["embed"].device
+        real = torch.ones((T, B), device=device) if lengths is None else (torch.arange(T, device=device)[:, None] < lengths).float()
+        return real / real.sum()
+
+    def _backward(self, dlogits, tokens, lengths, keep):
+        """The gradients behind those of the logits, and the update."""
+        p, w, g = self.p, self.w, self.g
+        D = self.sizes[1]
         outer = lambda a, b: torch.mm(a.flatten(0, -2).t(), b.flatten(0, -2)).float()        # sum over tokens of a b^T
         back = lambda a, weight: torch.mm(a.flatten(0, -2), weight).unflatten(0, a.shape[:-1])
         x, r, n = keep.pop()
@@ -115,6 +155,20 @@ class SsmStack:
         dx, dw = _norm_backward(back(dlogits, w["embed"]).float(), x, r, p["last_norm"])
         g["last_norm"].copy_(dw)
         for l in reversed(range(self.layers)):
+            if l in self.gated:
+                x, r, n, u, z, c, gates, decay, states, y = keep.pop()
+                out = dx.to(BF16)
+                g["out_proj%d" % l].copy_(outer(out, y))
+                s = bp.gated_scan_backward(back(out, w["out_proj%d" % l]), c, gates[..., :D], gates[..., D:], decay, states, z=z,
+                                           r_bias=p["r_bias%d" % l], i_bias=p["i_bias%d" % l], lengths=lengths)
+                g["decay_log%d" % l].copy_(s.ddecay * decay)
+                g["r_bias%d" % l].copy_(s.dr_bias)
+                g["i_bias%d" % l].copy_(s.di_bias)
+                dgates = torch.cat((s.dr, s.di), -1)
+                g["gate_proj%d" % l].copy_(outer(dgates, c))
+                dc = s.dx + back(dgates, w["gate_proj%d" % l])
+                dx = dx + self._front_backward(l, dc, s.dz, x, r, n, u, lengths, outer, back)
+                continue
             x, r, n, u, z, c, low, Bm, Cm, dt, A, states, y = keep.pop()
             out = dx.to(BF16)
             g["out_proj%d" % l].copy_(outer(out, y))
@@ -127,23 +181,28 @@ class SsmStack:
             dproj = torch.cat((back(s.ddt, w["dt_proj%d" % l]), s.dBm.flatten(2), s.dCm.flatten(2)), -1)
             g["x_proj%d" % l].copy_(outer(dproj, c))
             dc = s.du + back(dproj, w["x_proj%d" % l])
-            k = bp.ssm_conv_backward(dc, u, p["conv_w%d" % l], p["conv_b%d" % l], lengths=lengths)
-            g["conv_w%d" % l].copy_(k.dweight)
-            g["conv_b%d" % l].copy_(k.dbias)
-            dxz = torch.cat((k.dx, s.dz), -1)
-            g["in_proj%d" % l].copy_(outer(dxz, n))
-            dn, dw = _norm_backward(back(dxz, w["in_proj%d" % l]).float(), x, r, p["norm%d" % l])
-            g["norm%d" % l].copy_(dw)
-            dx = dx + dn
+            dx = dx + self._front_backward(l, dc, s.dz, x, r, n, u, lengths, outer, back)
         g["embed"].copy_(dembed.index_add_(0, tokens.flatten(), dx.flatten(0, 1)))
         self.optimiser.step()
-        return loss
+
+    def _front_backward(self, l, dc, dz, x, r, n, u, lengths, outer, back):
+        """The gradient for the stream through what a layer has in front of its recurrence."""
+        p, w, g = self.p, self.w, self.g
+        k = bp.ssm_conv_backward(dc, u, p["conv_w%d" % l], p["conv_b%d" % l], lengths=lengths)
+        g["conv_w%d" % l].copy_(k.dweight)
+        g["conv_b%d" % l].copy_(k.dbias)
+        dxz = torch.cat((k.dx, dz), -1)
+        g["in_proj%d" % l].copy_(outer(dxz, n))
+        dn, dw = _norm_backward(back(dxz, w["in_proj%d" % l]).float(), x, r, p["norm%d" % l])
+        g["norm%d" % l].copy_(dw)
+        return dn
 
     def caches(self, slots, device="cuda"):
-        """Empty states of `slots` streams: (scan [slots, D, N] float32, convolution [slots, taps - 1, D]) of each layer."""
+        """Empty states of `slots` streams: (scan [slots, D, N] float32, of a gated layer [slots, D], convolution
+        [slots, taps - 1, D]) of each layer."""
         _, D, N, _ = self.sizes
-        return [(torch.zeros((slots, D, N), device=device), torch.zeros((slots, self.taps - 1, D), dtype=BF16, device=device))
-                for _ in range(self.layers)]
+        return [(torch.zeros((slots, D) if l in self.gated else (slots, D, N), device=device),
+                 torch.zeros((slots, self.taps - 1, D), dtype=BF16, device=device)) for l in range(self.layers)]
 
     def token(self, tokens, caches, slots=None):
         """Logits [B, vocabulary] behind one more token [B] of the streams in `slots`, whose states move on."""
@@ -154,11 +213,46 @@ class SsmStack:
             h, last = caches[l]
             xz = _mm(_norm(x, p["norm%d" % l])[0].to(BF16), w["in_proj%d" % l])
             c = bp.ssm_conv_step(xz[:, :D], p["conv_w%d" % l], p["conv_b%d" % l], last, slots=slots)
+            if l in self.gated:
+                gates = _mm(c, w["gate_proj%d" % l])
+                y = bp.gated_scan_step(c, gates[:, :D], gates[:, D:], torch.exp(p["decay_log%d" % l]), h, z=xz[:, D:],
+                                       r_bias=p["r_bias%d" % l], i_bias=p["i_bias%d" % l], slots=slots)
+                x = x + _mm(y, w["out_proj%d" % l]).float()
+                continue
             low, Bm, Cm = self._cut(_mm(c, w["x_proj%d" % l]))
             y = bp.ssm_scan_step(c, _mm(low, w["dt_proj%d" % l]), -torch.exp(p["A_log%d" % l]), Bm, Cm, h,
                                  skip=p["skip%d" % l], z=xz[:, D:], dt_bias=p["dt_bias%d" % l], slots=slots)
             x = x + _mm(y, w["out_proj%d" % l]).float()
         return _mm(_norm(x, p["last_norm"])[0].to(BF16), w["embed"]).float()
+
+
+    def beams(self, tokens, width, steps, lengths=None, end=-1):
+        """The `width` best continuations of each prompt [T, B], of a token at least, that a beam search finds: (tokens
+        [B, width, steps], scores [B, width]), best first.  What comes behind an `end` is `end`."""
+        T, B = tokens.shape
+        device = tokens.device
+        prompt, caches = self.caches(B, device), self.caches(B * width, device)
+        logits = self.forward(tokens, lengths, caches=prompt)
+        last = torch.full((B,), T - 1, device=device) if lengths is None else (lengths - 1).long()
+        logits = logits[last, torch.arange(B, device=device)]
+        slots = torch.arange(B * width, dtype=torch.int32, device=device).view(B, width)
+        for have, cache in zip(prompt, caches):
+            for a, b in zip(have, cache):
+                b[::width] = a                 # the first beam of each search; the others do not count yet
+        scores = torch.full((B, width), -math.inf, device=device)
+        scores[:, 0] = 0.0
+        finished = torch.zeros((B, width), dtype=torch.bool, device=device) if end >= 0 else None
+        history = torch.zeros((B * width, steps), dtype=torch.int32, device=device)
+        states = bp.BeamStates([x for cache in caches for x in cache] + [history])
+        logits = logits[:, None].expand(B, width, -1).contiguous()
+        for k in range(steps):
+            c = bp.beam_select(logits, scores, finished=finished, end=end, slots=slots)
+            states.move(c.sources, c.slots)
+            scores, finished, slots = c.scores, c.finished, c.slots
+            history[slots.flatten().long(), k] = c.tokens.flatten()
+            if k + 1 < steps:
+                logits = self.token(c.tokens.flatten().long(), caches, slots.flatten()).view(B, width, -1)
+        return history[slots.long()], scores
 
 
 def delayed(T, B, delay=3, vocabulary=16, seed=0):
@@ -186,6 +280,15 @@ def main():
         right += int((token == s[t]).sum())
         logits = stack.token(token, caches)
     print("%d of 80 continued tokens are right" % right)
+    found, scores = stack.beams(s[:20], 3, 20)
+    print("%d of 80 tokens of the best of three beams are right" % int((found[:, 0].t() == s[20:40]).sum()))
+    student = SsmStack(width=32, layers=2, gated=(1,), seed=1)
+    for step in range(200):
+        s = delayed(64, 32, seed=step).cuda()
+        top, index = stack.forward(s[:-1]).topk(4)
+        loss = student.distil_step(s[:-1], top, index.int())
+        if step % 20 == 0:
+            print("step %3d  loss against the first stack %.4f" % (step, float(loss)), flush=True)
 
 
 if __name__ == "__main__":
