@@ -34,6 +34,7 @@ struct Loss {
   float* loss;
   int B, V;
   float tau, hard;
+  double scale;                    // 1 / tau
 };
 
 constexpr int kMost = BPPSA_DISTIL_MAX_K;
@@ -55,6 +56,14 @@ struct Exponential {
   __device__ __forceinline__ double log_off() const { return kExact<E> ? 0.0 : 0.69314718055994531 * (double)off; }
 };
 
+// log(v), within 2^-23: the exponent's part is exact, and the instruction sees values from 0.7 to 1.4 alone, whose logarithms are small.
+__device__ __forceinline__ double log_of(float v) {
+  int e = __builtin_amdgcn_frexp_expf(v);
+  float f = __builtin_amdgcn_frexp_mantf(v);
+  if (f < 0.70710678f) f += f, --e;
+  return ((double)e + (double)__builtin_amdgcn_logf(f)) * 0.69314718055994531;
+}
+
 // What the waves of a row tell each other, each by its first lane.
 template <int WAVES>
 struct Share {
@@ -69,11 +78,12 @@ template <typename E, int WAVES, int CHUNKS, bool SECOND>
 __global__ void __launch_bounds__(WAVES * 64, WAVES * CHUNKS <= 64 ? 6 : 4)
 distil_kernel(const Loss<E> l) {
   constexpr int N = Chunk<E>::N, THREADS = WAVES * 64, STEP = THREADS * N, HELD = CHUNKS ? CHUNKS : 1;
-  extern __shared__ uint32_t is_entry[];       // a bit a token, where the other tokens are a class
+  extern __shared__ uint32_t is_entry[];       // a bit a token
   __shared__ Share<WAVES> of;
   // of the entries: the place (-1: does not count), the student's logit there, the teacher's, the share
   __shared__ int place[kMost];
   __shared__ float at_place[kMost], logit[kMost], p[kMost];
+  __shared__ int twice;
   const int64_t row = blockIdx.x;
   const int t = (int)(row / l.B), b = (int)(row % l.B), K = l.top.K, first = threadIdx.x * N;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -91,7 +101,7 @@ distil_kernel(const Loss<E> l) {
   }
   const E* const x = l.x.at(t, b);
   const bool tail = l.top_norm != nullptr;
-  const float scale = 1.0f / l.tau;
+  const float scale = (float)l.scale;
   const int target = l.targets && l.hard != 0.0f ? l.targets[row] : -1;
   const bool known = target >= 0 && target < l.V;
   // the entries are asked for first, then the row, then the row's logits of the entries
@@ -148,12 +158,13 @@ distil_kernel(const Loss<E> l) {
       if (c[i] >= 0) top = fmaxf(top, raw[i]);
       if (k < K) place[k] = c[i], logit[k] = raw[i], at_place[k] = c[i] >= 0 ? (float)x[c[i]] : 0.0f;
     }
-  if (tail) {
-    for (int v = threadIdx.x; v <= (l.V + 31) / 32; v += THREADS) is_entry[v] = 0;
-    __syncthreads();
+  // an index that comes twice finds its bit set
+  for (int v = threadIdx.x; v <= (l.V + 31) / 32; v += THREADS) is_entry[v] = 0;
+  if (threadIdx.x == 0) twice = 0;
+  __syncthreads();
+  if (entries)
     for (int k = threadIdx.x; k < K; k += THREADS)
-      if (place[k] >= 0) atomicOr(&is_entry[place[k] / 32], 1u << place[k] % 32);
-  }
+      if (place[k] >= 0 && atomicOr(&is_entry[place[k] / 32], 1u << place[k] % 32) >> place[k] % 32 & 1) twice = 1;
   float m = -INFINITY;
   each([&](const Chunk<E>& x, int, int, auto) __attribute__((always_inline)) {
 #pragma unroll
@@ -185,7 +196,7 @@ distil_kernel(const Loss<E> l) {
         const uint32_t bits = (uint32_t)(((uint64_t)is_entry[from / 32 + 1] << 32 | is_entry[from / 32]) >> from % 32);
         float others = 0.0f;
 #pragma unroll
-        for (int k = 0; k < N; ++k) others += bits >> k & 1 ? 0.0f : e[k];
+        for (int k = 0; k < N; ++k) others += __uint_as_float(__float_as_uint(e[k]) & ~(uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1));
         rest += others;
       }
     });
@@ -198,10 +209,10 @@ distil_kernel(const Loss<E> l) {
       for (int k = threadIdx.x; k < K; k += THREADS) {
         if (place[k] < 0) continue;
         // the difference in 64 bits, its exponential in 32, corrected by what the difference loses there
-        const double over = tail ? (double)logit[k] / (double)l.tau - (double)l.top_norm[row] : ((double)logit[k] - (double)top) / (double)l.tau;
+        const double over = tail ? (double)logit[k] * l.scale - (double)l.top_norm[row] : ((double)logit[k] - (double)top) * l.scale;
         const float near = (float)over, e = exp_of<true>(near), share = e > 0.0f ? fmaf(e, (float)(over - (double)near), e) : 0.0f;
         shares += (double)share, p[k] = share;
-        if (share > 0.0f) terms += (double)share * (over - ((double)at_place[k] - (double)m) * (double)scale);
+        if (share > 0.0f) terms += (double)share * (over - ((double)at_place[k] - (double)m) * l.scale);
       }
       shares = lanes::sum(shares), terms = lanes::sum(terms);
     }
@@ -216,7 +227,7 @@ distil_kernel(const Loss<E> l) {
     }
     const bool any = shares > 0.0;
     const double p0 = tail && rest > 0.0f ? fmax(0.0, 1.0 - shares) : 0.0;
-    const float over = any && !tail ? (float)(1.0 / shares) : 1.0f;
+    const float over = any && !tail ? 1.0f / (float)shares : 1.0f;
     if (dx) {
     const float of_soft = weight * (1.0f - l.hard) * l.tau, hard = known ? weight * l.hard : 0.0f;
     const float one = 1.0f / s, of_e1 = SECOND ? hard / s1 : 0.0f, of_e = SECOND ? 0.0f : hard * one;
@@ -247,23 +258,24 @@ distil_kernel(const Loss<E> l) {
       for (int k = threadIdx.x; k < K; k += THREADS) {
         const int c = place[k];
         if (c < 0) continue;
-        float own = 0.0f;          // an index may come twice
-        for (int i = 0; i < K; ++i) own += place[i] == c ? p[i] : 0.0f;
+        float own = p[k];
+        if (twice) {
+          own = 0.0f;
+          for (int i = 0; i < K; ++i) own += place[i] == c ? p[i] : 0.0f;
+        }
         again(c, at_place[k], inside, of_soft * (own * over) + (c == target ? hard : 0.0f));
       }
     if (threadIdx.x == THREADS - 1 && known) {
-      bool entry = false;
-      for (int k = 0; k < K; ++k) entry |= place[k] == target;
-      if (!entry) again(target, at_target, elsewhere, hard);
+      if (!(is_entry[target / 32] >> target % 32 & 1)) again(target, at_target, elsewhere, hard);
     }
     }
     // last, when the row's registers are free
     if (wave == 0) {
       double soft = 0.0, ce = 0.0, log_s = 0.0;
-      if (tail || (known && !SECOND)) log_s = log((double)s) - of_tau.log_off();
-      if (tail) soft = terms + (shares + p0) * log_s + (p0 > 0.0 ? p0 * (log(p0 / (double)rest) + of_tau.log_off()) : 0.0);
-      else if (any) soft = terms / shares + log((double)s / shares) - of_tau.log_off();
-      if (known) ce = (double)m - (double)at_target + (SECOND ? log((double)s1) - of_one.log_off() : log_s);
+      if (tail || (known && !SECOND)) log_s = log_of(s) - of_tau.log_off();
+      if (tail) soft = terms + (shares + p0) * log_s + (p0 > 0.0 ? p0 * (log_of((float)p0) - log_of(rest) + of_tau.log_off()) : 0.0);
+      else if (any) soft = terms / shares + log_of(s) - log_of((float)shares) - of_tau.log_off();
+      if (known) ce = (double)m - (double)at_target + (SECOND ? log_of(s1) - of_one.log_off() : log_s);
       if (threadIdx.x == 0)
         l.loss[row] = (float)((double)weight * ((1.0 - (double)l.hard) * (double)l.tau * (double)l.tau * soft + (double)l.hard * ce));
     }
@@ -286,9 +298,9 @@ extern "C" bppsa_status bppsa_distil(const bppsa_distil_rows* r, float* loss, co
   return by_type(r->type, [&](auto e) {
     using E = decltype(e);
     const Loss<E> l{rows_of<const E>(r->logits), dlogits ? rows_of<E>(*dlogits) : Rows<E>{}, Entries{r->top_logits, r->top_index, r->K, r->top_type},
-                    r->top_norm, r->weight, r->targets, loss, r->B, r->V, r->temperature, r->hard};
+                    r->top_norm, r->weight, r->targets, loss, r->B, r->V, r->temperature, r->hard, 1.0 / (double)r->temperature};
     const auto run = [&](auto waves, auto chunks) {
-      const size_t bits = l.top_norm ? ((size_t)bppsa_ceil_div(l.V, 32) + 1) * sizeof(uint32_t) : 0;
+      const size_t bits = ((size_t)bppsa_ceil_div(l.V, 32) + 1) * sizeof(uint32_t);
       const auto kernel = l.hard != 0.0f && l.tau != 1.0f ? distil_kernel<E, waves.value, chunks.value, true>
                                                           : distil_kernel<E, waves.value, chunks.value, false>;
       kernel<<<(unsigned)(r->T * r->B), waves.value * 64, bits, (hipStream_t)stream>>>(l);
