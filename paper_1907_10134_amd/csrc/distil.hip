@@ -74,8 +74,12 @@ struct Share {
 // One workgroup a row.  CHUNKS > 0: the row is read once, into registers (16 bytes a lane and chunk), and its largest value, its sums
 // and its gradient are made of those; 0: a row too long for that is read three times.  SECOND: the data's own token has a
 // softmax of its own, at another temperature.
+//
+// As many waves a SIMD as the registers of the row let, and no more: two workgroups of sixteen waves are worth some spilled scalars of
+// the entries (2048 rows of 65536 bf16 with two softmaxes: 143 us, 180 by one workgroup a unit), four of eight instead of
+// three are not (8192 rows of 32768: 243 us, 226).
 template <typename E, int WAVES, int CHUNKS, bool SECOND>
-__global__ void __launch_bounds__(WAVES * 64, WAVES * CHUNKS <= 64 ? 6 : 4)
+__global__ void __launch_bounds__(WAVES * 64, CHUNKS == 16 ? 4 : WAVES == 16 || sizeof(E) == 4 ? 8 : 6)
 distil_kernel(const Loss<E> l) {
   constexpr int N = Chunk<E>::N, THREADS = WAVES * 64, STEP = THREADS * N, HELD = CHUNKS ? CHUNKS : 1;
   extern __shared__ uint32_t is_entry[];       // a bit a token

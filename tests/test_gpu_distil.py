@@ -77,7 +77,8 @@ def _check(got, c, ref, dtype):
 
 
 SIZES = [(1, 1, 1), (3, 2, 2), (7, 16, 8), (9, 63, 5), (6, 64, 64), (5, 65, 1), (12, 255, 256 - 1), (6, 512, 256), (5, 513, 50), (5, 1000, 31),
-         (6, 4001, 50), (4, 8192, 64), (3, 8193, 64), (3, 32001, 128), (3, 65537, 40), (5, 131073, 256), (2, 300001, 33)]
+         (6, 4001, 50), (4, 8192, 64), (3, 8193, 64), (3, 32001, 128), (3, 65537, 40), (5, 131073, 256), (2, 300001, 33),
+         (2, 1024, 6), (3, 2049, 9), (3, 2048, 9), (4, 16384, 20), (4, 16385, 20), (1, 1 << 20, 40)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
