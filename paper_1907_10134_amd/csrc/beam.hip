@@ -6,12 +6,12 @@
 // model with other sizes of a batch.
 #include <algorithm>
 
-#include "chunks.h"
+#include "logits.h"
 #include "lanes.h"
 
 namespace {
 
-using namespace chunks;
+using namespace logits;
 
 constexpr int kThreads = 256, kEach = 32, kPiece = kThreads * kEach, kFound = 1024;
 constexpr int kMostBeams = BPPSA_BEAM_MAX_W, kMostPieces = 64;
@@ -55,14 +55,14 @@ __device__ __forceinline__ bool alive(const Beams<E>& s, int row) {
   return fabsf(s.scores[row]) < INFINITY && !(s.finished && s.finished[row]);
 }
 
-// One workgroup a piece of a row, whose values stay in registers.  The W-th largest of a piece is no smaller than the smallest
-// of the largest values of W groups of threads; so few values reach that bound (22 of 8192 normal ones at W = 8) that
-// each can count those in front of it.  Where more than kFound do, equal ones that is, they are taken one after the other.
+// One workgroup a piece of a row, whose values stay in registers.  A bound that W of 64 columns of the piece pass, by their
+// largest values, is no larger than the W-th largest value; so few values pass it (some 10 of 8192 normal ones at W = 8) that each
+// can count those in front of it.  Where more than kFound do, equal ones that is, they are taken one after the other.
 template <typename E>
 __global__ void __launch_bounds__(kThreads, 8)
 beam_piece_kernel(const Beams<E> s, const Pieces out) {
   constexpr int N = Chunk<E>::N, LOADS = kEach / N, STEP = kThreads * N;
-  __shared__ float group[kThreads / 64][kMostBeams];
+  __shared__ float of_column[kThreads / 64][64];
   __shared__ double sums[kThreads / 64];
   __shared__ uint64_t found[kFound];
   __shared__ int n_found;
@@ -86,21 +86,35 @@ beam_piece_kernel(const Beams<E> s, const Pieces out) {
     for (int j = 0; j < N; ++j) of_chunk[k] = fmaxf(of_chunk[k], held[k][j]);
     m = fmaxf(m, of_chunk[k]);
   }
-  const int groups = s.W <= 1 ? 1 : 1 << (32 - __builtin_clz(s.W - 1));
   if (threadIdx.x == 0) n_found = 0;
-  float of_group = m;
-  for (int k = groups; k < 64; k <<= 1) of_group = fmaxf(of_group, __shfl_xor(of_group, k));
-  if (lane < groups) group[wave][lane] = of_group;
+  of_column[wave][lane] = m;
   __syncthreads();
+  const int64_t at = (int64_t)row * out.count + piece;
+  uint64_t* const to = out.key + at * s.W;
+  float column = m;
 #pragma unroll
-  for (int k = 0; k < kThreads / 64; ++k) of_group = fmaxf(of_group, group[k][lane & (groups - 1)]);
-  const float bound = -lanes::largest(-of_group), top = lanes::largest(of_group), zero = top == -INFINITY ? 0.0f : top;
+  for (int k = 0; k < kThreads / 64; ++k) column = fmaxf(column, of_column[k][lane]);
+  const float top = lanes::largest(column);
+  // as high a bound as W columns pass, within a 128th of the columns' range
+  const bool none = top == -INFINITY;          // no token has a share: the first ones come first
+  float bound = none ? INFINITY : -INFINITY;
+  if (!none && __popcll(__ballot(column > -INFINITY)) >= s.W) {
+    float over = top;
+    bound = -lanes::largest(column > -INFINITY ? -column : -INFINITY);
+#pragma unroll 1
+    for (int k = 0; k < 7; ++k) {
+      const float half = 0.5f * bound + 0.5f * over;
+      if (__popcll(__ballot(column >= half)) >= s.W) bound = half;
+      else over = half;
+    }
+  }
+  const float zero = none ? 0.0f : top;
   float e = 0.0f;
 #pragma unroll
   for (int k = 0; k < LOADS; ++k) {
     float part = 0.0f;
 #pragma unroll
-    for (int j = 0; j < N; ++j) part += exp2_fast((held[k][j] - zero) * kLog2e);
+    for (int j = 0; j < N; ++j) part += exp2_fast((held[k][j] - zero) * kLog2e);         // the largest is 1, exactly
     e += part;
   }
   if (m >= bound)
@@ -118,13 +132,15 @@ beam_piece_kernel(const Beams<E> s, const Pieces out) {
   if (lane == 0) sums[wave] = sum;
   __syncthreads();
   const int n = n_found;
-  const int64_t at = (int64_t)row * out.count + piece;
   if (threadIdx.x == 0) {
     double all = sums[0];
     for (int k = 1; k < kThreads / 64; ++k) all += sums[k];
     out.largest[at] = zero, out.sum[at] = all;
   }
-  uint64_t* const to = out.key + at * s.W;
+  if (none) {
+    if (threadIdx.x < s.W) to[threadIdx.x] = (int)threadIdx.x < left ? key_of(-INFINITY, piece * kPiece + threadIdx.x) : 0;
+    return;
+  }
   if (n <= kFound) {
     for (int i = threadIdx.x; i < n; i += kThreads) {
       const uint64_t mine = found[i];

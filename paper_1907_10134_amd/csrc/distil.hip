@@ -6,12 +6,12 @@
 // M = sum p + p0, p0 / q0 = 0 without the normaliser.  The other part, -log softmax(x)[target], has the gradient
 // softmax(x) - 1[target].  What is made of the K entries alone is made in 64 bits: there are few of them, and the parts of a
 // divergence cancel.
-#include "chunks.h"
+#include "logits.h"
 #include "lanes.h"
 
 namespace {
 
-using namespace chunks;
+using namespace logits;
 
 struct Entries {                   // of the teacher, [T,B,K]
   const void* logits;
@@ -38,31 +38,6 @@ struct Loss {
 };
 
 constexpr int kMost = BPPSA_DISTIL_MAX_K;
-
-// exp((x - m) scale) for logits of which m is the largest.  float32 logits take the corrected exponential.  For 16-bit ones it is one
-// multiply-add in front of the exponential, 2^(k x - k m) with k = scale log2(e): what the rounding of k m leaves is the same factor
-// 2^off in all of a row's, and is taken from the logarithm of their sum.  Where k m passes 2^20 the next smaller logit of 16
-// bits has no share left, with a k of 2^20 / m either: so nothing overflows.
-template <typename E>
-struct Exponential {
-  float m, scale, k, km, off;
-  __device__ __forceinline__ Exponential(float largest, float scale)
-      : m(largest), scale(scale), k(fminf(scale * kLog2e, 0x1p20f / fabsf(largest))), km(largest * k), off(fmaf(largest, k, -km)) {}
-  __device__ __forceinline__ float operator()(float x) const {
-    if constexpr (kExact<E>) return exp_of<true>((x - m) * scale);
-    else return exp2_fast(fmaf(x, k, -km));
-  }
-  // what comes off the logarithm of a sum of such
-  __device__ __forceinline__ double log_off() const { return kExact<E> ? 0.0 : 0.69314718055994531 * (double)off; }
-};
-
-// log(v), within 2^-23: the exponent's part is exact, and the instruction sees values from 0.7 to 1.4 alone, whose logarithms are small.
-__device__ __forceinline__ double log_of(float v) {
-  int e = __builtin_amdgcn_frexp_expf(v);
-  float f = __builtin_amdgcn_frexp_mantf(v);
-  if (f < 0.70710678f) f += f, --e;
-  return ((double)e + (double)__builtin_amdgcn_logf(f)) * 0.69314718055994531;
-}
 
 // What the waves of a row tell each other, each by its first lane.
 template <int WAVES>

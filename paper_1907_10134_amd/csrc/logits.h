@@ -1,9 +1,9 @@
-// Rows of logits, 16 bytes a lane at a time.
+// Rows of logits, 16 bytes a lane at a time, and their exponentials.
 #pragma once
 
 #include "ssm_common.h"
 
-namespace chunks {
+namespace logits {
 
 using namespace ssm;
 
@@ -70,4 +70,29 @@ __device__ __forceinline__ void store_chunk(E* x, int at, int V, const float (&v
     if (at + k < V) store(x + at + k, v[k]);
 }
 
-}  // namespace chunks
+// exp((x - m) scale) for logits of which m is the largest.  float32 logits take the corrected exponential.  For 16-bit ones it is one
+// multiply-add in front of the exponential, 2^(k x - k m) with k = scale log2(e): what the rounding of k m leaves is the same factor
+// 2^off in all of a row's, and is taken from the logarithm of their sum.  Where k m passes 2^20 the next smaller logit of 16
+// bits has no share left, with a k of 2^20 / m either: so nothing overflows.
+template <typename E>
+struct Exponential {
+  float m, scale, k, km, off;
+  __device__ __forceinline__ Exponential(float largest, float scale)
+      : m(largest), scale(scale), k(fminf(scale * kLog2e, 0x1p20f / fabsf(largest))), km(largest * k), off(fmaf(largest, k, -km)) {}
+  __device__ __forceinline__ float operator()(float x) const {
+    if constexpr (kExact<E>) return exp_of<true>((x - m) * scale);
+    else return exp2_fast(fmaf(x, k, -km));
+  }
+  // what comes off the logarithm of a sum of such
+  __device__ __forceinline__ double log_off() const { return kExact<E> ? 0.0 : 0.69314718055994531 * (double)off; }
+};
+
+// log(v), within 2^-23: the exponent's part is exact, and the instruction sees values from 0.7 to 1.4 alone, whose logarithms are small.
+__device__ __forceinline__ double log_of(float v) {
+  int e = __builtin_amdgcn_frexp_expf(v);
+  float f = __builtin_amdgcn_frexp_mantf(v);
+  if (f < 0.70710678f) f += f, --e;
+  return ((double)e + (double)__builtin_amdgcn_logf(f)) * 0.69314718055994531;
+}
+
+}  // namespace logits

@@ -113,6 +113,25 @@ def test_masked_broken_and_dead_beams():
     assert np.all(want[0][0] == -np.inf) and want[0][4, 0] == float(c["scores"][4, 1]) and np.all(want[0][4, 1:] == -np.inf)
 
 
+@pytest.mark.parametrize("W", (1, 5, 32))
+def test_vocabularies_with_few_tokens_left(W):
+    """All but a few tokens masked with minus infinity, in one piece of a row or over several, fewer of them than beams; a NaN among
+    masked tokens still breaks its row."""
+    import torch
+    import paper_1907_10134_amd as bp
+    rng = np.random.default_rng(W)
+    x = torch.full((6, W, 30000), float("-inf"), device="cuda")
+    for b, places in enumerate(([29999], [0, 8191, 8192], range(100, 140), rng.integers(0, 30000, 300), [5, 9000, 17000, 25000], [7])):
+        for w in range(W):
+            for v in places:
+                x[b, w, int(v)] = float(rng.standard_normal())
+    x[4, 0, 20000] = float("nan")              # its piece has a finite token too
+    x[5, W - 1, 12345] = float("nan")          # its piece has none
+    for t in (torch.float32, torch.float16):
+        c = dict(logits=x.to(t), scores=torch.zeros((6, W), device="cuda"))
+        _check(bp.beam_select(**c), c)
+
+
 def test_strides():
     """Beams first in memory, windows of wider rows, an odd offset."""
     import torch
