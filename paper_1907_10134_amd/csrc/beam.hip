@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(1024)
 beam_join_kernel(const Beams<E> s, const Pieces in, const Choice out) {
   extern __shared__ uint64_t lists[];          // of each wave, [piece][W]
   __shared__ double total[kMostBeams][kMostBeams];
-  __shared__ int token[kMostBeams][kMostBeams], parent[kMostBeams];
+  __shared__ int token[kMostBeams][kMostBeams];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, W = s.W;
   uint64_t* const list = lists + (int64_t)wave * in.count * W;
   for (int w = wave; w < W; w += waves) {
@@ -227,7 +227,7 @@ beam_join_kernel(const Beams<E> s, const Pieces in, const Choice out) {
   }
   __syncthreads();
   if (wave) return;
-  int next = 0;
+  int next = 0, parent = -1;
   for (int i = 0; i < W; ++i) {
     const bool any = lane < W && next < W && token[lane][next] >= 0;
     const double v = any ? total[lane][next] : 0.0;
@@ -238,31 +238,26 @@ beam_join_kernel(const Beams<E> s, const Pieces in, const Choice out) {
       out.scores[at] = (float)v, out.parents[at] = lane, out.tokens[at] = t;
       if (out.finished) out.finished[at] = (s.finished && s.finished[blockIdx.x * W + lane]) || t == s.end;
       ++next;
-      parent[i] = lane;
     }
+    if (lane == i) parent = who;
   }
   if (!s.slots) return;
-  __builtin_amdgcn_wave_barrier();
   // the first child of a beam goes on in its slot, the others take those of beams without one, in order
+  const uint32_t before = (1u << (lane & 31)) - 1;
+  uint32_t childless = 0, siblings = 0;
+  for (int w = 0; w < W; ++w) {
+    const uint32_t children = (uint32_t)__ballot(parent == w);
+    if (!children) childless |= 1u << w;
+    if (parent == w) siblings = children;
+  }
+  const bool more = siblings & before;
+  uint32_t free = childless;
+  for (int k = __popc((uint32_t)__ballot(lane < W && more) & before); k > 0; --k) free &= free - 1;
   if (lane < W) {
     const int32_t* const slots = s.slots + (int64_t)blockIdx.x * W;
-    const int p = parent[lane];
-    int more = 0, mine = 0;
-    for (int i = 0; i <= lane; ++i) {
-      bool first = true;
-      for (int k = 0; k < i; ++k) first &= parent[k] != parent[i];
-      if (!first) ++more;
-      if (i == lane) mine = !first;
-    }
-    int home = p;
-    if (mine)
-      for (int k = 0; k < W; ++k) {
-        bool childless = true;
-        for (int i = 0; i < W; ++i) childless &= parent[i] != k;
-        if (childless && --more == 0) home = k;
-      }
-    const int at = blockIdx.x * W + lane, to = slots[home], of = slots[p];
-    out.slots[at] = to, out.sources[at] = mine ? of : -1;
+    const int home = more ? __builtin_ctz(free) : parent;
+    const int at = blockIdx.x * W + lane, to = slots[home], of = slots[parent];
+    out.slots[at] = to, out.sources[at] = more ? of : -1;
   }
 }
 
