@@ -41,9 +41,10 @@ gated_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __r
     // a run with an end in it is another copy of the code: with its conditions in this one there are too few scalar registers
     auto gather = [&](auto all) __attribute__((always_inline)) {
       constexpr bool WHOLE = all.value;
+      Channel<E> channel[V];
+      channels_of(l, d, channel);
       uint32_t x[R], r[R], i[R];
       load_rows<WHOLE, R, V>(l.r, first, b, rows, byte, r), load_rows<WHOLE, R, V>(l.i, first, b, rows, byte, i), load_rows<WHOLE, R, V>(l.x, first, b, rows, byte, x);
-      const Channel<E> channel[2] = {Channel<E>(l, d), Channel<E>(l, d + V - 1)};
       float product[V], end[V];
 #pragma unroll
       for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = 0.0f;
@@ -138,15 +139,16 @@ gated_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int sl
   float out[V] = {};
   if (slot < 0 || slot >= slots_in_state) return store_some<E, V>(y.at(0, b) + d, out);
   float* const at = state + (int64_t)slot * l.D + d;
+  Channel<E> channel[V];
+  channels_of(l, d, channel);
   Some<float, V> h = load_some<float, V>(at);
   const auto x = load_some<E, V>(l.x.at(0, b) + d), r = load_some<E, V>(l.r.at(0, b) + d), i = load_some<E, V>(l.i.at(0, b) + d);
   Some<E, V> z = {};
   if (l.z.data) z = load_some<E, V>(l.z.at(0, b) + d);
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    const Channel<E> channel(l, d + c);
-    const float rho = channel.rho((float)r.v[c]), iota = channel.iota((float)i.v[c]), a = channel.a(rho);
-    h.v[c] = fmaf(a, h.v[c], __builtin_amdgcn_sqrtf(channel.m2(a, rho)) * iota * (float)x.v[c]);
+    const float rho = channel[c].rho((float)r.v[c]), iota = channel[c].iota((float)i.v[c]), a = channel[c].a(rho);
+    h.v[c] = fmaf(a, h.v[c], __builtin_amdgcn_sqrtf(channel[c].m2(a, rho)) * iota * (float)x.v[c]);
     out[c] = l.z.data ? h.v[c] * (float)z.v[c] * sigmoid<E>((float)z.v[c]) : h.v[c];
   }
   // in place: what is repeated has been read before or behind the neighbour's update, and is not stored

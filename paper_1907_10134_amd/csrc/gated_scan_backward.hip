@@ -55,13 +55,14 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
     float a[R][V], e[R][V], rho[R][V], iota[R][V], sum[3][V] = {};
     const int rows = len - first < R ? len - first : R;
     const uint32_t byte = (uint32_t)d * sizeof(E);
+    Channel<E> channel[V];
+    if (rows > 0) channels_of(l, d, channel);
     auto gather = [&](auto all) __attribute__((always_inline)) {
       constexpr bool WHOLE = all.value;
       uint32_t r[R], i[R];
       load_rows<WHOLE, R, V>(l.r, first, b, rows, byte, r), load_rows<WHOLE, R, V>(l.i, first, b, rows, byte, i), load_rows<WHOLE, R, V>(l.x, first, b, rows, byte, x);
       load_rows<WHOLE, R, V>(dy, first, b, rows, byte, go);
       if (GATE) load_rows<WHOLE, R, V>(l.z, first, b, rows, byte, z);
-      const Channel<E> channel[2] = {Channel<E>(l, d), Channel<E>(l, d + V - 1)};
       float product[V], end[V], back[V];
 #pragma unroll
       for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = back[c] = 0.0f;
@@ -141,7 +142,6 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
         as_loaded(x[j]), as_loaded(go[j]);
         if (GATE) as_loaded(z[j]);
       }
-      const Channel<E> channel[2] = {Channel<E>(l, d), Channel<E>(l, d + V - 1)};
       Run<E> to_x(o.dx, first, b), to_r(o.dr, first, b), to_i(o.di, first, b), to_z(GATE ? o.dz : o.dx, first, b);
       const int64_t last = rows - 1;
       to_x.move_by(last * to_x.step), to_r.move_by(last * to_r.step), to_i.move_by(last * to_i.step);
