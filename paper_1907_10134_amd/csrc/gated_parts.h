@@ -19,14 +19,16 @@ constexpr int kTile = kWaves * kRun, kKept = kWaves * kRunBack;      // steps of
 template <typename E>
 struct Layer {
   Rows<const E> x, r, i, z;
-  const float *decay, *r_bias, *i_bias, *h0;
+  const float *decay, *r_bias, *i_bias, *h0;   // a bias that there is not: the decays, with a mask that leaves nothing of them
   const int32_t* lengths;
   int T, B, D, columns;
+  uint32_t r_mask, i_mask;
 };
 template <typename E>
 Layer<E> layer_of(const bppsa_gated& l, int wide) {
-  return Layer<E>{rows_of<const E>(l.x), rows_of<const E>(l.r), rows_of<const E>(l.i), rows_of<const E>(l.z), l.decay, l.r_bias,
-                  l.i_bias, l.h0, l.lengths, l.T, l.B, l.D, bppsa_ceil_div(l.D, wide)};
+  return Layer<E>{rows_of<const E>(l.x), rows_of<const E>(l.r), rows_of<const E>(l.i), rows_of<const E>(l.z), l.decay,
+                  l.r_bias ? l.r_bias : l.decay, l.i_bias ? l.i_bias : l.decay, l.h0, l.lengths, l.T, l.B, l.D,
+                  bppsa_ceil_div(l.D, wide), l.r_bias ? ~0u : 0u, l.i_bias ? ~0u : 0u};
 }
 
 template <int V>
@@ -128,16 +130,16 @@ struct Channel {
   __device__ __forceinline__ float m2(float a, float rho) const { return one_minus(a, (decay + decay) * rho); }
 };
 
-// A lane's channels.  All of it is asked for together: a bias that there is not is read from the decays and left out, where a branch
-// around each would wait for it (a token of B = 64, D = 4096: 15 us instead of 4).
+// A lane's channels.  All of it is asked for together: a branch around a bias that may not be there would wait for it (T = 30000,
+// B = 1, D = 2048: 150 us instead of 134).
 template <typename E, int V>
 __device__ __forceinline__ void channels_of(const Layer<E>& l, int d, Channel<E> (&channel)[V]) {
-  const Some<float, V> decay = load_some<float, V>(l.decay + d), r = load_some<float, V>((l.r_bias ? l.r_bias : l.decay) + d),
-                       i = load_some<float, V>((l.i_bias ? l.i_bias : l.decay) + d);
+  const Some<float, V> decay = load_some<float, V>(l.decay + d), r = load_some<float, V>(l.r_bias + d), i = load_some<float, V>(l.i_bias + d);
   const float scale = kExact<E> ? 1.0f : -kLog2e;
 #pragma unroll
   for (int c = 0; c < V; ++c)
-    channel[c] = Channel<E>{l.r_bias ? r.v[c] * scale : 0.0f, l.i_bias ? i.v[c] * scale : 0.0f, decay.v[c], decay.v[c] * -kLog2e};
+    channel[c] = Channel<E>{__uint_as_float(__float_as_uint(r.v[c]) & l.r_mask) * scale,
+                            __uint_as_float(__float_as_uint(i.v[c]) & l.i_mask) * scale, decay.v[c], decay.v[c] * -kLog2e};
 }
 
 // One grid axis counts tiles, samples and columns; a launch has fewer than 2^32 threads, 512 a tile.

@@ -128,35 +128,37 @@ gated_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __r
 }
 
 // One token.  A thread has a lane's channels of one row of the batch; bound by the launch and one round of loads.
-template <typename E, int V>
+template <typename E, int V, bool GATE>
 __global__ void __launch_bounds__(64)
 gated_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int slots_in_state, const int32_t* __restrict__ slots) {
   const int b = blockIdx.x / l.columns;
   const Own<V> own(blockIdx.x % l.columns, threadIdx.x, l.D);
   if (!own.on) return;
-  const int d = own.d;
-  int slot = slots ? slots[b] : b;
+  const int d = own.d, slot = slots ? slots[b] : b;
   float out[V] = {};
   if (slot < 0 || slot >= slots_in_state) return store_some<E, V>(y.at(0, b) + d, out);
   float* const at = state + (int64_t)slot * l.D + d;
   Channel<E> channel[V];
   channels_of(l, d, channel);
-  Some<float, V> h = load_some<float, V>(at);
+  const auto was = load_some<float, V>(at);
   const auto x = load_some<E, V>(l.x.at(0, b) + d), r = load_some<E, V>(l.r.at(0, b) + d), i = load_some<E, V>(l.i.at(0, b) + d);
   Some<E, V> z = {};
-  if (l.z.data) z = load_some<E, V>(l.z.at(0, b) + d);
+  if (GATE) z = load_some<E, V>(l.z.at(0, b) + d);
+  float h[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) {
     const float rho = channel[c].rho((float)r.v[c]), iota = channel[c].iota((float)i.v[c]), a = channel[c].a(rho);
-    h.v[c] = fmaf(a, h.v[c], __builtin_amdgcn_sqrtf(channel[c].m2(a, rho)) * iota * (float)x.v[c]);
-    out[c] = l.z.data ? h.v[c] * (float)z.v[c] * sigmoid<E>((float)z.v[c]) : h.v[c];
+    h[c] = fmaf(a, was.v[c], __builtin_amdgcn_sqrtf(channel[c].m2(a, rho)) * iota * (float)x.v[c]);
+    out[c] = GATE ? h[c] * ((float)z.v[c] * sigmoid<E>((float)z.v[c])) : h[c];
   }
   // in place: what is repeated has been read before or behind the neighbour's update, and is not stored
   if (own.repeated) {
-    for (int c = own.repeated; c < V; ++c) at[c] = h.v[c], store(y.at(0, b) + d + c, out[c]);
+#pragma unroll
+    for (int c = 0; c < V; ++c)
+      if (c >= own.repeated) at[c] = h[c], store(y.at(0, b) + d + c, out[c]);
     return;
   }
-  *reinterpret_cast<Some<float, V>*>(at) = h;
+  store_some<float, V>(at, h);
   store_some<E, V>(y.at(0, b) + d, out);
 }
 
@@ -218,7 +220,8 @@ extern "C" bppsa_status bppsa_gated_scan_step(const bppsa_gated* layer, const bp
     return by_width<E>(layer->D, [&](auto width) {
       constexpr int V = width.value;
       const Layer<E> l = layer_of<E>(*layer, 64 * V);
-      gated_step_kernel<E, V><<<(unsigned)(l.columns * l.B), 64, 0, (hipStream_t)stream>>>(l, rows_of<E>(*y), state, slots_in_state, slots);
+      const auto kernel = l.z.data ? gated_step_kernel<E, V, true> : gated_step_kernel<E, V, false>;
+      kernel<<<(unsigned)(l.columns * l.B), 64, 0, (hipStream_t)stream>>>(l, rows_of<E>(*y), state, slots_in_state, slots);
       BPPSA_CHECK_LAUNCH();
       return BPPSA_OK;
     });
