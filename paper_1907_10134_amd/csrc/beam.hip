@@ -278,7 +278,7 @@ static inline bool beam_sizes_ok(int B, int W, int V) {
          (int64_t)B * W * bppsa_ceil_div(V, kPiece) < 1 << 24;
 }
 
-// A workgroup takes a piece of a tensor's slots for every so many rows, which it looks through 64 at a time.
+// A workgroup takes a piece of a tensor's slots for every so many rows.
 template <typename U>
 __device__ __forceinline__ void copy_bytes(char* to, const char* from, int n) {
   for (int k = threadIdx.x; k < n / (int)sizeof(U); k += kThreads) reinterpret_cast<U*>(to)[k] = reinterpret_cast<const U*>(from)[k];

@@ -51,10 +51,10 @@ struct Share {
 // softmax of its own, at another temperature.
 //
 // As many waves a SIMD as the registers of the row let, and no more: two workgroups of sixteen waves are worth some spilled scalars of
-// the entries (2048 rows of 65536 bf16 with two softmaxes: 143 us, 180 by one workgroup a unit), four of eight instead of
-// three are not (8192 rows of 32768: 243 us, 226).
+// the entries (2048 rows of 65536 bf16 with two softmaxes: 147 us, 180 by one workgroup a unit), four of eight instead of
+// three are not (8192 rows of 32768 bf16: 243 us, 226; 4096 rows of 8000 fp32: 64 us, 58).
 template <typename E, int WAVES, int CHUNKS, bool SECOND>
-__global__ void __launch_bounds__(WAVES * 64, CHUNKS == 16 ? 4 : WAVES == 16 || sizeof(E) == 4 ? 8 : 6)
+__global__ void __launch_bounds__(WAVES * 64, CHUNKS == 16 ? 4 : WAVES == 16 ? 8 : 6)
 distil_kernel(const Loss<E> l) {
   constexpr int N = Chunk<E>::N, THREADS = WAVES * 64, STEP = THREADS * N, HELD = CHUNKS ? CHUNKS : 1;
   extern __shared__ uint32_t is_entry[];       // a bit a token
@@ -158,56 +158,55 @@ distil_kernel(const Loss<E> l) {
     if (entries) top = lanes::largest(lane < with_entries ? of.top[lane % WAVES] : -INFINITY);
   }
 
-  {
-    forget();
-    const Exponential<E> of_tau(m, scale), of_one(m, 1.0f);
-    float s = 0.0f, s1 = 0.0f, rest = 0.0f;
-    each([&](const Chunk<E>& x, int at, int, auto) __attribute__((always_inline)) {
-      float e[N], sum = 0.0f, sum1 = 0.0f;
+  forget();
+  const Exponential<E> of_tau(m, scale), of_one(m, 1.0f);
+  float s = 0.0f, s1 = 0.0f, rest = 0.0f;
+  each([&](const Chunk<E>& x, int at, int, auto) __attribute__((always_inline)) {
+    float e[N], sum = 0.0f, sum1 = 0.0f;
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        e[k] = of_tau(x[k]), sum += e[k];
-        if (SECOND) sum1 += of_one(x[k]);
-      }
-      s += sum, s1 += sum1;
-      if (tail) {
-        const int from = first + at;
-        const uint32_t bits = (uint32_t)(((uint64_t)is_entry[from / 32 + 1] << 32 | is_entry[from / 32]) >> from % 32);
-        float others = 0.0f;
+    for (int k = 0; k < N; ++k) {
+      e[k] = of_tau(x[k]), sum += e[k];
+      if (SECOND) sum1 += of_one(x[k]);
+    }
+    s += sum, s1 += sum1;
+    if (tail) {
+      const int from = first + at;
+      const uint32_t bits = (uint32_t)(((uint64_t)is_entry[from / 32 + 1] << 32 | is_entry[from / 32]) >> from % 32);
+      float others = 0.0f;
 #pragma unroll
-        for (int k = 0; k < N; ++k) others += __uint_as_float(__float_as_uint(e[k]) & ~(uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1));
-        rest += others;
-      }
-    });
-    s = lanes::sum(s);
-    if (SECOND) s1 = lanes::sum(s1);
-    if (tail) rest = lanes::sum(rest);
-    // the entries' shares, before they are divided by their sum where they are all there is, and what they leave of the divergence
-    double shares = 0.0, terms = 0.0;
-    if (entries) {
-      for (int k = threadIdx.x; k < K; k += THREADS) {
-        if (place[k] < 0) continue;
-        // the difference in 64 bits, its exponential in 32, corrected by what the difference loses there
-        const double over = tail ? (double)logit[k] * l.scale - (double)l.top_norm[row] : ((double)logit[k] - (double)top) * l.scale;
-        const float near = (float)over, e = exp_of<true>(near), share = e > 0.0f ? fmaf(e, (float)(over - (double)near), e) : 0.0f;
-        shares += (double)share, p[k] = share;
-        if (share > 0.0f) terms += (double)share * (over - ((double)at_place[k] - (double)m) * l.scale);
-      }
-      shares = lanes::sum(shares), terms = lanes::sum(terms);
+      for (int k = 0; k < N; ++k) others += __uint_as_float(__float_as_uint(e[k]) & ~(uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1));
+      rest += others;
     }
-    if (lane == 0) of.sums[0][wave] = s, of.sums[1][wave] = s1, of.sums[2][wave] = rest, of.shares[wave] = shares, of.terms[wave] = terms;
-    __syncthreads();
-    if (WAVES > 1) {               // a lane a wave
-      s = lanes::sum(lane < WAVES ? of.sums[0][lane % WAVES] : 0.0f);
-      if (SECOND) s1 = lanes::sum(lane < WAVES ? of.sums[1][lane % WAVES] : 0.0f);
-      if (tail) rest = lanes::sum(lane < WAVES ? of.sums[2][lane % WAVES] : 0.0f);
-      shares = lanes::sum(lane < with_entries ? of.shares[lane % WAVES] : 0.0);
-      if (wave == 0) terms = lanes::sum(lane < with_entries ? of.terms[lane % WAVES] : 0.0);
+  });
+  s = lanes::sum(s);
+  if (SECOND) s1 = lanes::sum(s1);
+  if (tail) rest = lanes::sum(rest);
+  // the entries' shares, before they are divided by their sum where they are all there is, and what they leave of the divergence
+  double shares = 0.0, terms = 0.0;
+  if (entries) {
+    for (int k = threadIdx.x; k < K; k += THREADS) {
+      if (place[k] < 0) continue;
+      // the difference in 64 bits, its exponential in 32, corrected by what the difference loses there
+      const double over = tail ? (double)logit[k] * l.scale - (double)l.top_norm[row] : ((double)logit[k] - (double)top) * l.scale;
+      const float near = (float)over, e = exp_of<true>(near), share = e > 0.0f ? fmaf(e, (float)(over - (double)near), e) : 0.0f;
+      shares += (double)share, p[k] = share;
+      if (share > 0.0f) terms += (double)share * (over - ((double)at_place[k] - (double)m) * l.scale);
     }
-    const bool any = shares > 0.0;
-    const double p0 = tail && rest > 0.0f ? fmax(0.0, 1.0 - shares) : 0.0;
-    const float over = any && !tail ? 1.0f / (float)shares : 1.0f;
-    if (dx) {
+    shares = lanes::sum(shares), terms = lanes::sum(terms);
+  }
+  if (lane == 0) of.sums[0][wave] = s, of.sums[1][wave] = s1, of.sums[2][wave] = rest, of.shares[wave] = shares, of.terms[wave] = terms;
+  __syncthreads();
+  if (WAVES > 1) {               // a lane a wave
+    s = lanes::sum(lane < WAVES ? of.sums[0][lane % WAVES] : 0.0f);
+    if (SECOND) s1 = lanes::sum(lane < WAVES ? of.sums[1][lane % WAVES] : 0.0f);
+    if (tail) rest = lanes::sum(lane < WAVES ? of.sums[2][lane % WAVES] : 0.0f);
+    shares = lanes::sum(lane < with_entries ? of.shares[lane % WAVES] : 0.0);
+    if (wave == 0) terms = lanes::sum(lane < with_entries ? of.terms[lane % WAVES] : 0.0);
+  }
+  const bool any = shares > 0.0;
+  const double p0 = tail && rest > 0.0f ? fmax(0.0, 1.0 - shares) : 0.0;
+  const float over = any && !tail ? 1.0f / (float)shares : 1.0f;
+  if (dx) {
     const float of_soft = weight * (1.0f - l.hard) * l.tau, hard = known ? weight * l.hard : 0.0f;
     const float one = 1.0f / s, of_e1 = SECOND ? hard / s1 : 0.0f, of_e = SECOND ? 0.0f : hard * one;
     const float M = (tail ? (float)shares : any ? 1.0f : 0.0f) + (float)p0, ratio = p0 > 0.0 ? (float)p0 * (s / rest) : 0.0f;
@@ -222,6 +221,7 @@ distil_kernel(const Loss<E> l) {
       }
       if constexpr (CHUNKS == 0) store_chunk<E>(dx, first + at, l.V, g);
       else if constexpr (whole.value) store_whole(dx + at, first * sizeof(E), g);
+      else if (shared == 0) store_whole(dx, (first + at) * sizeof(E), g);
       else
 #pragma unroll
         for (int k = 0; k < N; ++k)
@@ -247,17 +247,16 @@ distil_kernel(const Loss<E> l) {
     if (threadIdx.x == THREADS - 1 && known) {
       if (!(is_entry[target / 32] >> target % 32 & 1)) again(target, at_target, elsewhere, hard);
     }
-    }
-    // last, when the row's registers are free
-    if (wave == 0) {
-      double soft = 0.0, ce = 0.0, log_s = 0.0;
-      if (tail || (known && !SECOND)) log_s = log_of(s) - of_tau.log_off();
-      if (tail) soft = terms + (shares + p0) * log_s + (p0 > 0.0 ? p0 * (log_of((float)p0) - log_of(rest) + of_tau.log_off()) : 0.0);
-      else if (any) soft = terms / shares + log_of(s) - log_of((float)shares) - of_tau.log_off();
-      if (known) ce = (double)m - (double)at_target + (SECOND ? log_of(s1) - of_one.log_off() : log_s);
-      if (threadIdx.x == 0)
-        l.loss[row] = (float)((double)weight * ((1.0 - (double)l.hard) * (double)l.tau * (double)l.tau * soft + (double)l.hard * ce));
-    }
+  }
+  // last, when the row's registers are free
+  if (wave == 0) {
+    double soft = 0.0, ce = 0.0, log_s = 0.0;
+    if (tail || (known && !SECOND)) log_s = log_of(s) - of_tau.log_off();
+    if (tail) soft = terms + (shares + p0) * log_s + (p0 > 0.0 ? p0 * (log_of((float)p0) - log_of(rest) + of_tau.log_off()) : 0.0);
+    else if (any) soft = terms / shares + log_of(s) - log_of((float)shares) - of_tau.log_off();
+    if (known) ce = (double)m - (double)at_target + (SECOND ? log_of(s1) - of_one.log_off() : log_s);
+    if (threadIdx.x == 0)
+      l.loss[row] = (float)((double)weight * ((1.0 - (double)l.hard) * (double)l.tau * (double)l.tau * soft + (double)l.hard * ce));
   }
 }
 

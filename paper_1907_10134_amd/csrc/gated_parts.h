@@ -236,7 +236,7 @@ __device__ __forceinline__ float look_back(const uint64_t* mine, uint32_t at, in
 constexpr int kQueues = 8, kTicketStride = 32, kTicketBytes = kQueues * kTicketStride * 4;
 __device__ __forceinline__ int2 take(int* tickets, int chains, int each, int tiles) {        // (chain, number of its tile)
   const int own = __builtin_amdgcn_s_getreg(20 | 3 << 11) & (kQueues - 1);
-  for (int k = 0; k < 2 * kQueues; ++k) {
+  for (int k = 0; k < kQueues; ++k) {
     const int q = (own + k) & (kQueues - 1), first = q * each, n = chains - first < each ? chains - first : each;
     if (n < 1) continue;
     const int t = __hip_atomic_fetch_add(tickets + q * kTicketStride, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -246,8 +246,8 @@ __device__ __forceinline__ int2 take(int* tickets, int chains, int each, int til
 }
 
 // Chains of a queue.  Columns of one die alone fall into few of its L2's channels where rows lie a power of two apart, so few chains
-// are one queue, whose tiles are neighbours in memory: T = 30000, B = 1, D = 2048 bf16, 16 chains: 146 us, 155 in eight queues;
-// T = 1000, B = 16, D = 330 fp32, 96 chains: 26 us and 20.
+// are one queue, whose tiles are neighbours in memory: T = 30000, B = 1 bf16, D = 2048 and 4096 (16 and 32 chains): 131 and 235 us,
+// 141 and 249 in eight queues; T = 512, D = 4096, 64 chains: 18 and 17; T = 1000, B = 16, D = 330 fp32, 96 chains: 30 and 23.
 static inline int chains_of_queue(int chains) { return chains >= 64 ? bppsa_ceil_div(chains, kQueues) : chains; }
 
 // Empties the words of a call and its tickets, which lie in front of them.

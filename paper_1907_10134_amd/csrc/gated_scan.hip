@@ -5,9 +5,9 @@ namespace {
 
 using namespace gated;
 
-// A workgroup takes tiles of kTile steps of 64 V channels, one after the other.  Each wave has a run of the steps in registers:
-// it turns them into decays and what enters, finds what its run does to a state, and when the state before it is known walks
-// them again.  Outputs of a tile are on their way while the next one's inputs are asked for.
+// A workgroup takes a tile of 8 R steps of 64 V channels.  Each wave has a run of the steps in registers: it turns them into decays
+// and what enters, finds what its run does to a state, and when the state before it is known walks them again.  The gate is asked for
+// while the tile waits for that state.
 template <typename E, int V, int R, bool GATE, bool JOINED>
 __global__ void __launch_bounds__(kWaves * 64, sizeof(E) == 4 ? 6 : 4)
 gated_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, int* tickets, uint64_t* words, int tiles, int each) {
@@ -22,108 +22,106 @@ gated_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __r
     chain = __builtin_amdgcn_readfirstlane(taken.x), tile = __builtin_amdgcn_readfirstlane(taken.y);
     if (chain < 0) return;
   }
-  {
-    const int column = chain % l.columns, b = chain / l.columns;
-    const Own<V> own(column, lane, l.D);
-    const int d = own.d, len = clamp_length(l.lengths, b, l.T), t0 = tile * kWaves * R, first = t0 + w * R;
-    // behind an end
-    if (own.on)
-      for (int t = first > len ? first : len; t < first + R && t < l.T; ++t) {
-        const float zero[V] = {};
-        store_some<E, V>(y.at(t, b) + d, zero);
-      }
-    if (len == 0 && tile == 0 && w == 0 && h_last && own.on)
-      for (int c = 0; c < V; ++c) h_last[(int64_t)b * l.D + d + c] = l.h0 ? l.h0[(int64_t)b * l.D + d + c] : 0.0f;
+  const int column = chain % l.columns, b = chain / l.columns;
+  const Own<V> own(column, lane, l.D);
+  const int d = own.d, len = clamp_length(l.lengths, b, l.T), t0 = tile * kWaves * R, first = t0 + w * R;
+  // behind an end
+  if (own.on)
+    for (int t = first > len ? first : len; t < first + R && t < l.T; ++t) {
+      const float zero[V] = {};
+      store_some<E, V>(y.at(t, b) + d, zero);
+    }
+  if (len == 0 && tile == 0 && w == 0 && h_last && own.on)
+    for (int c = 0; c < V; ++c) h_last[(int64_t)b * l.D + d + c] = l.h0 ? l.h0[(int64_t)b * l.D + d + c] : 0.0f;
 
-    float a[R][V], e[R][V];
-    const int rows = len - first < R ? len - first : R;
-    const uint32_t byte = (uint32_t)d * sizeof(E);
-    // a run with an end in it is another copy of the code: with its conditions in this one there are too few scalar registers
-    auto gather = [&](auto all) __attribute__((always_inline)) {
-      constexpr bool WHOLE = all.value;
-      Channel<E> channel[V];
-      channels_of(l, d, channel);
-      uint32_t x[R], r[R], i[R];
-      load_rows<WHOLE, R, V>(l.r, first, b, rows, byte, r), load_rows<WHOLE, R, V>(l.i, first, b, rows, byte, i), load_rows<WHOLE, R, V>(l.x, first, b, rows, byte, x);
-      float product[V], end[V];
+  float a[R][V], e[R][V];
+  const int rows = len - first < R ? len - first : R;
+  const uint32_t byte = (uint32_t)d * sizeof(E);
+  // a run with an end in it is another copy of the code: with its conditions in this one there are too few scalar registers
+  auto gather = [&](auto all) __attribute__((always_inline)) {
+    constexpr bool WHOLE = all.value;
+    Channel<E> channel[V];
+    channels_of(l, d, channel);
+    uint32_t x[R], r[R], i[R];
+    load_rows<WHOLE, R, V>(l.r, first, b, rows, byte, r), load_rows<WHOLE, R, V>(l.i, first, b, rows, byte, i), load_rows<WHOLE, R, V>(l.x, first, b, rows, byte, x);
+    float product[V], end[V];
 #pragma unroll
-      for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = 0.0f;
+    for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < R; ++j) {
-        apart(j);
+    for (int j = 0; j < R; ++j) {
+      apart(j);
 #pragma unroll
-        for (int c = 0; c < V; ++c) {
-          const float rho = channel[c].rho(part<E>(r[j], c)), iota = channel[c].iota(part<E>(i[j], c));
-          a[j][c] = channel[c].a(rho), e[j][c] = __builtin_amdgcn_sqrtf(channel[c].m2(a[j][c], rho)) * iota * part<E>(x[j], c);
-          if (!WHOLE && j >= rows) a[j][c] = 1.0f, e[j][c] = 0.0f;
-          product[c] *= a[j][c], end[c] = fmaf(a[j][c], end[c], e[j][c]);
-        }
+      for (int c = 0; c < V; ++c) {
+        const float rho = channel[c].rho(part<E>(r[j], c)), iota = channel[c].iota(part<E>(i[j], c));
+        a[j][c] = channel[c].a(rho), e[j][c] = __builtin_amdgcn_sqrtf(channel[c].m2(a[j][c], rho)) * iota * part<E>(x[j], c);
+        if (!WHOLE && j >= rows) a[j][c] = 1.0f, e[j][c] = 0.0f;
+        product[c] *= a[j][c], end[c] = fmaf(a[j][c], end[c], e[j][c]);
       }
-#pragma unroll
-      for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float2(product[c], end[c]);
-    };
-    if (rows == R) gather(std::true_type{});
-    else if (rows > 0) gather(std::false_type{});
-    else
-#pragma unroll
-      for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float2(1.0f, 0.0f);
-    lds_barrier();
-    uint32_t z[R];                // asked for now and used when the tile is joined
-    if (GATE && rows == R) load_rows<true, R, V>(l.z, first, b, rows, byte, z);
-    else if (GATE && rows > 0) load_rows<false, R, V>(l.z, first, b, rows, byte, z);
-    if (w < V && t0 < len) {                   // the tile's own share, a channel a lane
-      const uint32_t at = w * 64 + lane;
-      float p = 1.0f, s = 0.0f, in = 0.0f;
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) {
-        const float2 run = runs[k][at];
-        p *= run.x, s = fmaf(run.x, s, run.y);
-      }
-      if (tile == 0 && l.h0) {
-        const int channel = channel_of<V>(column, at, l.D);
-        if (channel < l.D) in = l.h0[(int64_t)b * l.D + channel];
-      }
-      if (JOINED) {
-        const int64_t step = (int64_t)l.B * l.columns * 64 * V;
-        uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V;
-        if (tile) leave(mine + at, word_of(p, s)), in = look_back(mine, at, step, tile);
-        leave(mine + at, settled(through(word_of(p, s), in)));
-      }
-      before[at] = in;
     }
-    lds_barrier();
-    if (rows > 0 && own.on) {
-      if (GATE)
 #pragma unroll
-        for (int j = 0; j < R; ++j) as_loaded(z[j]);
-      float h[V];
+    for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float2(product[c], end[c]);
+  };
+  if (rows == R) gather(std::true_type{});
+  else if (rows > 0) gather(std::false_type{});
+  else
 #pragma unroll
-      for (int c = 0; c < V; ++c) h[c] = before[lane * V + c];
-      for (int k = 0; k < w; ++k)
+    for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float2(1.0f, 0.0f);
+  lds_barrier();
+  uint32_t z[R];                // asked for now and used when the tile is joined
+  if (GATE && rows == R) load_rows<true, R, V>(l.z, first, b, rows, byte, z);
+  else if (GATE && rows > 0) load_rows<false, R, V>(l.z, first, b, rows, byte, z);
+  if (w < V && t0 < len) {                   // the tile's own share, a channel a lane
+    const uint32_t at = w * 64 + lane;
+    float p = 1.0f, s = 0.0f, in = 0.0f;
 #pragma unroll
-        for (int c = 0; c < V; ++c) {
-          const float2 run = runs[k][lane * V + c];
-          h[c] = fmaf(run.x, h[c], run.y);
-        }
-      if (states && first % kKept == 0)
-#pragma unroll
-        for (int c = 0; c < V; ++c) states[((int64_t)(first / kKept) * l.B + b) * l.D + d + c] = h[c];
-      Run<E> to(y, first, b);
-#pragma unroll
-      for (int j = 0; j < R; ++j) {
-        float out[V];
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-          h[c] = fmaf(a[j][c], h[c], e[j][c]);
-          out[c] = GATE ? h[c] * (part<E>(z[j], c) * sigmoid<E>(part<E>(z[j], c))) : h[c];
-        }
-        if (j < rows) to.store(byte, out);
-        to.move();
-      }
-      if (h_last && len <= first + R)
-#pragma unroll
-        for (int c = 0; c < V; ++c) h_last[(int64_t)b * l.D + d + c] = h[c];
+    for (int k = 0; k < kWaves; ++k) {
+      const float2 run = runs[k][at];
+      p *= run.x, s = fmaf(run.x, s, run.y);
     }
+    if (tile == 0 && l.h0) {
+      const int channel = channel_of<V>(column, at, l.D);
+      if (channel < l.D) in = l.h0[(int64_t)b * l.D + channel];
+    }
+    if (JOINED) {
+      const int64_t step = (int64_t)l.B * l.columns * 64 * V;
+      uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V;
+      if (tile) leave(mine + at, word_of(p, s)), in = look_back(mine, at, step, tile);
+      leave(mine + at, settled(through(word_of(p, s), in)));
+    }
+    before[at] = in;
+  }
+  lds_barrier();
+  if (rows > 0 && own.on) {
+    if (GATE)
+#pragma unroll
+      for (int j = 0; j < R; ++j) as_loaded(z[j]);
+    float h[V];
+#pragma unroll
+    for (int c = 0; c < V; ++c) h[c] = before[lane * V + c];
+    for (int k = 0; k < w; ++k)
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        const float2 run = runs[k][lane * V + c];
+        h[c] = fmaf(run.x, h[c], run.y);
+      }
+    if (states && first % kKept == 0)
+#pragma unroll
+      for (int c = 0; c < V; ++c) states[((int64_t)(first / kKept) * l.B + b) * l.D + d + c] = h[c];
+    Run<E> to(y, first, b);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      float out[V];
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        h[c] = fmaf(a[j][c], h[c], e[j][c]);
+        out[c] = GATE ? h[c] * (part<E>(z[j], c) * sigmoid<E>(part<E>(z[j], c))) : h[c];
+      }
+      if (j < rows) to.store(byte, out);
+      to.move();
+    }
+    if (h_last && len <= first + R)
+#pragma unroll
+      for (int c = 0; c < V; ++c) h_last[(int64_t)b * l.D + d + c] = h[c];
   }
 }
 

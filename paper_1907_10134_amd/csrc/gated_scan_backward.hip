@@ -36,159 +36,157 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
     chain = __builtin_amdgcn_readfirstlane(taken.x), tile = tiles - 1 - __builtin_amdgcn_readfirstlane(taken.y);
     if (chain < 0) return;
   }
-  {
-    const int column = chain % l.columns, b = chain / l.columns;
-    const Own<V> own(column, lane, l.D);
-    const int d = own.d, len = clamp_length(l.lengths, b, l.T), t0 = tile * kKept, first = t0 + w * R;
-    const int last_tile = (len + kKept - 1) / kKept - 1;
-    // behind an end
-    if (own.on)
-      for (int t = first > len ? first : len; t < first + R && t < l.T; ++t) {
-        const float zero[V] = {};
-        store_some<E, V>(o.dx.at(t, b) + d, zero), store_some<E, V>(o.dr.at(t, b) + d, zero), store_some<E, V>(o.di.at(t, b) + d, zero);
-        if (GATE) store_some<E, V>(o.dz.at(t, b) + d, zero);
-      }
-    if (len == 0 && tile == 0 && w == 0 && o.dh0 && own.on)
-      for (int c = 0; c < V; ++c) o.dh0[(int64_t)b * l.D + d + c] = dh_last ? dh_last[(int64_t)b * l.D + d + c] : 0.0f;
-
-    uint32_t x[R], go[R], z[R];
-    float a[R][V], e[R][V], rho[R][V], iota[R][V], sum[3][V] = {};
-    const int rows = len - first < R ? len - first : R;
-    const uint32_t byte = (uint32_t)d * sizeof(E);
-    Channel<E> channel[V];
-    if (rows > 0) channels_of(l, d, channel);
-    auto gather = [&](auto all) __attribute__((always_inline)) {
-      constexpr bool WHOLE = all.value;
-      uint32_t r[R], i[R];
-      load_rows<WHOLE, R, V>(l.r, first, b, rows, byte, r), load_rows<WHOLE, R, V>(l.i, first, b, rows, byte, i), load_rows<WHOLE, R, V>(l.x, first, b, rows, byte, x);
-      load_rows<WHOLE, R, V>(dy, first, b, rows, byte, go);
-      if (GATE) load_rows<WHOLE, R, V>(l.z, first, b, rows, byte, z);
-      float product[V], end[V], back[V];
-#pragma unroll
-      for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = back[c] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < R; ++j) {
-        apart(j);
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-          rho[j][c] = channel[c].rho(part<E>(r[j], c)), iota[j][c] = channel[c].iota(part<E>(i[j], c));
-          a[j][c] = channel[c].a(rho[j][c]);
-          e[j][c] = __builtin_amdgcn_sqrtf(channel[c].m2(a[j][c], rho[j][c])) * iota[j][c] * part<E>(x[j], c);
-          float q = part<E>(go[j], c);
-          if (GATE) q *= part<E>(z[j], c) * sigmoid<E>(part<E>(z[j], c));
-          if (!WHOLE && j >= rows) a[j][c] = 1.0f, e[j][c] = q = 0.0f;
-          product[c] *= a[j][c], end[c] = fmaf(a[j][c], end[c], e[j][c]), back[c] = fmaf(product[c], q, back[c]);
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float4(product[c], end[c], back[c], 0.0f);
-    };
-    if (rows == R) gather(std::true_type{});
-    else if (rows > 0) gather(std::false_type{});
-    else
-#pragma unroll
-      for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float4(1.0f, 0.0f, 0.0f, 0.0f);
-    lds_barrier();
-    if (w < V && t0 < len) {                   // the tile's own share, a channel a lane
-      const uint32_t at = w * 64 + lane;
-      float p = 1.0f, s = 0.0f, in = 0.0f;
-#pragma unroll
-      for (int k = kWaves - 1; k >= 0; --k) {
-        const float4 run = runs[k][at];
-        p *= run.x, s = fmaf(run.x, s, run.z);
-      }
-      const int channel = channel_of<V>(column, at, l.D);
-      const bool on = channel < l.D;
-      if (tile == last_tile && dh_last && on) in = dh_last[(int64_t)b * l.D + channel];
-      if (JOINED) {
-        const int64_t step = (int64_t)l.B * l.columns * 64 * V;
-        uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V;
-        if (tile < last_tile) leave(mine + at, word_of(p, s)), in = look_back(mine, at, -step, last_tile - tile);
-        leave(mine + at, settled(through(word_of(p, s), in)));
-      }
-      border[at] = make_float2(on ? states[((int64_t)tile * l.B + b) * l.D + channel] : 0.0f, in);
+  const int column = chain % l.columns, b = chain / l.columns;
+  const Own<V> own(column, lane, l.D);
+  const int d = own.d, len = clamp_length(l.lengths, b, l.T), t0 = tile * kKept, first = t0 + w * R;
+  const int last_tile = (len + kKept - 1) / kKept - 1;
+  // behind an end
+  if (own.on)
+    for (int t = first > len ? first : len; t < first + R && t < l.T; ++t) {
+      const float zero[V] = {};
+      store_some<E, V>(o.dx.at(t, b) + d, zero), store_some<E, V>(o.dr.at(t, b) + d, zero), store_some<E, V>(o.di.at(t, b) + d, zero);
+      if (GATE) store_some<E, V>(o.dz.at(t, b) + d, zero);
     }
-    lds_barrier();
-    if (rows > 0 && own.on) {
-      float h[V], g[V];
+  if (len == 0 && tile == 0 && w == 0 && o.dh0 && own.on)
+    for (int c = 0; c < V; ++c) o.dh0[(int64_t)b * l.D + d + c] = dh_last ? dh_last[(int64_t)b * l.D + d + c] : 0.0f;
+
+  uint32_t x[R], go[R], z[R];
+  float a[R][V], e[R][V], rho[R][V], iota[R][V], sum[3][V] = {};
+  const int rows = len - first < R ? len - first : R;
+  const uint32_t byte = (uint32_t)d * sizeof(E);
+  Channel<E> channel[V];
+  if (rows > 0) channels_of(l, d, channel);
+  auto gather = [&](auto all) __attribute__((always_inline)) {
+    constexpr bool WHOLE = all.value;
+    uint32_t r[R], i[R];
+    load_rows<WHOLE, R, V>(l.r, first, b, rows, byte, r), load_rows<WHOLE, R, V>(l.i, first, b, rows, byte, i), load_rows<WHOLE, R, V>(l.x, first, b, rows, byte, x);
+    load_rows<WHOLE, R, V>(dy, first, b, rows, byte, go);
+    if (GATE) load_rows<WHOLE, R, V>(l.z, first, b, rows, byte, z);
+    float product[V], end[V], back[V];
+#pragma unroll
+    for (int c = 0; c < V; ++c) product[c] = 1.0f, end[c] = back[c] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      apart(j);
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        const float2 both = border[lane * V + c];
-        h[c] = both.x, g[c] = both.y;
+        rho[j][c] = channel[c].rho(part<E>(r[j], c)), iota[j][c] = channel[c].iota(part<E>(i[j], c));
+        a[j][c] = channel[c].a(rho[j][c]);
+        e[j][c] = __builtin_amdgcn_sqrtf(channel[c].m2(a[j][c], rho[j][c])) * iota[j][c] * part<E>(x[j], c);
+        float q = part<E>(go[j], c);
+        if (GATE) q *= part<E>(z[j], c) * sigmoid<E>(part<E>(z[j], c));
+        if (!WHOLE && j >= rows) a[j][c] = 1.0f, e[j][c] = q = 0.0f;
+        product[c] *= a[j][c], end[c] = fmaf(a[j][c], end[c], e[j][c]), back[c] = fmaf(product[c], q, back[c]);
       }
-      for (int k = 0; k < w; ++k)
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-          const float4 run = runs[k][lane * V + c];
-          h[c] = fmaf(run.x, h[c], run.y);
-        }
-      for (int k = kWaves - 1; k > w; --k)
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-          const float4 run = runs[k][lane * V + c];
-          g[c] = fmaf(run.x, g[c], run.z);
-        }
-      // the states before each step, in the place of what enters
-#pragma unroll
-      for (int j = 0; j < R; ++j)
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-          const float before = h[c];
-          h[c] = fmaf(a[j][c], h[c], e[j][c]);
-          e[j][c] = before;
-        }
-#pragma unroll
-      for (int j = 0; j < R; ++j) {
-        as_loaded(x[j]), as_loaded(go[j]);
-        if (GATE) as_loaded(z[j]);
-      }
-      Run<E> to_x(o.dx, first, b), to_r(o.dr, first, b), to_i(o.di, first, b), to_z(GATE ? o.dz : o.dx, first, b);
-      const int64_t last = rows - 1;
-      to_x.move_by(last * to_x.step), to_r.move_by(last * to_r.step), to_i.move_by(last * to_i.step);
-      if (GATE) to_z.move_by(last * to_z.step);
-#pragma unroll
-      for (int j = R - 1; j >= 0; --j) {
-        apart(j + 1);
-        float dx[V], dr[V], di[V], dz[V];
-        if (j >= rows) continue;
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-          const float of_x = part<E>(x[j], c), m2 = channel[c].m2(a[j][c], rho[j][c]), root = m2 > 0x1p-120f ? __builtin_amdgcn_rsqf(m2) : 0.0f, m = m2 * root;
-          float q = part<E>(go[j], c);
-          if (GATE) {
-            const float of_z = part<E>(z[j], c), sg = sigmoid<E>(of_z), q_sg = q * sg;
-            dz[c] = q_sg * h[c] * fmaf(of_z, 1.0f - sg, 1.0f);
-            q = q_sg * of_z;
-          }
-          const float gh = q + g[c];
-          g[c] = a[j][c] * gh;
-          const float s = g[c] * rho[j][c] * fmaf(a[j][c] * iota[j][c] * of_x, root, -e[j][c]);
-          dx[c] = gh * m * iota[j][c];
-          di[c] = dx[c] * fmaf(-of_x, iota[j][c], of_x);
-          dr[c] = channel[c].decay * fmaf(-rho[j][c], s, s);
-          h[c] = e[j][c];
-          sum[0][c] += s, sum[1][c] += dr[c], sum[2][c] += di[c];
-        }
-        to_x.store(byte, dx), to_r.store(byte, dr), to_i.store(byte, di);
-        to_x.move_by(-to_x.step), to_r.move_by(-to_r.step), to_i.move_by(-to_i.step);
-        if (GATE) to_z.store(byte, dz), to_z.move_by(-to_z.step);
-      }
-      if (o.dh0 && first == 0)
-#pragma unroll
-        for (int c = 0; c < V; ++c) o.dh0[(int64_t)b * l.D + d + c] = g[c];
     }
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
+    for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float4(product[c], end[c], back[c], 0.0f);
+  };
+  if (rows == R) gather(std::true_type{});
+  else if (rows > 0) gather(std::false_type{});
+  else
 #pragma unroll
-      for (int c = 0; c < V; ++c) sums[k][w][lane * V + c] = sum[k][c];
-    lds_barrier();
-    for (int at = threadIdx.x; at < 3 * 64 * V; at += kWaves * 64) {
-      const int k = at / (64 * V), place = at % (64 * V), channel = channel_of<V>(column, place, l.D);
-      float all = 0.0f;
+    for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float4(1.0f, 0.0f, 0.0f, 0.0f);
+  lds_barrier();
+  if (w < V && t0 < len) {                   // the tile's own share, a channel a lane
+    const uint32_t at = w * 64 + lane;
+    float p = 1.0f, s = 0.0f, in = 0.0f;
 #pragma unroll
-      for (int n = 0; n < kWaves; ++n) all += sums[k][n][place];
-      if (channel < l.D) o.parts[(((int64_t)tile * l.B + b) * 3 + k) * l.D + channel] = all;
+    for (int k = kWaves - 1; k >= 0; --k) {
+      const float4 run = runs[k][at];
+      p *= run.x, s = fmaf(run.x, s, run.z);
     }
+    const int channel = channel_of<V>(column, at, l.D);
+    const bool on = channel < l.D;
+    if (tile == last_tile && dh_last && on) in = dh_last[(int64_t)b * l.D + channel];
+    if (JOINED) {
+      const int64_t step = (int64_t)l.B * l.columns * 64 * V;
+      uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V;
+      if (tile < last_tile) leave(mine + at, word_of(p, s)), in = look_back(mine, at, -step, last_tile - tile);
+      leave(mine + at, settled(through(word_of(p, s), in)));
+    }
+    border[at] = make_float2(on ? states[((int64_t)tile * l.B + b) * l.D + channel] : 0.0f, in);
+  }
+  lds_barrier();
+  if (rows > 0 && own.on) {
+    float h[V], g[V];
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      const float2 both = border[lane * V + c];
+      h[c] = both.x, g[c] = both.y;
+    }
+    for (int k = 0; k < w; ++k)
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        const float4 run = runs[k][lane * V + c];
+        h[c] = fmaf(run.x, h[c], run.y);
+      }
+    for (int k = kWaves - 1; k > w; --k)
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        const float4 run = runs[k][lane * V + c];
+        g[c] = fmaf(run.x, g[c], run.z);
+      }
+    // the states before each step, in the place of what enters
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        const float before = h[c];
+        h[c] = fmaf(a[j][c], h[c], e[j][c]);
+        e[j][c] = before;
+      }
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      as_loaded(x[j]), as_loaded(go[j]);
+      if (GATE) as_loaded(z[j]);
+    }
+    Run<E> to_x(o.dx, first, b), to_r(o.dr, first, b), to_i(o.di, first, b), to_z(GATE ? o.dz : o.dx, first, b);
+    const int64_t last = rows - 1;
+    to_x.move_by(last * to_x.step), to_r.move_by(last * to_r.step), to_i.move_by(last * to_i.step);
+    if (GATE) to_z.move_by(last * to_z.step);
+#pragma unroll
+    for (int j = R - 1; j >= 0; --j) {
+      apart(j + 1);
+      float dx[V], dr[V], di[V], dz[V];
+      if (j >= rows) continue;
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        const float of_x = part<E>(x[j], c), m2 = channel[c].m2(a[j][c], rho[j][c]), root = m2 > 0x1p-120f ? __builtin_amdgcn_rsqf(m2) : 0.0f, m = m2 * root;
+        float q = part<E>(go[j], c);
+        if (GATE) {
+          const float of_z = part<E>(z[j], c), sg = sigmoid<E>(of_z), q_sg = q * sg;
+          dz[c] = q_sg * h[c] * fmaf(of_z, 1.0f - sg, 1.0f);
+          q = q_sg * of_z;
+        }
+        const float gh = q + g[c];
+        g[c] = a[j][c] * gh;
+        const float s = g[c] * rho[j][c] * fmaf(a[j][c] * iota[j][c] * of_x, root, -e[j][c]);
+        dx[c] = gh * m * iota[j][c];
+        di[c] = dx[c] * fmaf(-of_x, iota[j][c], of_x);
+        dr[c] = channel[c].decay * fmaf(-rho[j][c], s, s);
+        h[c] = e[j][c];
+        sum[0][c] += s, sum[1][c] += dr[c], sum[2][c] += di[c];
+      }
+      to_x.store(byte, dx), to_r.store(byte, dr), to_i.store(byte, di);
+      to_x.move_by(-to_x.step), to_r.move_by(-to_r.step), to_i.move_by(-to_i.step);
+      if (GATE) to_z.store(byte, dz), to_z.move_by(-to_z.step);
+    }
+    if (o.dh0 && first == 0)
+#pragma unroll
+      for (int c = 0; c < V; ++c) o.dh0[(int64_t)b * l.D + d + c] = g[c];
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int c = 0; c < V; ++c) sums[k][w][lane * V + c] = sum[k][c];
+  lds_barrier();
+  for (int at = threadIdx.x; at < 3 * 64 * V; at += kWaves * 64) {
+    const int k = at / (64 * V), place = at % (64 * V), channel = channel_of<V>(column, place, l.D);
+    float all = 0.0f;
+#pragma unroll
+    for (int n = 0; n < kWaves; ++n) all += sums[k][n][place];
+    if (channel < l.D) o.parts[(((int64_t)tile * l.B + b) * 3 + k) * l.D + channel] = all;
   }
 }
 
