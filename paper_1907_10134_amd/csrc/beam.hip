@@ -190,14 +190,15 @@ beam_join_kernel(const Beams<E> s, const Pieces in, const Choice out) {
     const int row = blockIdx.x * W + w;
     const float score = s.scores[row];
     double norm = NAN;
+    // what the pieces left is asked for together with what tells whether they left anything
+    const int64_t at = (int64_t)row * in.count;
+    const float largest = lane < in.count ? in.largest[at + lane] : -INFINITY;
+    const double sum = lane < in.count ? in.sum[at + lane] : 0.0;
+    for (int k = lane; k < in.count * W; k += 64) list[k] = in.key[at * W + k];
     if (alive(s, row)) {
-      const int64_t at = (int64_t)row * in.count;
-      const float largest = lane < in.count ? in.largest[at + lane] : -INFINITY;
-      const double sum = lane < in.count ? in.sum[at + lane] : 0.0;
       const float m = lanes::largest(sum > 0.0 ? largest : -INFINITY);
       const double all = lanes::sum(sum == 0.0 ? 0.0 : sum * exp((double)largest - (double)m));
       norm = (double)m + log(all);
-      for (int k = lane; k < in.count * W; k += 64) list[k] = in.key[at * W + k];
     }
     if (!(fabs(norm) < INFINITY)) {            // only a finished beam's end counts; of equal candidates the first tokens
       const bool ends = s.finished && s.finished[row] && fabsf(score) < INFINITY;
@@ -212,34 +213,46 @@ beam_join_kernel(const Beams<E> s, const Pieces in, const Choice out) {
       }
       continue;
     }
-    // a lane has the first of a piece's list that is not yet taken
+    // a lane has the first of a piece's list that is not yet taken; of equal values the first piece has the lower tokens
     int next = 0;
     __builtin_amdgcn_wave_barrier();
+    uint64_t mine = lane < in.count ? list[lane * W] : 0;
     for (int i = 0; i < W; ++i) {
-      const uint64_t mine = lane < in.count && next < W ? list[lane * W + next] : 0;
-      const uint64_t best = lanes::largest(mine);
-      if (mine == best) ++next;
-      if (lane == 0) {
-        const double v = (double)score + ((double)value_of(best) - norm);
-        total[w][i] = v, token[w][i] = best ? place_of(best) : -1;
-      }
+      const uint32_t value = (uint32_t)(mine >> 32);
+      if (lane != __builtin_ctzll(__ballot(value == lanes::largest(value)))) continue;
+      total[w][i] = (double)score + ((double)value_of(mine) - norm), token[w][i] = mine ? place_of(mine) : -1;
+      mine = ++next < W ? list[lane * W + next] : 0;
     }
   }
   __syncthreads();
   if (wave) return;
-  int next = 0, parent = -1;
+  const bool was_finished = s.finished && lane < W && s.finished[blockIdx.x * W + lane];
+  int next = 0, parent = -1, t;
+  double v;
+  uint64_t mine;
+  auto head = [&]() {
+    t = lane < W && next < W ? token[lane][next] : -1;
+    if (t >= 0) v = total[lane][next];
+    mine = t >= 0 ? order_of(v) : 0;
+  };
+  head();
   for (int i = 0; i < W; ++i) {
-    const bool any = lane < W && next < W && token[lane][next] >= 0;
-    const double v = any ? total[lane][next] : 0.0;
-    const uint64_t mine = any ? order_of(v) : 0;
-    const int who = __builtin_ctzll(__ballot(mine == lanes::largest(mine)));         // the lowest beam of equal ones
-    if (lane == who) {
-      const int at = blockIdx.x * W + i, t = token[lane][next];
-      out.scores[at] = (float)v, out.parents[at] = lane, out.tokens[at] = t;
-      if (out.finished) out.finished[at] = (s.finished && s.finished[blockIdx.x * W + lane]) || t == s.end;
-      ++next;
+    // by the upper half; the lower one tells equal ones apart, and of those that are equal in both the lowest beam is first
+    const uint32_t upper = (uint32_t)(mine >> 32);
+    bool best = upper == lanes::largest(upper);
+    uint64_t who = __ballot(best);
+    if (who & (who - 1)) {
+      const uint32_t lower = best ? (uint32_t)mine : 0;
+      best = best && lower == lanes::largest(lower);
+      who = __ballot(best);
     }
-    if (lane == i) parent = who;
+    const int first = __builtin_ctzll(who);
+    if (lane == i) parent = first;
+    if (lane != first) continue;
+    const int at = blockIdx.x * W + i;
+    out.scores[at] = (float)v, out.parents[at] = lane, out.tokens[at] = t;
+    if (out.finished) out.finished[at] = was_finished || t == s.end;
+    ++next, head();
   }
   if (!s.slots) return;
   // the first child of a beam goes on in its slot, the others take those of beams without one, in order

@@ -95,10 +95,13 @@ class BeamStates:
         self._n_pieces = int(_lib.bppsa_beam_pieces(len(sizes), n, None))
         if self._n_pieces < 1:
             raise ValueError("BeamStates: a slot's states are too large")
-        pieces = torch.empty((self._n_pieces, 2), dtype=_i32)
-        _lib.bppsa_beam_pieces(len(sizes), n, pieces.data_ptr())
-        self._pieces = pieces.to(first.device)
-        self._table = torch.frombuffer(bytearray(b"".join(rows)), dtype=torch.uint8).to(first.device)
+        # the table of tensors and the list of pieces behind it, in one copy
+        both = torch.empty(16 * len(rows) + 8 * self._n_pieces, dtype=torch.uint8)
+        ctypes.memmove(both.data_ptr(), b"".join(rows), 16 * len(rows))
+        _lib.bppsa_beam_pieces(len(sizes), n, both.data_ptr() + 16 * len(rows))
+        self._lists = both.to(first.device)
+        self._table = self._lists.data_ptr()
+        self._pieces = self._table + 16 * len(rows)
 
     def move(self, sources, slots, stream=None):
         """bppsa_beam_move: copies the states of slot sources[...] to slot slots[...], int32 of the same shape; a source of -1 is
@@ -114,5 +117,5 @@ class BeamStates:
         if sources is None:
             raise TypeError("sources must be a torch.Tensor")
         to, of = _whole(slots, _i32, "slots", self._device), _param(sources, slots.shape, "sources", self._device, _i32)
-        _check(_lib.bppsa_beam_move(self._table.data_ptr(), self._n_pieces, self._pieces.data_ptr(), slots.numel(), of, to, self.slots,
+        _check(_lib.bppsa_beam_move(self._table, self._n_pieces, self._pieces, slots.numel(), of, to, self.slots,
                                     _here(self._device)), "bppsa_beam_move")
