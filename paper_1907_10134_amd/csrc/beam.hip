@@ -58,6 +58,9 @@ __device__ __forceinline__ bool alive(const Beams<E>& s, int row) {
 // One workgroup a piece of a row, whose values stay in registers.  A bound that W of 64 columns of the piece pass, by their
 // largest values, is no larger than the W-th largest value; so few values pass it (some 10 of 8192 normal ones at W = 8) that each
 // can count those in front of it.  Where more than kFound do, equal ones that is, they are taken one after the other.
+//
+// 512 rows of 131072 bf16, W = 8: 38 us, 3.5 TB/s, about 26 of them the read itself, 6 the bound and the values behind it, 5 the
+// exponentials.  The next piece's read beside that, two pieces a workgroup in registers, has fewer waves: 66 us a call instead of 46.
 template <typename E>
 __global__ void __launch_bounds__(kThreads, 8)
 beam_piece_kernel(const Beams<E> s, const Pieces out) {
@@ -172,7 +175,8 @@ beam_piece_kernel(const Beams<E> s, const Pieces out) {
   }
 }
 
-// One workgroup a sequence: a wave merges the pieces' lists of a beam, then the first one the beams' lists.
+// One workgroup a sequence: a wave merges the pieces' lists of a beam, then the first one the beams' lists.  Bound by the chain of what it
+// waits for (W = 8, 16 pieces: 8 us; by comparisons of 32 bits, 64 where those are equal: B = 16, W = 32 74 us a call, 85 by 64 at once).
 struct Choice {
   float* scores;
   int32_t *parents, *tokens, *slots, *sources;
@@ -291,7 +295,7 @@ static inline bool beam_sizes_ok(int B, int W, int V) {
          (int64_t)B * W * bppsa_ceil_div(V, kPiece) < 1 << 24;
 }
 
-// A workgroup takes a piece of a tensor's slots for every so many rows.
+// A workgroup takes a piece of a tensor's slots for every so many rows.  Bound by memory: 147 MB read and written in 48 us, 6.1 TB/s.
 template <typename U>
 __device__ __forceinline__ void copy_bytes(char* to, const char* from, int n) {
   for (int k = threadIdx.x; k < n / (int)sizeof(U); k += kThreads) reinterpret_cast<U*>(to)[k] = reinterpret_cast<const U*>(from)[k];
