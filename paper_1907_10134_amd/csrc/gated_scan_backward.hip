@@ -28,7 +28,9 @@ __global__ void __launch_bounds__(kWaves * 64, sizeof(E) == 4 && !GATE ? 6 : 4)
 gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ dh_last, const float* __restrict__ states,
                       const Grads<E> o, int* tickets, uint64_t* words, int tiles, int each) {
   constexpr int R = kRunBack;
-  __shared__ float4 runs[kWaves][64 * V];             // product of the decays, state from zero, gradient from zero
+  // product of the decays, state from zero, gradient from zero; a lane's channels 64 apart, so that a wave's accesses lie side by side (T =
+  // 4096, B = 4, D = 4096 bf16 without a gate, both passes: 321 us, 335 with them next to each other)
+  __shared__ float4 runs[kWaves][64 * V];
   __shared__ float2 border[64 * V];                   // the state before the tile, the gradient behind it
   __shared__ float sums[3][kWaves][64 * V];
   __shared__ int2 taken;
@@ -84,13 +86,13 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
       }
     }
 #pragma unroll
-    for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float4(product[c], end[c], back[c], 0.0f);
+    for (int c = 0; c < V; ++c) runs[w][c * 64 + lane] = make_float4(product[c], end[c], back[c], 0.0f);
   };
   if (rows == R) gather(std::true_type{});
   else if (rows > 0) gather(std::false_type{});
   else
 #pragma unroll
-    for (int c = 0; c < V; ++c) runs[w][lane * V + c] = make_float4(1.0f, 0.0f, 0.0f, 0.0f);
+    for (int c = 0; c < V; ++c) runs[w][c * 64 + lane] = make_float4(1.0f, 0.0f, 0.0f, 0.0f);
   lds_barrier();
   if (w < V && t0 < len) {                   // the tile's own share, a channel a lane
     const uint32_t at = w * 64 + lane;
@@ -100,8 +102,8 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
       const float4 run = runs[k][at];
       p *= run.x, s = fmaf(run.x, s, run.z);
     }
-    const int channel = channel_of<V>(column, at, l.D);
-    const bool on = channel < l.D;
+    const int channel = d + w;
+    const bool on = own.on;
     if (tile == last_tile && dh_last && on) in = dh_last[(int64_t)b * l.D + channel];
     if (JOINED) {
       const int64_t step = (int64_t)l.B * l.columns * 64 * V;
@@ -116,19 +118,19 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
     float h[V], g[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      const float2 both = border[lane * V + c];
+      const float2 both = border[c * 64 + lane];
       h[c] = both.x, g[c] = both.y;
     }
     for (int k = 0; k < w; ++k)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        const float4 run = runs[k][lane * V + c];
+        const float4 run = runs[k][c * 64 + lane];
         h[c] = fmaf(run.x, h[c], run.y);
       }
     for (int k = kWaves - 1; k > w; --k)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        const float4 run = runs[k][lane * V + c];
+        const float4 run = runs[k][c * 64 + lane];
         g[c] = fmaf(run.x, g[c], run.z);
       }
     // the states before each step, in the place of what enters
