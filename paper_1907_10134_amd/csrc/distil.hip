@@ -18,10 +18,15 @@ struct Entries {                   // of the teacher, [T,B,K]
   const int32_t* index;
   int K, type;
 };
-__device__ __forceinline__ float entry_logit(const Entries& e, int64_t at) {
-  if (e.type == BPPSA_F32) return static_cast<const float*>(e.logits)[at];
-  if (e.type == BPPSA_BF16) return static_cast<float>(static_cast<const bf16_t*>(e.logits)[at]);
-  return static_cast<float>(static_cast<const f16_t*>(e.logits)[at]);
+// as it is stored, and its value: whoever asks for it does not wait for it
+__device__ __forceinline__ uint32_t entry_bits(const Entries& e, int64_t at) {
+  if (e.type == BPPSA_F32) return static_cast<const uint32_t*>(e.logits)[at];
+  return static_cast<const uint16_t*>(e.logits)[at];
+}
+__device__ __forceinline__ float entry_logit(const Entries& e, uint32_t bits) {
+  if (e.type == BPPSA_F32) return __uint_as_float(bits);
+  if (e.type == BPPSA_BF16) return __uint_as_float(bits << 16);
+  return static_cast<float>(__builtin_bit_cast(f16_t, (uint16_t)bits));
 }
 
 template <typename E>
@@ -66,6 +71,7 @@ distil_kernel(const Loss<E> l) {
   // of the entries: the place (-1: does not count), the student's logit there, the teacher's, the share
   __shared__ int place[kMost];
   __shared__ float at_place[kMost], logit[kMost], p[kMost];
+  __shared__ float at_target;
   __shared__ int twice;
   const int64_t row = blockIdx.x;
   const int t = (int)(row / l.B), b = (int)(row % l.B), K = l.top.K, first = threadIdx.x * N;
@@ -84,18 +90,21 @@ distil_kernel(const Loss<E> l) {
   }
   const E* const x = l.x.at(t, b);
   const bool tail = l.top_norm != nullptr;
+  const float top_norm = tail ? l.top_norm[row] : 0.0f;
   const float scale = (float)l.scale;
   const int target = l.targets && l.hard != 0.0f ? l.targets[row] : -1;
   const bool known = target >= 0 && target < l.V;
-  // the entries are asked for first, then the row, then the row's logits of the entries
+  // the entries are asked for first, then the row, then the row's logits of the entries; nothing of it in a branch of its own, which would
+  // wait for it
   constexpr int ENTRIES = (kMost + THREADS - 1) / THREADS;
   int c[ENTRIES];
-  float raw[ENTRIES];
+  uint32_t raw[ENTRIES];
   if (entries)
 #pragma unroll
     for (int i = 0; i < ENTRIES; ++i) {
       const int k = threadIdx.x + i * THREADS;
-      c[i] = k < K ? l.top.index[row * K + k] : -1, raw[i] = k < K ? entry_logit(l.top, row * K + k) : -INFINITY;
+      const int64_t at = row * K + (k < K ? k : K - 1);
+      if (wave * 64 + i * THREADS < K) c[i] = l.top.index[at], raw[i] = entry_bits(l.top, at);
     }
   // f(chunk, its first token less the thread's, how many of its tokens are a neighbour's, whether the step is whole).  A step in which not all of the
   // workgroup's chunks are whole is apart from the others: there is code for its ends but once.  The last chunk of a row begins early
@@ -116,30 +125,34 @@ distil_kernel(const Loss<E> l) {
     }
   };
   if constexpr (CHUNKS > 0) {
+    // 16-bit chunks behind the last whole one are left out, of fp32 ones that is read again: as each has less or more room than it needs, the
+    // other way takes some of the row out of registers (2048 rows of 40000 bf16 82 us, 95; of 32000 fp32 with two softmaxes 130, 202)
+    if (sizeof(E) == 2 || steps > 0)
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k)
-      if (k < steps) held[k] = load_whole(x + k * STEP, first * sizeof(E));
-    if (ends) {
-      end = __builtin_bit_cast(Chunk<E>, load_some<E, N>(x + end_from));
-      end.leave_out(end_at - end_from);
-    }
+      for (int k = 0; k < CHUNKS; ++k)
+        if (sizeof(E) == 4 || k < steps) held[k] = load_whole(x + (k < steps ? k : steps - 1) * STEP, first * sizeof(E));
+    if (ends) end = load_whole(x, end_from * sizeof(E));
   }
   // between two passes: the compiler would keep what the first made of the row for the second, in several times the registers
   auto forget = [&]() __attribute__((always_inline)) {
     if constexpr (CHUNKS > 0)
 #pragma unroll
-      for (int k = 0; k < CHUNKS; ++k) asm volatile("" : "+v"(held[k].w[0]), "+v"(held[k].w[1]), "+v"(held[k].w[2]), "+v"(held[k].w[3]));
-    asm volatile("" : "+v"(end.w[0]), "+v"(end.w[1]), "+v"(end.w[2]), "+v"(end.w[3]));
+      for (int k = 0; k < CHUNKS; ++k) asm volatile("" : "+v"(held[k].w));
+    asm volatile("" : "+v"(end.w));
   };
-  const float at_target = known ? (float)x[target] : 0.0f;
+  const E of_target = x[known ? target : 0];
+  E of_entry[ENTRIES];
   float top = -INFINITY;
   if (entries)
 #pragma unroll
     for (int i = 0; i < ENTRIES; ++i) {
       const int k = threadIdx.x + i * THREADS;
-      if (c[i] >= l.V || raw[i] == -INFINITY) c[i] = -1;
-      if (c[i] >= 0) top = fmaxf(top, raw[i]);
-      if (k < K) place[k] = c[i], logit[k] = raw[i], at_place[k] = c[i] >= 0 ? (float)x[c[i]] : 0.0f;
+      if (wave * 64 + i * THREADS >= K) continue;
+      const float value = entry_logit(l.top, raw[i]);
+      if (k >= K || c[i] >= l.V || value == -INFINITY) c[i] = -1;
+      of_entry[i] = x[c[i] >= 0 ? c[i] : 0];
+      if (c[i] >= 0) top = fmaxf(top, value);
+      if (k < K) place[k] = c[i], logit[k] = value;
     }
   // an index that comes twice finds its bit set
   for (int v = threadIdx.x; v <= (l.V + 31) / 32; v += THREADS) is_entry[v] = 0;
@@ -149,12 +162,19 @@ distil_kernel(const Loss<E> l) {
     for (int k = threadIdx.x; k < K; k += THREADS)
       if (place[k] >= 0 && atomicOr(&is_entry[place[k] / 32], 1u << place[k] % 32) >> place[k] % 32 & 1) twice = 1;
   float m = -INFINITY;
+  end.leave_out(end_at - end_from);
   each([&](const Chunk<E>& x, int, int, auto) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < N; ++k) m = fmaxf(m, x[k]);
   });
   m = lanes::largest(m);
-  if (entries) top = lanes::largest(top);
+  if (entries) {
+    top = lanes::largest(top);
+#pragma unroll
+    for (int i = 0; i < ENTRIES; ++i)
+      if (threadIdx.x + i * THREADS < K) at_place[threadIdx.x + i * THREADS] = static_cast<float>(of_entry[i]);
+  }
+  if (threadIdx.x == 0) at_target = static_cast<float>(of_target);
   if (lane == 0) of.largest[wave] = m, of.top[wave] = top;
   __syncthreads();
   if (WAVES > 1) {
@@ -191,7 +211,7 @@ distil_kernel(const Loss<E> l) {
     for (int k = threadIdx.x; k < K; k += THREADS) {
       if (place[k] < 0) continue;
       // the difference in 64 bits, its exponential in 32, corrected by what the difference loses there
-      const double over = tail ? (double)logit[k] * l.scale - (double)l.top_norm[row] : ((double)logit[k] - (double)top) * l.scale;
+      const double over = tail ? (double)logit[k] * l.scale - (double)top_norm : ((double)logit[k] - (double)top) * l.scale;
       const float near = (float)over, e = exp_of<true>(near), share = e > 0.0f ? fmaf(e, (float)(over - (double)near), e) : 0.0f;
       shares += (double)share, p[k] = share;
       if (share > 0.0f) terms += (double)share * (over - ((double)at_place[k] - (double)m) * l.scale);
@@ -220,7 +240,7 @@ distil_kernel(const Loss<E> l) {
       float g[N];
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        g[k] = elsewhere * of_tau(x[k]);
+          g[k] = elsewhere * of_tau(x[k]);
         if (SECOND) g[k] = fmaf(of_e1, of_one(x[k]), g[k]);
       }
       if constexpr (CHUNKS == 0) store_chunk<E>(dx, first + at, l.V, g);

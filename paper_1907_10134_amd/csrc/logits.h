@@ -7,11 +7,15 @@ namespace logits {
 
 using namespace ssm;
 
-// Eight 16-bit or four 32-bit logits as they were loaded, and the value of one.
+typedef uint32_t Four __attribute__((ext_vector_type(4)));
+typedef Four Loose __attribute__((aligned(2)));
+
+// Eight 16-bit or four 32-bit logits as they were loaded, and the value of one.  (Of one vector: an array that is loaded in a branch is taken apart
+// there, which waits for the load.)
 template <typename E>
 struct Chunk {
   static constexpr int N = 16 / sizeof(E);
-  uint32_t w[4];
+  Four w;
   // the first n become minus infinity
   __device__ __forceinline__ void leave_out(int n) {
     constexpr uint32_t none = sizeof(E) == 4 ? 0xFF800000u : std::is_same_v<E, bf16_t> ? 0xFF80u : 0xFC00u;
@@ -31,21 +35,18 @@ struct Chunk {
     else return static_cast<float>(__builtin_bit_cast(E, (uint16_t)(k & 1 ? w[k / 2] >> 16 : w[k / 2])));
   }
 };
-typedef uint32_t Four __attribute__((ext_vector_type(4)));
-typedef Four Loose __attribute__((aligned(2)));
 // A whole chunk at a place that is the same for all threads and a thread's offset of 32 bits: one address of scalar registers for
 // each, where sixteen of vector registers would push the row out.
 template <typename E>
 __device__ __forceinline__ Chunk<E> load_whole(const E* place, uint32_t byte) {
   uint64_t at = (uint64_t)place;
-  asm("" : "+s"(at));
-  const Four w = *(const __attribute__((address_space(1))) Loose*)(at + byte);
-  return Chunk<E>{{w.x, w.y, w.z, w.w}};
+  asm("" : "+s"(at), "+v"(byte));
+  return Chunk<E>{*(const __attribute__((address_space(1))) Loose*)(at + byte)};
 }
 template <typename E>
 __device__ __forceinline__ void store_whole(E* place, uint32_t byte, const float (&v)[Chunk<E>::N]) {
   uint64_t at = (uint64_t)place;
-  asm("" : "+s"(at));
+  asm("" : "+s"(at), "+v"(byte));
   Some<E, Chunk<E>::N> s;
 #pragma unroll
   for (int k = 0; k < Chunk<E>::N; ++k) s.v[k] = static_cast<E>(v[k]);
