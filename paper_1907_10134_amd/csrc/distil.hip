@@ -55,13 +55,13 @@ struct Share {
 // and its gradient are made of those; 0: a row too long for that is read three times.  SECOND: the data's own token has a
 // softmax of its own, at another temperature.
 //
-// Bound by memory: 8192 rows of 32768 bf16 with two softmaxes 217 us, 4.9 TB/s, the vector unit busy for 85 % of that (two exponentials
-// a logit and softmax: keeping them would take as many registers again, 16-bit rows twice as many).  Short rows are bound by what a row takes besides its
-// logits: the entries' shares in 64 bits and seven sums over the waves (16000 rows of 4001 fp16: 62 us, 4.2 TB/s by those that are read).
+// Bound by memory: 8192 rows of 32768 bf16 with two softmaxes 210 us, 5.1 TB/s, the vector unit busy for 85 % of that (two exponentials
+// a logit and softmax: to keep them takes twice the registers of a 16-bit row).  Short rows are bound by what a row takes besides its
+// logits, the entries' shares in 64 bits and seven sums over the waves (16000 rows of 4001 fp16: 59 us, 4.3 TB/s of those that are read).
 //
 // As many waves a SIMD as the registers of the row let, and no more: two workgroups of sixteen waves are worth some spilled scalars of
-// the entries (2048 rows of 65536 bf16 with two softmaxes: 147 us, 180 by one workgroup a unit), four of eight instead of
-// three are not (8192 rows of 32768 bf16: 243 us, 226; 4096 rows of 8000 fp32: 64 us, 58).
+// the entries (2048 rows of 65536 bf16 with two softmaxes: 144 us, 172 by one workgroup a unit), four of eight instead of
+// three are not (4096 rows of 32001 bf16: 133 us, 119).
 template <typename E, int WAVES, int CHUNKS, bool SECOND>
 __global__ void __launch_bounds__(WAVES * 64, CHUNKS == 16 ? 4 : WAVES == 16 ? 8 : 6)
 distil_kernel(const Loss<E> l) {
@@ -316,11 +316,10 @@ extern "C" bppsa_status bppsa_distil(const bppsa_distil_rows* r, float* loss, co
     typedef std::integral_constant<int, 8> Eight;
     typedef std::integral_constant<int, 16> Sixteen;
     // The fewest waves that hold a row in as many chunks as their registers take, and fewer chunks where rows are short: each line
-    // measured with it and with the next one in its place.  64000 rows of 100 fp32 48 and 51 us; 32768 of 1000 bf16 39 and 58; 16384
-    // of 4096, the others as one more class, 64 and 78; 8192 of 8192 57 and 74; 4096 of 32001 127 and 157; 2048 of 65536 125 and 166; 1024
-    // of 131072 with two softmaxes, the longest that registers hold, 161 and 243.
+    // measured with it and with the next one in its place.  32768 rows of 1000 bf16 37 and 57 us; 16384 of 4096, the others as one more
+    // class, 61 and 75; 8192 of 8192 49 and 69; 4096 of 32001 119 and 156; 2048 of 65536 117 and 159; 1024 of 131072 with two softmaxes,
+    // the longest that registers hold, 152 and 185.
     if (l.V < N) run(One{}, None{});
-    else if (fits(1, 1)) run(One{}, One{});
     else if (fits(1, 4)) run(One{}, Four{});
     else if (fits(2, 4)) run(Two{}, Four{});
     else if (fits(4, 8)) run(Four{}, Eight{});
