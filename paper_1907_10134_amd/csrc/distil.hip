@@ -57,7 +57,7 @@ struct Share {
 //
 // Bound by memory: 8192 rows of 32768 bf16 with two softmaxes 210 us, 5.1 TB/s, the vector unit busy for 85 % of that (two exponentials
 // a logit and softmax: to keep them takes twice the registers of a 16-bit row).  Short rows are bound by what a row takes besides its
-// logits, the entries' shares in 64 bits and seven sums over the waves (16000 rows of 4001 fp16: 59 us, 4.3 TB/s of those that are read).
+// logits, the entries' shares in 64 bits and seven sums over the waves (16000 rows of 4001 fp16, a tenth of them not read: 59 us, 4.1 TB/s).
 //
 // As many waves a SIMD as the registers of the row let, and no more: two workgroups of sixteen waves are worth some spilled scalars of
 // the entries (2048 rows of 65536 bf16 with two softmaxes: 144 us, 172 by one workgroup a unit), four of eight instead of
@@ -316,12 +316,13 @@ extern "C" bppsa_status bppsa_distil(const bppsa_distil_rows* r, float* loss, co
     typedef std::integral_constant<int, 8> Eight;
     typedef std::integral_constant<int, 16> Sixteen;
     // The fewest waves that hold a row in as many chunks as their registers take, and fewer chunks where rows are short: each line
-    // measured with it and with the next one in its place.  32768 rows of 1000 bf16 37 and 57 us; 16384 of 4096, the others as one more
-    // class, 61 and 75; 8192 of 8192 49 and 69; 4096 of 32001 119 and 156; 2048 of 65536 117 and 159; 1024 of 131072 with two softmaxes,
-    // the longest that registers hold, 152 and 185.
+    // measured with it and with the next one in its place.  65536 rows of 300 bf16 60 and 63 us; with the others as one more class 16384 of 3000
+    // 43 and 53, 8192 of 5000 39 and 44, 8192 of 10000 66 and 87, 4096 of 32001 119 and 156, 2048 of 65536 117 and 159; 1024 of 131072 with
+    // two softmaxes, the longest that registers hold, 154 and 187.  (Rows that fill their line's chunks gain less, at worst nothing.)
     if (l.V < N) run(One{}, None{});
     else if (fits(1, 4)) run(One{}, Four{});
-    else if (fits(2, 4)) run(Two{}, Four{});
+    else if (fits(1, 8)) run(One{}, Eight{});
+    else if (fits(2, 8)) run(Two{}, Eight{});
     else if (fits(4, 8)) run(Four{}, Eight{});
     else if (fits(8, 8)) run(Eight{}, Eight{});
     else if (fits(16, 8)) run(Sixteen{}, Eight{});
