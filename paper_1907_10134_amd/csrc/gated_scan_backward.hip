@@ -96,22 +96,22 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
   lds_barrier();
   if (w < V && t0 < len) {                   // the tile's own share, a channel a lane
     const uint32_t at = w * 64 + lane;
+    const int channel = d + w;
+    const float kept = states[((int64_t)tile * l.B + b) * l.D + channel];      // asked for before the wait, by lanes without a channel too
     float p = 1.0f, s = 0.0f, in = 0.0f;
 #pragma unroll
     for (int k = kWaves - 1; k >= 0; --k) {
       const float4 run = runs[k][at];
       p *= run.x, s = fmaf(run.x, s, run.z);
     }
-    const int channel = d + w;
-    const bool on = own.on;
-    if (tile == last_tile && dh_last && on) in = dh_last[(int64_t)b * l.D + channel];
+    if (tile == last_tile && dh_last && own.on) in = dh_last[(int64_t)b * l.D + channel];
     if (JOINED) {
       const int64_t step = (int64_t)l.B * l.columns * 64 * V;
       uint64_t* const mine = words + tile * step + ((int64_t)b * l.columns + column) * 64 * V;
       if (tile < last_tile) leave(mine + at, word_of(p, s)), in = look_back(mine, at, -step, last_tile - tile);
       leave(mine + at, settled(through(word_of(p, s), in)));
     }
-    border[at] = make_float2(on ? states[((int64_t)tile * l.B + b) * l.D + channel] : 0.0f, in);
+    border[at] = make_float2(kept, in);
   }
   lds_barrier();
   if (rows > 0 && own.on) {
