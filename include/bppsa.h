@@ -600,7 +600,7 @@ bppsa_status bppsa_ssm_conv_step(const bppsa_conv* conv, const bppsa_rows* y, vo
  *     h[t] = a h[t-1] + sqrt(1 - a^2) iota x[t,b,d],     y[t,b,d] = h[t] * ( z ? silu(z[t,b,d]) : 1 )
  * x, r, i, z are [T,B,D]; decay [D] (not negative), r_bias, i_bias [D], h0 [B,D] fp32.  z.data, r_bias, i_bias, h0 and
  * lengths may be NULL (no gate, 0, 0, zeros, all of T); lengths, outputs behind an end and the last state as in bppsa_ssm.
- * The state is held in fp32; from a step on where an input is NaN or x infinite, a channel's states are NaN or infinite.
+ * The state is held in fp32; from a step on where x, r or i is NaN or x infinite, a channel's states are NaN or infinite.
  * Sizes that no launch can hold are BPPSA_EOVERFLOW before anything is launched (D over 2^24, 2^23
  * and more tiles of 64 steps and 64 channels over all samples); the byte counts of such sizes are 0.
  */

@@ -245,6 +245,23 @@ def test_another_stream_and_a_graph():
         assert torch.equal(bp.beam_select(**c).tokens, want.tokens)
 
 
+def test_two_streams_at_once():
+    """Each call has a workspace of its own: two searches side by side are what they are by themselves."""
+    import torch
+    import paper_1907_10134_amd as bp
+    torch.manual_seed(5)
+    x = [torch.randn((9, 7, 30001), device="cuda").bfloat16() for _ in range(2)]
+    s = torch.randn((9, 7), device="cuda")
+    want = [bp.beam_select(y, s) for y in x]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[bp.beam_select(y, s, stream=q) for y, q in zip(x, streams)] for _ in range(4)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for a, b in zip(pair, want):
+            assert torch.equal(a.scores, b.scores) and torch.equal(a.tokens, b.tokens) and torch.equal(a.parents, b.parents)
+
+
 def test_refusals():
     import torch
     import paper_1907_10134_amd as bp

@@ -228,6 +228,41 @@ def test_another_stream_and_a_graph():
         assert torch.equal(bp.distil(**c).dlogits, want.dlogits)
 
 
+def test_many_rows_and_two_streams():
+    """More rows than 16 bits count, on two streams side by side: no call knows of the other."""
+    import torch
+    import paper_1907_10134_amd as bp
+    c, ref = _case(12, 70001, 9, 3, "bfloat16", True, 0.3, True, 2.0)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[bp.distil(stream=s, **c) for s in streams] for _ in range(3)]
+    torch.cuda.synchronize()
+    _check(got[0][0], c, ref, "bfloat16")
+    assert all(torch.equal(x.loss, got[0][0].loss) and torch.equal(x.dlogits, got[0][0].dlogits) for pair in got for x in pair)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", (7, 8, 9, 2047, 4095, 4096, 4097, 8191, 16383, 32769, 65535))
+def test_rows_around_what_waves_hold(V, dtype):
+    """As many entries as there may be, some of them twice, where rows begin to take more waves or chunks; every logit an odd
+    number of elements off a multiple of 16 bytes."""
+    import torch
+    import paper_1907_10134_amd as bp
+    K = min(V, 256)
+    c, ref = _case(13, 3, V, K, dtype, True, 0.25, False, 1.5)
+    if K > 4:
+        for x in (c["top_index"], ref["top_index"]):
+            x[1, ..., 1] = x[1, ..., 3]
+    wide = torch.full((3, 1, V + 9), 3.0, dtype=c["logits"].dtype, device="cuda")
+    wide[:, :, 1:V + 1] = c["logits"]
+    c["logits"] = wide[:, :, 1:V + 1]
+    got = bp.distil(**c)
+    _check(got, c, ref, dtype)
+    place = bp.distil(dlogits=c["logits"], **c)
+    assert torch.equal(place.dlogits, got.dlogits) and torch.equal(place.loss, got.loss)
+    assert bool((wide[:, :, 0] == 3).all()) and bool((wide[:, :, V + 1:] == 3).all())
+
+
 def test_refusals():
     import torch
     import paper_1907_10134_amd as bp

@@ -384,6 +384,22 @@ def test_two_streams_at_once():
     assert all(torch.equal(y, want) for pair in got for y in pair)
 
 
+def test_infinite_inputs_stay_in_their_channel():
+    """An infinite x leaves its channel's states infinite or NaN from its step on, over tiles whose decays' product is zero too; no
+    other channel of its lane or workgroup, and nothing before it."""
+    import torch
+    import paper_1907_10134_amd as bp
+    for dtype in TYPES:
+        c, _, _, _, _ = _case(7, 700, 2, 97, dtype, False, True, False, "tb")
+        c["decay"][40] = 30.0
+        want = bp.gated_scan(**c)
+        c["x"][130, 0, 40], c["x"][5, 1, 96] = float("inf"), float("-inf")
+        y = bp.gated_scan(**c)
+        bad = ~torch.isfinite(y)
+        assert bool(bad[130:, 0, 40].all()) and bool(bad[5:, 1, 96].all()) and int(bad.sum()) == 570 + 695
+        assert torch.equal(y[~bad], want[~bad])
+
+
 def test_refusals():
     import torch
     import paper_1907_10134_amd as bp
