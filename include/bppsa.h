@@ -614,8 +614,9 @@ typedef struct bppsa_gated {
 /*
  * Forward over whole sequences.  Writes y [T,B,D]; h_last [B,D], the state after each sample's last token, if not NULL;
  * `states`, bppsa_gated_scan_states_bytes bytes of device memory on a multiple of 16 in a layout of the library's own, if
- * not NULL: what the backward pass reads (4 bytes for each channel and 64 steps).  The workspace may be of size 0.  The
- * results are the same bits on every call with the same sizes.
+ * not NULL: what the backward pass reads (4 bytes for each channel and 64 steps).  The workspace may be of size 0, and serves
+ * one call at a time: where two at once share one, as two graphs replayed side by side may, their states are of no use, or NaN after
+ * some seconds.  The results are the same bits on every call with the same sizes.
  */
 size_t bppsa_gated_scan_states_bytes(int T, int B, int D);
 size_t bppsa_gated_scan_workspace_bytes(int T, int B, int D);

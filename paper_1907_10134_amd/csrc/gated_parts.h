@@ -195,7 +195,10 @@ __device__ __forceinline__ uint64_t peek(const uint64_t* p) { return __hip_atomi
 __device__ __forceinline__ void leave(uint64_t* p, uint64_t w) { __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // The state that comes into a tile: `mine` are this tile's words, the same for a wave, `at` a lane's place in them, `step` the words to
-// the next tile, `tiles` how many lie in front of it (the farthest one's words become settled without waiting for any other).
+// the next tile, `tiles` how many lie in front of it (the farthest one's words become settled without waiting for any other).  Every
+// word that is waited for comes, unless another call at the same time works in the same workspace: then the wait ends after
+// kLooks looks, of a microsecond and more each, and an empty word's product is NaN.
+constexpr int kLooks = 1 << 24;
 __device__ __forceinline__ float look_back(const uint64_t* mine, uint32_t at, int64_t step, int tiles) {
   constexpr int WINDOW = 4;
   int far = 0;                                 // windows behind this one that hold no settled word
@@ -207,7 +210,8 @@ __device__ __forceinline__ float look_back(const uint64_t* mine, uint32_t at, in
       w[j] = peek(mine - step * (back <= tiles ? back : tiles) + at);
     }
   };
-  for (bool again = true; again;) {
+  bool again = true;
+  for (int looks = 0; again && looks < kLooks; ++looks) {
     window(far);
     bool wait = false, found = false;
 #pragma unroll
