@@ -55,9 +55,9 @@ struct Share {
 // and its gradient are made of those; 0: a row too long for that is read three times.  SECOND: the data's own token has a
 // softmax of its own, at another temperature.
 //
-// Bound by memory: 8192 rows of 32768 bf16 with two softmaxes 210 us, 5.1 TB/s, the vector unit busy for 85 % of that (two exponentials
+// Bound by memory: 8192 rows of 32768 bf16 with two softmaxes 210 us, 5.1 TB/s, the vector unit busy for 93 % of that (two exponentials
 // a logit and softmax: to keep them takes twice the registers of a 16-bit row).  Short rows are bound by what a row takes besides its
-// logits, the entries' shares in 64 bits and seven sums over the waves (16000 rows of 4001 fp16, a sixth of them not read: 59 us, 4.1 TB/s).
+// logits, the entries' shares in 64 bits and seven sums over a wave or more (16000 rows of 4001 fp16, a sixth of them not read: 59 us, 4.1 TB/s).
 //
 // As many waves a SIMD as the registers of the row let, and no more: two workgroups of sixteen waves are worth some spilled scalars of
 // the entries (2048 rows of 65536 bf16 with two softmaxes: 144 us, 172 by one workgroup a unit), four of eight instead of
