@@ -696,7 +696,8 @@ bppsa_status bppsa_adamw_step(int n_tensors, const bppsa_adamw_tensor* tensors, 
  * A term with p = 0 is 0, and so is that of p_0 where the other tokens' sum is below 2^-126 of the largest term.  An index may
  * come twice: its shares add up in the gradient.  A target outside [0, V) has no second term; a row without entries no first.
  * Rows of weight 0 are not read: their loss and gradient are zero.  Otherwise infinities and NaN mean what the formulas say
- * (a student's logit of minus infinity is a token that has no share).
+ * (a student's logit of minus infinity is a token that has no share): an entry that counts whose logit is NaN or plus infinity, or
+ * whose share passes fp32's range, and a NaN for their top_norm leave the row's loss and gradient NaN or infinite.
  * logits and dlogits are [T,B,V] with strides as above, dlogits of the logits' type, or the logits themselves (same address and
  * strides: the gradient takes their place), or NULL: the loss alone.  top_logits [T,B,K] of top_type and top_index [T,B,K]
  * int32, top_norm, weight (NULL: 1), targets (may be NULL where hard is 0) and loss [T,B] are contiguous.

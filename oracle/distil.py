@@ -7,7 +7,8 @@ import numpy as np
 
 def _log_softmax(x):
     m = np.max(x)
-    return x - (m + np.log(np.sum(np.exp(x - m))))
+    with np.errstate(invalid="ignore"):        # a largest value that is infinite: NaN
+        return x - (m + np.log(np.sum(np.exp(x - m))))
 
 
 def loss(logits, top_logits, top_index, temperature=1.0, top_norm=None, targets=None, hard=0.0, weight=None):
@@ -18,7 +19,7 @@ def loss(logits, top_logits, top_index, temperature=1.0, top_norm=None, targets=
         w = 1.0 if weight is None else weight[k]
         if w == 0:
             continue
-        on = (top_index[k] >= 0) & (top_index[k] < V) & (top_logits[k] > -np.inf)
+        on = (top_index[k] >= 0) & (top_index[k] < V) & (top_logits[k] != -np.inf)       # NaN counts
         c, t = top_index[k][on], top_logits[k][on] / temperature
         logq = _log_softmax(logits[k] / temperature)
         q = np.exp(logq)
@@ -26,14 +27,15 @@ def loss(logits, top_logits, top_index, temperature=1.0, top_norm=None, targets=
         if len(c):
             logp = _log_softmax(t) if top_norm is None else t - top_norm[k]
             p = np.exp(logp)
-            soft = np.sum(np.where(p > 0, p * (logp - logq[c]), 0.0))
+            soft = np.sum(np.where(p == 0, 0.0, p * (logp - logq[c])))
             d = q * p.sum()
-            np.subtract.at(d, c, p)
+            with np.errstate(invalid="ignore"):
+                np.subtract.at(d, c, p)
         if top_norm is not None:
             rest = np.ones(V, dtype=bool)
             rest[c] = False
-            p0, q0 = max(0.0, 1.0 - (p.sum() if len(c) else 0.0)), q[rest].sum()
-            if p0 > 0 and q0 > 0:
+            p0, q0 = np.maximum(0.0, 1.0 - (p.sum() if len(c) else 0.0)), q[rest].sum()
+            if p0 != 0 and q0 > 0:
                 soft += p0 * np.log(p0 / q0)
                 d += p0 * q
                 d[rest] -= p0 * q[rest] / q0

@@ -210,11 +210,11 @@ distil_kernel(const Loss<E> l) {
   if (entries) {
     for (int k = threadIdx.x; k < K; k += THREADS) {
       if (place[k] < 0) continue;
-      // the difference in 64 bits, its exponential in 32, corrected by what the difference loses there
+      // the difference in 64 bits, its exponential in 32, corrected by what the difference loses there; what is NaN stays it
       const double over = tail ? (double)logit[k] * l.scale - (double)top_norm : ((double)logit[k] - (double)top) * l.scale;
-      const float near = (float)over, e = exp_of<true>(near), share = e > 0.0f ? fmaf(e, (float)(over - (double)near), e) : 0.0f;
+      const float near = (float)over, e = exp_of<true>(near), share = e == 0.0f ? 0.0f : fmaf(e, (float)(over - (double)near), e);
       shares += (double)share, p[k] = share;
-      if (share > 0.0f) terms += (double)share * (over - ((double)at_place[k] - (double)m) * l.scale);
+      if (share != 0.0f) terms += (double)share * (over - ((double)at_place[k] - (double)m) * l.scale);
     }
     shares = lanes::sum(shares), terms = lanes::sum(terms);
   }
@@ -227,13 +227,13 @@ distil_kernel(const Loss<E> l) {
     shares = lanes::sum(lane < with_entries ? of.shares[lane % WAVES] : 0.0);
     if (wave == 0) terms = lanes::sum(lane < with_entries ? of.terms[lane % WAVES] : 0.0);
   }
-  const bool any = shares > 0.0;
+  const bool any = shares != 0.0;
   const double p0 = tail && rest > 0.0f ? fmax(0.0, 1.0 - shares) : 0.0;
   const float over = any && !tail ? 1.0f / (float)shares : 1.0f;
   if (dx) {
     const float of_soft = weight * (1.0f - l.hard) * l.tau, hard = known ? weight * l.hard : 0.0f;
     const float one = 1.0f / s, of_e1 = SECOND ? hard / s1 : 0.0f, of_e = SECOND ? 0.0f : hard * one;
-    const float M = (tail ? (float)shares : any ? 1.0f : 0.0f) + (float)p0, ratio = p0 > 0.0 ? (float)p0 * (s / rest) : 0.0f;
+    const float M = (tail ? (float)shares : shares > 0.0 ? 1.0f : (float)shares) + (float)p0, ratio = p0 > 0.0 ? (float)p0 * (s / rest) : 0.0f;
     const float elsewhere = fmaf(of_soft * (M - ratio), one, of_e), inside = fmaf(of_soft * M, one, of_e);
     forget();
     each([&](const Chunk<E>& x, int at, int shared, auto whole) __attribute__((always_inline)) {
