@@ -44,6 +44,9 @@ struct Loss {
 
 constexpr int kMost = BPPSA_DISTIL_MAX_K;
 
+// A value that is the same in all lanes, in a scalar register: the rows of sixteen waves have no vector register to spare.
+__device__ __forceinline__ float scalar(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
+
 // What the waves of a row tell each other, each by its first lane.
 template <int WAVES>
 struct Share {
@@ -53,7 +56,7 @@ struct Share {
 };
 // One workgroup a row.  CHUNKS > 0: the row is read once, into registers (16 bytes a lane and chunk), and its largest value, its sums
 // and its gradient are made of those; 0: a row too long for that is read three times.  SECOND: the data's own token has a
-// softmax of its own, at another temperature.
+// softmax of its own, at another temperature.  TAIL: all other tokens are one more class.
 //
 // Bound by memory: 8192 rows of 32768 bf16 with two softmaxes 210 us, 5.1 TB/s, the vector unit busy for 93 % of that (two exponentials
 // a logit and softmax: to keep them takes twice the registers of a 16-bit row).  Short rows are bound by what a row takes besides its
@@ -62,7 +65,7 @@ struct Share {
 // As many waves a SIMD as the registers of the row let, and no more: two workgroups of sixteen waves are worth some spilled scalars of
 // the entries (2048 rows of 65536 bf16 with two softmaxes: 144 us, 172 by one workgroup a unit), four of eight instead of
 // three are not (4096 rows of 32001 bf16: 133 us, 119).
-template <typename E, int WAVES, int CHUNKS, bool SECOND>
+template <typename E, int WAVES, int CHUNKS, bool SECOND, bool TAIL>
 __global__ void __launch_bounds__(WAVES * 64, CHUNKS == 16 ? 4 : WAVES == 16 ? 8 : 6)
 distil_kernel(const Loss<E> l) {
   constexpr int N = Chunk<E>::N, THREADS = WAVES * 64, STEP = THREADS * N, HELD = CHUNKS ? CHUNKS : 1;
@@ -89,8 +92,7 @@ distil_kernel(const Loss<E> l) {
     return;
   }
   const E* const x = l.x.at(t, b);
-  const bool tail = l.top_norm != nullptr;
-  const float top_norm = tail ? l.top_norm[row] : 0.0f;
+  const float top_norm = TAIL ? l.top_norm[row] : 0.0f;
   const float scale = (float)l.scale;
   const int target = l.targets && l.hard != 0.0f ? l.targets[row] : -1;
   const bool known = target >= 0 && target < l.V;
@@ -193,7 +195,7 @@ distil_kernel(const Loss<E> l) {
       if (SECOND) sum1 += of_one(x[k]);
     }
     s += sum, s1 += sum1;
-    if (tail) {
+    if (TAIL) {
       const int from = first + at;
       const uint32_t bits = (uint32_t)(((uint64_t)is_entry[from / 32 + 1] << 32 | is_entry[from / 32]) >> from % 32);
       float others = 0.0f;
@@ -204,14 +206,14 @@ distil_kernel(const Loss<E> l) {
   });
   s = lanes::sum(s);
   if (SECOND) s1 = lanes::sum(s1);
-  if (tail) rest = lanes::sum(rest);
+  if (TAIL) rest = lanes::sum(rest);
   // the entries' shares, before they are divided by their sum where they are all there is, and what they leave of the divergence
   double shares = 0.0, terms = 0.0;
   if (entries) {
     for (int k = threadIdx.x; k < K; k += THREADS) {
       if (place[k] < 0) continue;
       // the difference in 64 bits, its exponential in 32, corrected by what the difference loses there; what is NaN stays it
-      const double over = tail ? (double)logit[k] * l.scale - (double)top_norm : ((double)logit[k] - (double)top) * l.scale;
+      const double over = TAIL ? (double)logit[k] * l.scale - (double)top_norm : ((double)logit[k] - (double)top) * l.scale;
       const float near = (float)over, e = exp_of<true>(near), share = e == 0.0f ? 0.0f : fmaf(e, (float)(over - (double)near), e);
       shares += (double)share, p[k] = share;
       if (share != 0.0f) terms += (double)share * (over - ((double)at_place[k] - (double)m) * l.scale);
@@ -223,24 +225,30 @@ distil_kernel(const Loss<E> l) {
   if (WAVES > 1) {               // a lane a wave
     s = lanes::sum(lane < WAVES ? of.sums[0][lane % WAVES] : 0.0f);
     if (SECOND) s1 = lanes::sum(lane < WAVES ? of.sums[1][lane % WAVES] : 0.0f);
-    if (tail) rest = lanes::sum(lane < WAVES ? of.sums[2][lane % WAVES] : 0.0f);
+    if (TAIL) rest = lanes::sum(lane < WAVES ? of.sums[2][lane % WAVES] : 0.0f);
     shares = lanes::sum(lane < with_entries ? of.shares[lane % WAVES] : 0.0);
     if (wave == 0) terms = lanes::sum(lane < with_entries ? of.terms[lane % WAVES] : 0.0);
   }
+  s = scalar(s), s1 = scalar(s1), rest = scalar(rest);
   const bool any = shares != 0.0;
-  const double p0 = tail && rest > 0.0f ? fmax(0.0, 1.0 - shares) : 0.0;
-  const float over = any && !tail ? 1.0f / (float)shares : 1.0f;
+  const double p0 = TAIL && rest > 0.0f ? fmax(0.0, 1.0 - shares) : 0.0;
+  const float over = any && !TAIL ? 1.0f / (float)shares : 1.0f;
   if (dx) {
     const float of_soft = weight * (1.0f - l.hard) * l.tau, hard = known ? weight * l.hard : 0.0f;
-    const float one = 1.0f / s, of_e1 = SECOND ? hard / s1 : 0.0f, of_e = SECOND ? 0.0f : hard * one;
-    const float M = (tail ? (float)shares : shares > 0.0 ? 1.0f : (float)shares) + (float)p0, ratio = p0 > 0.0 ? (float)p0 * (s / rest) : 0.0f;
-    const float elsewhere = fmaf(of_soft * (M - ratio), one, of_e), inside = fmaf(of_soft * M, one, of_e);
+    const float one = 1.0f / s, of_e1 = SECOND ? scalar(hard / s1) : 0.0f, of_e = SECOND ? 0.0f : hard * one;
+    const float M = (TAIL ? (float)shares : shares > 0.0 ? 1.0f : (float)shares) + (float)p0;
+    // where the student gives the others next to nothing, p0 / q0 and with it elsewhere would be out of range, which the product with their
+    // exponentials is not: these are lifted first, and elsewhere is as much smaller
+    const bool far = TAIL && p0 > 0.0 && rest < 0x1p-64f;
+    const float lift = far ? 0x1p64f : 1.0f, drop = far ? 0x1p-64f : 1.0f, ratio = p0 > 0.0 ? (float)p0 * (s / (rest * lift)) : 0.0f;
+    const float elsewhere = scalar(fmaf(of_soft * fmaf(M, drop, -ratio), one, of_e * drop)), inside = scalar(fmaf(of_soft * M, one, of_e));
+    const auto lifted = [&](float e) { return TAIL ? e * lift : e; };
     forget();
     each([&](const Chunk<E>& x, int at, int shared, auto whole) __attribute__((always_inline)) {
       float g[N];
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-          g[k] = elsewhere * of_tau(x[k]);
+        g[k] = elsewhere * lifted(of_tau(x[k]));
         if (SECOND) g[k] = fmaf(of_e1, of_one(x[k]), g[k]);
       }
       if constexpr (CHUNKS == 0) store_chunk<E>(dx, first + at, l.V, g);
@@ -252,8 +260,8 @@ distil_kernel(const Loss<E> l) {
           if (k >= shared) store(dx + first + at + k, g[k]);
     });
     __syncthreads();               // behind it the places of the entries and of the target are written again
-    auto again = [&](int at, float value, float coefficient, float own) __attribute__((always_inline)) {
-      float g = coefficient * of_tau(value) - own;
+    auto again = [&](int at, float e, float value, float coefficient, float own) __attribute__((always_inline)) {
+      float g = coefficient * e - own;
       if (SECOND) g = fmaf(of_e1, of_one(value), g);
       store(dx + at, g);
     };
@@ -266,17 +274,17 @@ distil_kernel(const Loss<E> l) {
           own = 0.0f;
           for (int i = 0; i < K; ++i) own += place[i] == c ? p[i] : 0.0f;
         }
-        again(c, at_place[k], inside, of_soft * (own * over) + (c == target ? hard : 0.0f));
+        again(c, of_tau(at_place[k]), at_place[k], inside, of_soft * (own * over) + (c == target ? hard : 0.0f));
       }
     if (threadIdx.x == THREADS - 1 && known) {
-      if (!(is_entry[target / 32] >> target % 32 & 1)) again(target, at_target, elsewhere, hard);
+      if (!(is_entry[target / 32] >> target % 32 & 1)) again(target, lifted(of_tau(at_target)), at_target, elsewhere, hard);
     }
   }
   // last, when the row's registers are free
   if (wave == 0) {
     double soft = 0.0, ce = 0.0, log_s = 0.0;
-    if (tail || (known && !SECOND)) log_s = log_of(s) - of_tau.log_off();
-    if (tail) soft = terms + (shares + p0) * log_s + (p0 > 0.0 ? p0 * (log_of((float)p0) - log_of(rest) + of_tau.log_off()) : 0.0);
+    if (TAIL || (known && !SECOND)) log_s = log_of(s) - of_tau.log_off();
+    if (TAIL) soft = terms + (shares + p0) * log_s + (p0 > 0.0 ? p0 * (log_of((float)p0) - log_of(rest) + of_tau.log_off()) : 0.0);
     else if (any) soft = terms / shares + log_of(s) - log_of((float)shares) - of_tau.log_off();
     if (known) ce = (double)m - (double)at_target + (SECOND ? log_of(s1) - of_one.log_off() : log_s);
     if (threadIdx.x == 0)
@@ -303,8 +311,9 @@ extern "C" bppsa_status bppsa_distil(const bppsa_distil_rows* r, float* loss, co
                     r->top_norm, r->weight, r->targets, loss, r->B, r->V, r->temperature, r->hard, 1.0 / (double)r->temperature};
     const auto run = [&](auto waves, auto chunks) {
       const size_t bits = ((size_t)bppsa_ceil_div(l.V, 32) + 1) * sizeof(uint32_t);
-      const auto kernel = l.hard != 0.0f && l.tau != 1.0f ? distil_kernel<E, waves.value, chunks.value, true>
-                                                          : distil_kernel<E, waves.value, chunks.value, false>;
+      const bool second = l.hard != 0.0f && l.tau != 1.0f;
+      const auto kernel = l.top_norm ? second ? distil_kernel<E, waves.value, chunks.value, true, true> : distil_kernel<E, waves.value, chunks.value, false, true>
+                                     : second ? distil_kernel<E, waves.value, chunks.value, true, false> : distil_kernel<E, waves.value, chunks.value, false, false>;
       kernel<<<(unsigned)(r->T * r->B), waves.value * 64, bits, (hipStream_t)stream>>>(l);
     };
     constexpr int N = Chunk<E>::N;
