@@ -73,7 +73,8 @@ def beam_select(logits, scores, finished=None, end=-1, slots=None, workspace=Non
 class BeamStates:
     """States of many kinds, each a contiguous tensor [slots, ...] of any type, that move together by one launch.
 
-    The tensors' addresses are taken once, here: replace their values, not the tensors."""
+    The tensors' addresses are taken once, here: replace their values, not the tensors.  A captured graph reads this object's lists
+    at every replay: the object has to live as long as the graph."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -99,6 +100,7 @@ class BeamStates:
         both = torch.empty(16 * len(rows) + 8 * self._n_pieces, dtype=torch.uint8)
         ctypes.memmove(both.data_ptr(), b"".join(rows), 16 * len(rows))
         _lib.bppsa_beam_pieces(len(sizes), n, both.data_ptr() + 16 * len(rows))
+        self._streams = {torch.cuda.current_stream(first.device).cuda_stream}      # that the lists are kept for
         self._lists = both.to(first.device)
         self._table = self._lists.data_ptr()
         self._pieces = self._table + 16 * len(rows)
@@ -117,5 +119,9 @@ class BeamStates:
         if sources is None:
             raise TypeError("sources must be a torch.Tensor")
         to, of = _whole(slots, _i32, "slots", self._device), _param(sources, slots.shape, "sources", self._device, _i32)
-        _check(_lib.bppsa_beam_move(self._table, self._n_pieces, self._pieces, slots.numel(), of, to, self.slots,
-                                    _here(self._device)), "bppsa_beam_move")
+        stream = _here(self._device)
+        if stream not in self._streams:            # the object may go before that stream has read what only it keeps
+            self._streams.add(stream)
+            for x in (self._lists, *self.tensors):
+                x.record_stream(torch.cuda.current_stream())
+        _check(_lib.bppsa_beam_move(self._table, self._n_pieces, self._pieces, slots.numel(), of, to, self.slots, stream), "bppsa_beam_move")
