@@ -89,6 +89,8 @@ class AdamW:
         _lib.bppsa_adamw_pieces(len(params), n, pieces.data_ptr())
         self._pieces = pieces.to(device)
         self._tensors = torch.frombuffer(self._table, dtype=torch.uint8).to(device)
+        # the streams that what lasts is kept for, and the table with its gradients
+        self._streams, self._readers = ({torch.cuda.current_stream(device).cuda_stream} for _ in range(2))
 
     def read_gradients(self, grads):
         """Reads the gradients from these tensors from now on, of the sizes and the type of those before."""
@@ -105,6 +107,16 @@ class AdamW:
         table[1::_ROW] = memoryview(bytearray(struct.pack("@%dq" % len(at), *at))).cast("q")
         self.grads = grads
         self._tensors = torch.frombuffer(self._table, dtype=torch.uint8).to(device)
+        self._readers = {torch.cuda.current_stream(device).cuda_stream}
+
+    def _keep(self, on, stream):
+        """For a stream that steps run on: the optimiser may go before it is done, and read_gradients() lets the table go."""
+        for kept, held in ((self._streams, (self._pieces, *self.params, *(self.copies or ()), *sum(self.state.values(), []))),
+                           (self._readers, (self._tensors, *self.grads))):
+            if on not in kept:
+                kept.add(on)
+                for x in held:
+                    x.record_stream(stream)
 
     def step(self, seed=None, stream=None):
         """One update.  With 8-bit moments `seed` (the number of the step unless given) decides which values that are
@@ -114,9 +126,10 @@ class AdamW:
         now = torch.cuda.current_device() if stream is None else stream.device.index
         if now != self._device:
             raise ValueError("AdamW: the tensors are on cuda:%d, the stream is cuda:%d's" % (self._device, now))
-        if stream is not None:
-            self._tensors.record_stream(stream)        # read_gradients() lets the table go
+        on = _stream(stream)
+        if on not in self._streams or on not in self._readers:
+            self._keep(on, torch.cuda.current_stream() if stream is None else stream)
         _check(_lib.bppsa_adamw_step(len(self.params), self._tensors.data_ptr(), self._n_pieces, self._pieces.data_ptr(),
                                      self._grad_type, self.state_bits, t, self.lr, self.beta1, self.beta2, self.eps,
-                                     seed & 0xFFFFFFFF, _stream(stream)), "bppsa_adamw_step")
+                                     seed & 0xFFFFFFFF, on), "bppsa_adamw_step")
         self.t = t
