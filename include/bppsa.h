@@ -861,6 +861,16 @@ bppsa_status bppsa_gru_scan_fused_relay_diag(int T, int B, int I,
                                              int workers, int64_t patience);
 
 /*
+ * The wait by which a tile of bppsa_gated_scan finds the state that comes into it, by itself, for tests: words [tiles][64] (device
+ * memory on a multiple of 8) are what the tiles before it have left for 64 channels, and h [64] receives the states.  A word is
+ * (product of the decays << 32 | end), both as the bits of an fp32 number; with the product's sign set the end is the state
+ * itself; all ones: not there yet.  The first tile's words have the sign or are not there.  After `looks` looks, 1 to 2^24 (the number
+ * that bppsa_gated_scan takes), the wait ends, and what depends on a word that is not there is NaN.
+ * Errors: BPPSA_EINVAL.
+ */
+bppsa_status bppsa_gated_wait_diag(const uint64_t* words, int tiles, int looks, float* h, void* stream);
+
+/*
  * Plain streaming copy dst[i] = src[i] of n fp32 values (n a multiple of 4,
  * both pointers 16-byte aligned, non-overlapping).  It moves exactly 4n bytes
  * in and 4n bytes out of HBM, which makes it the unit against which hardware

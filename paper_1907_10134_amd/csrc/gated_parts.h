@@ -197,9 +197,9 @@ __device__ __forceinline__ void leave(uint64_t* p, uint64_t w) { __hip_atomic_st
 // The state that comes into a tile: `mine` are this tile's words, the same for a wave, `at` a lane's place in them, `step` the words to
 // the next tile, `tiles` how many lie in front of it (the farthest one's words become settled without waiting for any other).  Every
 // word that is waited for comes, unless another call at the same time works in the same workspace: then the wait ends after
-// kLooks looks, of a microsecond and more each, and an empty word's product is NaN.
+// kLooks looks, of a microsecond and more each, and channels whose state was not found get NaN.
 constexpr int kLooks = 1 << 24;
-__device__ __forceinline__ float look_back(const uint64_t* mine, uint32_t at, int64_t step, int tiles) {
+__device__ __forceinline__ float look_back(const uint64_t* mine, uint32_t at, int64_t step, int tiles, int most = kLooks) {
   constexpr int WINDOW = 4;
   int far = 0;                                 // windows behind this one that hold no settled word
   uint64_t w[WINDOW];
@@ -211,7 +211,7 @@ __device__ __forceinline__ float look_back(const uint64_t* mine, uint32_t at, in
     }
   };
   bool again = true;
-  for (int looks = 0; again && looks < kLooks; ++looks) {
+  for (int looks = 0; again && looks < most; ++looks) {
     window(far);
     bool wait = false, found = false;
 #pragma unroll
@@ -224,7 +224,7 @@ __device__ __forceinline__ float look_back(const uint64_t* mine, uint32_t at, in
     else far += on;
     again = stay || on;
   }
-  float h = 0.0f;
+  float h = NAN;                               // of a wait that was given up; every other has found a state
   for (;; --far) {
 #pragma unroll
     for (int j = WINDOW - 1; j >= 0; --j) h = through(w[j], h);

@@ -165,6 +165,12 @@ gated_step_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ state, int sl
   store_some<E, V>(y.at(0, b) + d, out);
 }
 
+// A wave's wait by itself, on words that the caller fills in: [tiles][64], the first tile's first.
+__global__ void __launch_bounds__(64)
+gated_wait_kernel(const uint64_t* words, int tiles, int looks, float* __restrict__ h) {
+  h[threadIdx.x] = look_back(words + (int64_t)tiles * 64, threadIdx.x, 64, tiles, looks);
+}
+
 }  // namespace
 
 extern "C" size_t bppsa_gated_scan_states_bytes(int T, int B, int D) {
@@ -229,4 +235,11 @@ extern "C" bppsa_status bppsa_gated_scan_step(const bppsa_gated* layer, const bp
       return BPPSA_OK;
     });
   });
+}
+
+extern "C" bppsa_status bppsa_gated_wait_diag(const uint64_t* words, int tiles, int looks, float* h, void* stream) {
+  if (!words || ((uintptr_t)words & 7) || tiles < 1 || looks < 1 || looks > kLooks || !h) return BPPSA_EINVAL;
+  gated_wait_kernel<<<1, 64, 0, (hipStream_t)stream>>>(words, tiles, looks, h);
+  BPPSA_CHECK_LAUNCH();
+  return BPPSA_OK;
 }
