@@ -58,13 +58,14 @@ struct Share {
 // and its gradient are made of those; 0: a row too long for that is read three times.  SECOND: the data's own token has a
 // softmax of its own, at another temperature.  TAIL: all other tokens are one more class.
 //
-// Bound by memory: 8192 rows of 32768 bf16 with two softmaxes 210 us, 5.1 TB/s, the vector unit busy for 93 % of that (two exponentials
+// Bound by memory: 8192 rows of 32768 bf16 with two softmaxes 210 us, 5.1 TB/s, the vector unit busy for 92 % of that (two exponentials
 // a logit and softmax: to keep them takes twice the registers of a 16-bit row).  Short rows are bound by what a row takes besides its
-// logits, the entries' shares in 64 bits and seven sums over a wave or more (16000 rows of 4001 fp16, a sixth of them not read: 59 us, 4.1 TB/s).
+// logits, the entries' shares in 64 bits and seven sums over a wave or more (16000 rows of 4001 fp16: 62 us, 4.2 TB/s; 65536 of 100 fp32
+// 47 us, 1.3 TB/s; 262144 of 16 fp32 167 us).  Rows that are read three times: 1024 of 150001 bf16 252 us, of 128001 fp32 395.
 //
-// As many waves a SIMD as the registers of the row let, and no more: two workgroups of sixteen waves are worth some spilled scalars of
-// the entries (2048 rows of 65536 bf16 with two softmaxes: 144 us, 172 by one workgroup a unit), four of eight instead of
-// three are not (4096 rows of 32001 bf16: 133 us, 119).
+// As many waves a SIMD as the registers of the row let, and no more: two workgroups of sixteen waves are worth the 4 to
+// 10 vector registers that most of them spill (2048 rows of 65536 bf16 with two softmaxes: 137 to 143 us, 172 by one workgroup a unit; with
+// the others as one more class 119 and 151), four of eight instead of three are not (4096 rows of 32001 bf16: 130 us, 119).
 template <typename E, int WAVES, int CHUNKS, bool SECOND, bool TAIL>
 __global__ void __launch_bounds__(WAVES * 64, CHUNKS == 16 ? 4 : WAVES == 16 ? 8 : 6)
 distil_kernel(const Loss<E> l) {
@@ -325,9 +326,10 @@ extern "C" bppsa_status bppsa_distil(const bppsa_distil_rows* r, float* loss, co
     typedef std::integral_constant<int, 8> Eight;
     typedef std::integral_constant<int, 16> Sixteen;
     // The fewest waves that hold a row in as many chunks as their registers take, and fewer chunks where rows are short: each line
-    // measured with it and with the next one in its place.  65536 rows of 300 bf16 60 and 63 us; with the others as one more class 16384 of 3000
-    // 43 and 53, 8192 of 5000 39 and 44, 8192 of 10000 66 and 87, 4096 of 32001 119 and 156, 2048 of 65536 117 and 159; 1024 of 131072 with
-    // two softmaxes, the longest that registers hold, 154 and 187.  (Rows that fill their line's chunks gain less, at worst nothing.)
+    // measured with it and with the next one in its place.  65536 rows of 300 bf16 and 16 entries 59 and 61 us; of 50 entries, with the others as
+    // one more class, 16384 of 3000 48 and 55, 8192 of 5000 39 and 47, 8192 of 10000 65 and 92, 4096 of 32001 119 and 156; of 64 2048 of 65536
+    // 119 and 156, and 1024 of 131072 with two softmaxes, the longest that registers hold, 154 and 189.  (Rows that fill their line's chunks
+    // gain less, at worst nothing.)
     if (l.V < N) run(One{}, None{});
     else if (fits(1, 4)) run(One{}, Four{});
     else if (fits(1, 8)) run(One{}, Eight{});

@@ -9,10 +9,12 @@ using namespace gated;
 // and what enters, finds what its run does to a state, and when the state before it is known walks them again.  The gate is asked for
 // while the tile waits for that state.
 //
-// Bound by memory: T = 4096, B = 4, D = 4096 bf16 with a gate 136 us, 4.9 TB/s; T = 30000, B = 1, D = 2048 130 us with the words'
-// emptying; less where tiles are few: T = 1000, B = 16, D = 641 fp16 25 us, 768 workgroups where 512 run at once.  By runs of eight steps
-// instead of sixteen the three calls take 150, 162 and 30 us where these take 136, 131 and 29.5.  Two workgroups a unit is what 16-bit runs of
-// two channels have registers for, fp32 ones of one channel leave three.
+// Bound by memory (calls with the words' emptying, gated): T = 4096, B = 4, D = 4096 bf16 132 us, 5.1 TB/s; T = 30000, B = 1, D = 2048 130 us;
+// T = 4096, B = 4, D = 2048 fp32 105 us without a gate, 5.1 TB/s; less where tiles are few: T = 1000, B = 16, D = 641 fp16 28.7 us,
+// 768 workgroups where 512 run at once.  Two workgroups a unit is what 16-bit runs of two channels have registers for, fp32 ones of one channel
+// leave three.  Runs of eight steps, in the same session: 147, 162, 106 and 28.8 us, and with registers for a third workgroup 135, 149, 106 and
+// 27.2: a twentieth less where tiles are few, a seventh more where they are many.  No vector register is spilled; scalars are, 2 to
+// 93 of them, each a write and a read of a lane.
 template <typename E, int V, int R, bool GATE, bool JOINED>
 __global__ void __launch_bounds__(kWaves * 64, sizeof(E) == 4 ? 6 : 4)
 gated_kernel(const Layer<E> l, Rows<E> y, float* __restrict__ h_last, float* __restrict__ states, int* tickets, uint64_t* words, int tiles, int each) {

@@ -20,9 +20,9 @@ struct Grads {
 // gradient that comes in from behind.  A run's states are found again from the one kept before its tile and the shares of the
 // runs in front of it, so a tile's inputs are read once.
 //
-// Bound by memory: T = 4096, B = 4, D = 4096 bf16 with a gate 257 us, 1.25 GB at 4.9 TB/s, the vector unit busy for 71 % of it.  Five values
+// Bound by memory: T = 4096, B = 4, D = 4096 bf16 with a gate 257 us, 1.25 GB at 4.9 TB/s, the vector unit busy for 75 % of it.  Five values
 // a step and channel stay in registers, so runs are of eight steps; fp32 without a gate leaves registers for three workgroups a
-// unit (T = 1000, B = 16, D = 330: 33 us), the others for two.
+// unit (T = 1000, B = 16, D = 330: 33 us), the others for two; 10 to 70 scalars are spilled.
 template <typename E, int V, bool GATE, bool JOINED>
 __global__ void __launch_bounds__(kWaves * 64, sizeof(E) == 4 && !GATE ? 6 : 4)
 gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restrict__ dh_last, const float* __restrict__ states,
@@ -197,7 +197,8 @@ gated_backward_kernel(const Layer<E> l, Rows<const E> dy, const float* __restric
 }
 
 // The sums over parts, in order: sixteen waves a sixteenth each, then those.  In 64 bits, which cost nothing beside the loads.  Bound by
-// the launch and two rounds of loads (256 parts of 4096 channels: 4.8 us).
+// the launch and two rounds of loads (256 parts of 4096 channels: 5 us).  A workgroup has all parts of 64 sums: few channels of many parts are
+// left to few workgroups (4096 parts of 16 channels: 13 us, of a call of 181).
 struct Joined {
   float *ddecay, *dr_bias, *di_bias;
 };
